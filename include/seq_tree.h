@@ -65,7 +65,11 @@ enum {
   SEQ_DEV_TIMEOUT = 16,    /* a bounded on-chip wait ran out; outputs of that call are undefined, but for the verification's
                               path_len and bonus_token: 0 and -1, or what had been decided */
   SEQ_DEV_BAD_PATH = 32,   /* seq_tree_kv_commit: path not a root-to-node path (see there); nothing was moved */
-  SEQ_DEV_BAD_LENGTH = 64  /* *prefix_len_dev outside [0, prefix_len]: clamped into that range */
+  SEQ_DEV_BAD_LENGTH = 64, /* *prefix_len_dev outside [0, prefix_len] (lengths[r] above max_len or the page table's reach):
+                              clamped into that range */
+  SEQ_DEV_BAD_PAGE = 128,  /* a page number outside [0, num_pages): read as page 0, never written */
+  SEQ_DEV_BAD_SLOT = 256,  /* seq_tree_pages_*: a slot, count or reference that contradicts the others (see there) */
+  SEQ_DEV_NO_PAGES = 512   /* seq_tree_pages_*: the pool has too few free pages for every request; the rest was served */
 };
 
 /*
@@ -419,6 +423,205 @@ typedef struct {
 } seq_tree_kv_commit_params;
 
 int seq_tree_kv_commit(const seq_tree_kv_commit_params* p, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * The paged 4-bit key/value cache: a cache that requests share and that holds a token of a kv head in 136 bytes
+ * instead of 512.  (The paper keeps its cache in the models' implementation and has no counterpart; Section 4.1 only
+ * says that decoding is bound by what is read from memory.)
+ *
+ * A PAGE holds page_size tokens (16, 32, 64 or 128) of every kv head, and of every layer when the layers share a pool.
+ * One kv head's part is page_size * 136 contiguous bytes, in GRANULES of 16 tokens, SEQ_KV4_GRANULE_BYTES each:
+ *     K codes [16][64] bytes, V codes [16][64] bytes, K (scale, mid) [16][2] half, V (scale, mid) [16][2] half.
+ * Channel c of a row is 4 bits of byte c/2: the low ones for even c.  A code x stands for scale * (x - 8) + mid.
+ * Scales and mids are half precision whatever the type of the rows, so magnitudes are below 65504; they have to be
+ * finite (seq_tree_kv4_append sees to it).  What pages hold behind a request's last token is never read into a result.
+ *
+ * A page table [slots][max_pages] int32 names the pages of each slot (a slot is one request's place in the batch):
+ * token t of slot r is in page page_table[r * table_stride + t / page_size].  Entries behind the last page are not read.
+ * lengths[r] is the number of tokens of slot r in the pages; a negative length marks an idle slot, which is skipped:
+ * what a call would write for it is left as it was.
+ */
+#define SEQ_KV4_GRANULE 16
+#define SEQ_KV4_GRANULE_BYTES (16 * 136)
+#define SEQ_MAX_BATCH 1024
+
+/*
+ * seq_tree_kv4_attention -- seq_tree_attention for `batch` requests whose prefixes are in 4-bit pages and whose tree
+ * rows are 16-bit arrays of their own.  For query head h (kv head h / (num_q_heads / num_kv_heads)) and node i of
+ * request r at position lengths[r] + depth(i):
+ *     out[r,i,h,:] = sum_j softmax_j(softmax_scale * q[r,i,h,:].k_j) v_j
+ * over the visible tokens j < lengths[r] of the request's pages and the visible tree rows a in i's mask row.
+ *   window   0: everything is visible.  W > 0: a key is visible if its position is above the query's position - W
+ *            (the position of tree row a is lengths[r] + depth(a)), or
+ *   sinks    below `sinks` (0 and more; not read without a window): the first tokens that stay visible.
+ * depth(i) is the number of i's ancestors, the set bits of its mask row less one; a node always sees itself.
+ * n_tree = 1 is a plain decoding step of one token.
+ *   q, out           element (r,i,h,c) at r*stride_req + i*stride_tok + h*stride_head + c, f16 or bf16
+ *   k_tree, v_tree   element (r,i,g,c) at r*t_stride_req + i*t_stride_tok + g*t_stride_head + c, the same type.  Rows that a
+ *                    node does not see may hold anything; one that it does see with an inf or NaN among its values (or a
+ *                    magnitude above 65504) makes the node's whole output row NaN.
+ *   pages            device, 16-byte aligned: kv head g of page p starts at p*page_stride_bytes + g*page_size*136
+ *   max_len          the largest length a request can have: sizes the launch; <= max_pages * page_size.  A longer one raises
+ *                    SEQ_DEV_BAD_LENGTH and is cut.
+ *   mask_bits        nullable: ancestor words as seq_tree_mask_from_parents writes them, request r's at
+ *                    r*mask_stride_req (words; 0: one tree for all).  NULL: node i sees the nodes 0..i (a chain).
+ *   lse              nullable, [batch][num_q_heads][n_tree] fp32 natural-log sum-exp.
+ *   workspace        seq_tree_kv4_attention_workspace_bytes(p) bytes, 256-byte aligned, device, contents undefined before
+ *                    and after: the pieces of work that several CTAs share.  Two calls that can run at the same time
+ *                    need one each.
+ * All rows 16-byte aligned, head_dim 128, SEQ_F16 or SEQ_BF16.  Products run in half precision with fp32 sums: q enters
+ * exactly (scaled by a power of two per row), a key's codes exactly or as its value rounded to half, V and the probabilities rounded to
+ * half (2^-12 of the value); tree rows of bf16 as half as well.  Softmax and sums are fp32.  The same call on the same
+ * inputs returns the same bits.  Returns SEQ_OK, SEQ_ERR_INVALID_ARG, SEQ_ERR_UNSUPPORTED (head_dim, dtype, page size),
+ * SEQ_ERR_WORKSPACE or SEQ_ERR_CUDA.
+ */
+typedef struct {
+  int32_t batch, n_tree, max_len, num_q_heads, num_kv_heads, head_dim;
+  int32_t dtype;       /* SEQ_F16 or SEQ_BF16 */
+  float softmax_scale; /* <= 0 selects 1/sqrt(head_dim) */
+  int32_t window, sinks;
+  const void* q;
+  int64_t q_stride_req, q_stride_tok, q_stride_head;
+  const void* k_tree;
+  const void* v_tree;
+  int64_t t_stride_req, t_stride_tok, t_stride_head;
+  const void* pages;
+  int64_t page_stride_bytes;
+  int32_t num_pages, page_size;
+  const int32_t* page_table;
+  int64_t table_stride; /* entries between the slots' rows */
+  int32_t max_pages;    /* entries of a row */
+  const int32_t* lengths;
+  const uint32_t* mask_bits;
+  int32_t mask_words_per_row;
+  int64_t mask_stride_req;
+  void* out;
+  int64_t o_stride_req, o_stride_tok, o_stride_head;
+  float* lse;
+  void* workspace;
+  size_t workspace_bytes;
+  int32_t* dev_status;
+} seq_tree_kv4_attention_params;
+
+size_t seq_tree_kv4_attention_workspace_bytes(const seq_tree_kv4_attention_params* p);
+int seq_tree_kv4_attention(const seq_tree_kv4_attention_params* p, void* stream);
+
+/*
+ * seq_tree_kv4_append -- rows of 16-bit keys and values behind the tokens that the pages hold: a prompt's rows, or, with
+ * `path`, the accepted path's rows out of the tree's (the commit of a verified step), of all layers in one call.
+ * For request r, i < m = count[r] (every row without count): token lengths[r] + i of every layer and kv head becomes the 4-bit
+ * form of row i (with path: of row path[r][i], any order, repeats allowed):
+ *     scale = half((max - min) / 15),  mid = half(min + 8 scale),  code = 8 + clamp(rint((x - mid) / scale), -8, 7)
+ * each step in fp32, rint to even; scale 0 gives code 8.  A row with an inf, a NaN or a magnitude above 65504 raises
+ * SEQ_DEV_NONFINITE and is stored as zeros.
+ *   k, v          element (l,r,i,g,c) at l*stride_layer + r*stride_req + i*stride_tok + g*stride_head + c, f16 or bf16, rows
+ *                 16-byte aligned, i < n_rows
+ *   pages         layer l, kv head g of page p at p*page_stride_bytes + l*layer_stride_bytes + g*page_size*136
+ *   count         nullable [batch]; as path_len of seq_tree_verify_batch.  path nullable, request r's at r*path_stride.
+ *                 A count outside [0, n_rows], or a path entry outside it, raises SEQ_DEV_BAD_PATH; tokens that would lie
+ *                 behind the page table's reach raise SEQ_DEV_BAD_LENGTH; the request is then left alone, new length included.
+ *                 A page number outside the pool raises SEQ_DEV_BAD_PAGE and that page's tokens are not written.
+ *   new_lengths   nullable [batch]: lengths[r] + m (idle slots: lengths[r]).  Not the same array as lengths.
+ * The pages must be there (seq_tree_pages_resize) and be no other slot's (seq_tree_pages_fork).  Requests have disjoint
+ * pages behind their lengths, so every byte has one writer.  Idle slots are skipped.
+ */
+typedef struct {
+  int32_t num_layers, batch, n_rows, num_kv_heads, head_dim;
+  int32_t dtype;
+  const void* k;
+  const void* v;
+  int64_t stride_layer, stride_req, stride_tok, stride_head;
+  void* pages;
+  int64_t page_stride_bytes, layer_stride_bytes;
+  int32_t num_pages, page_size;
+  const int32_t* page_table;
+  int64_t table_stride;
+  int32_t max_pages;
+  const int32_t* lengths;
+  const int32_t* count;
+  const int32_t* path;
+  int64_t path_stride;
+  int32_t* new_lengths;
+  int32_t* dev_status;
+} seq_tree_kv4_append_params;
+
+int seq_tree_kv4_append(const seq_tree_kv4_append_params* p, void* stream);
+
+/*
+ * seq_tree_kv4_read -- tokens of the pages as 16-bit rows (to look at them, to hand a prefix to a 16-bit cache, or to
+ * attend over what later steps will see): row i < m = count[r] (all n_rows without count) of request r, layer l, head g is
+ * token start[r] + i (i without start), scale * (code - 8) + mid in fp32, rounded once.  Rows i >= m are left as they are, as
+ * are all rows of a request whose start is negative.  The struct is seq_tree_kv4_append_params with `lengths` as start
+ * (nullable), k and v written; path, new_lengths must be NULL.  Bad counts, tokens behind the page table's reach and page
+ * numbers outside the pool raise what they raise there, and the rows concerned are left as they are.
+ */
+int seq_tree_kv4_read(const seq_tree_kv4_append_params* p, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * seq_tree_pages_resize, _fork, _compact -- the bookkeeping of a paged cache, on the device and capturable: which pages a
+ * slot holds, which pages requests share, which are free.  What a page holds does not matter here (any page size, any format).
+ * The state is four arrays of the caller:
+ *   page_table   [slots][max_pages] (rows table_stride apart): the pages of each slot; entries from page_count[r] on are -1
+ *   page_count   [slots]: pages held, 0..max_pages
+ *   ref_count    [num_pages]: how many slots hold the page; 0 = free
+ *   lengths      [slots] (fork only): tokens stored, at most page_count[r] * page_size
+ * Every call reads them and writes the state after it to table_out (rows table_out_stride apart), count_out, refs_out and
+ * lengths_out: either all of them the arrays they came from (then only what changes is written) or none, and nothing overlaps
+ * (then they are written whole).  Free pages are always taken lowest number first, slots are served in order, so the
+ * result is the same whatever runs first.  slots <= SEQ_MAX_SLOTS, num_pages below 2^30.
+ *
+ * _resize   tokens[slots]: slot r holds ceil(tokens[r] / page_size) pages afterwards (0 frees it; negative: left alone).
+ *           Pages given up lose a reference; pages that are needed are free ones, after all that this call gives up.
+ *           A slot whose growth, with that of the slots before it, exceeds the free pages raises SEQ_DEV_NO_PAGES and
+ *           keeps what it has.  More pages than max_pages: SEQ_DEV_BAD_SLOT, the slot is left alone.
+ * _fork     source[slots]: an empty slot r (page_count 0) with source[r] = s becomes a fork of slot s: it shares the pages
+ *           that are full, gets a copy of the one that is not (a free page, pages' contents copied), and lengths[s].  Negative:
+ *           left alone.  Pages that s holds behind its length are not shared.  A source outside [0, slots), a slot that
+ *           holds pages already, or a length beyond the source's pages raises SEQ_DEV_BAD_SLOT; too few free pages (counting
+ *           the forks before) SEQ_DEV_NO_PAGES; the slot then stays empty, with the length it had.  A slot that is forked in this call is
+ *           an empty source.  Afterwards a page with several references is full: appending never writes to it.
+ * _compact  moves the pages that are held to the front of the pool: the held pages numbered `live` and above, in order, go to
+ *           the free numbers below it, in order; live (nullable) receives how many are held.  Contents, tables and counts
+ *           follow; page_count stays (count_out is not used).
+ *
+ *   pages        device, 16-byte aligned (fork, compact): plane x of page p is page_bytes bytes (a multiple of 16) at
+ *                p*page_stride_bytes + x*plane_stride_bytes, x < num_planes (a pool of all layers: one plane; a pool per
+ *                layer: a plane each)
+ *   workspace    seq_tree_pages_workspace_bytes(p) bytes, 16-byte aligned, device (fork, compact); contents undefined; two
+ *                calls that can run at the same time need one each.
+ * Table entries outside [0, num_pages) that a call meets raise SEQ_DEV_BAD_PAGE and count as no page (compact leaves -1); a
+ * page_count outside [0, max_pages] raises SEQ_DEV_BAD_SLOT and the slot is left alone; a ref_count below what is
+ * given up, or negative, raises SEQ_DEV_BAD_SLOT and counts as 0.  Returns SEQ_OK, SEQ_ERR_INVALID_ARG, SEQ_ERR_WORKSPACE or
+ * SEQ_ERR_CUDA.
+ */
+#define SEQ_MAX_SLOTS 2048
+typedef struct {
+  int32_t slots, max_pages, num_pages, page_size;
+  const int32_t* page_table;
+  int64_t table_stride;
+  const int32_t* page_count;
+  const int32_t* ref_count;
+  const int32_t* lengths; /* fork */
+  int32_t* table_out;
+  int64_t table_out_stride;
+  int32_t* count_out; /* resize, fork */
+  int32_t* refs_out;
+  int32_t* lengths_out;  /* fork */
+  const int32_t* tokens; /* resize */
+  const int32_t* source; /* fork */
+  void* pages;           /* fork, compact */
+  int32_t num_planes;
+  int64_t plane_stride_bytes, page_stride_bytes, page_bytes;
+  int32_t* live; /* compact, nullable */
+  void* workspace;
+  size_t workspace_bytes;
+  int32_t* dev_status;
+} seq_tree_pages_params;
+
+size_t seq_tree_pages_workspace_bytes(const seq_tree_pages_params* p);
+int seq_tree_pages_resize(const seq_tree_pages_params* p, void* stream);
+int seq_tree_pages_fork(const seq_tree_pages_params* p, void* stream);
+int seq_tree_pages_compact(const seq_tree_pages_params* p, void* stream);
 
 /* ---------------------------------------------------------------------------
  * seq_tree_build -- Sequoia's tree construction (Section 3.1: score function, F(tree) = sum of the nodes' scores,

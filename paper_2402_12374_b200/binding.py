@@ -24,6 +24,9 @@ SEQ_VERIFY_SCHED_WALK, SEQ_VERIFY_SCHED_NODES = 16, 32
 SEQ_VERIFY_LOGITS_BF16 = 8
 SEQ_DEV_BAD_PATH = 32
 SEQ_DEV_BAD_LENGTH = 64
+SEQ_DEV_BAD_PAGE, SEQ_DEV_BAD_SLOT, SEQ_DEV_NO_PAGES = 128, 256, 512
+SEQ_KV4_GRANULE, SEQ_KV4_GRANULE_BYTES = 16, 16 * 136
+SEQ_MAX_BATCH, SEQ_MAX_SLOTS = 1024, 2048
 SEQ_MAX_TREE = 1024
 SEQ_NOALLOC_SCRATCH_BYTES = 384 << 10
 KERNEL_AUTO, KERNEL_CUDA_CORE, KERNEL_TENSOR_CORE = 0, 1, 2
@@ -45,6 +48,14 @@ EXPORTED_SYMBOLS = (
     "seq_tree_draft_sample",
     "seq_tree_kv_commit",
     "seq_tree_top_p_filter",
+    "seq_tree_kv4_attention_workspace_bytes",
+    "seq_tree_kv4_attention",
+    "seq_tree_kv4_append",
+    "seq_tree_kv4_read",
+    "seq_tree_pages_workspace_bytes",
+    "seq_tree_pages_resize",
+    "seq_tree_pages_fork",
+    "seq_tree_pages_compact",
     "seq_tree_build",
     "seq_tree_speedup_search",
     "seq_tree_probe_stream_read",
@@ -123,6 +134,16 @@ def load() -> C.CDLL:
         lib.seq_tree_kv_commit.restype = C.c_int
         lib.seq_tree_top_p_filter.argtypes = [C.POINTER(TopPParams), C.c_void_p]
         lib.seq_tree_top_p_filter.restype = C.c_int
+        lib.seq_tree_kv4_attention_workspace_bytes.argtypes = [C.POINTER(Kv4AttentionParams)]
+        lib.seq_tree_kv4_attention_workspace_bytes.restype = C.c_size_t
+        lib.seq_tree_kv4_attention.argtypes = [C.POINTER(Kv4AttentionParams), C.c_void_p]
+        lib.seq_tree_kv4_attention.restype = C.c_int
+        for fn in (lib.seq_tree_kv4_append, lib.seq_tree_kv4_read):
+            fn.argtypes, fn.restype = [C.POINTER(Kv4AppendParams), C.c_void_p], C.c_int
+        lib.seq_tree_pages_workspace_bytes.argtypes = [C.POINTER(PagesParams)]
+        lib.seq_tree_pages_workspace_bytes.restype = C.c_size_t
+        for fn in (lib.seq_tree_pages_resize, lib.seq_tree_pages_fork, lib.seq_tree_pages_compact):
+            fn.argtypes, fn.restype = [C.POINTER(PagesParams), C.c_void_p], C.c_int
         lib.seq_tree_build.argtypes = [C.POINTER(TreeBuildParams)]
         lib.seq_tree_build.restype = C.c_int
         lib.seq_tree_speedup_search.argtypes = [C.c_void_p, C.c_int32, C.c_int32, C.c_void_p, C.c_double, C.POINTER(C.c_int32),
@@ -449,6 +470,253 @@ def seq_tree_top_p_filter(logits, temperature: float, top_p: float, *, out=None,
                    _dev(kept_out, "kept_out", torch.int32), _dev(dev_status, "dev_status", torch.int32))
     _check("seq_tree_top_p_filter", load().seq_tree_top_p_filter(C.byref(p), _stream(stream)))
     return out
+
+
+class Kv4AttentionParams(C.Structure):
+    _fields_ = [
+        ("batch", C.c_int32), ("n_tree", C.c_int32), ("max_len", C.c_int32), ("num_q_heads", C.c_int32),
+        ("num_kv_heads", C.c_int32), ("head_dim", C.c_int32), ("dtype", C.c_int32), ("softmax_scale", C.c_float),
+        ("window", C.c_int32), ("sinks", C.c_int32),
+        ("q", C.c_void_p), ("q_stride_req", C.c_int64), ("q_stride_tok", C.c_int64), ("q_stride_head", C.c_int64),
+        ("k_tree", C.c_void_p), ("v_tree", C.c_void_p),
+        ("t_stride_req", C.c_int64), ("t_stride_tok", C.c_int64), ("t_stride_head", C.c_int64),
+        ("pages", C.c_void_p), ("page_stride_bytes", C.c_int64), ("num_pages", C.c_int32), ("page_size", C.c_int32),
+        ("page_table", C.c_void_p), ("table_stride", C.c_int64), ("max_pages", C.c_int32), ("lengths", C.c_void_p),
+        ("mask_bits", C.c_void_p), ("mask_words_per_row", C.c_int32), ("mask_stride_req", C.c_int64),
+        ("out", C.c_void_p), ("o_stride_req", C.c_int64), ("o_stride_tok", C.c_int64), ("o_stride_head", C.c_int64),
+        ("lse", C.c_void_p), ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t), ("dev_status", C.c_void_p),
+    ]
+
+
+class Kv4AppendParams(C.Structure):
+    _fields_ = [
+        ("num_layers", C.c_int32), ("batch", C.c_int32), ("n_rows", C.c_int32), ("num_kv_heads", C.c_int32),
+        ("head_dim", C.c_int32), ("dtype", C.c_int32),
+        ("k", C.c_void_p), ("v", C.c_void_p),
+        ("stride_layer", C.c_int64), ("stride_req", C.c_int64), ("stride_tok", C.c_int64), ("stride_head", C.c_int64),
+        ("pages", C.c_void_p), ("page_stride_bytes", C.c_int64), ("layer_stride_bytes", C.c_int64),
+        ("num_pages", C.c_int32), ("page_size", C.c_int32),
+        ("page_table", C.c_void_p), ("table_stride", C.c_int64), ("max_pages", C.c_int32), ("lengths", C.c_void_p),
+        ("count", C.c_void_p), ("path", C.c_void_p), ("path_stride", C.c_int64), ("new_lengths", C.c_void_p),
+        ("dev_status", C.c_void_p),
+    ]
+
+
+class PagesParams(C.Structure):
+    _fields_ = [
+        ("slots", C.c_int32), ("max_pages", C.c_int32), ("num_pages", C.c_int32), ("page_size", C.c_int32),
+        ("page_table", C.c_void_p), ("table_stride", C.c_int64), ("page_count", C.c_void_p), ("ref_count", C.c_void_p),
+        ("lengths", C.c_void_p), ("table_out", C.c_void_p), ("table_out_stride", C.c_int64), ("count_out", C.c_void_p),
+        ("refs_out", C.c_void_p), ("lengths_out", C.c_void_p), ("tokens", C.c_void_p), ("source", C.c_void_p),
+        ("pages", C.c_void_p), ("num_planes", C.c_int32), ("plane_stride_bytes", C.c_int64), ("page_stride_bytes", C.c_int64),
+        ("page_bytes", C.c_int64), ("live", C.c_void_p), ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t),
+        ("dev_status", C.c_void_p),
+    ]
+
+
+def _kv4_pool(pool, what: str):
+    """(layers, kv heads, page size, page stride, layer stride) of a pool uint8 [pages, heads, page_size * 136] or
+    [pages, layers, heads, page_size * 136]: a head's part contiguous, the heads of a page one behind the other."""
+    if pool.dim() == 3:
+        pool = pool.unsqueeze(1)
+    if pool.dim() != 4 or pool.dtype is not torch.uint8:
+        raise ValueError(f"{what} must be uint8 [pages, heads, page_size * 136] or [pages, layers, heads, page_size * 136]")
+    _, layers, heads, part = pool.shape
+    page, layer, head, one = pool.stride()
+    if part % 136 or one != 1 or (heads > 1 and head != part):
+        raise ValueError(f"{what}: page_size * 136 bytes a head, contiguous over heads")
+    return layers, heads, part // 136, page if pool.shape[0] > 1 else layers * heads * part, layer if layers > 1 else heads * part
+
+
+def _table(page_table):
+    if page_table.dim() != 2 or page_table.stride(1) != 1:
+        raise ValueError("page_table must be [slots, max_pages] with contiguous rows")
+    return _dev(page_table, "page_table", torch.int32), page_table.stride(0) if page_table.shape[0] > 1 else page_table.shape[1]
+
+
+def _per_slot(t, slots: int, name: str):
+    if t is not None and (t.shape != (slots,) or not t.is_contiguous()):
+        raise ValueError(f"{name} must be [{slots}], contiguous")
+    return _dev(t, name, torch.int32)
+
+
+class KV4AttentionCall:
+    """A prepared seq_tree_kv4_attention call: attention of ``R`` requests' tree tokens over prefixes in 4-bit pages.
+
+    q [R, n, Hq, 128]; k_tree, v_tree [R, n, Hkv, 128] (the tree's own rows, 16-bit); pool uint8 [pages, Hkv, page_size *
+    136]; page_table int32 [R, max_pages]; lengths int32 [R], negative for an idle slot.  mask_bits: int32 words [n, w] of
+    ``seq_tree_mask_from_parents`` for all requests, or [R, n, w]; None: a chain.  max_len bounds the lengths (default: what
+    the page table reaches).  window > 0: only keys less than ``window`` positions back are seen, and the first ``sinks``."""
+
+    def __init__(self, q, k_tree, v_tree, pool, page_table, lengths, *, mask_bits=None, max_len: int | None = None, window: int = 0,
+                 sinks: int = 0, out=None, lse=None, softmax_scale: float = 0.0, workspace=None, dev_status=None):
+        if q.dtype not in (torch.float16, torch.bfloat16) or k_tree.dtype != q.dtype or v_tree.dtype != q.dtype:
+            raise ValueError("q, k_tree, v_tree must share one of float16/bfloat16")
+        R, n, Hq, d = q.shape
+        layers, Hkv, page_size, page_stride, _ = _kv4_pool(pool, "pool")
+        if layers != 1:
+            raise ValueError("pool must be one layer's: pool[:, layer]")
+        if k_tree.shape != (R, n, Hkv, d) or v_tree.shape != k_tree.shape:
+            raise ValueError("k_tree and v_tree must be [requests, nodes, kv heads, head_dim], the heads those of the pool")
+        if out is None:
+            out = torch.empty_like(q)
+        if out.shape != q.shape or out.dtype != q.dtype:
+            raise ValueError("out must be like q")
+        for t, nm in ((q, "q"), (k_tree, "k_tree"), (v_tree, "v_tree"), (out, "out")):
+            if t.stride(-1) != 1:
+                raise ValueError(f"{nm}: head_dim must be contiguous")
+        if k_tree.stride() != v_tree.stride():
+            raise ValueError("k_tree and v_tree must share strides")
+        if page_table.shape[0] != R:
+            raise ValueError("one row of page_table per request")
+        if lse is not None and (lse.shape != (R, Hq, n) or not lse.is_contiguous()):
+            raise ValueError("lse must be [requests, heads, nodes], contiguous")
+        p = Kv4AttentionParams()
+        p.batch, p.n_tree, p.num_q_heads, p.num_kv_heads, p.head_dim = R, n, Hq, Hkv, d
+        p.max_len = page_table.shape[1] * page_size if max_len is None else max_len
+        p.dtype, p.softmax_scale, p.window, p.sinks = _DTYPES[q.dtype], softmax_scale, window, sinks
+        p.q, p.q_stride_req, p.q_stride_tok, p.q_stride_head = _dev(q, "q"), *q.stride()[:3]
+        p.k_tree, p.v_tree = _dev(k_tree, "k_tree"), _dev(v_tree, "v_tree")
+        p.t_stride_req, p.t_stride_tok, p.t_stride_head = k_tree.stride()[:3]
+        p.pages, p.page_stride_bytes, p.num_pages, p.page_size = _dev(pool, "pool"), page_stride, pool.shape[0], page_size
+        p.page_table, p.table_stride = _table(page_table)
+        p.max_pages = page_table.shape[1]
+        p.lengths = _per_slot(lengths, R, "lengths")
+        if mask_bits is not None:
+            if mask_bits.stride(-1) != 1 or mask_bits.shape[-2] != n or (mask_bits.dim() == 3 and mask_bits.shape[0] != R) or mask_bits.dim() not in (2, 3):
+                raise ValueError("mask_bits must be [nodes, words] or [requests, nodes, words] with contiguous words")
+            p.mask_bits = _dev(mask_bits, "mask_bits", torch.int32)
+            p.mask_words_per_row = mask_bits.stride(-2) if n > 1 else mask_bits.shape[-1]
+            p.mask_stride_req = mask_bits.stride(0) if mask_bits.dim() == 3 else 0
+            if mask_bits.shape[-1] * 32 < n:
+                raise ValueError("mask_bits: too few words per row")
+        p.out, p.o_stride_req, p.o_stride_tok, p.o_stride_head = _dev(out, "out"), *out.stride()[:3]
+        p.lse = _dev(lse, "lse", torch.float32)
+        p.dev_status = _dev(dev_status, "dev_status", torch.int32)
+        need = load().seq_tree_kv4_attention_workspace_bytes(C.byref(p))
+        if workspace is None and need:
+            workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+        if workspace is not None:
+            p.workspace, p.workspace_bytes = _dev(workspace, "workspace"), workspace.numel() * workspace.element_size()
+        self.params, self.out, self.lse, self.workspace, self.workspace_bytes_needed = p, out, lse, workspace, need
+        self._ref, self._fn = C.byref(p), load().seq_tree_kv4_attention
+        self._keep = (q, k_tree, v_tree, pool, page_table, lengths, mask_bits, out, lse, workspace, dev_status)
+
+    def run(self, stream=None):
+        rc = self._fn(self._ref, _raw_stream(_raw_device()) if stream is None else _stream(stream))
+        if rc:
+            _check("seq_tree_kv4_attention", rc)
+        return self.out
+
+
+def seq_tree_kv4_attention(q, k_tree, v_tree, pool, page_table, lengths, **kw):
+    """Attention of tree tokens over prefixes in 4-bit pages (see ``KV4AttentionCall``); returns out [R, n, Hq, 128]."""
+    stream = kw.pop("stream", None)
+    return KV4AttentionCall(q, k_tree, v_tree, pool, page_table, lengths, **kw).run(stream)
+
+
+def _kv4_rows(k, v, pool, page_table, lengths, count, dev_status, what):
+    layers, Hkv, page_size, page_stride, layer_stride = _kv4_pool(pool, "pool")
+    if k.dim() == 4:
+        k, v = k.unsqueeze(0), v.unsqueeze(0)
+    if k.dim() != 5 or k.shape != v.shape or k.stride() != v.stride() or k.dtype != v.dtype or k.stride(4) != 1:
+        raise ValueError(f"{what} must be [layers, requests, rows, kv heads, head_dim] (layers optional) with the same strides, rows contiguous")
+    if k.dtype not in (torch.float16, torch.bfloat16):
+        raise ValueError(f"{what} must be float16 or bfloat16")
+    if k.shape[0] != layers or k.shape[3] != Hkv or page_table.shape[0] != k.shape[1]:
+        raise ValueError(f"{what}: layers and kv heads as in the pool, one row of page_table per request")
+    sl, sr, st, sh, _ = k.stride()
+    table, table_stride = _table(page_table)
+    R = k.shape[1]
+    return Kv4AppendParams(layers, R, k.shape[2], Hkv, k.shape[4], _DTYPES[k.dtype], _dev(k, "k"), _dev(v, "v"), sl, sr, st, sh,
+                           _dev(pool, "pool"), page_stride, layer_stride, pool.shape[0], page_size, table, table_stride, page_table.shape[1],
+                           _per_slot(lengths, R, "lengths"), _per_slot(count, R, "count"), None, 0, None, _dev(dev_status, "dev_status", torch.int32))
+
+
+def seq_tree_kv4_append(k, v, pool, page_table, lengths, *, count=None, path=None, new_lengths=None, dev_status=None, stream=None):
+    """Rows k, v [layers, R, rows, Hkv, 128] (layers optional) become 4-bit tokens behind the ``lengths[r]`` that request r has in
+    its pages: the first ``count[r]`` rows (all without it), or the rows ``path[r, :count[r]]`` - as
+    ``seq_tree_verify_batch`` left the accepted path.  pool uint8 [pages, layers, Hkv, page_size * 136]."""
+    p = _kv4_rows(k, v, pool, page_table, lengths, count, dev_status, "k and v")
+    if path is not None:
+        if path.dim() != 2 or path.shape[0] != p.batch or path.shape[1] < p.n_rows or path.stride(1) != 1:
+            raise ValueError("path must be [requests, rows] with contiguous rows")
+        p.path, p.path_stride = _dev(path, "path", torch.int32), path.stride(0) if p.batch > 1 else path.shape[1]
+    p.new_lengths = _per_slot(new_lengths, p.batch, "new_lengths")
+    _check("seq_tree_kv4_append", load().seq_tree_kv4_append(C.byref(p), _stream(stream)))
+
+
+def seq_tree_kv4_read(pool, page_table, k_out, v_out, *, start=None, count=None, dev_status=None, stream=None):
+    """Tokens start[r] (0 without it) .. start[r] + count[r] - 1 of each request as 16-bit rows into k_out, v_out [layers, R, rows,
+    Hkv, 128] (layers optional); rows from count[r] on are left as they are."""
+    p = _kv4_rows(k_out, v_out, pool, page_table, start, count, dev_status, "k_out and v_out")
+    _check("seq_tree_kv4_read", load().seq_tree_kv4_read(C.byref(p), _stream(stream)))
+    return k_out, v_out
+
+
+def _pages_params(page_table, page_count, ref_count, page_size, table_out, count_out, refs_out, dev_status):
+    slots = page_table.shape[0]
+    table, table_stride = _table(page_table)
+    out, out_stride = (table, table_stride) if table_out is None else _table(table_out)
+    if table_out is not None and table_out.shape != page_table.shape:
+        raise ValueError("table_out must be like page_table")
+    if ref_count.dim() != 1 or not ref_count.is_contiguous() or (refs_out is not None and (refs_out.shape != ref_count.shape or not refs_out.is_contiguous())):
+        raise ValueError("ref_count and refs_out must be [pages], contiguous")
+    p = PagesParams()
+    p.slots, p.max_pages, p.num_pages, p.page_size = slots, page_table.shape[1], ref_count.shape[0], page_size
+    p.page_table, p.table_stride, p.table_out, p.table_out_stride = table, table_stride, out, out_stride
+    p.page_count, p.ref_count = _per_slot(page_count, slots, "page_count"), _dev(ref_count, "ref_count", torch.int32)
+    p.count_out = p.page_count if count_out is None else _per_slot(count_out, slots, "count_out")
+    p.refs_out = p.ref_count if refs_out is None else _dev(refs_out, "refs_out", torch.int32)
+    p.dev_status = _dev(dev_status, "dev_status", torch.int32)
+    return p
+
+
+def _pages_pool(p, pool, planes: bool, workspace):
+    """pool [pages, ...] (planes: [planes, pages, ...]) of any type, a page contiguous."""
+    if not planes:
+        pool = pool.unsqueeze(0)
+    one = pool[0, 0]
+    if pool.dim() < 3 or not one.is_contiguous() or pool.shape[1] != p.num_pages:
+        raise ValueError("pool must be [pages, ...] ([planes, pages, ...] with planes=True), as many pages as ref_count, each contiguous")
+    e = pool.element_size()
+    p.pages, p.num_planes, p.page_bytes = _dev(pool, "pool"), pool.shape[0], one.numel() * e
+    p.page_stride_bytes = pool.stride(1) * e if pool.shape[1] > 1 else p.page_bytes
+    p.plane_stride_bytes = pool.stride(0) * e if pool.shape[0] > 1 else p.page_stride_bytes * p.num_pages
+    if workspace is None:
+        workspace = torch.empty(load().seq_tree_pages_workspace_bytes(C.byref(p)), dtype=torch.uint8, device=pool.device)
+    p.workspace, p.workspace_bytes = _dev(workspace, "workspace"), workspace.numel() * workspace.element_size()
+    return workspace
+
+
+def seq_tree_pages_resize(page_table, page_count, ref_count, tokens, page_size: int, *, table_out=None, count_out=None, refs_out=None,
+                          dev_status=None, stream=None):
+    """Slot r holds ceil(tokens[r] / page_size) pages afterwards (0: freed, negative: left alone).  In place, or into
+    table_out, count_out, refs_out (all of them)."""
+    p = _pages_params(page_table, page_count, ref_count, page_size, table_out, count_out, refs_out, dev_status)
+    p.tokens = _per_slot(tokens, p.slots, "tokens")
+    _check("seq_tree_pages_resize", load().seq_tree_pages_resize(C.byref(p), _stream(stream)))
+
+
+def seq_tree_pages_fork(pool, page_table, page_count, ref_count, lengths, source, page_size: int, *, table_out=None, count_out=None,
+                        refs_out=None, lengths_out=None, planes: bool = False, workspace=None, dev_status=None, stream=None):
+    """Empty slot r with source[r] = s >= 0 becomes a fork of slot s: full pages are shared, the open one is copied.  pool [pages,
+    ...] of any type (planes=True: [planes, pages, ...]).  In place, or into the four outputs (all of them)."""
+    p = _pages_params(page_table, page_count, ref_count, page_size, table_out, count_out, refs_out, dev_status)
+    p.lengths, p.source = _per_slot(lengths, p.slots, "lengths"), _per_slot(source, p.slots, "source")
+    p.lengths_out = p.lengths if lengths_out is None else _per_slot(lengths_out, p.slots, "lengths_out")
+    workspace = _pages_pool(p, pool, planes, workspace)
+    _check("seq_tree_pages_fork", load().seq_tree_pages_fork(C.byref(p), _stream(stream)))
+
+
+def seq_tree_pages_compact(pool, page_table, page_count, ref_count, *, table_out=None, refs_out=None, live=None, planes: bool = False,
+                           workspace=None, dev_status=None, stream=None):
+    """Moves the pages that are held to the front of the pool, contents, tables and reference counts; ``live`` int32 [1] receives how
+    many they are.  In place, or (tables and counts) into table_out, refs_out."""
+    p = _pages_params(page_table, page_count, ref_count, 1, table_out, None, refs_out, dev_status)
+    p.live = _dev(live, "live", torch.int32)
+    workspace = _pages_pool(p, pool, planes, workspace)
+    _check("seq_tree_pages_compact", load().seq_tree_pages_compact(C.byref(p), _stream(stream)))
 
 
 class TreeBuildParams(C.Structure):

@@ -1,0 +1,160 @@
+// What the kernels of seq_tree_kv4_attention share: their arguments, how the work is laid out and cut, and the pieces that
+// CTAs leave for one another.
+//
+// A unit is (request, kv head, tile of query rows); a row is a (node, head in group) pair.  A unit's keys come in steps: those of the prefix that
+// some row can see (the sinks, then the window: the steps in between are left out), then the tree's.  The steps of all
+// units are laid end to end and cut into equal ranges, one a CTA, whatever lengths the requests have.  A unit inside one range is
+// finished there; the pieces of one that is cut go to the workspace and are added by a second launch in the order of their CTAs.
+#pragma once
+
+#include "kv4.cuh"
+
+namespace seqtree {
+
+struct Kv4Args {
+  int32_t batch, n, max_len, Hq, Hkv, group, rows;  // rows: n * group
+  int32_t window, sinks;
+  int32_t num_pages, page_size;
+  int32_t row_tile, tiles, tree_steps, ctas, min_steps;
+  const uint8_t* q; int64_t q_req, q_tok, q_head;  // all strides in bytes
+  const uint8_t* kt; const uint8_t* vt; int64_t t_req, t_tok, t_head;
+  const uint8_t* pages; int64_t page_stride;
+  const int32_t* table; int64_t table_stride;
+  const int32_t* lengths;
+  const uint32_t* mask; int32_t mask_wpr; int64_t mask_req;
+  uint8_t* out; int64_t o_req, o_tok, o_head;
+  float* lse;
+  float2* ws_ml;  // [2 * ctas][row_tile] (m, l): reference maximum (log2 units) and sum of a piece
+  float* ws_o;    // [2 * ctas][row_tile][128] its unnormalised rows
+  float scale_log2;
+  int32_t* status;
+};
+
+struct Kv4Plan {
+  int32_t start[SEQ_MAX_BATCH + 1];  // steps before each request's
+  int32_t len[SEQ_MAX_BATCH];        // its prefix, -1: idle
+  int32_t warp_sum[32];
+};
+
+// The prefix steps of kStep keys that a request's rows can see: step t holds the keys from key_step(t) * kStep on.
+struct Kv4Prefix {
+  int32_t steps, split, gap;
+  __device__ __forceinline__ int key_step(int t) const { return t < split ? t : t + gap; }
+};
+template <int kStep>
+__device__ __forceinline__ Kv4Prefix kv4_prefix(const Kv4Args& a, int L) {
+  const int all = (L + kStep - 1) / kStep;
+  if (a.window == 0) return {all, all, 0};
+  const int first = max(0, L + 1 - a.window);  // what the root's window begins with; a deeper node's begins later
+  const int sink_steps = (min(a.sinks, L) + kStep - 1) / kStep, window_step = first / kStep;
+  if (window_step <= sink_steps) return {all, all, 0};
+  return {sink_steps + max(all - window_step, 0), sink_steps, window_step - sink_steps};
+}
+
+// Every thread of the CTA calls it; the plan is there behind the next barrier that it ends with.
+template <int kStep, int kThreads>
+__device__ __forceinline__ void kv4_plan(Kv4Plan* plan, const Kv4Args& a) {
+  const int per = (a.batch + kThreads - 1) / kThreads, first = threadIdx.x * per;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  int sum = 0;
+  for (int j = first; j < first + per && j < a.batch; ++j) {
+    int L = a.lengths[j];
+    if (L > a.max_len) {
+      if (blockIdx.x == 0) dev_flag(a.status, SEQ_DEV_BAD_LENGTH);
+      L = a.max_len;
+    }
+    plan->len[j] = max(L, -1);
+    if (L >= 0) sum += a.Hkv * a.tiles * (kv4_prefix<kStep>(a, L).steps + a.tree_steps);
+  }
+  int incl = sum;
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    const int v = __shfl_up_sync(0xffffffffu, incl, d);
+    if (lane >= d) incl += v;
+  }
+  if (lane == 31) plan->warp_sum[warp] = incl;
+  __syncthreads();
+  int at = incl - sum;
+  for (int w = 0; w < warp; ++w) at += plan->warp_sum[w];
+  for (int j = first; j < first + per && j < a.batch; ++j) {
+    plan->start[j] = at;
+    const int L = plan->len[j];
+    if (L >= 0) at += a.Hkv * a.tiles * (kv4_prefix<kStep>(a, L).steps + a.tree_steps);
+    if (j == a.batch - 1) plan->start[a.batch] = at;
+  }
+  __syncthreads();
+}
+
+// The ranges: no more than one for every min_steps steps.
+struct Kv4Ranges {
+  int32_t total, ctas;
+  __device__ __forceinline__ int lo(int c) const { return (int)((int64_t)total * c / ctas); }
+};
+__device__ __forceinline__ Kv4Ranges kv4_ranges(const Kv4Plan* plan, const Kv4Args& a) {
+  const int total = plan->start[a.batch];
+  return {total, max(1, min(a.ctas, (total + a.min_steps - 1) / a.min_steps))};
+}
+
+struct Kv4Unit {
+  int32_t r, g, m, L;
+  int32_t begin, end;  // positions
+  Kv4Prefix prefix;
+};
+template <int kStep>
+__device__ __forceinline__ Kv4Unit kv4_unit(const Kv4Plan* plan, const Kv4Args& a, int pos) {
+  int lo = 0, hi = a.batch - 1;  // the last request that starts at or before pos and has steps
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (plan->start[mid] <= pos) lo = mid; else hi = mid - 1;
+  }
+  Kv4Unit u;
+  u.r = lo;
+  u.L = plan->len[lo];
+  u.prefix = kv4_prefix<kStep>(a, max(u.L, 0));
+  const int steps = u.prefix.steps + a.tree_steps, rem = pos - plan->start[lo], x = rem / steps;
+  u.g = x / a.tiles;
+  u.m = x - u.g * a.tiles;
+  u.begin = pos - (rem - x * steps);
+  u.end = u.begin + steps;
+  return u;
+}
+// Where CTA c leaves its piece of a unit that begins at `begin`: the piece that opens its range, or the one that closes it.
+__device__ __forceinline__ int kv4_slot(const Kv4Ranges& ranges, int c, int begin) { return 2 * c + (max(begin, ranges.lo(c)) == ranges.lo(c) ? 0 : 1); }
+
+__device__ __forceinline__ const uint32_t* kv4_mask_row(const Kv4Args& a, int r, int node) {
+  return a.mask != nullptr ? a.mask + r * a.mask_req + (int64_t)node * a.mask_wpr : nullptr;
+}
+// Bits of the tree rows [32 w, 32 w + 32) that `node` sees, the window aside
+__device__ __forceinline__ uint32_t kv4_mask_word(const Kv4Args& a, const uint32_t* row, int node, int w) {
+  const int left = a.n - 32 * w;
+  if (left <= 0) return 0u;
+  uint32_t bits;
+  if (row != nullptr) bits = row[w];
+  else bits = node >= 32 * w + 31 ? 0xffffffffu : (node < 32 * w ? 0u : (2u << (node - 32 * w)) - 1u);
+  return left < 32 ? bits & ((1u << left) - 1u) : bits;
+}
+__device__ __forceinline__ int kv4_depth(const Kv4Args& a, int r, int node) {
+  const uint32_t* row = kv4_mask_row(a, r, node);
+  if (row == nullptr) return node;
+  int c = 0;
+  for (int w = 0; w < (a.n + 31) >> 5; ++w) c += __popc(kv4_mask_word(a, row, node, w));
+  return max(c - 1, 0);
+}
+// ... with the window: rows a of the tree at L + depth(a)
+__device__ __forceinline__ uint32_t kv4_window_word(const Kv4Args& a, int r, int L, int depth, int w, uint32_t bits) {
+  if (a.window == 0 || depth < a.window) return bits;  // (no ancestor is further away than the root)
+  for (uint32_t left = bits; left != 0; left &= left - 1) {
+    const int b = __ffs(left) - 1, d = kv4_depth(a, r, 32 * w + b);
+    if (d <= depth - a.window && L + d >= a.sinks) bits &= ~(1u << b);
+  }
+  return bits;
+}
+
+size_t kv4_rows_workspace_bytes(const seq_tree_kv4_attention_params& p);
+int launch_kv4_rows(const seq_tree_kv4_attention_params& p, cudaStream_t stream);
+// Arguments that do not depend on the kernel
+Kv4Args kv4_args(const seq_tree_kv4_attention_params& p);
+// Adds the pieces that `ctas` CTAs left: steps of `step` keys
+int launch_kv4_combine(const Kv4Args& a, int step, bool bf16, cudaStream_t stream);
+
+}  // namespace seqtree

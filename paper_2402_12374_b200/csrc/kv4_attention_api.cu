@@ -1,0 +1,117 @@
+// seq_tree_kv4_attention: checks, the choice of kernel, and the launch that adds the pieces of units that ranges cut.
+#include "kv4_attention.cuh"
+#include "umma.cuh"
+
+namespace seqtree {
+
+// One block (x: a range's start, y: 16 rows) for each range that may begin inside a unit: the first range that begins in
+// it adds all its pieces, in the order of their CTAs, so the sum does not depend on who finished when.
+constexpr int kCombineRows = 16;
+template <int kStep, bool kBf16>
+__global__ void __launch_bounds__(kHeadDim) kv4_combine_kernel(const Kv4Args a) {
+  __shared__ Kv4Plan plan;
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  kv4_plan<kStep, kHeadDim>(&plan, a);
+  const Kv4Ranges ranges = kv4_ranges(&plan, a);
+  const int b = blockIdx.x + 1;
+  if (b >= ranges.ctas) return;
+  const int at = ranges.lo(b);
+  if (at >= ranges.total) return;
+  const Kv4Unit u = kv4_unit<kStep>(&plan, a, at);
+  if (u.begin == at || ranges.lo(b - 1) > u.begin) return;  // not cut here, or cut before
+  int last = b;
+  while (last + 1 < ranges.ctas && ranges.lo(last + 1) < u.end) ++last;
+  const int row0 = u.m * a.row_tile, live = min(a.row_tile, a.rows - row0), c = threadIdx.x;
+  for (int row = blockIdx.y * kCombineRows; row < min(live, (int)(blockIdx.y + 1) * kCombineRows); ++row) {
+    float M = -INFINITY;
+    for (int x = b - 1; x <= last; ++x) M = fmaxf(M, a.ws_ml[(int64_t)kv4_slot(ranges, x, u.begin) * a.row_tile + row].x);
+    float sum = 0.f, acc = 0.f;
+    for (int x = b - 1; x <= last; ++x) {
+      const int64_t s = (int64_t)kv4_slot(ranges, x, u.begin) * a.row_tile + row;
+      const float2 ml = a.ws_ml[s];
+      const float f = ml.x == -INFINITY ? 0.f : ex2(ml.x - M);
+      sum = fmaf(ml.y, f, sum);
+      acc = fmaf(a.ws_o[s * kHeadDim + c], f, acc);
+    }
+    const int rw = row0 + row, nd = rw / a.group, h = u.g * a.group + rw - nd * a.group;
+    using T = typename std::conditional<kBf16, __nv_bfloat16, __half>::type;
+    reinterpret_cast<T*>(a.out + u.r * a.o_req + nd * a.o_tok + h * a.o_head)[c] = from_float<T>(acc / sum);
+    if (a.lse != nullptr && c == 0) a.lse[((int64_t)u.r * a.Hq + h) * a.n + nd] = (M + log2f(sum)) * kLn2;
+  }
+}
+
+int launch_kv4_combine(const Kv4Args& a, int step, bool bf16, cudaStream_t stream) {
+  if (a.ctas < 2) return SEQ_OK;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(a.ctas - 1, (a.row_tile + kCombineRows - 1) / kCombineRows);
+  cfg.blockDim = dim3(kHeadDim);
+  cfg.stream = stream;
+  cudaLaunchAttribute early[1];
+  early[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  early[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = early;
+  cfg.numAttrs = 1;
+  (void)step;
+  if (bf16) SEQ_CUDA_OK(cudaLaunchKernelEx(&cfg, kv4_combine_kernel<32, true>, a));
+  else SEQ_CUDA_OK(cudaLaunchKernelEx(&cfg, kv4_combine_kernel<32, false>, a));
+  return SEQ_OK;
+}
+
+Kv4Args kv4_args(const seq_tree_kv4_attention_params& p) {
+  Kv4Args a = {};
+  a.batch = p.batch; a.n = p.n_tree; a.max_len = p.max_len; a.Hq = p.num_q_heads; a.Hkv = p.num_kv_heads;
+  a.group = p.num_q_heads / p.num_kv_heads;
+  a.rows = a.n * a.group;
+  a.window = p.window; a.sinks = p.sinks;
+  a.num_pages = p.num_pages; a.page_size = p.page_size;
+  a.q = static_cast<const uint8_t*>(p.q); a.q_req = 2 * p.q_stride_req; a.q_tok = 2 * p.q_stride_tok; a.q_head = 2 * p.q_stride_head;
+  a.kt = static_cast<const uint8_t*>(p.k_tree); a.vt = static_cast<const uint8_t*>(p.v_tree);
+  a.t_req = 2 * p.t_stride_req; a.t_tok = 2 * p.t_stride_tok; a.t_head = 2 * p.t_stride_head;
+  a.pages = static_cast<const uint8_t*>(p.pages); a.page_stride = p.page_stride_bytes;
+  a.table = p.page_table; a.table_stride = p.table_stride; a.lengths = p.lengths;
+  a.mask = p.mask_bits; a.mask_wpr = p.mask_words_per_row; a.mask_req = p.mask_stride_req;
+  a.out = static_cast<uint8_t*>(p.out); a.o_req = 2 * p.o_stride_req; a.o_tok = 2 * p.o_stride_tok; a.o_head = 2 * p.o_stride_head;
+  a.lse = p.lse;
+  a.scale_log2 = (p.softmax_scale > 0.f ? p.softmax_scale : 0.08838834764831845f) * kLog2e;
+  a.status = p.dev_status;
+  return a;
+}
+
+static int check_kv4_attention(const seq_tree_kv4_attention_params* p) {
+  if (p == nullptr || p->q == nullptr || p->k_tree == nullptr || p->v_tree == nullptr || p->pages == nullptr || p->page_table == nullptr ||
+      p->lengths == nullptr || p->out == nullptr)
+    return SEQ_ERR_INVALID_ARG;
+  if (p->batch < 1 || p->batch > SEQ_MAX_BATCH || p->n_tree < 1 || p->n_tree > SEQ_MAX_TREE || p->max_len < 0 || p->num_kv_heads < 1 ||
+      p->num_q_heads < 1 || p->num_q_heads % p->num_kv_heads != 0 || p->num_q_heads > 4096 || p->window < 0 || p->window > (1 << 30) || p->sinks < 0 ||
+      p->sinks > (1 << 30) || p->num_pages < 1 || p->max_pages < 1)
+    return SEQ_ERR_INVALID_ARG;
+  if (p->head_dim != kHeadDim || !kv4_page_size_ok(p->page_size) || (p->dtype != SEQ_F16 && p->dtype != SEQ_BF16)) return SEQ_ERR_UNSUPPORTED;
+  if (!(p->softmax_scale >= 0.f || p->softmax_scale < 0.f) || p->softmax_scale > 1e30f) return SEQ_ERR_INVALID_ARG;  // NaN, inf
+  if (p->max_len > (1 << 30) || p->max_len > (int64_t)p->max_pages * p->page_size || p->table_stride < p->max_pages) return SEQ_ERR_INVALID_ARG;
+  if (p->page_stride_bytes < (int64_t)p->num_kv_heads * p->page_size * 136 || p->page_stride_bytes % 16 != 0) return SEQ_ERR_INVALID_ARG;
+  for (const void* x : {p->q, p->k_tree, p->v_tree, p->pages, static_cast<const void*>(p->out)})
+    if (reinterpret_cast<uintptr_t>(x) % 16 != 0) return SEQ_ERR_INVALID_ARG;
+  for (int64_t s : {p->q_stride_req, p->q_stride_tok, p->q_stride_head, p->t_stride_req, p->t_stride_tok, p->t_stride_head, p->o_stride_req,
+                    p->o_stride_tok, p->o_stride_head})
+    if (s < 0 || s % 8 != 0) return SEQ_ERR_INVALID_ARG;
+  if (p->mask_bits != nullptr && (p->mask_words_per_row < (p->n_tree + 31) / 32 || p->mask_stride_req < 0)) return SEQ_ERR_INVALID_ARG;
+  return SEQ_OK;
+}
+
+}  // namespace seqtree
+
+using namespace seqtree;
+
+extern "C" size_t seq_tree_kv4_attention_workspace_bytes(const seq_tree_kv4_attention_params* p) {
+  if (p == nullptr || p->num_kv_heads < 1 || p->num_q_heads < 1 || p->n_tree < 1) return 0;
+  return kv4_rows_workspace_bytes(*p);
+}
+
+extern "C" int seq_tree_kv4_attention(const seq_tree_kv4_attention_params* p, void* stream) {
+  const int rc = check_kv4_attention(p);
+  if (rc != SEQ_OK) return rc;
+  if (p->workspace == nullptr || p->workspace_bytes < seq_tree_kv4_attention_workspace_bytes(p)) return SEQ_ERR_WORKSPACE;
+  if (reinterpret_cast<uintptr_t>(p->workspace) % 256 != 0) return SEQ_ERR_INVALID_ARG;
+  return launch_kv4_rows(*p, static_cast<cudaStream_t>(stream));
+}

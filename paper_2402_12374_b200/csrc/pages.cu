@@ -1,0 +1,620 @@
+// seq_tree_pages_resize, _fork, _compact: the page tables of a paged cache (include/seq_tree.h states what they do).
+//
+// Which page goes where is a chain of counts over all slots and all pages, so one cluster of 16 CTAs plans a call: each CTA
+// owns a sixteenth of the pages, counts its free (or held) ones, reads the other CTAs' counts from their shared memory, and
+// from then on knows the number of every page in its share among all of them.  No order of atomics enters a result: counts
+// are sums, and a page's rank says who gets it.  What is only moved - rows of the table, contents of pages - goes over the
+// whole device: further clusters of the planning launch copy the table's rows, a second launch behind it the pages.
+// Bound by latency for small states (a plan is four exchanges across the cluster), by HBM where pages move.
+#include "common.cuh"
+
+namespace seqtree {
+
+constexpr int kPlanCtas = 16;
+constexpr int kPlanThreads = 1024;
+constexpr int kMoveThreads = 256;
+constexpr int kSlotsPerThread = SEQ_MAX_SLOTS / kPlanThreads;
+
+struct PagesArgs {
+  int32_t slots, max_pages, num_pages, page_size;
+  const int32_t* table; int64_t table_stride;
+  const int32_t* count; const int32_t* refs; const int32_t* lengths;
+  int32_t* table_out; int64_t table_out_stride;
+  int32_t* count_out; int32_t* refs_out; int32_t* lengths_out;
+  const int32_t* tokens; const int32_t* source;
+  int32_t* live;
+  int32_t* ws;  // fork, compact: [0] how many pages move, then from[], to[] (fork: slots each, compact: num_pages each), map[num_pages] (compact)
+  int32_t* status;
+};
+
+__device__ __forceinline__ uint32_t cluster_rank() {
+  uint32_t r;
+  asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+// Also orders the CTAs' global memory accesses: what one wrote before it, every other one reads behind it.
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
+}
+__device__ __forceinline__ int peer_word(const int* p, uint32_t cta) {
+  uint32_t at;
+  int v;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"((uint32_t)__cvta_generic_to_shared(p)), "r"(cta));
+  asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
+  return v;
+}
+
+struct PlanSmem {
+  int32_t before[SEQ_MAX_SLOTS + 1];  // pages that the slots before need
+  int32_t source[SEQ_MAX_SLOTS];      // fork: a slot's source, -1 for none, and the source's length
+  int32_t length[SEQ_MAX_SLOTS];
+  int32_t warp_sum[kPlanThreads / 32];
+  int32_t total;
+  int32_t mine;  // what this CTA counted; read by the others
+  int32_t base, all;
+};
+
+// Exclusive sum of v over the CTA's threads; sm->total is the sum of all.  All threads call it.
+__device__ __forceinline__ int block_scan(PlanSmem* sm, int v) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  int incl = v;
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    const int u = __shfl_up_sync(0xffffffffu, incl, d);
+    if (lane >= d) incl += u;
+  }
+  __syncthreads();  // (the last scan's results are out of use)
+  if (lane == 31) sm->warp_sum[warp] = incl;
+  __syncthreads();
+  if (warp == 0) {
+    const int s = sm->warp_sum[lane];
+    int t = s;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const int u = __shfl_up_sync(0xffffffffu, t, d);
+      if (lane >= d) t += u;
+    }
+    sm->warp_sum[lane] = t - s;
+    if (lane == 31) sm->total = t;
+  }
+  __syncthreads();
+  return sm->warp_sum[warp] + incl - v;
+}
+
+// The CTAs' counts `mine` become sm->base (those of the CTAs before this one) and sm->all.
+__device__ __forceinline__ void cluster_count(PlanSmem* sm, uint32_t rank, int mine) {
+  if (threadIdx.x == 0) sm->mine = mine;
+  cluster_sync();
+  if (threadIdx.x < 32) {
+    const int v = threadIdx.x < kPlanCtas ? peer_word(&sm->mine, threadIdx.x) : 0;
+    const int before = __reduce_add_sync(0xffffffffu, threadIdx.x < rank ? v : 0);
+    const int all = __reduce_add_sync(0xffffffffu, v);
+    if (threadIdx.x == 0) { sm->base = before; sm->all = all; }
+  }
+  cluster_sync();  // (nobody's count is read any more)
+}
+
+// The slot whose pages hold number k: the last with before[slot] <= k
+__device__ __forceinline__ int slot_of(const PlanSmem* sm, int slots, int k) {
+  int lo = 0, hi = slots - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (sm->before[mid] <= k) lo = mid; else hi = mid - 1;
+  }
+  return lo;
+}
+
+__device__ __forceinline__ int ceil_pages(int tokens, int page_size) { return tokens / page_size + (tokens % page_size != 0); }
+
+// One CTA's share of the pages, a multiple of four (16-byte loads; only the last share's end is ragged)
+struct Share { int lo, hi; };
+__device__ __forceinline__ Share share_of(int num_pages, uint32_t rank) {
+  const int per = ((num_pages + kPlanCtas - 1) / kPlanCtas + 3) & ~3;
+  const int64_t lo = (int64_t)per * rank;
+  return {(int)min(lo, (int64_t)num_pages), (int)min(lo + per, (int64_t)num_pages)};
+}
+
+// How slot r is resized: pages before and after
+__device__ __forceinline__ bool wanted_of(const PagesArgs& a, int r, int& have, int& want, bool tell) {
+  have = a.count[r];
+  want = have;
+  if (have < 0 || have > a.max_pages) {
+    if (tell) dev_flag(a.status, SEQ_DEV_BAD_SLOT);
+    have = want = min(max(have, 0), a.max_pages);
+    return false;
+  }
+  const int t = a.tokens[r];
+  if (t < 0) return false;
+  const int w = ceil_pages(t, a.page_size);
+  if (w > a.max_pages) {
+    if (tell) dev_flag(a.status, SEQ_DEV_BAD_SLOT);
+    return false;
+  }
+  want = w;
+  return true;
+}
+
+// Slot r's source if it becomes a fork, else -1
+__device__ __forceinline__ int fork_source(const PagesArgs& a, int r, bool tell) {
+  const int s = a.source[r];
+  if (s < 0) return -1;
+  int ok = s < a.slots && s != r && a.count[r] == 0;
+  if (ok) {
+    const int n = a.lengths[s], have = a.count[s];
+    ok = n >= 0 && have >= 0 && have <= a.max_pages && ceil_pages(n, a.page_size) <= have;
+  }
+  if (!ok && tell) dev_flag(a.status, SEQ_DEV_BAD_SLOT);
+  return ok ? s : -1;
+}
+
+// Rows of a table that is not written in place, by the clusters behind the planning one: a warp a row.  `Mode` 0 resize: the
+// plan writes what lies between the old and the new count.  1 fork: rows of slots that do not become forks.
+template <int kMode>
+__device__ void copy_rows(const PagesArgs& a) {
+  const int lane = threadIdx.x & 31;
+  const int warps = (gridDim.x - kPlanCtas) * (kPlanThreads / 32);
+  for (int r = (blockIdx.x - kPlanCtas) * (kPlanThreads / 32) + (threadIdx.x >> 5); r < a.slots; r += warps) {
+    int have, want;
+    if (kMode == 0) {
+      wanted_of(a, r, have, want, false);
+    } else {
+      if (fork_source(a, r, false) >= 0) continue;
+      have = want = min(max(a.count[r], 0), a.max_pages);
+    }
+    const int keep = min(have, want), end = max(have, want);
+    const int32_t* from = a.table + r * a.table_stride;
+    int32_t* to = a.table_out + r * a.table_out_stride;
+#pragma unroll 8
+    for (int i = lane; i < keep; i += 32) to[i] = from[i];
+    for (int i = end + lane; i < a.max_pages; i += 32) to[i] = -1;
+  }
+}
+
+// The reference counts of this CTA's share into the output
+__device__ __forceinline__ void copy_refs(const PagesArgs& a, Share s) {
+  if (a.refs == a.refs_out) return;
+  if (((reinterpret_cast<uintptr_t>(a.refs) | reinterpret_cast<uintptr_t>(a.refs_out)) & 15) == 0) {
+    const int n4 = (s.hi - s.lo) >> 2;
+    const int4* from = reinterpret_cast<const int4*>(a.refs + s.lo);
+    int4* to = reinterpret_cast<int4*>(a.refs_out + s.lo);
+#pragma unroll 4
+    for (int i = threadIdx.x; i < n4; i += kPlanThreads) to[i] = from[i];
+    for (int i = s.lo + 4 * n4 + threadIdx.x; i < s.hi; i += kPlanThreads) a.refs_out[i] = a.refs[i];
+  } else {
+    for (int i = s.lo + threadIdx.x; i < s.hi; i += kPlanThreads) a.refs_out[i] = a.refs[i];
+  }
+}
+
+// Calls take(rank, page) for the pages of this CTA's share with free(refs_out[page]), in order, until `limit` of all CTAs'
+// are told.  The threads' pages are neighbours, so that a scan of their counts numbers them.
+template <typename Free, typename Take>
+__device__ __forceinline__ void number_pages(PlanSmem* sm, uint32_t rank, Share s, const int32_t* refs, int limit_or_all, Free is_free, Take take, int& total) {
+  int mine = 0;
+  for (int i = s.lo + threadIdx.x; i < s.hi; i += kPlanThreads) mine += is_free(__ldcg(refs + i));
+  block_scan(sm, mine);
+  cluster_count(sm, rank, sm->total);
+  total = sm->all;
+  const int limit = min(limit_or_all, total);
+  int base = sm->base;
+  for (int i0 = s.lo; i0 < s.hi && base < limit; i0 += kPlanThreads) {
+    const int i = i0 + threadIdx.x;
+    const int f = i < s.hi && is_free(__ldcg(refs + i));
+    const int at = base + block_scan(sm, f);
+    if (f && at < limit) take(at, i);
+    base += sm->total;
+  }
+}
+
+__global__ void __launch_bounds__(kPlanThreads, 1) pages_resize_kernel(const PagesArgs a) {
+  __shared__ PlanSmem smem;
+  PlanSmem* sm = &smem;
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  if (blockIdx.x >= kPlanCtas) {
+    copy_rows<0>(a);
+    return;
+  }
+  const uint32_t rank = cluster_rank();
+  const Share share = share_of(a.num_pages, rank);
+  copy_refs(a, share);
+  cluster_sync();
+
+  // What is given up.  A warp a slot.
+  const int lane = threadIdx.x & 31;
+  for (int r = rank * (kPlanThreads / 32) + (threadIdx.x >> 5); r < a.slots; r += kPlanCtas * (kPlanThreads / 32)) {
+    int have, want;
+    wanted_of(a, r, have, want, lane == 0);
+    for (int i = want + lane; i < have; i += 32) {
+      const int page = a.table[r * a.table_stride + i];
+      a.table_out[r * a.table_out_stride + i] = -1;
+      if (page < 0 || page >= a.num_pages) dev_flag(a.status, SEQ_DEV_BAD_PAGE);
+      else atomicSub(a.refs_out + page, 1);
+    }
+  }
+  // Meanwhile, every CTA for itself: how many pages the slots before each one need
+  const int first = threadIdx.x * kSlotsPerThread;
+  int need[kSlotsPerThread], sum = 0;
+#pragma unroll
+  for (int j = 0; j < kSlotsPerThread; ++j) {
+    int have, want;
+    need[j] = 0;
+    if (first + j < a.slots) {
+      wanted_of(a, first + j, have, want, false);
+      need[j] = max(want - have, 0);
+    }
+    sum += need[j];
+  }
+  int at = block_scan(sm, sum);
+#pragma unroll
+  for (int j = 0; j < kSlotsPerThread; ++j) {
+    if (first + j < a.slots) sm->before[first + j] = at;
+    at += need[j];
+  }
+  if (threadIdx.x == 0) sm->before[a.slots] = sm->total;
+  cluster_sync();
+
+  // a reference too many was given up
+  for (int i = share.lo + threadIdx.x; i < share.hi; i += kPlanThreads)
+    if (__ldcg(a.refs_out + i) < 0) {
+      dev_flag(a.status, SEQ_DEV_BAD_SLOT);
+      a.refs_out[i] = 0;
+    }
+  __syncthreads();
+
+  // The free pages, lowest first: number k goes to the slot whose growth holds it, if that fits as a whole.
+  const int needed = sm->before[a.slots];
+  int free_pages = 0;
+  const auto give = [&](int k, int page) {
+    const int r = slot_of(sm, a.slots, k);
+    if (sm->before[r + 1] > sm->all) return;
+    a.table_out[r * a.table_out_stride + a.count[r] + k - sm->before[r]] = page;
+    a.refs_out[page] = 1;
+  };
+  number_pages(sm, rank, share, a.refs_out, needed, [](int v) { return v <= 0; }, give, free_pages);
+  cluster_sync();  // nobody looks at an old count any more (in place they are overwritten now)
+  // the slots' counts, and what is not there for those that do not grow
+  for (int r = rank * kPlanThreads + threadIdx.x; r < a.slots; r += kPlanCtas * kPlanThreads) {
+    int have, want;
+    const bool sound = wanted_of(a, r, have, want, false);
+    const bool grows = want > have;
+    const bool fits = !grows || sm->before[r + 1] <= free_pages;
+    if (!fits) {
+      dev_flag(a.status, SEQ_DEV_NO_PAGES);
+      for (int i = have; i < want; ++i) a.table_out[r * a.table_out_stride + i] = -1;
+    }
+    const int c = fits ? want : have;
+    if (a.count_out != a.count || (sound && c != have)) a.count_out[r] = c;
+  }
+}
+
+__global__ void __launch_bounds__(kPlanThreads, 1) pages_fork_kernel(const PagesArgs a) {
+  __shared__ PlanSmem smem;
+  PlanSmem* sm = &smem;
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  if (blockIdx.x >= kPlanCtas) {
+    copy_rows<1>(a);
+    return;
+  }
+  const uint32_t rank = cluster_rank();
+  const Share share = share_of(a.num_pages, rank);
+  copy_refs(a, share);
+  const int first = threadIdx.x * kSlotsPerThread;
+  int need[kSlotsPerThread], sum = 0;
+#pragma unroll
+  for (int j = 0; j < kSlotsPerThread; ++j) {
+    need[j] = 0;
+    if (first + j < a.slots) {
+      const int s = fork_source(a, first + j, rank == 0);
+      const int n = s >= 0 ? a.lengths[s] : 0;
+      sm->source[first + j] = s;  // (kept: in place, counts and lengths change below)
+      sm->length[first + j] = n;
+      need[j] = n % a.page_size != 0;
+    }
+    sum += need[j];
+  }
+  int at = block_scan(sm, sum);
+#pragma unroll
+  for (int j = 0; j < kSlotsPerThread; ++j) {
+    if (first + j < a.slots) sm->before[first + j] = at;
+    at += need[j];
+  }
+  if (threadIdx.x == 0) sm->before[a.slots] = sm->total;
+  cluster_sync();
+
+  const int needed = sm->before[a.slots];
+  int32_t* from = a.ws + 1;
+  int32_t* to = from + a.slots;
+  int free_pages = 0;
+  const auto give = [&](int k, int page) {
+    const int r = slot_of(sm, a.slots, k);
+    const int s = sm->source[r], full = sm->length[r] / a.page_size;
+    const int old = a.table[s * a.table_stride + full];
+    const bool good = old >= 0 && old < a.num_pages;
+    if (!good) dev_flag(a.status, SEQ_DEV_BAD_PAGE);
+    from[k] = good ? old : page;
+    to[k] = page;
+    a.table_out[r * a.table_out_stride + full] = page;
+  };
+  number_pages(sm, rank, share, a.refs_out, needed, [](int v) { return v <= 0; }, give, free_pages);
+  const int given = min(needed, free_pages);
+  if (rank == 0 && threadIdx.x == 0) a.ws[0] = given;
+  cluster_sync();  // every free page is numbered: from here on counts change
+  for (int k = rank * kPlanThreads + threadIdx.x; k < given; k += kPlanCtas * kPlanThreads) a.refs_out[__ldcg(to + k)] = 1;
+  // The forks' rows, a warp each
+  const int lane = threadIdx.x & 31;
+  for (int r = rank * (kPlanThreads / 32) + (threadIdx.x >> 5); r < a.slots; r += kPlanCtas * (kPlanThreads / 32)) {
+    const int s = sm->source[r], n = sm->length[r];
+    const bool copied = sm->before[r + 1] > sm->before[r];
+    const bool fits = s >= 0 && (!copied || sm->before[r + 1] <= free_pages);
+    if (s >= 0) {
+      const int full = fits ? n / a.page_size : 0, held = fits ? full + copied : 0;
+      int32_t* row = a.table_out + r * a.table_out_stride;
+      for (int i = lane; i < a.max_pages; i += 32) {
+        if (i < full) {
+          const int page = a.table[s * a.table_stride + i];
+          row[i] = page;
+          if (page < 0 || page >= a.num_pages) dev_flag(a.status, SEQ_DEV_BAD_PAGE);
+          else atomicAdd(a.refs_out + page, 1);
+        } else if (i >= held) {
+          row[i] = -1;
+        }
+      }
+      if (!fits && lane == 0) dev_flag(a.status, SEQ_DEV_NO_PAGES);
+      if (lane == 0) {
+        if (fits || a.count_out != a.count) a.count_out[r] = held;
+        if (fits) a.lengths_out[r] = n;
+        else if (a.lengths_out != a.lengths) a.lengths_out[r] = a.lengths[r];
+      }
+    } else if (lane == 0) {
+      if (a.count_out != a.count) a.count_out[r] = min(max(a.count[r], 0), a.max_pages);
+      if (a.lengths_out != a.lengths) a.lengths_out[r] = a.lengths[r];
+    }
+  }
+}
+
+__global__ void __launch_bounds__(kPlanThreads, 1) pages_compact_kernel(const PagesArgs a) {
+  __shared__ PlanSmem smem;
+  PlanSmem* sm = &smem;
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const uint32_t rank = cluster_rank();
+  const Share share = share_of(a.num_pages, rank);
+  int32_t* from = a.ws + 1;
+  int32_t* to = from + a.num_pages;
+  int32_t* map = to + a.num_pages;
+  int mine = 0;
+  for (int i = share.lo + threadIdx.x; i < share.hi; i += kPlanThreads) {
+    const int v = a.refs[i];
+    mine += v > 0;
+    if (v < 0) dev_flag(a.status, SEQ_DEV_BAD_SLOT);
+  }
+  block_scan(sm, mine);
+  cluster_count(sm, rank, sm->total);
+  const int live = sm->all;
+  // far = held pages from `live` on, holes = free ones below it: as many of the one as of the other
+  const Share below = {min(share.lo, live), min(share.hi, live)}, above = {max(share.lo, live), max(share.hi, live)};
+  int holes = 0, far = 0;
+  number_pages(sm, rank, below, a.refs, 0x7fffffff, [](int v) { return v <= 0; }, [&](int k, int page) { to[k] = page; }, holes);
+  number_pages(sm, rank, above, a.refs, 0x7fffffff, [](int v) { return v > 0; }, [&](int k, int page) { from[k] = page; }, far);
+  if (rank == 0 && threadIdx.x == 0) {
+    a.ws[0] = far;
+    if (a.live != nullptr) *a.live = live;
+  }
+  cluster_sync();  // both lists are there
+  // Where each held page is found (the table is rewritten by it), and the counts.  A page that moves is written by the holder
+  // of its number in the lists, the others by the holder of their share.
+  for (int i = below.lo + threadIdx.x; i < below.hi; i += kPlanThreads) {
+    const int v = a.refs[i];
+    map[i] = v > 0 ? i : -1;
+    if (a.refs_out != a.refs && v > 0) a.refs_out[i] = v;
+  }
+  for (int i = above.lo + threadIdx.x; i < above.hi; i += kPlanThreads)
+    if (a.refs[i] <= 0) {
+      map[i] = -1;
+      if (a.refs_out != a.refs || a.refs[i] < 0) a.refs_out[i] = 0;
+    }
+  cluster_sync();  // (in place: what is moved below was free above)
+  for (int k = rank * kPlanThreads + threadIdx.x; k < far; k += kPlanCtas * kPlanThreads) {
+    const int p = __ldcg(from + k), q = __ldcg(to + k);
+    const int v = a.refs[p];
+    map[p] = q;
+    a.refs_out[q] = v;
+    a.refs_out[p] = 0;
+  }
+}
+
+struct MoveArgs {
+  const int32_t* list;  // [0] how many, then from[stride], to[stride]
+  int32_t list_stride, num_pages;
+  uint8_t* pages; int32_t planes; int64_t plane_stride, page_stride; int32_t chunks;  // pieces of a plane's page
+  int64_t page_bytes;
+  // the table, rewritten by `map` where there is one
+  const int32_t* map; int32_t slots, max_pages;
+  const int32_t* table; int64_t table_stride; const int32_t* count;
+  int32_t* table_out; int64_t table_out_stride;
+  int32_t* status;
+};
+
+constexpr int kMoveUnroll = 8;
+constexpr int kMoveChunk = kMoveThreads * kMoveUnroll * 16;  // bytes a CTA moves at a time
+
+__global__ void __launch_bounds__(kMoveThreads) pages_move_kernel(const MoveArgs a) {
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  if (a.map != nullptr) {
+    for (int r = blockIdx.x; r < a.slots; r += gridDim.x) {
+      const int have = a.count[r];
+      const bool bad = have < 0 || have > a.max_pages;
+      if (bad && threadIdx.x == 0) dev_flag(a.status, SEQ_DEV_BAD_SLOT);
+      if (bad && a.table == a.table_out) continue;
+      for (int i = threadIdx.x; i < a.max_pages; i += kMoveThreads) {
+        if (i >= have && a.table == a.table_out) break;
+        int page = -1;
+        if (i < have && !bad) {
+          page = a.table[r * a.table_stride + i];
+          if (page < 0 || page >= a.num_pages) {
+            dev_flag(a.status, SEQ_DEV_BAD_PAGE);
+            page = -1;
+          } else {
+            page = a.map[page];
+            if (page < 0) dev_flag(a.status, SEQ_DEV_BAD_SLOT);  // held, but counted as free
+          }
+        }
+        a.table_out[r * a.table_out_stride + i] = page;
+      }
+    }
+  }
+  const int64_t per_page = (int64_t)a.planes * a.chunks;
+  const int64_t total = a.list[0] * per_page;
+  for (int64_t w = blockIdx.x; w < total; w += gridDim.x) {
+    const int k = (int)(w / per_page);
+    const int rest = (int)(w - k * per_page), x = rest / a.chunks, c = rest - x * a.chunks;
+    const int src = a.list[1 + k], dst = a.list[1 + a.list_stride + k];
+    if (src == dst) continue;
+    const int64_t at = (int64_t)c * kMoveChunk + threadIdx.x * 16;
+    const uint8_t* from = a.pages + src * a.page_stride + x * a.plane_stride + at;
+    uint8_t* to = a.pages + dst * a.page_stride + x * a.plane_stride + at;
+    const int64_t left = a.page_bytes - at;
+    uint4 v[kMoveUnroll];
+#pragma unroll
+    for (int u = 0; u < kMoveUnroll; ++u)
+      if (u * kMoveThreads * 16 < left) v[u] = __ldcs(reinterpret_cast<const uint4*>(from + u * kMoveThreads * 16));
+#pragma unroll
+    for (int u = 0; u < kMoveUnroll; ++u)
+      if (u * kMoveThreads * 16 < left) __stcs(reinterpret_cast<uint4*>(to + u * kMoveThreads * 16), v[u]);
+  }
+}
+
+// ---------------------------------------------------------------- host side ---------------------
+static int check_pages(const seq_tree_pages_params* p) {
+  if (p == nullptr || p->page_table == nullptr || p->page_count == nullptr || p->ref_count == nullptr || p->table_out == nullptr ||
+      p->refs_out == nullptr)
+    return SEQ_ERR_INVALID_ARG;
+  if (p->slots < 1 || p->slots > SEQ_MAX_SLOTS || p->max_pages < 1 || p->max_pages >= (1 << 30) || p->num_pages < 1 || p->num_pages >= (1 << 30) ||
+      p->table_stride < p->max_pages || p->table_out_stride < p->max_pages)
+    return SEQ_ERR_INVALID_ARG;
+  // all arrays in place, or none: what copies rows of the one reads the others while the plan writes them
+  const bool in_place = p->table_out == p->page_table;
+  if (in_place != (p->refs_out == p->ref_count) || (in_place && p->table_out_stride != p->table_stride)) return SEQ_ERR_INVALID_ARG;
+  return SEQ_OK;
+}
+static int check_pool(const seq_tree_pages_params* p) {
+  if (p->pages == nullptr || reinterpret_cast<uintptr_t>(p->pages) % 16 != 0 || p->num_planes < 1) return SEQ_ERR_INVALID_ARG;
+  if (p->page_bytes < 16 || p->page_bytes % 16 != 0 || p->page_stride_bytes < p->page_bytes || p->page_stride_bytes % 16 != 0) return SEQ_ERR_INVALID_ARG;
+  if (p->num_planes > 1 && (p->plane_stride_bytes < p->page_bytes || p->plane_stride_bytes % 16 != 0)) return SEQ_ERR_INVALID_ARG;
+  if (p->page_bytes / kMoveChunk > (1 << 24)) return SEQ_ERR_INVALID_ARG;
+  if (p->workspace == nullptr || p->workspace_bytes < seq_tree_pages_workspace_bytes(p)) return SEQ_ERR_WORKSPACE;
+  if (reinterpret_cast<uintptr_t>(p->workspace) % 16 != 0) return SEQ_ERR_INVALID_ARG;
+  return SEQ_OK;
+}
+
+static PagesArgs pages_args(const seq_tree_pages_params* p) {
+  PagesArgs a;
+  a.slots = p->slots; a.max_pages = p->max_pages; a.num_pages = p->num_pages; a.page_size = p->page_size;
+  a.table = p->page_table; a.table_stride = p->table_stride; a.count = p->page_count; a.refs = p->ref_count; a.lengths = p->lengths;
+  a.table_out = p->table_out; a.table_out_stride = p->table_out_stride;
+  a.count_out = p->count_out; a.refs_out = p->refs_out; a.lengths_out = p->lengths_out;
+  a.tokens = p->tokens; a.source = p->source; a.live = p->live;
+  a.ws = static_cast<int32_t*>(p->workspace); a.status = p->dev_status;
+  return a;
+}
+
+template <typename Kernel>
+static int launch_plan(Kernel kernel, int* done, const seq_tree_pages_params* p, bool rows_are_copied, void* stream) {
+  const int rc = once_per_device(done, [&]() -> int {
+    SEQ_CUDA_OK(cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
+    return SEQ_OK;
+  });
+  if (rc != SEQ_OK) return rc;
+  // clusters that copy the table: one for every 64 Ki entries, no more than there is room for beside the plan
+  int copiers = 0;
+  if (rows_are_copied) {
+    const int64_t want = ((int64_t)p->slots * p->max_pages + 65535) / 65536;
+    copiers = (int)(want < 6 ? want : 6);
+  }
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(kPlanCtas * (1 + copiers));
+  cfg.blockDim = dim3(kPlanThreads);
+  cfg.stream = static_cast<cudaStream_t>(stream);
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = kPlanCtas; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  SEQ_CUDA_OK(cudaLaunchKernelEx(&cfg, kernel, pages_args(p)));
+  return SEQ_OK;
+}
+
+static int launch_move(const seq_tree_pages_params* p, int list_stride, const int32_t* map, int64_t most_pages, void* stream) {
+  MoveArgs a;
+  a.list = static_cast<const int32_t*>(p->workspace); a.list_stride = list_stride; a.num_pages = p->num_pages;
+  a.pages = static_cast<uint8_t*>(p->pages); a.planes = p->num_planes; a.plane_stride = p->plane_stride_bytes; a.page_stride = p->page_stride_bytes;
+  a.chunks = (int)((p->page_bytes + kMoveChunk - 1) / kMoveChunk);
+  a.page_bytes = p->page_bytes;
+  a.map = map; a.slots = p->slots; a.max_pages = p->max_pages;
+  a.table = p->page_table; a.table_stride = p->table_stride; a.count = p->page_count;
+  a.table_out = p->table_out; a.table_out_stride = p->table_out_stride;
+  a.status = p->dev_status;
+  int64_t want = most_pages * a.planes * a.chunks;
+  if (map != nullptr && want < p->slots) want = p->slots;
+  const int64_t cap = (int64_t)device_sm_count() * 8;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(want < cap ? want : cap));
+  cfg.blockDim = dim3(kMoveThreads);
+  cfg.stream = static_cast<cudaStream_t>(stream);
+  cudaLaunchAttribute early[1];
+  early[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  early[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = early;
+  cfg.numAttrs = 1;
+  SEQ_CUDA_OK(cudaLaunchKernelEx(&cfg, pages_move_kernel, a));
+  return SEQ_OK;
+}
+
+}  // namespace seqtree
+
+using namespace seqtree;
+
+extern "C" size_t seq_tree_pages_workspace_bytes(const seq_tree_pages_params* p) {
+  if (p == nullptr || p->slots < 1 || p->num_pages < 1) return 0;
+  const size_t fork = 1 + 2 * (size_t)p->slots, compact = 1 + 3 * (size_t)p->num_pages;
+  return (fork > compact ? fork : compact) * sizeof(int32_t);
+}
+
+extern "C" int seq_tree_pages_resize(const seq_tree_pages_params* p, void* stream) {
+  const int rc = check_pages(p);
+  if (rc != SEQ_OK) return rc;
+  if (p->tokens == nullptr || p->count_out == nullptr || p->page_size < 1) return SEQ_ERR_INVALID_ARG;
+  if ((p->count_out == p->page_count) != (p->table_out == p->page_table)) return SEQ_ERR_INVALID_ARG;
+  static int done[64];
+  return launch_plan(pages_resize_kernel, done, p, p->table_out != p->page_table, stream);
+}
+
+extern "C" int seq_tree_pages_fork(const seq_tree_pages_params* p, void* stream) {
+  int rc = check_pages(p);
+  if (rc != SEQ_OK) return rc;
+  if (p->source == nullptr || p->lengths == nullptr || p->lengths_out == nullptr || p->count_out == nullptr || p->page_size < 1) return SEQ_ERR_INVALID_ARG;
+  const bool in_place = p->table_out == p->page_table;
+  if ((p->count_out == p->page_count) != in_place || (p->lengths_out == p->lengths) != in_place) return SEQ_ERR_INVALID_ARG;
+  rc = check_pool(p);
+  if (rc != SEQ_OK) return rc;
+  static int done[64];
+  rc = launch_plan(pages_fork_kernel, done, p, p->table_out != p->page_table, stream);
+  if (rc != SEQ_OK) return rc;
+  return launch_move(p, p->slots, nullptr, p->slots, stream);
+}
+
+extern "C" int seq_tree_pages_compact(const seq_tree_pages_params* p, void* stream) {
+  int rc = check_pages(p);
+  if (rc != SEQ_OK) return rc;
+  rc = check_pool(p);
+  if (rc != SEQ_OK) return rc;
+  static int done[64];
+  rc = launch_plan(pages_compact_kernel, done, p, false, stream);
+  if (rc != SEQ_OK) return rc;
+  const int32_t* map = static_cast<const int32_t*>(p->workspace) + 1 + 2 * (size_t)p->num_pages;
+  return launch_move(p, p->num_pages, map, p->num_pages, stream);
+}
