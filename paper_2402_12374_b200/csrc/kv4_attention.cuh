@@ -32,7 +32,6 @@ struct Kv4Args {
 
 struct Kv4Plan {
   int32_t start[SEQ_MAX_BATCH + 1];  // steps before each request's
-  int32_t len[SEQ_MAX_BATCH];        // its prefix, -1: idle
   int32_t warp_sum[32];
 };
 
@@ -51,6 +50,9 @@ __device__ __forceinline__ Kv4Prefix kv4_prefix(const Kv4Args& a, int L) {
   return {sink_steps + max(all - window_step, 0), sink_steps, window_step - sink_steps};
 }
 
+// Request r's prefix; -1: idle
+__device__ __forceinline__ int kv4_len(const Kv4Args& a, int r) { return min(max(a.lengths[r], -1), a.max_len); }
+
 // Every thread of the CTA calls it; the plan is there behind the next barrier that it ends with.
 template <int kStep, int kThreads>
 __device__ __forceinline__ void kv4_plan(Kv4Plan* plan, const Kv4Args& a) {
@@ -58,12 +60,8 @@ __device__ __forceinline__ void kv4_plan(Kv4Plan* plan, const Kv4Args& a) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   int sum = 0;
   for (int j = first; j < first + per && j < a.batch; ++j) {
-    int L = a.lengths[j];
-    if (L > a.max_len) {
-      if (blockIdx.x == 0) dev_flag(a.status, SEQ_DEV_BAD_LENGTH);
-      L = a.max_len;
-    }
-    plan->len[j] = max(L, -1);
+    const int L = kv4_len(a, j);
+    if (blockIdx.x == 0 && a.lengths[j] > a.max_len) dev_flag(a.status, SEQ_DEV_BAD_LENGTH);
     if (L >= 0) sum += a.Hkv * a.tiles * (kv4_prefix<kStep>(a, L).steps + a.tree_steps);
   }
   int incl = sum;
@@ -78,7 +76,7 @@ __device__ __forceinline__ void kv4_plan(Kv4Plan* plan, const Kv4Args& a) {
   for (int w = 0; w < warp; ++w) at += plan->warp_sum[w];
   for (int j = first; j < first + per && j < a.batch; ++j) {
     plan->start[j] = at;
-    const int L = plan->len[j];
+    const int L = kv4_len(a, j);
     if (L >= 0) at += a.Hkv * a.tiles * (kv4_prefix<kStep>(a, L).steps + a.tree_steps);
     if (j == a.batch - 1) plan->start[a.batch] = at;
   }
@@ -109,8 +107,8 @@ __device__ __forceinline__ Kv4Unit kv4_unit(const Kv4Plan* plan, const Kv4Args& 
   }
   Kv4Unit u;
   u.r = lo;
-  u.L = plan->len[lo];
-  u.prefix = kv4_prefix<kStep>(a, max(u.L, 0));
+  u.L = max(kv4_len(a, lo), 0);
+  u.prefix = kv4_prefix<kStep>(a, u.L);
   const int steps = u.prefix.steps + a.tree_steps, rem = pos - plan->start[lo], x = rem / steps;
   u.g = x / a.tiles;
   u.m = x - u.g * a.tiles;
@@ -152,6 +150,8 @@ __device__ __forceinline__ uint32_t kv4_window_word(const Kv4Args& a, int r, int
 
 size_t kv4_rows_workspace_bytes(const seq_tree_kv4_attention_params& p);
 int launch_kv4_rows(const seq_tree_kv4_attention_params& p, cudaStream_t stream);
+size_t kv4_tiles_workspace_bytes(const seq_tree_kv4_attention_params& p);
+int launch_kv4_tiles(const seq_tree_kv4_attention_params& p, cudaStream_t stream);
 // Arguments that do not depend on the kernel
 Kv4Args kv4_args(const seq_tree_kv4_attention_params& p);
 // Adds the pieces that `ctas` CTAs left: steps of `step` keys

@@ -52,9 +52,8 @@ int launch_kv4_combine(const Kv4Args& a, int step, bool bf16, cudaStream_t strea
   early[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = early;
   cfg.numAttrs = 1;
-  (void)step;
-  if (bf16) SEQ_CUDA_OK(cudaLaunchKernelEx(&cfg, kv4_combine_kernel<32, true>, a));
-  else SEQ_CUDA_OK(cudaLaunchKernelEx(&cfg, kv4_combine_kernel<32, false>, a));
+  if (step == 32) SEQ_CUDA_OK(cudaLaunchKernelEx(&cfg, bf16 ? kv4_combine_kernel<32, true> : kv4_combine_kernel<32, false>, a));
+  else SEQ_CUDA_OK(cudaLaunchKernelEx(&cfg, bf16 ? kv4_combine_kernel<128, true> : kv4_combine_kernel<128, false>, a));
   return SEQ_OK;
 }
 
@@ -77,6 +76,9 @@ Kv4Args kv4_args(const seq_tree_kv4_attention_params& p) {
   a.status = p.dev_status;
   return a;
 }
+
+// The kernel in registers takes 16 query rows of a kv head at a time, the tensor-core one 128.
+static bool few_rows(const seq_tree_kv4_attention_params& p) { return p.n_tree * (p.num_q_heads / p.num_kv_heads) <= 16; }
 
 static int check_kv4_attention(const seq_tree_kv4_attention_params* p) {
   if (p == nullptr || p->q == nullptr || p->k_tree == nullptr || p->v_tree == nullptr || p->pages == nullptr || p->page_table == nullptr ||
@@ -105,7 +107,7 @@ using namespace seqtree;
 
 extern "C" size_t seq_tree_kv4_attention_workspace_bytes(const seq_tree_kv4_attention_params* p) {
   if (p == nullptr || p->num_kv_heads < 1 || p->num_q_heads < 1 || p->n_tree < 1) return 0;
-  return kv4_rows_workspace_bytes(*p);
+  return few_rows(*p) ? kv4_rows_workspace_bytes(*p) : kv4_tiles_workspace_bytes(*p);
 }
 
 extern "C" int seq_tree_kv4_attention(const seq_tree_kv4_attention_params* p, void* stream) {
@@ -113,5 +115,5 @@ extern "C" int seq_tree_kv4_attention(const seq_tree_kv4_attention_params* p, vo
   if (rc != SEQ_OK) return rc;
   if (p->workspace == nullptr || p->workspace_bytes < seq_tree_kv4_attention_workspace_bytes(p)) return SEQ_ERR_WORKSPACE;
   if (reinterpret_cast<uintptr_t>(p->workspace) % 256 != 0) return SEQ_ERR_INVALID_ARG;
-  return launch_kv4_rows(*p, static_cast<cudaStream_t>(stream));
+  return few_rows(*p) ? launch_kv4_rows(*p, static_cast<cudaStream_t>(stream)) : launch_kv4_tiles(*p, static_cast<cudaStream_t>(stream));
 }

@@ -1,0 +1,626 @@
+// Attention over the 4-bit pages on the 5th-generation tensor cores: tiles of 128 query rows against 128 keys.
+//
+//     S = Q K^T   128x128x128, both operands in shared memory
+//     P = 2^(scale*S - m), masked, a thread a row, half precision, over S in tensor memory
+//     O += P V    128x128x128, P from tensor memory, V from shared memory
+//
+// What is special is where K and V come from.  Bulk copies bring granules (16 tokens, 2176 bytes) of 4-bit codes into a ring;
+// four warps turn them into half-precision tiles in the layout that the tensor core reads (128-byte swizzle): scale * (code - 8) +
+// mid, one rounding.  Eight channels leave a code word in the order 0,4,1,5,2,6,3,7 (two nibbles of a 32-bit word per instruction);
+// Q's channels are stored in that order too, and O's columns are put back when the rows are written.  The tree's 16-bit rows go
+// through the same warps.
+//
+// Two chains of four row warps, each with its own S/P and O in tensor memory, keep the tensor core busy in turn: with kTwo a
+// unit is 256 rows, a chain has a 128-row tile of its own and both use every K/V tile; otherwise a unit is 128 rows, the
+// chains take the key tiles in turns and meet at the unit's end.  One warp each issues a chain's products.
+//
+// Every mbarrier wait is bounded; one that runs out raises SEQ_DEV_TIMEOUT and the CTA drains.
+#include "kv4_attention.cuh"
+#include "umma.cuh"
+
+namespace seqtree {
+
+constexpr int kTilesThreads = 512;  // warp groups: loader and two issuers; codes to halves; chain A; chain B
+constexpr int kTilesStep = 128;     // keys
+constexpr int kRegsIssue = 40, kRegsUnpack = 96, kRegsChain = 184;  // 40 + 96 + 2 * 184 = 504 <= 4 * 128
+constexpr int kHalfKeys = 64;       // keys of a ring stage
+constexpr int kStageBytes = kHalfKeys / kGranule * kGranuleBytes;
+constexpr int kTreeTiles = SEQ_MAX_TREE / kTilesStep;
+
+template <bool kTwo>
+struct TilesSmem {
+  static constexpr int kStages = kTwo ? 3 : 6;
+  uint8_t q[kTwo ? 2 : 1][kTileBytes];  // tiles: 1024-byte aligned
+  uint8_t k[2][kTileBytes];
+  uint8_t v[2][kTileBytes];
+  uint8_t ring[kStages][kStageBytes];
+  uint64_t raw_full[kStages], raw_empty[kStages];
+  uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2];  // [tile parity]
+  uint64_t q_full[2], s_full[2], p_full[2], pv_done[2];   // [chain]
+  uint64_t drained[2];
+  float2 ml[2][kTileM];  // the chains' (m, l), where they share rows
+  uint32_t bad[4][kTreeTiles][4];  // [segment mod 4]: tree rows whose V is not finite in half precision
+  uint32_t tmem_base;
+  volatile int abort_flag;
+  Kv4Plan plan;
+};
+template <bool kTwo>
+constexpr size_t tiles_smem_bytes() { return sizeof(TilesSmem<kTwo>) + 1024; }
+static_assert(tiles_smem_bytes<true>() <= 227 * 1024 && tiles_smem_bytes<false>() <= 227 * 1024, "one CTA's shared memory");
+
+__device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+               ::"r"(smem_u32(dst)), "l"(src), "r"(bytes), "r"(smem_u32(bar)) : "memory");
+}
+__device__ __forceinline__ void sts128(uint32_t at, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
+__device__ __forceinline__ uint32_t bits_below(int x) { return x <= 0 ? 0u : (x >= 32 ? 0xffffffffu : (1u << x) - 1u); }
+
+// The steps of a unit that fall into a CTA's range.  Steps of the tree behind the unit's last node are nobody's.
+struct TilesSeg {
+  Kv4Unit u;
+  int32_t end, next, t0, steps;  // positions [pos, end), the next segment, first step, how many steps there are to do
+  bool whole;
+};
+__device__ __forceinline__ TilesSeg tiles_seg(const Kv4Plan* plan, const Kv4Args& a, int pos, int range_hi) {
+  TilesSeg s;
+  s.u = kv4_unit<kTilesStep>(plan, a, pos);
+  s.end = s.next = min(s.u.end, range_hi);
+  s.whole = pos == s.u.begin && s.end == s.u.end;
+  const int nodes = min(a.n, ((s.u.m + 1) * a.row_tile + a.group - 1) / a.group);
+  const int live_end = s.u.begin + s.u.prefix.steps + (nodes + kTilesStep - 1) / kTilesStep;
+  s.t0 = pos - s.u.begin;
+  s.steps = max(min(s.end, live_end) - pos, 0);
+  return s;
+}
+
+template <bool kTwo, bool kBf16>
+__global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Args a) {
+  extern __shared__ uint8_t smem_raw[];
+  using Smem = TilesSmem<kTwo>;
+  constexpr int kStages = Smem::kStages;
+  Smem* sm = reinterpret_cast<Smem*>(smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u));
+  const int warp = uniform((int)threadIdx.x >> 5), lane = threadIdx.x & 31;
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < kStages; ++s) { mbar_init(&sm->raw_full[s], 1); mbar_init(&sm->raw_empty[s], 4); }
+    for (int b = 0; b < 2; ++b) {
+      mbar_init(&sm->k_full[b], 4); mbar_init(&sm->k_empty[b], kTwo ? 2 : 1);
+      mbar_init(&sm->v_full[b], 4); mbar_init(&sm->v_empty[b], kTwo ? 2 : 1);
+      mbar_init(&sm->q_full[b], kTwo ? 4 : 8);
+      mbar_init(&sm->s_full[b], 1); mbar_init(&sm->p_full[b], 4); mbar_init(&sm->pv_done[b], 1);
+      mbar_init(&sm->drained[b], 1);
+    }
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    sm->abort_flag = 0;
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  }
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  if (warp == 1) {  // all 512 tensor-memory columns
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&sm->tmem_base)) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  kv4_plan<kTilesStep, kTilesThreads>(&sm->plan, a);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = uniform(sm->tmem_base);
+  const Kv4Ranges ranges = kv4_ranges(&sm->plan, a);
+  const bool works = (int)blockIdx.x < ranges.ctas && ranges.total > 0;
+  const int range_lo = works ? ranges.lo(blockIdx.x) : 0, range_hi = works ? ranges.lo(blockIdx.x + 1) : 0;
+
+  if (warp < 4) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsIssue));
+    if (warp == 0) {
+      // ============================ loader: 64 keys a stage ============================
+      int issued = 0;
+      int r_known = -1, page0 = 0, id = 0;  // lane x holds the number of request r_known's page page0 + x
+      bool ok = true;
+      for (int pos = range_lo; pos < range_hi && ok;) {
+        const TilesSeg sg = tiles_seg(&sm->plan, a, pos, range_hi);
+        for (int i = 0; i < sg.steps && ok; ++i) {
+          if (sg.t0 + i >= sg.u.prefix.steps) break;  // the tree's
+          for (int h = 0; h < 2; ++h) {
+            const int key = sg.u.prefix.key_step(sg.t0 + i) * kTilesStep + h * kHalfKeys;
+            if (key >= sg.u.L) break;
+            const int granules = min(kHalfKeys / kGranule, (sg.u.L - key + kGranule - 1) / kGranule);
+            const int st = issued % kStages, w = issued / kStages;
+            const int first = key / a.page_size, last = (key + granules * kGranule - 1) / a.page_size;
+            if (r_known != sg.u.r || first < page0 || last >= page0 + 32) {
+              r_known = sg.u.r;
+              page0 = first;
+              const int x = first + lane;
+              id = 0;
+              if ((int64_t)x * a.page_size < sg.u.L) {
+                id = a.table[sg.u.r * a.table_stride + x];
+                if ((unsigned)id >= (unsigned)a.num_pages) {
+                  dev_flag(a.status, SEQ_DEV_BAD_PAGE);
+                  id = 0;
+                }
+              }
+            }
+            if (w > 0 && !mbar_wait(sm, &sm->raw_empty[st], (w - 1) & 1, a.status)) { ok = false; break; }
+            if (lane == 0) mbar_expect_tx(&sm->raw_full[st], granules * kGranuleBytes);
+            __syncwarp();
+            // lane x: the x-th page's part
+            const int per = min(kHalfKeys, a.page_size) / kGranule;  // granules of a page in the stage
+            const int mine = __shfl_sync(0xffffffffu, id, (first - page0 + lane) & 31);
+            if (lane * per < granules) {
+              const uint8_t* src = a.pages + mine * a.page_stride + (int64_t)sg.u.g * a.page_size * 136 + (key & (a.page_size - 1)) / kGranule * kGranuleBytes;
+              bulk_load(sm->ring[st] + lane * per * kGranuleBytes, src, min(per, granules - lane * per) * kGranuleBytes, &sm->raw_full[st]);
+            }
+            __syncwarp();
+            ++issued;
+          }
+        }
+        pos = sg.next;
+      }
+      // (after a wait that ran out: nobody leaves while a copy into its shared memory is under way)
+      if (sm->abort_flag)
+        for (int x = max(issued - kStages, 0); x < issued; ++x)
+          for (uint32_t it = 0; it < (1u << 16); ++it)
+            if (mbar_try_wait(&sm->raw_full[x % kStages], (x / kStages) & 1)) break;
+    } else if (warp < 3) {
+      // ============================ issuer of a chain ============================
+      const int c = warp - 1;
+      const uint32_t tmem_o = tmem + 128u * c, tmem_s = tmem + 256u + 128u * c;
+      const uint32_t idesc = (1u << 4) | ((uint32_t)(kTileM >> 4) << 24) | ((uint32_t)(kTilesStep >> 3) << 17);  // fp16, sums fp32, N = 128
+      const uint32_t idesc_pv = idesc | (1u << 16);                                                             // V is MN-major
+      int step = 0, done = 0, seg = 0;  // K/V tiles before this segment, this chain's products, segments
+      bool ok = true;
+      for (int pos = range_lo; pos < range_hi && ok; ++seg) {
+        const TilesSeg sg = tiles_seg(&sm->plan, a, pos, range_hi);
+        ok = mbar_wait(sm, &sm->q_full[c], seg & 1, a.status);
+        const uint32_t q_lo = desc_lo(smem_u32(sm->q[kTwo ? c : 0]), 16);
+        bool first = true;
+        for (int i = 0; i < sg.steps && ok; ++i) {
+          const int x = step + i, b = x & 1, w = x >> 1;
+          if (!kTwo && b != c) continue;
+          // S goes where the last P was: its product has completed
+          ok = mbar_wait(sm, &sm->k_full[b], w & 1, a.status) && (done == 0 || mbar_wait(sm, &sm->pv_done[c], (done - 1) & 1, a.status));
+          if (!ok) break;
+          tc_fence_after();
+          if (elect_one()) {
+            mma_qk<kHalfBytes, kHalfBytes>(tmem_s, q_lo, desc_lo(smem_u32(sm->k[b]), 16), idesc);
+            tc_commit(&sm->s_full[c]);
+            tc_commit(&sm->k_empty[b]);
+          }
+          __syncwarp();
+          ok = mbar_wait(sm, &sm->v_full[b], w & 1, a.status) && mbar_wait(sm, &sm->p_full[c], done & 1, a.status);
+          if (!ok) break;
+          tc_fence_after();
+          const uint32_t v_lo = desc_lo(smem_u32(sm->v[b]), kHalfBytes);
+          if (elect_one()) {
+            mma_pv(tmem_o, tmem_s, v_lo, idesc_pv, first ? 0u : 1u);
+            mma_pv(tmem_o, tmem_s + 32u, v_lo + (kHalfKeys * 128 >> 4), idesc_pv, 1u);
+            tc_commit(&sm->pv_done[c]);
+            tc_commit(&sm->v_empty[b]);
+          }
+          __syncwarp();
+          first = false;
+          ++done;
+        }
+        step += sg.steps;
+        pos = sg.next;
+      }
+      if (!ok) {  // what has been issued reads shared and tensor memory
+        if (elect_one()) tc_commit(&sm->drained[c]);
+        __syncwarp();
+        for (uint32_t it = 0; it < (1u << 16); ++it)
+          if (mbar_try_wait(&sm->drained[c], 0)) break;
+      }
+    }
+  } else if (warp < 8) {
+    // ============================ codes, and the tree's rows, to half-precision tiles ============================
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsUnpack));
+    const int w4 = warp - 4, quad = lane & 3, r8 = lane >> 2;
+    int step = 0, taken = 0, seg = 0;  // (segments with steps)
+    bool ok = true;
+    // A thread's 32 channels of a row are four 16-byte pieces.  Quads 2, 3 write to the tile's second half, 16 KiB on, that is, to the same
+    // banks: they go through their pieces in another order.
+    const uint32_t piece0 = (quad & 1) * 4, swap = quad >= 2 ? 2u : 0u;
+    const uint32_t tile_half = (quad >> 1) * kHalfBytes;
+    for (int pos = range_lo; pos < range_hi && ok;) {
+      const TilesSeg sg = tiles_seg(&sm->plan, a, pos, range_hi);
+      for (int i = 0; i < sg.steps && ok; ++i) {
+        const int x = step + i, b = x & 1, w = x >> 1, t = sg.t0 + i;
+        const bool tree = t >= sg.u.prefix.steps;
+        const int key0 = tree ? (t - sg.u.prefix.steps) * kTilesStep : sg.u.prefix.key_step(t) * kTilesStep;
+        const int left = (tree ? a.n : sg.u.L) - key0;  // keys of the tile that there are
+        const int halves = left > kHalfKeys ? 2 : 1;
+        if (!tree)
+          for (int h = 0; h < halves && ok; ++h) ok = mbar_wait(sm, &sm->raw_full[(taken + h) % kStages], ((taken + h) / kStages) & 1, a.status);
+#pragma unroll 1
+        for (int which = 0; which < 2 && ok; ++which) {
+          if (w > 0) ok = mbar_wait(sm, which ? &sm->v_empty[b] : &sm->k_empty[b], (w - 1) & 1, a.status);
+          if (!ok) break;
+          const uint32_t tile = smem_u32(which ? sm->v[b] : sm->k[b]) + tile_half;
+          if (!tree) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              const uint32_t granule = smem_u32(sm->ring[(taken + h) % kStages]) + w4 * kGranuleBytes;
+#pragma unroll
+              for (int y = 0; y < 2; ++y) {
+                const int row = 8 * y + r8, key = h * kHalfKeys + w4 * kGranule + row;
+                uint4 code = make_uint4(0u, 0u, 0u, 0u);
+                uint32_t params = 0;  // a key behind the prefix: zeros
+                if (key < left) {
+                  asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(code.x), "=r"(code.y), "=r"(code.z), "=r"(code.w)
+                               : "r"(granule + which * kGranuleV + row * kCodeBytes + quad * 16) : "memory");
+                  asm volatile("ld.shared.u32 %0, [%1];" : "=r"(params) : "r"(granule + kGranuleParams + which * (kGranule * 4) + row * 4) : "memory");
+                }
+                const uint32_t scale = __byte_perm(params, params, 0x1010), mid = __byte_perm(params, params, 0x3232);
+                const uint32_t words[4] = {swap ? code.z : code.x, swap ? code.w : code.y, swap ? code.x : code.z, swap ? code.y : code.w};
+                const uint32_t line = tile + key * 128;
+#pragma unroll
+                for (int p = 0; p < 4; ++p) {
+                  uint32_t v[4];
+                  unpack4(words[p], v);
+                  sts128(line + (((piece0 + (p ^ swap)) ^ (key & 7)) << 4), hfma2_bits(v[0], scale, mid), hfma2_bits(v[1], scale, mid),
+                         hfma2_bits(v[2], scale, mid), hfma2_bits(v[3], scale, mid));
+                }
+              }
+            }
+          } else {
+            uint32_t bad = 0;  // of the warp's 32 rows
+            const uint8_t* rows = (which ? a.vt : a.kt) + sg.u.r * a.t_req + sg.u.g * a.t_head + quad * 64;
+#pragma unroll 1
+            for (int y = 0; y < 4; ++y) {
+              const int key = w4 * 32 + 8 * y + r8;
+              uint4 in[4];
+#pragma unroll
+              for (int p = 0; p < 4; ++p) {
+                in[p] = make_uint4(0u, 0u, 0u, 0u);
+                if (key < left) in[p] = reinterpret_cast<const uint4*>(rows + (int64_t)(key0 + key) * a.t_tok)[p ^ swap];
+              }
+              uint32_t big = 0;
+#pragma unroll
+              for (int p = 0; p < 4; ++p) {
+                if (kBf16) {
+                  in[p].x = pack2<false>(__uint_as_float(in[p].x << 16), __uint_as_float(in[p].x & 0xffff0000u));
+                  in[p].y = pack2<false>(__uint_as_float(in[p].y << 16), __uint_as_float(in[p].y & 0xffff0000u));
+                  in[p].z = pack2<false>(__uint_as_float(in[p].z << 16), __uint_as_float(in[p].z & 0xffff0000u));
+                  in[p].w = pack2<false>(__uint_as_float(in[p].w << 16), __uint_as_float(in[p].w & 0xffff0000u));
+                }
+                big = __vmaxu2(__vmaxu2(big, in[p].x & 0x7c007c00u), __vmaxu2(in[p].y & 0x7c007c00u, __vmaxu2(in[p].z & 0x7c007c00u, in[p].w & 0x7c007c00u)));
+              }
+              uint32_t keep = 0xffffffffu;
+              if (which == 1) {
+                // a row of V that is not finite counts as zeros, so that it stays out of the rows that do not see it; those
+                // that do become NaN when they are written
+                const uint32_t b4 = __ballot_sync(0xffffffffu, (big & 0xffffu) == 0x7c00u || (big >> 16) == 0x7c00u);
+                if ((b4 >> (lane & 28)) & 15u) keep = 0u;
+#pragma unroll
+                for (int z = 0; z < 8; ++z) bad |= (b4 >> (4 * z)) & 15u ? 1u << (8 * y + z) : 0u;
+              }
+              const uint32_t line = tile + key * 128;
+#pragma unroll
+              for (int p = 0; p < 4; ++p)
+                sts128(line + (((piece0 + (p ^ swap)) ^ (key & 7)) << 4), __byte_perm(in[p].x, in[p].z, 0x5410) & keep, __byte_perm(in[p].x, in[p].z, 0x7632) & keep,
+                       __byte_perm(in[p].y, in[p].w, 0x5410) & keep, __byte_perm(in[p].y, in[p].w, 0x7632) & keep);
+            }
+            // (four segments' words: this warp is two tiles ahead of the rows that look at them, at most)
+            if (which == 1 && lane == 0) sm->bad[seg & 3][key0 / kTilesStep][w4] = bad;
+          }
+          fence_async_smem();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(which ? &sm->v_full[b] : &sm->k_full[b]);
+        }
+        if (!ok) break;
+        if (!tree) {
+          if (lane == 0)
+            for (int h = 0; h < halves; ++h) mbar_arrive(&sm->raw_empty[(taken + h) % kStages]);
+          taken += halves;
+        }
+      }
+      step += sg.steps;
+      seg += sg.steps > 0;
+      pos = sg.next;
+    }
+  } else {
+    // ============================ chains: one thread a row ============================
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsChain));
+    const int c = (warp >> 2) - 2, quarter = warp & 3, row = quarter * 32 + lane;
+    const uint32_t lane_sel = (uint32_t)(quarter * 32) << 16;
+    const uint32_t tmem_s = tmem + 256u + 128u * c + lane_sel;
+    int step = 0, done = 0, seg = 0;  // (segments with steps)
+    bool ok = true;
+    for (int pos = range_lo; pos < range_hi;) {
+      const TilesSeg sg = tiles_seg(&sm->plan, a, pos, range_hi);
+      const int L = sg.u.L, r = sg.u.r;
+      const int rw = sg.u.m * a.row_tile + (kTwo ? c * kTileM : 0) + row;
+      const bool valid = rw < a.rows;
+      const int node = min(rw, a.rows - 1) / a.group, h = sg.u.g * a.group + min(rw, a.rows - 1) % a.group;
+      const bool warp_live = rw - lane < a.rows;  // (a warp of padding rows only keeps in step)
+      // ---- q: half precision (a bfloat16 row scaled by a power of two, exactly), channels in the codes' order
+      float rs = a.scale_log2;
+      {
+        const uint4* src = reinterpret_cast<const uint4*>(a.q + r * a.q_req + node * a.q_tok + h * a.q_head);
+        // with one tile for both chains each brings half of the channels
+        const int from = kTwo ? 0 : 8 * c, pieces = kTwo ? 16 : 8;
+        float f = 1.f;
+        if (kBf16) {
+          uint32_t top = 0;
+#pragma unroll 4
+          for (int p = 0; p < 16; ++p) {
+            const uint4 x = src[p];
+            top = max(max(top, max((x.x << 16) & 0x7fffffffu, x.x & 0x7fff0000u)), max((x.y << 16) & 0x7fffffffu, x.y & 0x7fff0000u));
+            top = max(max(top, max((x.z << 16) & 0x7fffffffu, x.z & 0x7fff0000u)), max((x.w << 16) & 0x7fffffffu, x.w & 0x7fff0000u));
+          }
+          const int e = (int)(top >> 23);
+          if (e > 8 && e < 255) {  // the largest magnitude into [2^8, 2^9)
+            const int up = min(max(8 + 127 - e, -100), 100);
+            f = __uint_as_float((uint32_t)(127 + up) << 23);
+            rs *= __uint_as_float((uint32_t)(127 - up) << 23);
+          }
+        }
+        const uint32_t line = smem_u32(sm->q[kTwo ? c : 0]) + row * 128;
+#pragma unroll 4
+        for (int p = 0; p < pieces; ++p) {
+          uint4 x = valid ? src[from + p] : make_uint4(0u, 0u, 0u, 0u);
+          if (kBf16) {
+            x.x = pack2<false>(__uint_as_float(x.x << 16) * f, __uint_as_float(x.x & 0xffff0000u) * f);
+            x.y = pack2<false>(__uint_as_float(x.y << 16) * f, __uint_as_float(x.y & 0xffff0000u) * f);
+            x.z = pack2<false>(__uint_as_float(x.z << 16) * f, __uint_as_float(x.z & 0xffff0000u) * f);
+            x.w = pack2<false>(__uint_as_float(x.w << 16) * f, __uint_as_float(x.w & 0xffff0000u) * f);
+          }
+          sts128(line + ((from + p) >> 3) * kHalfBytes + ((((from + p) & 7) ^ (row & 7)) << 4), __byte_perm(x.x, x.z, 0x5410), __byte_perm(x.x, x.z, 0x7632),
+                 __byte_perm(x.y, x.w, 0x5410), __byte_perm(x.y, x.w, 0x7632));
+        }
+        fence_async_smem();
+        __syncwarp();
+        if (lane == 0) {
+          if (kTwo) {
+            mbar_arrive(&sm->q_full[c]);
+          } else {
+            mbar_arrive(&sm->q_full[0]);
+            mbar_arrive(&sm->q_full[1]);
+          }
+        }
+      }
+      const uint32_t* mask_row = kv4_mask_row(a, r, node);
+      const int depth = a.window > 0 ? kv4_depth(a, r, node) : 0;
+      const int begin = a.window > 0 ? L + depth + 1 - a.window : 0;  // where the row's window begins
+
+      float m_used = -INFINITY, l = 0.f;
+      bool any = false;  // the chain has had a tile
+      uint32_t poison = 0;
+      for (int i = 0; i < sg.steps && ok; ++i) {
+        const int x = step + i, t = sg.t0 + i;
+        if (!kTwo && (x & 1) != c) continue;
+        const bool tree = t >= sg.u.prefix.steps;
+        const int key0 = tree ? (t - sg.u.prefix.steps) * kTilesStep : sg.u.prefix.key_step(t) * kTilesStep;
+        uint32_t vis[4];
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          if (tree) vis[w] = kv4_window_word(a, r, L, depth, (key0 >> 5) + w, kv4_mask_word(a, mask_row, node, (key0 >> 5) + w));
+          else vis[w] = bits_below(L - key0 - 32 * w) & (~bits_below(begin - key0 - 32 * w) | bits_below(a.sinks - key0 - 32 * w));
+        }
+        const bool masked = __any_sync(0xffffffffu, (vis[0] & vis[1] & vis[2] & vis[3]) != 0xffffffffu);
+        ok = mbar_wait(sm, &sm->s_full[c], done & 1, a.status);
+        __syncwarp();
+        if (!ok) break;
+        if (warp_live) {
+          tc_fence_after();
+          uint32_t s[128];
+          tmem_ld32(tmem_s, s, 0);
+          tmem_ld32(tmem_s + 32u, s, 32);
+          tmem_ld32(tmem_s + 64u, s, 64);
+          tmem_ld32(tmem_s + 96u, s, 96);
+          tc_wait_ld();
+#pragma unroll
+          for (int e = 0; e < 128; ++e) asm volatile("" : "+r"(s[e]));
+          if (masked) {
+#pragma unroll
+            for (int e = 0; e < 128; ++e)
+              if (!((vis[e >> 5] >> (e & 31)) & 1u)) s[e] = __float_as_uint(-INFINITY);
+          }
+          // The exponentials are taken against the reference as it stands; their sum tells whether that was right (see
+          // tree_attention_stream.cu): the maximum is taken, the reference moved, O rescaled and the pass repeated only then.
+          bool settle = __any_sync(0xffffffffu, m_used == -INFINITY);
+          float sum;
+#pragma unroll 1
+          for (;;) {
+            if (settle) {
+              float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+              for (int e = 0; e < 128; e += 2) mx[(e >> 1) & 3] = max3(mx[(e >> 1) & 3], __uint_as_float(s[e]), __uint_as_float(s[e + 1]));
+              const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * rs;  // rs > 0
+              const bool move = top > m_used + kRescaleThreshold || (m_used == -INFINITY && top != -INFINITY);
+              if (__any_sync(0xffffffffu, move)) {
+                float alpha = 1.f;
+                if (move) {
+                  alpha = m_used == -INFINITY ? 0.f : ex2(m_used - top);
+                  l *= alpha;
+                  m_used = top;
+                }
+                __syncwarp();
+                if (any) {  // (the product before this S has completed: see the issuer)
+#pragma unroll 1
+                  for (int x4 = 0; x4 < 4; ++x4) {
+                    uint32_t o[32];
+                    tmem_ld32(tmem + 128u * c + lane_sel + 32u * x4, o, 0);
+                    tc_wait_ld();
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * alpha);
+                    tmem_st32(tmem + 128u * c + lane_sel + 32u * x4, o, 0);
+                  }
+                }
+              }
+            }
+            const float neg_m = m_used == -INFINITY ? 0.f : -m_used;
+            const uint64_t rs2 = pair_of(rs, rs), neg_m2 = pair_of(neg_m, neg_m);
+            uint64_t sums[2] = {pair_of(0.f, 0.f), pair_of(0.f, 0.f)};
+#pragma unroll
+            for (int x4 = 0; x4 < 4; ++x4) {
+              uint32_t packed[16];
+#pragma unroll
+              for (int e = 0; e < 16; ++e) {
+                float y0, y1;
+                unpair(fma2(pair_of(__uint_as_float(s[32 * x4 + 2 * e]), __uint_as_float(s[32 * x4 + 2 * e + 1])), rs2, neg_m2), y0, y1);
+                const float p0 = ex2(y0), p1 = ex2(y1);
+                sums[e & 1] = add2(sums[e & 1], pair_of(p0, p1));
+                packed[e] = pack2<false>(p0, p1);
+              }
+              tmem_st16(tmem_s + 16u * x4, packed);
+            }
+            float s0, s1, s2, s3;
+            unpair(sums[0], s0, s1);
+            unpair(sums[1], s2, s3);
+            sum = (s0 + s1) + (s2 + s3);
+            if (settle) break;
+            settle = __any_sync(0xffffffffu, !(sum <= kRescaleLimit));
+            if (!settle) break;
+            tc_wait_st();
+          }
+          l += sum;
+          tc_wait_st();
+          tc_fence_before();
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sm->p_full[c]);
+        any = true;
+        ++done;
+      }
+      // ---- the chain's last product
+      if (any && ok) ok = mbar_wait(sm, &sm->pv_done[c], (done - 1) & 1, a.status);
+      __syncwarp();
+      tc_fence_after();
+      if (!ok) any = false;
+      for (int i = max(sg.u.prefix.steps - sg.t0, 0); i < sg.steps; ++i) {  // tree rows that are not finite and that the row sees
+        if (!kTwo && ((step + i) & 1) != c) continue;
+        const int tile = sg.t0 + i - sg.u.prefix.steps;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          const uint32_t bad = sm->bad[seg & 3][tile][w];
+          if (bad != 0) poison |= bad & kv4_window_word(a, r, L, depth, 4 * tile + w, kv4_mask_word(a, mask_row, node, 4 * tile + w));
+        }
+      }
+      if (poison != 0) l = NAN;
+      // ---- out: a chain with a tile of its own writes 128 columns, chains that share one 64 each of their sum
+      float M = m_used, sum = l, fA = 1.f, fB = 0.f;
+      if (!kTwo) {
+        sm->ml[c][row] = any ? make_float2(m_used, l) : make_float2(-INFINITY, l != l ? l : 0.f);
+        asm volatile("bar.sync 1, 256;" ::: "memory");
+        const float2 A = sm->ml[0][row], Bv = sm->ml[1][row];
+        M = fmaxf(A.x, Bv.x);
+        fA = A.x == -INFINITY ? 0.f : ex2(A.x - M);
+        fB = Bv.x == -INFINITY ? 0.f : ex2(Bv.x - M);
+        sum = fmaf(A.y, fA, Bv.y * fB);
+      }
+      const bool own = kTwo ? any : true;
+      const float inv = 1.f / sum;
+      const int slot = 2 * blockIdx.x + (pos == range_lo ? 0 : 1);
+      const int64_t ws_row = (int64_t)slot * a.row_tile + (kTwo ? c * kTileM : 0) + row;
+      uint8_t* out = a.out + r * a.o_req + node * a.o_tok + h * a.o_head;
+#pragma unroll 1
+      for (int x4 = kTwo ? 0 : 2 * c; x4 < (kTwo ? 4 : 2 * c + 2); ++x4) {
+        float o[32];
+        __syncwarp();
+        if (kTwo) {
+          if (own) {
+            tmem_ld32(tmem + 128u * c + lane_sel + 32u * x4, reinterpret_cast<uint32_t*>(o), 0);
+            tc_wait_ld();
+          } else {
+#pragma unroll
+            for (int e = 0; e < 32; ++e) o[e] = 0.f;
+          }
+        } else {
+          float ob[32];
+          tmem_ld32(tmem + lane_sel + 32u * x4, reinterpret_cast<uint32_t*>(o), 0);
+          tmem_ld32(tmem + 128u + lane_sel + 32u * x4, reinterpret_cast<uint32_t*>(ob), 0);
+          tc_wait_ld();
+#pragma unroll
+          for (int e = 0; e < 32; ++e) o[e] = (fA == 0.f ? 0.f : o[e] * fA) + (fB == 0.f ? 0.f : ob[e] * fB);  // (an accumulator nobody wrote may hold anything)
+        }
+        if (valid && sg.whole) {
+#pragma unroll
+          for (int e = 0; e < 32; e += 8) {  // columns 0,2,4,6,1,3,5,7 are channels 0..7
+            uint4 val;
+            val.x = pack2<kBf16>(o[e] * inv, o[e + 2] * inv);
+            val.y = pack2<kBf16>(o[e + 4] * inv, o[e + 6] * inv);
+            val.z = pack2<kBf16>(o[e + 1] * inv, o[e + 3] * inv);
+            val.w = pack2<kBf16>(o[e + 5] * inv, o[e + 7] * inv);
+            *reinterpret_cast<uint4*>(out + 64 * x4 + 2 * e) = val;
+          }
+        } else if (valid) {
+          float4* to = reinterpret_cast<float4*>(a.ws_o + ws_row * kHeadDim + 32 * x4);
+#pragma unroll
+          for (int e = 0; e < 32; e += 8) {
+            to[e / 4] = make_float4(o[e], o[e + 2], o[e + 4], o[e + 6]);
+            to[e / 4 + 1] = make_float4(o[e + 1], o[e + 3], o[e + 5], o[e + 7]);
+          }
+        }
+      }
+      if (valid && (kTwo || c == 0)) {
+        if (sg.whole) {
+          if (a.lse != nullptr) a.lse[((int64_t)r * a.Hq + h) * a.n + node] = (M + log2f(sum)) * kLn2;
+        } else {
+          a.ws_ml[ws_row] = make_float2(own ? M : -INFINITY, sum);
+        }
+      }
+      tc_fence_before();
+      if (!kTwo) asm volatile("bar.sync 1, 256;" ::: "memory");  // both accumulators are read, both chains are through with Q
+      step += sg.steps;
+      seg += sg.steps > 0;
+      pos = sg.next;
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 1) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+  }
+}
+
+// ---------------------------------------------------------------- host side ---------------------
+static bool tiles_two(const seq_tree_kv4_attention_params& p) { return p.n_tree * (p.num_q_heads / p.num_kv_heads) > kTileM; }
+
+size_t kv4_tiles_workspace_bytes(const seq_tree_kv4_attention_params& p) {
+  return (size_t)2 * device_sm_count() * (tiles_two(p) ? 2 : 1) * kTileM * (kHeadDim * sizeof(float) + sizeof(float2));
+}
+
+int launch_kv4_tiles(const seq_tree_kv4_attention_params& p, cudaStream_t stream) {
+  const bool two = tiles_two(p);
+  const int sms = device_sm_count();
+  Kv4Args a = kv4_args(p);
+  a.row_tile = two ? 2 * kTileM : kTileM;
+  a.tiles = (a.rows + a.row_tile - 1) / a.row_tile;
+  a.tree_steps = (a.n + kTilesStep - 1) / kTilesStep;
+  a.min_steps = 2;
+  const int64_t most = (int64_t)a.batch * a.Hkv * a.tiles * ((p.max_len + kTilesStep - 1) / kTilesStep + 1 + a.tree_steps);
+  if (most > 0x7fffffff) return SEQ_ERR_UNSUPPORTED;
+  const int64_t want = (most + a.min_steps - 1) / a.min_steps;
+  a.ctas = want < sms ? (int)want : sms;
+  a.ws_o = static_cast<float*>(p.workspace);
+  a.ws_ml = reinterpret_cast<float2*>(a.ws_o + (size_t)2 * sms * a.row_tile * kHeadDim);
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(a.ctas);
+  cfg.blockDim = dim3(kTilesThreads);
+  cfg.stream = stream;
+  cudaLaunchAttribute early[1];
+  early[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  early[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = early;
+  cfg.numAttrs = 1;
+  auto launch = [&](auto kernel, int which, size_t smem) -> int {
+    static int done[4][64];
+    const int rc = once_per_device(done[which], [&]() -> int {
+      SEQ_CUDA_OK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+      return SEQ_OK;
+    });
+    if (rc != SEQ_OK) return rc;
+    cfg.dynamicSmemBytes = smem;
+    SEQ_CUDA_OK(cudaLaunchKernelEx(&cfg, kernel, a));
+    return SEQ_OK;
+  };
+  const bool bf16 = p.dtype == SEQ_BF16;
+  int rc;
+  if (two) rc = bf16 ? launch(kv4_tiles_kernel<true, true>, 0, tiles_smem_bytes<true>()) : launch(kv4_tiles_kernel<true, false>, 1, tiles_smem_bytes<true>());
+  else rc = bf16 ? launch(kv4_tiles_kernel<false, true>, 2, tiles_smem_bytes<false>()) : launch(kv4_tiles_kernel<false, false>, 3, tiles_smem_bytes<false>());
+  if (rc != SEQ_OK) return rc;
+  return launch_kv4_combine(a, kTilesStep, bf16, stream);
+}
+
+}  // namespace seqtree
