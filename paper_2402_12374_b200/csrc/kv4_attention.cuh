@@ -4,7 +4,8 @@
 // A unit is (request, kv head, tile of query rows); a row is a (node, head in group) pair.  A unit's keys come in steps: those of the prefix that
 // some row can see (the sinks, then the window: the steps in between are left out), then the tree's.  The steps of all
 // units are laid end to end and cut into equal ranges, one a CTA, whatever lengths the requests have.  A unit inside one range is
-// finished there; the pieces of one that is cut go to the workspace and are added by a second launch in the order of their CTAs.
+// finished there; the pieces of one that is cut go to the workspace, and the CTA that leaves the last of them adds them in the
+// order of their CTAs.
 #pragma once
 
 #include "kv4.cuh"
@@ -24,8 +25,9 @@ struct Kv4Args {
   const uint32_t* mask; int32_t mask_wpr; int64_t mask_req;
   uint8_t* out; int64_t o_req, o_tok, o_head;
   float* lse;
-  float2* ws_ml;  // [2 * ctas][row_tile] (m, l): reference maximum (log2 units) and sum of a piece
-  float* ws_o;    // [2 * ctas][row_tile][128] its unnormalised rows
+  int32_t* ws_count;  // [2 * ctas] pieces left of a unit that begins in the CTA's range: zero when the kernel starts
+  float2* ws_ml;      // [2 * ctas][row_tile] (m, l): reference maximum (log2 units) and sum of a piece
+  float* ws_o;        // [2 * ctas][row_tile][128] its unnormalised rows
   float scale_log2;
   int32_t* status;
 };
@@ -119,6 +121,17 @@ __device__ __forceinline__ Kv4Unit kv4_unit(const Kv4Plan* plan, const Kv4Args& 
 // Where CTA c leaves its piece of a unit that begins at `begin`: the piece that opens its range, or the one that closes it.
 __device__ __forceinline__ int kv4_slot(const Kv4Ranges& ranges, int c, int begin) { return 2 * c + (max(begin, ranges.lo(c)) == ranges.lo(c) ? 0 : 1); }
 
+// The CTAs whose ranges hold a unit's steps
+struct Kv4Pieces { int32_t first, last; };
+__device__ __forceinline__ Kv4Pieces kv4_pieces(const Kv4Ranges& ranges, const Kv4Unit& u) {
+  Kv4Pieces p;
+  p.first = blockIdx.x;
+  while (ranges.lo(p.first) > u.begin) --p.first;
+  p.last = blockIdx.x;
+  while (p.last + 1 < ranges.ctas && ranges.lo(p.last + 1) < u.end) ++p.last;
+  return p;
+}
+
 __device__ __forceinline__ const uint32_t* kv4_mask_row(const Kv4Args& a, int r, int node) {
   return a.mask != nullptr ? a.mask + r * a.mask_req + (int64_t)node * a.mask_wpr : nullptr;
 }
@@ -154,7 +167,8 @@ size_t kv4_tiles_workspace_bytes(const seq_tree_kv4_attention_params& p);
 int launch_kv4_tiles(const seq_tree_kv4_attention_params& p, cudaStream_t stream);
 // Arguments that do not depend on the kernel
 Kv4Args kv4_args(const seq_tree_kv4_attention_params& p);
-// Adds the pieces that `ctas` CTAs left: steps of `step` keys
-int launch_kv4_combine(const Kv4Args& a, int step, bool bf16, cudaStream_t stream);
+// Zeroes the counts
+int launch_kv4_zero(const Kv4Args& a, cudaStream_t stream);
+inline size_t kv4_count_bytes(size_t ctas) { return (2 * ctas * sizeof(int32_t) + 255) & ~(size_t)255; }
 
 }  // namespace seqtree

@@ -1,59 +1,28 @@
-// seq_tree_kv4_attention: checks, the choice of kernel, and the launch that adds the pieces of units that ranges cut.
+// seq_tree_kv4_attention: checks and the choice of kernel.
 #include "kv4_attention.cuh"
-#include "umma.cuh"
 
 namespace seqtree {
 
-// One block (x: a range's start, y: 16 rows) for each range that may begin inside a unit: the first range that begins in
-// it adds all its pieces, in the order of their CTAs, so the sum does not depend on who finished when.
-constexpr int kCombineRows = 16;
-template <int kStep, bool kBf16>
-__global__ void __launch_bounds__(kHeadDim) kv4_combine_kernel(const Kv4Args a) {
-  __shared__ Kv4Plan plan;
+// A kernel of one's own, not a memset: it is scheduled under the tail of the launch before and lets the attention's set-up run
+// under itself.
+__global__ void kv4_zero_kernel(int32_t* words, int n) {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  kv4_plan<kStep, kHeadDim>(&plan, a);
-  const Kv4Ranges ranges = kv4_ranges(&plan, a);
-  const int b = blockIdx.x + 1;
-  if (b >= ranges.ctas) return;
-  const int at = ranges.lo(b);
-  if (at >= ranges.total) return;
-  const Kv4Unit u = kv4_unit<kStep>(&plan, a, at);
-  if (u.begin == at || ranges.lo(b - 1) > u.begin) return;  // not cut here, or cut before
-  int last = b;
-  while (last + 1 < ranges.ctas && ranges.lo(last + 1) < u.end) ++last;
-  const int row0 = u.m * a.row_tile, live = min(a.row_tile, a.rows - row0), c = threadIdx.x;
-  for (int row = blockIdx.y * kCombineRows; row < min(live, (int)(blockIdx.y + 1) * kCombineRows); ++row) {
-    float M = -INFINITY;
-    for (int x = b - 1; x <= last; ++x) M = fmaxf(M, a.ws_ml[(int64_t)kv4_slot(ranges, x, u.begin) * a.row_tile + row].x);
-    float sum = 0.f, acc = 0.f;
-    for (int x = b - 1; x <= last; ++x) {
-      const int64_t s = (int64_t)kv4_slot(ranges, x, u.begin) * a.row_tile + row;
-      const float2 ml = a.ws_ml[s];
-      const float f = ml.x == -INFINITY ? 0.f : ex2(ml.x - M);
-      sum = fmaf(ml.y, f, sum);
-      acc = fmaf(a.ws_o[s * kHeadDim + c], f, acc);
-    }
-    const int rw = row0 + row, nd = rw / a.group, h = u.g * a.group + rw - nd * a.group;
-    using T = typename std::conditional<kBf16, __nv_bfloat16, __half>::type;
-    reinterpret_cast<T*>(a.out + u.r * a.o_req + nd * a.o_tok + h * a.o_head)[c] = from_float<T>(acc / sum);
-    if (a.lse != nullptr && c == 0) a.lse[((int64_t)u.r * a.Hq + h) * a.n + nd] = (M + log2f(sum)) * kLn2;
-  }
+  for (int i = threadIdx.x; i < n; i += blockDim.x) words[i] = 0;
 }
 
-int launch_kv4_combine(const Kv4Args& a, int step, bool bf16, cudaStream_t stream) {
-  if (a.ctas < 2) return SEQ_OK;
+int launch_kv4_zero(const Kv4Args& a, cudaStream_t stream) {
+  if (a.ctas < 2) return SEQ_OK;  // nothing is cut
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(a.ctas - 1, (a.row_tile + kCombineRows - 1) / kCombineRows);
-  cfg.blockDim = dim3(kHeadDim);
+  cfg.gridDim = dim3(1);
+  cfg.blockDim = dim3(512);
   cfg.stream = stream;
   cudaLaunchAttribute early[1];
   early[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   early[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = early;
   cfg.numAttrs = 1;
-  if (step == 32) SEQ_CUDA_OK(cudaLaunchKernelEx(&cfg, bf16 ? kv4_combine_kernel<32, true> : kv4_combine_kernel<32, false>, a));
-  else SEQ_CUDA_OK(cudaLaunchKernelEx(&cfg, bf16 ? kv4_combine_kernel<128, true> : kv4_combine_kernel<128, false>, a));
+  SEQ_CUDA_OK(cudaLaunchKernelEx(&cfg, kv4_zero_kernel, a.ws_count, 2 * a.ctas));
   return SEQ_OK;
 }
 

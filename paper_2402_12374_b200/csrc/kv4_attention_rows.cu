@@ -28,6 +28,7 @@ struct RowsSmem {
   uint64_t full[kRowsWarps][kStages];
   Kv4Plan plan;
   volatile int abort_flag;
+  int32_t last;  // this CTA completes the unit
 };
 
 __device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
@@ -479,9 +480,15 @@ __global__ void __launch_bounds__(32 * kRowsWarps, NT == 1 ? 3 : 2) kv4_rows_ker
       }
     __syncthreads();
     const bool whole = pos == u.begin && seg_end == u.end;
-    const int slot = 2 * blockIdx.x + (pos == range_lo ? 0 : 1);
+    const int c = threadIdx.x;
+    using T = typename std::conditional<kBf16, __nv_bfloat16, __half>::type;
+    auto write_row = [&](int row, float M, float sum, float acc) {
+      const int rw = row0 + row, nd = rw / a.group, h = u.g * a.group + rw - nd * a.group;
+      reinterpret_cast<T*>(a.out + u.r * a.o_req + nd * a.o_tok + h * a.o_head)[c] = from_float<T>(acc / sum);
+      if (a.lse != nullptr && c == 0) a.lse[((int64_t)u.r * a.Hq + h) * a.n + nd] = (M + log2f(sum)) * kLn2;
+    };
+    const int64_t slot = (int64_t)kv4_slot(ranges, blockIdx.x, u.begin) * a.row_tile;
     for (int row = 0; row < live_rows; ++row) {
-      const int c = threadIdx.x;
       float M = -INFINITY;
 #pragma unroll
       for (int w = 0; w < kRowsWarps; ++w) M = fmaxf(M, sm->ml[w][row].x);
@@ -494,13 +501,34 @@ __global__ void __launch_bounds__(32 * kRowsWarps, NT == 1 ? 3 : 2) kv4_rows_ker
         acc = fmaf(sm->o[w][row][c], f, acc);
       }
       if (whole) {
-        const int rw = row0 + row, nd = rw / a.group, h = u.g * a.group + rw - nd * a.group;
-        using T = typename std::conditional<kBf16, __nv_bfloat16, __half>::type;
-        reinterpret_cast<T*>(a.out + u.r * a.o_req + nd * a.o_tok + h * a.o_head)[c] = from_float<T>(acc / sum);
-        if (a.lse != nullptr && c == 0) a.lse[((int64_t)u.r * a.Hq + h) * a.n + nd] = (M + log2f(sum)) * kLn2;
+        write_row(row, M, sum, acc);
       } else {
-        a.ws_o[((int64_t)slot * a.row_tile + row) * kHeadDim + c] = acc;
-        if (c == 0) a.ws_ml[(int64_t)slot * a.row_tile + row] = make_float2(M, sum);
+        a.ws_o[(slot + row) * kHeadDim + c] = acc;
+        if (c == 0) a.ws_ml[slot + row] = make_float2(M, sum);
+      }
+    }
+    if (!whole) {
+      // The piece is counted; the CTA that counts the last one adds them all, in the order of their CTAs.  Nobody waits.
+      const Kv4Pieces pieces = kv4_pieces(ranges, u);
+      __threadfence();
+      __syncthreads();
+      if (c == 0) sm->last = atomicAdd(a.ws_count + 2 * pieces.first, 1) == pieces.last - pieces.first;
+      __syncthreads();
+      if (sm->last) {
+        __threadfence();
+        for (int row = 0; row < live_rows; ++row) {
+          float M = -INFINITY;
+          for (int x = pieces.first; x <= pieces.last; ++x) M = fmaxf(M, __ldcg(a.ws_ml + (int64_t)kv4_slot(ranges, x, u.begin) * a.row_tile + row).x);
+          float sum = 0.f, acc = 0.f;
+          for (int x = pieces.first; x <= pieces.last; ++x) {
+            const int64_t s = (int64_t)kv4_slot(ranges, x, u.begin) * a.row_tile + row;
+            const float2 ml = __ldcg(a.ws_ml + s);
+            const float f = ml.x == -INFINITY ? 0.f : ex2(ml.x - M);
+            sum = fmaf(ml.y, f, sum);
+            acc = fmaf(__ldcg(a.ws_o + s * kHeadDim + c), f, acc);
+          }
+          write_row(row, M, sum, acc);
+        }
       }
     }
     __syncthreads();
@@ -518,7 +546,7 @@ static int rows_ctas(int nt) { return device_sm_count() * (nt == 1 ? 3 : 2); }
 
 size_t kv4_rows_workspace_bytes(const seq_tree_kv4_attention_params& p) {
   const int nt = rows_nt(p);
-  return (size_t)2 * rows_ctas(nt) * 8 * nt * (kHeadDim * sizeof(float) + sizeof(float2));
+  return kv4_count_bytes(rows_ctas(nt)) + (size_t)2 * rows_ctas(nt) * 8 * nt * (kHeadDim * sizeof(float) + sizeof(float2));
 }
 
 int launch_kv4_rows(const seq_tree_kv4_attention_params& p, cudaStream_t stream) {
@@ -532,8 +560,11 @@ int launch_kv4_rows(const seq_tree_kv4_attention_params& p, cudaStream_t stream)
   if (most > 0x7fffffff) return SEQ_ERR_UNSUPPORTED;
   const int64_t want = (most + a.min_steps - 1) / a.min_steps;
   a.ctas = want < rows_ctas(nt) ? (int)want : rows_ctas(nt);
-  a.ws_o = static_cast<float*>(p.workspace);
+  a.ws_count = static_cast<int32_t*>(p.workspace);
+  a.ws_o = reinterpret_cast<float*>(static_cast<uint8_t*>(p.workspace) + kv4_count_bytes(rows_ctas(nt)));
   a.ws_ml = reinterpret_cast<float2*>(a.ws_o + (size_t)2 * rows_ctas(nt) * a.row_tile * kHeadDim);
+  const int rc0 = launch_kv4_zero(a, stream);
+  if (rc0 != SEQ_OK) return rc0;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(a.ctas);
   cfg.blockDim = dim3(32 * kRowsWarps);
@@ -558,8 +589,7 @@ int launch_kv4_rows(const seq_tree_kv4_attention_params& p, cudaStream_t stream)
   int rc;
   if (nt == 1) rc = bf16 ? launch(kv4_rows_kernel<1, true>, 0, sizeof(RowsSmem<1>)) : launch(kv4_rows_kernel<1, false>, 1, sizeof(RowsSmem<1>));
   else rc = bf16 ? launch(kv4_rows_kernel<2, true>, 2, sizeof(RowsSmem<2>)) : launch(kv4_rows_kernel<2, false>, 3, sizeof(RowsSmem<2>));
-  if (rc != SEQ_OK) return rc;
-  return launch_kv4_combine(a, kRowsStep, bf16, stream);
+  return rc;
 }
 
 }  // namespace seqtree

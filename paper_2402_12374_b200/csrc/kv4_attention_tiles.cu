@@ -20,9 +20,10 @@
 
 namespace seqtree {
 
-constexpr int kTilesThreads = 512;  // warp groups: loader and two issuers; codes to halves; chain A; chain B
+constexpr int kTilesThreads = 896;  // warps: loader, two issuers, one idle; eight that unpack; 16 for the chains
+constexpr int kUnpackWarp = 4, kChainWarp = 12;
 constexpr int kTilesStep = 128;     // keys
-constexpr int kRegsIssue = 40, kRegsUnpack = 96, kRegsChain = 184;  // 40 + 96 + 2 * 184 = 504 <= 4 * 128
+constexpr int kRegsIssue = 40, kRegsChain = 80;  // 128 * 40 + 256 * 72 + 512 * 80 = 896 * 72
 constexpr int kHalfKeys = 64;       // keys of a ring stage
 constexpr int kStageBytes = kHalfKeys / kGranule * kGranuleBytes;
 constexpr int kTreeTiles = SEQ_MAX_TREE / kTilesStep;
@@ -37,8 +38,12 @@ struct TilesSmem {
   uint64_t raw_full[kStages], raw_empty[kStages];
   uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2];  // [tile parity]
   uint64_t q_full[2], s_full[2], p_full[2], pv_done[2];   // [chain]
+  uint64_t turn[2][4];  // [chain][lane quarter], with kTwo: most of the chain's exponentials of a tile are under way
   uint64_t drained[2];
-  float2 ml[2][kTileM];  // the chains' (m, l), where they share rows
+  float xchg[2][2][kTileM];        // [chain][half]: what the two threads of a row tell each other
+  float2 ml[kTwo ? 1 : 2][kTwo ? 1 : kTileM];  // the chains' (m, l), where they share rows
+  int32_t above[2][2][2][4];       // [step parity][chain][half][lane quarter]: a score is far above its row's reference
+  int32_t last[2];                 // [chain]: this CTA completes the unit
   uint32_t bad[4][kTreeTiles][4];  // [segment mod 4]: tree rows whose V is not finite in half precision
   uint32_t tmem_base;
   volatile int abort_flag;
@@ -85,10 +90,11 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
   if (threadIdx.x == 0) {
     for (int s = 0; s < kStages; ++s) { mbar_init(&sm->raw_full[s], 1); mbar_init(&sm->raw_empty[s], 4); }
     for (int b = 0; b < 2; ++b) {
-      mbar_init(&sm->k_full[b], 4); mbar_init(&sm->k_empty[b], kTwo ? 2 : 1);
-      mbar_init(&sm->v_full[b], 4); mbar_init(&sm->v_empty[b], kTwo ? 2 : 1);
-      mbar_init(&sm->q_full[b], kTwo ? 4 : 8);
-      mbar_init(&sm->s_full[b], 1); mbar_init(&sm->p_full[b], 4); mbar_init(&sm->pv_done[b], 1);
+      mbar_init(&sm->k_full[b], 8); mbar_init(&sm->k_empty[b], kTwo ? 2 : 1);
+      mbar_init(&sm->v_full[b], 8); mbar_init(&sm->v_empty[b], kTwo ? 2 : 1);
+      mbar_init(&sm->q_full[b], kTwo ? 8 : 16);
+      mbar_init(&sm->s_full[b], 1); mbar_init(&sm->p_full[b], 8); mbar_init(&sm->pv_done[b], 1);
+      for (int x = 0; x < 4; ++x) mbar_init(&sm->turn[b][x], 2);
       mbar_init(&sm->drained[b], 1);
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -192,7 +198,7 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
           const uint32_t v_lo = desc_lo(smem_u32(sm->v[b]), kHalfBytes);
           if (elect_one()) {
             mma_pv(tmem_o, tmem_s, v_lo, idesc_pv, first ? 0u : 1u);
-            mma_pv(tmem_o, tmem_s + 32u, v_lo + (kHalfKeys * 128 >> 4), idesc_pv, 1u);
+            mma_pv(tmem_o, tmem_s + 64u, v_lo + (kHalfKeys * 128 >> 4), idesc_pv, 1u);
             tc_commit(&sm->pv_done[c]);
             tc_commit(&sm->v_empty[b]);
           }
@@ -210,10 +216,10 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
           if (mbar_try_wait(&sm->drained[c], 0)) break;
       }
     }
-  } else if (warp < 8) {
-    // ============================ codes, and the tree's rows, to half-precision tiles ============================
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsUnpack));
-    const int w4 = warp - 4, quad = lane & 3, r8 = lane >> 2;
+  } else if (warp < kChainWarp) {
+    // ============================ codes, and the tree's rows, to half-precision tiles: 16 rows a warp ============================
+    const int w8 = warp - kUnpackWarp, quad = lane & 3, r8 = lane >> 2;
+    const int half = w8 >> 2;
     int step = 0, taken = 0, seg = 0;  // (segments with steps)
     bool ok = true;
     // A thread's 32 channels of a row are four 16-byte pieces.  Quads 2, 3 write to the tile's second half, 16 KiB on, that is, to the same
@@ -228,45 +234,60 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
         const int key0 = tree ? (t - sg.u.prefix.steps) * kTilesStep : sg.u.prefix.key_step(t) * kTilesStep;
         const int left = (tree ? a.n : sg.u.L) - key0;  // keys of the tile that there are
         const int halves = left > kHalfKeys ? 2 : 1;
-        if (!tree)
-          for (int h = 0; h < halves && ok; ++h) ok = mbar_wait(sm, &sm->raw_full[(taken + h) % kStages], ((taken + h) / kStages) & 1, a.status);
-#pragma unroll 1
-        for (int which = 0; which < 2 && ok; ++which) {
+        // The codes of the thread's rows, of K and of V, into registers: the ring's stages are free again before they are unpacked.
+        uint4 code[2][2];
+        uint32_t params[2][2];
+        if (!tree) {
+          if (half < halves) ok = mbar_wait(sm, &sm->raw_full[(taken + half) % kStages], ((taken + half) / kStages) & 1, a.status);
+          __syncwarp();
+          if (!ok) break;
+          const uint32_t granule = smem_u32(sm->ring[(taken + half) % kStages]) + (w8 & 3) * kGranuleBytes;
+#pragma unroll
+          for (int y = 0; y < 2; ++y) {
+            const int row = 8 * y + r8;
+#pragma unroll
+            for (int which = 0; which < 2; ++which) {
+              code[which][y] = make_uint4(0u, 0u, 0u, 0u);
+              params[which][y] = 0;  // a key behind the prefix: zeros
+              if (w8 * kGranule + row < left) {
+                asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(code[which][y].x), "=r"(code[which][y].y), "=r"(code[which][y].z), "=r"(code[which][y].w)
+                             : "r"(granule + which * kGranuleV + row * kCodeBytes + quad * 16) : "memory");
+                asm volatile("ld.shared.u32 %0, [%1];" : "=r"(params[which][y]) : "r"(granule + kGranuleParams + which * (kGranule * 4) + row * 4) : "memory");
+              }
+            }
+          }
+          __syncwarp();
+          if (lane == 0 && half < halves) mbar_arrive(&sm->raw_empty[(taken + half) % kStages]);
+          taken += halves;
+        }
+#pragma unroll
+        for (int which = 0; which < 2; ++which) {
           if (w > 0) ok = mbar_wait(sm, which ? &sm->v_empty[b] : &sm->k_empty[b], (w - 1) & 1, a.status);
+          __syncwarp();
           if (!ok) break;
           const uint32_t tile = smem_u32(which ? sm->v[b] : sm->k[b]) + tile_half;
           if (!tree) {
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              const uint32_t granule = smem_u32(sm->ring[(taken + h) % kStages]) + w4 * kGranuleBytes;
+            for (int y = 0; y < 2; ++y) {
+              const uint4 cd = code[which][y];
+              const int key = w8 * kGranule + 8 * y + r8;
+              const uint32_t scale = __byte_perm(params[which][y], 0u, 0x1010), mid = __byte_perm(params[which][y], 0u, 0x3232);
+              const uint32_t words[4] = {swap ? cd.z : cd.x, swap ? cd.w : cd.y, swap ? cd.x : cd.z, swap ? cd.y : cd.w};
+              const uint32_t line = tile + key * 128;
 #pragma unroll
-              for (int y = 0; y < 2; ++y) {
-                const int row = 8 * y + r8, key = h * kHalfKeys + w4 * kGranule + row;
-                uint4 code = make_uint4(0u, 0u, 0u, 0u);
-                uint32_t params = 0;  // a key behind the prefix: zeros
-                if (key < left) {
-                  asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(code.x), "=r"(code.y), "=r"(code.z), "=r"(code.w)
-                               : "r"(granule + which * kGranuleV + row * kCodeBytes + quad * 16) : "memory");
-                  asm volatile("ld.shared.u32 %0, [%1];" : "=r"(params) : "r"(granule + kGranuleParams + which * (kGranule * 4) + row * 4) : "memory");
-                }
-                const uint32_t scale = __byte_perm(params, params, 0x1010), mid = __byte_perm(params, params, 0x3232);
-                const uint32_t words[4] = {swap ? code.z : code.x, swap ? code.w : code.y, swap ? code.x : code.z, swap ? code.y : code.w};
-                const uint32_t line = tile + key * 128;
-#pragma unroll
-                for (int p = 0; p < 4; ++p) {
-                  uint32_t v[4];
-                  unpack4(words[p], v);
-                  sts128(line + (((piece0 + (p ^ swap)) ^ (key & 7)) << 4), hfma2_bits(v[0], scale, mid), hfma2_bits(v[1], scale, mid),
-                         hfma2_bits(v[2], scale, mid), hfma2_bits(v[3], scale, mid));
-                }
+              for (int p = 0; p < 4; ++p) {
+                uint32_t v[4];
+                unpack4(words[p], v);
+                sts128(line + (((piece0 + (p ^ swap)) ^ (key & 7)) << 4), hfma2_bits(v[0], scale, mid), hfma2_bits(v[1], scale, mid),
+                       hfma2_bits(v[2], scale, mid), hfma2_bits(v[3], scale, mid));
               }
             }
           } else {
-            uint32_t bad = 0;  // of the warp's 32 rows
+            uint32_t bad = 0;  // of the warp's 16 rows
             const uint8_t* rows = (which ? a.vt : a.kt) + sg.u.r * a.t_req + sg.u.g * a.t_head + quad * 64;
 #pragma unroll 1
-            for (int y = 0; y < 4; ++y) {
-              const int key = w4 * 32 + 8 * y + r8;
+            for (int y = 0; y < 2; ++y) {
+              const int key = w8 * 16 + 8 * y + r8;
               uint4 in[4];
 #pragma unroll
               for (int p = 0; p < 4; ++p) {
@@ -300,17 +321,11 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
                        __byte_perm(in[p].y, in[p].w, 0x5410) & keep, __byte_perm(in[p].y, in[p].w, 0x7632) & keep);
             }
             // (four segments' words: this warp is two tiles ahead of the rows that look at them, at most)
-            if (which == 1 && lane == 0) sm->bad[seg & 3][key0 / kTilesStep][w4] = bad;
+            if (which == 1 && lane == 0) reinterpret_cast<uint16_t*>(sm->bad[seg & 3][key0 / kTilesStep])[w8] = (uint16_t)bad;
           }
           fence_async_smem();
           __syncwarp();
           if (lane == 0) mbar_arrive(which ? &sm->v_full[b] : &sm->k_full[b]);
-        }
-        if (!ok) break;
-        if (!tree) {
-          if (lane == 0)
-            for (int h = 0; h < halves; ++h) mbar_arrive(&sm->raw_empty[(taken + h) % kStages]);
-          taken += halves;
         }
       }
       step += sg.steps;
@@ -318,11 +333,28 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
       pos = sg.next;
     }
   } else {
-    // ============================ chains: one thread a row ============================
+    // ============================ chains: two threads a row, 64 keys (and columns of O) each ============================
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsChain));
-    const int c = (warp >> 2) - 2, quarter = warp & 3, row = quarter * 32 + lane;
+    const int c = (warp - kChainWarp) >> 3, half = ((warp - kChainWarp) >> 2) & 1, quarter = warp & 3, row = quarter * 32 + lane;
     const uint32_t lane_sel = (uint32_t)(quarter * 32) << 16;
-    const uint32_t tmem_s = tmem + 256u + 128u * c + lane_sel;
+    const uint32_t tmem_s = tmem + 256u + 128u * c + 64u * half + lane_sel;
+    const int pair_bar = 2 + 4 * c + quarter;
+    // The two warps of a quarter's rows.  A warp that gives up says so here, once, so that both leave: false if either does.
+    auto pair_sync = [&](bool fine) -> bool {
+      uint32_t out;
+      asm volatile(
+          "{\n\t.reg .pred p, q;\n\t"
+          "setp.eq.u32 q, %1, 0;\n\t"
+          "bar.red.or.pred p, %2, 64, q;\n\t"
+          "selp.u32 %0, 0, 1, p;\n\t}"
+          : "=r"(out) : "r"((uint32_t)fine), "r"(pair_bar) : "memory");
+      return out != 0;
+    };
+    // those that write a unit's rows together: the chain's, or all where the chains share them
+    auto rows_sync = [&]() {
+      if (kTwo) asm volatile("bar.sync %0, 256;" ::"r"(10 + c) : "memory");
+      else asm volatile("bar.sync 1, 512;" ::: "memory");
+    };
     int step = 0, done = 0, seg = 0;  // (segments with steps)
     bool ok = true;
     for (int pos = range_lo; pos < range_hi;) {
@@ -336,8 +368,9 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
       float rs = a.scale_log2;
       {
         const uint4* src = reinterpret_cast<const uint4*>(a.q + r * a.q_req + node * a.q_tok + h * a.q_head);
-        // with one tile for both chains each brings half of the channels
-        const int from = kTwo ? 0 : 8 * c, pieces = kTwo ? 16 : 8;
+        // each thread of a row brings its share of the channels: two share a row, or four where the chains do
+        constexpr int kPieces = kTwo ? 8 : 4;
+        const int from = kTwo ? 8 * half : 8 * half + 4 * c;
         float f = 1.f;
         if (kBf16) {
           uint32_t top = 0;
@@ -354,9 +387,9 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
             rs *= __uint_as_float((uint32_t)(127 - up) << 23);
           }
         }
-        const uint32_t line = smem_u32(sm->q[kTwo ? c : 0]) + row * 128;
-#pragma unroll 4
-        for (int p = 0; p < pieces; ++p) {
+        const uint32_t line = smem_u32(sm->q[kTwo ? c : 0]) + row * 128 + half * kHalfBytes;
+#pragma unroll
+        for (int p = 0; p < kPieces; ++p) {
           uint4 x = valid ? src[from + p] : make_uint4(0u, 0u, 0u, 0u);
           if (kBf16) {
             x.x = pack2<false>(__uint_as_float(x.x << 16) * f, __uint_as_float(x.x & 0xffff0000u) * f);
@@ -364,7 +397,7 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
             x.z = pack2<false>(__uint_as_float(x.z << 16) * f, __uint_as_float(x.z & 0xffff0000u) * f);
             x.w = pack2<false>(__uint_as_float(x.w << 16) * f, __uint_as_float(x.w & 0xffff0000u) * f);
           }
-          sts128(line + ((from + p) >> 3) * kHalfBytes + ((((from + p) & 7) ^ (row & 7)) << 4), __byte_perm(x.x, x.z, 0x5410), __byte_perm(x.x, x.z, 0x7632),
+          sts128(line + ((((from + p) & 7) ^ (row & 7)) << 4), __byte_perm(x.x, x.z, 0x5410), __byte_perm(x.x, x.z, 0x7632),
                  __byte_perm(x.y, x.w, 0x5410), __byte_perm(x.y, x.w, 0x7632));
         }
         fence_async_smem();
@@ -384,48 +417,65 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
 
       float m_used = -INFINITY, l = 0.f;
       bool any = false;  // the chain has had a tile
-      uint32_t poison = 0;
       for (int i = 0; i < sg.steps && ok; ++i) {
         const int x = step + i, t = sg.t0 + i;
         if (!kTwo && (x & 1) != c) continue;
         const bool tree = t >= sg.u.prefix.steps;
-        const int key0 = tree ? (t - sg.u.prefix.steps) * kTilesStep : sg.u.prefix.key_step(t) * kTilesStep;
-        uint32_t vis[4];
+        const int key0 = (tree ? t - sg.u.prefix.steps : sg.u.prefix.key_step(t)) * kTilesStep + half * kHalfKeys;
+        uint32_t vis[2];
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
+        for (int w = 0; w < 2; ++w) {
           if (tree) vis[w] = kv4_window_word(a, r, L, depth, (key0 >> 5) + w, kv4_mask_word(a, mask_row, node, (key0 >> 5) + w));
           else vis[w] = bits_below(L - key0 - 32 * w) & (~bits_below(begin - key0 - 32 * w) | bits_below(a.sinks - key0 - 32 * w));
         }
-        const bool masked = __any_sync(0xffffffffu, (vis[0] & vis[1] & vis[2] & vis[3]) != 0xffffffffu);
+        const bool masked = __any_sync(0xffffffffu, (vis[0] & vis[1]) != 0xffffffffu);
         ok = mbar_wait(sm, &sm->s_full[c], done & 1, a.status);
-        __syncwarp();
-        if (!ok) break;
+        // Chains that work on the same keys would do so in step, the tensor core idle meanwhile: they take turns at the
+        // exponentials, a tile of chain A, one of chain B.  (Neither is ever more than one turn ahead.)
+        if (kTwo && ok && (c == 1 || done > 0)) ok = mbar_wait(sm, &sm->turn[c ^ 1][quarter], (c == 1 ? done : done - 1) & 1, a.status);
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) {
+          if (warp_live) pair_sync(false);
+          break;
+        }
+        bool passed = false;
         if (warp_live) {
           tc_fence_after();
-          uint32_t s[128];
-          tmem_ld32(tmem_s, s, 0);
-          tmem_ld32(tmem_s + 32u, s, 32);
-          tmem_ld32(tmem_s + 64u, s, 64);
-          tmem_ld32(tmem_s + 96u, s, 96);
-          tc_wait_ld();
+          // 32 scores, -inf where masked
+          auto scores = [&](int x2, uint32_t (&s)[32]) {
+            tmem_ld32(tmem_s + 32u * x2, s, 0);
+            tc_wait_ld();
 #pragma unroll
-          for (int e = 0; e < 128; ++e) asm volatile("" : "+r"(s[e]));
-          if (masked) {
+            for (int e = 0; e < 32; ++e) asm volatile("" : "+r"(s[e]));
+            if (masked) {
+              const uint32_t bits = x2 ? vis[1] : vis[0];
 #pragma unroll
-            for (int e = 0; e < 128; ++e)
-              if (!((vis[e >> 5] >> (e & 31)) & 1u)) s[e] = __float_as_uint(-INFINITY);
-          }
+              for (int e = 0; e < 32; ++e)
+                if (!((bits >> e) & 1u)) s[e] = __float_as_uint(-INFINITY);
+            }
+          };
           // The exponentials are taken against the reference as it stands; their sum tells whether that was right (see
-          // tree_attention_stream.cu): the maximum is taken, the reference moved, O rescaled and the pass repeated only then.
+          // tree_attention_stream.cu): the maximum is taken, the reference moved, O rescaled and the pass repeated only then.  The scores
+          // stay in tensor memory until then; the row's two threads share the reference and decide together.
           bool settle = __any_sync(0xffffffffu, m_used == -INFINITY);
           float sum;
+          uint32_t packed[2][16];
 #pragma unroll 1
           for (;;) {
             if (settle) {
-              float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+              float mx[2] = {-INFINITY, -INFINITY};
+#pragma unroll 1
+              for (int x2 = 0; x2 < 2; ++x2) {
+                uint32_t s[32];
+                scores(x2, s);
 #pragma unroll
-              for (int e = 0; e < 128; e += 2) mx[(e >> 1) & 3] = max3(mx[(e >> 1) & 3], __uint_as_float(s[e]), __uint_as_float(s[e + 1]));
-              const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * rs;  // rs > 0
+                for (int e = 0; e < 32; e += 2) mx[(e >> 1) & 1] = max3(mx[(e >> 1) & 1], __uint_as_float(s[e]), __uint_as_float(s[e + 1]));
+              }
+              sm->xchg[c][half][row] = fmaxf(mx[0], mx[1]);
+              ok = pair_sync(true);
+              const float top = fmaxf(fmaxf(mx[0], mx[1]), sm->xchg[c][half ^ 1][row]) * rs;  // rs > 0
+              if (ok) ok = pair_sync(true);  // (read: the next exchange may follow at once)
+              if (!ok) break;
               const bool move = top > m_used + kRescaleThreshold || (m_used == -INFINITY && top != -INFINITY);
               if (__any_sync(0xffffffffu, move)) {
                 float alpha = 1.f;
@@ -437,13 +487,14 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
                 __syncwarp();
                 if (any) {  // (the product before this S has completed: see the issuer)
 #pragma unroll 1
-                  for (int x4 = 0; x4 < 4; ++x4) {
+                  for (int x2 = 0; x2 < 2; ++x2) {
+                    const uint32_t at = tmem + 128u * c + 64u * half + 32u * x2 + lane_sel;
                     uint32_t o[32];
-                    tmem_ld32(tmem + 128u * c + lane_sel + 32u * x4, o, 0);
+                    tmem_ld32(at, o, 0);
                     tc_wait_ld();
 #pragma unroll
                     for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * alpha);
-                    tmem_st32(tmem + 128u * c + lane_sel + 32u * x4, o, 0);
+                    tmem_st32(at, o, 0);
                   }
                 }
               }
@@ -452,17 +503,21 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
             const uint64_t rs2 = pair_of(rs, rs), neg_m2 = pair_of(neg_m, neg_m);
             uint64_t sums[2] = {pair_of(0.f, 0.f), pair_of(0.f, 0.f)};
 #pragma unroll
-            for (int x4 = 0; x4 < 4; ++x4) {
-              uint32_t packed[16];
+            for (int x2 = 0; x2 < 2; ++x2) {
+              uint32_t s[32];
+              scores(x2, s);
 #pragma unroll
               for (int e = 0; e < 16; ++e) {
                 float y0, y1;
-                unpair(fma2(pair_of(__uint_as_float(s[32 * x4 + 2 * e]), __uint_as_float(s[32 * x4 + 2 * e + 1])), rs2, neg_m2), y0, y1);
+                unpair(fma2(pair_of(__uint_as_float(s[2 * e]), __uint_as_float(s[2 * e + 1])), rs2, neg_m2), y0, y1);
                 const float p0 = ex2(y0), p1 = ex2(y1);
                 sums[e & 1] = add2(sums[e & 1], pair_of(p0, p1));
-                packed[e] = pack2<false>(p0, p1);
+                packed[x2][e] = pack2<false>(p0, p1);
               }
-              tmem_st16(tmem_s + 16u * x4, packed);
+              if (kTwo && x2 == 0 && !passed) {
+                passed = true;
+                if (lane == 0) mbar_arrive(&sm->turn[c][quarter]);
+              }
             }
             float s0, s1, s2, s3;
             unpair(sums[0], s0, s1);
@@ -470,12 +525,21 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
             sum = (s0 + s1) + (s2 + s3);
             if (settle) break;
             settle = __any_sync(0xffffffffu, !(sum <= kRescaleLimit));
+            if (lane == 0) sm->above[done & 1][c][half][quarter] = settle;
+            ok = pair_sync(true);
+            if (!ok) break;
+            settle = settle || sm->above[done & 1][c][half ^ 1][quarter];
             if (!settle) break;
-            tc_wait_st();
           }
+          if (!ok) break;
+          // over this thread's scores
+          tmem_st16(tmem_s, packed[0]);
+          tmem_st16(tmem_s + 16u, packed[1]);
           l += sum;
           tc_wait_st();
           tc_fence_before();
+        } else if (kTwo && lane == 0) {
+          mbar_arrive(&sm->turn[c][quarter]);
         }
         __syncwarp();
         if (lane == 0) mbar_arrive(&sm->p_full[c]);
@@ -487,6 +551,7 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
       __syncwarp();
       tc_fence_after();
       if (!ok) any = false;
+      uint32_t poison = 0;
       for (int i = max(sg.u.prefix.steps - sg.t0, 0); i < sg.steps; ++i) {  // tree rows that are not finite and that the row sees
         if (!kTwo && ((step + i) & 1) != c) continue;
         const int tile = sg.t0 + i - sg.u.prefix.steps;
@@ -497,28 +562,26 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
         }
       }
       if (poison != 0) l = NAN;
-      // ---- out: a chain with a tile of its own writes 128 columns, chains that share one 64 each of their sum
-      float M = m_used, sum = l, fA = 1.f, fB = 0.f;
-      if (!kTwo) {
-        sm->ml[c][row] = any ? make_float2(m_used, l) : make_float2(-INFINITY, l != l ? l : 0.f);
-        asm volatile("bar.sync 1, 256;" ::: "memory");
-        const float2 A = sm->ml[0][row], Bv = sm->ml[1][row];
-        M = fmaxf(A.x, Bv.x);
-        fA = A.x == -INFINITY ? 0.f : ex2(A.x - M);
-        fB = Bv.x == -INFINITY ? 0.f : ex2(Bv.x - M);
-        sum = fmaf(A.y, fA, Bv.y * fB);
+      // ---- the row's sum: of its two threads, of the two chains where they share it
+      rows_sync();  // (nobody looks at what was exchanged last any more)
+      sm->xchg[c][half][row] = l;
+      if (!kTwo && half == 0) sm->ml[kTwo ? 0 : c][kTwo ? 0 : row].x = any ? m_used : -INFINITY;
+      rows_sync();
+      float M = any ? m_used : -INFINITY, fA = 1.f, fB = 0.f, sum;
+      if (kTwo) {
+        sum = sm->xchg[c][0][row] + sm->xchg[c][1][row];
+      } else {
+        const float mA = sm->ml[0][kTwo ? 0 : row].x, mB = sm->ml[kTwo ? 0 : 1][kTwo ? 0 : row].x;
+        M = fmaxf(mA, mB);
+        fA = mA == -INFINITY ? 0.f : ex2(mA - M);
+        fB = mB == -INFINITY ? 0.f : ex2(mB - M);
+        sum = fmaf(sm->xchg[0][0][row] + sm->xchg[0][1][row], fA, (sm->xchg[1][0][row] + sm->xchg[1][1][row]) * fB);
       }
-      const bool own = kTwo ? any : true;
-      const float inv = 1.f / sum;
-      const int slot = 2 * blockIdx.x + (pos == range_lo ? 0 : 1);
-      const int64_t ws_row = (int64_t)slot * a.row_tile + (kTwo ? c * kTileM : 0) + row;
-      uint8_t* out = a.out + r * a.o_req + node * a.o_tok + h * a.o_head;
-#pragma unroll 1
-      for (int x4 = kTwo ? 0 : 2 * c; x4 < (kTwo ? 4 : 2 * c + 2); ++x4) {
-        float o[32];
+      // 32 columns of the accumulator, unnormalised; first column 32 * x4
+      auto columns = [&](int x4, float (&o)[32]) {
         __syncwarp();
         if (kTwo) {
-          if (own) {
+          if (any) {
             tmem_ld32(tmem + 128u * c + lane_sel + 32u * x4, reinterpret_cast<uint32_t*>(o), 0);
             tc_wait_ld();
           } else {
@@ -526,41 +589,103 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
             for (int e = 0; e < 32; ++e) o[e] = 0.f;
           }
         } else {
-          float ob[32];
+          // (an accumulator that nobody wrote may hold anything)
           tmem_ld32(tmem + lane_sel + 32u * x4, reinterpret_cast<uint32_t*>(o), 0);
-          tmem_ld32(tmem + 128u + lane_sel + 32u * x4, reinterpret_cast<uint32_t*>(ob), 0);
           tc_wait_ld();
 #pragma unroll
-          for (int e = 0; e < 32; ++e) o[e] = (fA == 0.f ? 0.f : o[e] * fA) + (fB == 0.f ? 0.f : ob[e] * fB);  // (an accumulator nobody wrote may hold anything)
-        }
-        if (valid && sg.whole) {
+          for (int e = 0; e < 32; ++e) o[e] = fA == 0.f ? 0.f : o[e] * fA;
 #pragma unroll
-          for (int e = 0; e < 32; e += 8) {  // columns 0,2,4,6,1,3,5,7 are channels 0..7
-            uint4 val;
-            val.x = pack2<kBf16>(o[e] * inv, o[e + 2] * inv);
-            val.y = pack2<kBf16>(o[e + 4] * inv, o[e + 6] * inv);
-            val.z = pack2<kBf16>(o[e + 1] * inv, o[e + 3] * inv);
-            val.w = pack2<kBf16>(o[e + 5] * inv, o[e + 7] * inv);
-            *reinterpret_cast<uint4*>(out + 64 * x4 + 2 * e) = val;
+          for (int y = 0; y < 2; ++y) {
+            uint32_t b[16];
+            asm volatile(
+                "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+                : "=r"(b[0]), "=r"(b[1]), "=r"(b[2]), "=r"(b[3]), "=r"(b[4]), "=r"(b[5]), "=r"(b[6]), "=r"(b[7]), "=r"(b[8]), "=r"(b[9]), "=r"(b[10]),
+                  "=r"(b[11]), "=r"(b[12]), "=r"(b[13]), "=r"(b[14]), "=r"(b[15]) : "r"(tmem + 128u + lane_sel + 32u * x4 + 16u * y) : "memory");
+            tc_wait_ld();
+#pragma unroll
+            for (int e = 0; e < 16; ++e) o[16 * y + e] += fB == 0.f ? 0.f : __uint_as_float(b[e]) * fB;
           }
-        } else if (valid) {
-          float4* to = reinterpret_cast<float4*>(a.ws_o + ws_row * kHeadDim + 32 * x4);
+        }
+      };
+      constexpr int kRuns = kTwo ? 2 : 1;  // of 32 columns a thread
+      const int first_run = kTwo ? 2 * half : 2 * half + c;
+      bool complete = sg.whole;
+      Kv4Pieces pieces;
+      if (!sg.whole) {
+        // This CTA's piece goes to the workspace and is counted; the one that counts the last piece adds them all, in the order
+        // of their CTAs, and writes the rows.  Nobody waits for anybody.
+        pieces = kv4_pieces(ranges, sg.u);
+        int32_t* const count = a.ws_count + 2 * pieces.first + (kTwo ? c : 0);
+        const int64_t mine = (int64_t)kv4_slot(ranges, blockIdx.x, sg.u.begin) * a.row_tile + (kTwo ? c * kTileM : 0);
+        float4* to = reinterpret_cast<float4*>(a.ws_o + mine * kHeadDim) + row;  // [channel / 4][row]
+#pragma unroll 1
+        for (int run = first_run; run < first_run + kRuns; ++run) {
+          float o[32];
+          columns(run, o);
 #pragma unroll
-          for (int e = 0; e < 32; e += 8) {
-            to[e / 4] = make_float4(o[e], o[e + 2], o[e + 4], o[e + 6]);
-            to[e / 4 + 1] = make_float4(o[e + 1], o[e + 3], o[e + 5], o[e + 7]);
+          for (int e = 0; e < 32; e += 4) to[(int64_t)(8 * run + (e >> 2)) * kTileM] = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+        }
+        if (half == 0 && (kTwo || c == 0)) a.ws_ml[mine + row] = make_float2(M, sum);
+        __threadfence();
+        rows_sync();
+        const bool teller = half == 0 && quarter == 0 && lane == 0 && (kTwo || c == 0);
+        if (teller) sm->last[kTwo ? c : 0] = atomicAdd(count, 1) == pieces.last - pieces.first;
+        rows_sync();
+        complete = sm->last[kTwo ? c : 0] != 0;
+        if (complete) {
+          __threadfence();
+          M = -INFINITY;
+          for (int x = pieces.first; x <= pieces.last; ++x)
+            M = fmaxf(M, __ldcg(a.ws_ml + (int64_t)kv4_slot(ranges, x, sg.u.begin) * a.row_tile + (kTwo ? c * kTileM : 0) + row).x);
+          sum = 0.f;
+          for (int x = pieces.first; x <= pieces.last; ++x) {
+            const float2 ml = __ldcg(a.ws_ml + (int64_t)kv4_slot(ranges, x, sg.u.begin) * a.row_tile + (kTwo ? c * kTileM : 0) + row);
+            sum = fmaf(ml.y, ml.x == -INFINITY ? 0.f : ex2(ml.x - M), sum);
           }
         }
       }
-      if (valid && (kTwo || c == 0)) {
-        if (sg.whole) {
-          if (a.lse != nullptr) a.lse[((int64_t)r * a.Hq + h) * a.n + node] = (M + log2f(sum)) * kLn2;
-        } else {
-          a.ws_ml[ws_row] = make_float2(own ? M : -INFINITY, sum);
+      if (complete) {
+        const float inv = 1.f / sum;
+        uint8_t* out = a.out + r * a.o_req + node * a.o_tok + h * a.o_head;
+#pragma unroll 1
+        for (int run = first_run; run < first_run + kRuns; ++run) {
+          float o[32];
+          if (sg.whole) {
+            columns(run, o);
+          } else {
+#pragma unroll
+            for (int e = 0; e < 32; ++e) o[e] = 0.f;
+            for (int x = pieces.first; x <= pieces.last; ++x) {
+              const int64_t at = (int64_t)kv4_slot(ranges, x, sg.u.begin) * a.row_tile + (kTwo ? c * kTileM : 0);
+              const float mx = __ldcg(a.ws_ml + at + row).x;
+              const float f = mx == -INFINITY ? 0.f : ex2(mx - M);
+              const float4* from = reinterpret_cast<const float4*>(a.ws_o + at * kHeadDim) + row;
+#pragma unroll
+              for (int e = 0; e < 32; e += 4) {
+                const float4 v = __ldcg(from + (int64_t)(8 * run + (e >> 2)) * kTileM);
+                o[e] = fmaf(v.x, f, o[e]);
+                o[e + 1] = fmaf(v.y, f, o[e + 1]);
+                o[e + 2] = fmaf(v.z, f, o[e + 2]);
+                o[e + 3] = fmaf(v.w, f, o[e + 3]);
+              }
+            }
+          }
+          if (valid) {
+#pragma unroll
+            for (int e = 0; e < 32; e += 8) {  // columns 0,2,4,6,1,3,5,7 are channels 0..7
+              uint4 val;
+              val.x = pack2<kBf16>(o[e] * inv, o[e + 2] * inv);
+              val.y = pack2<kBf16>(o[e + 4] * inv, o[e + 6] * inv);
+              val.z = pack2<kBf16>(o[e + 1] * inv, o[e + 3] * inv);
+              val.w = pack2<kBf16>(o[e + 5] * inv, o[e + 7] * inv);
+              *reinterpret_cast<uint4*>(out + 64 * run + 2 * e) = val;
+            }
+          }
         }
+        if (valid && half == 0 && (kTwo || c == 0) && a.lse != nullptr) a.lse[((int64_t)r * a.Hq + h) * a.n + node] = (M + log2f(sum)) * kLn2;
       }
       tc_fence_before();
-      if (!kTwo) asm volatile("bar.sync 1, 256;" ::: "memory");  // both accumulators are read, both chains are through with Q
+      rows_sync();  // the accumulators are read, the rows are through with Q and with what they exchanged
       step += sg.steps;
       seg += sg.steps > 0;
       pos = sg.next;
@@ -578,7 +703,8 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
 static bool tiles_two(const seq_tree_kv4_attention_params& p) { return p.n_tree * (p.num_q_heads / p.num_kv_heads) > kTileM; }
 
 size_t kv4_tiles_workspace_bytes(const seq_tree_kv4_attention_params& p) {
-  return (size_t)2 * device_sm_count() * (tiles_two(p) ? 2 : 1) * kTileM * (kHeadDim * sizeof(float) + sizeof(float2));
+  const size_t sms = device_sm_count();
+  return kv4_count_bytes(sms) + 2 * sms * (tiles_two(p) ? 2 : 1) * kTileM * (kHeadDim * sizeof(float) + sizeof(float2));
 }
 
 int launch_kv4_tiles(const seq_tree_kv4_attention_params& p, cudaStream_t stream) {
@@ -593,8 +719,11 @@ int launch_kv4_tiles(const seq_tree_kv4_attention_params& p, cudaStream_t stream
   if (most > 0x7fffffff) return SEQ_ERR_UNSUPPORTED;
   const int64_t want = (most + a.min_steps - 1) / a.min_steps;
   a.ctas = want < sms ? (int)want : sms;
-  a.ws_o = static_cast<float*>(p.workspace);
+  a.ws_count = static_cast<int32_t*>(p.workspace);
+  a.ws_o = reinterpret_cast<float*>(static_cast<uint8_t*>(p.workspace) + kv4_count_bytes(sms));
   a.ws_ml = reinterpret_cast<float2*>(a.ws_o + (size_t)2 * sms * a.row_tile * kHeadDim);
+  const int rc0 = launch_kv4_zero(a, stream);
+  if (rc0 != SEQ_OK) return rc0;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(a.ctas);
   cfg.blockDim = dim3(kTilesThreads);
@@ -619,8 +748,7 @@ int launch_kv4_tiles(const seq_tree_kv4_attention_params& p, cudaStream_t stream
   int rc;
   if (two) rc = bf16 ? launch(kv4_tiles_kernel<true, true>, 0, tiles_smem_bytes<true>()) : launch(kv4_tiles_kernel<true, false>, 1, tiles_smem_bytes<true>());
   else rc = bf16 ? launch(kv4_tiles_kernel<false, true>, 2, tiles_smem_bytes<false>()) : launch(kv4_tiles_kernel<false, false>, 3, tiles_smem_bytes<false>());
-  if (rc != SEQ_OK) return rc;
-  return launch_kv4_combine(a, kTilesStep, bf16, stream);
+  return rc;
 }
 
 }  // namespace seqtree
