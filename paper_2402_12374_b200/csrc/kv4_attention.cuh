@@ -15,7 +15,7 @@ namespace seqtree {
 struct Kv4Args {
   int32_t batch, n, max_len, Hq, Hkv, group, rows;  // rows: n * group
   int32_t window, sinks;
-  int32_t num_pages, page_size;
+  int32_t num_pages, page_size, page_shift;
   int32_t row_tile, tiles, tree_steps, ctas, min_steps;
   const uint8_t* q; int64_t q_req, q_tok, q_head;  // all strides in bytes
   const uint8_t* kt; const uint8_t* vt; int64_t t_req, t_tok, t_head;
@@ -163,7 +163,7 @@ __device__ __forceinline__ uint32_t kv4_window_word(const Kv4Args& a, int r, int
 
 size_t kv4_rows_workspace_bytes(const seq_tree_kv4_attention_params& p);
 int launch_kv4_rows(const seq_tree_kv4_attention_params& p, cudaStream_t stream);
-size_t kv4_tiles_workspace_bytes(const seq_tree_kv4_attention_params& p);
+size_t kv4_tiles_workspace_bytes();
 int launch_kv4_tiles(const seq_tree_kv4_attention_params& p, cudaStream_t stream);
 // Arguments that do not depend on the kernel
 Kv4Args kv4_args(const seq_tree_kv4_attention_params& p);

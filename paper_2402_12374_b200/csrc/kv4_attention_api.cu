@@ -33,6 +33,7 @@ Kv4Args kv4_args(const seq_tree_kv4_attention_params& p) {
   a.rows = a.n * a.group;
   a.window = p.window; a.sinks = p.sinks;
   a.num_pages = p.num_pages; a.page_size = p.page_size;
+  a.page_shift = p.page_size == 16 ? 4 : p.page_size == 32 ? 5 : p.page_size == 64 ? 6 : 7;
   a.q = static_cast<const uint8_t*>(p.q); a.q_req = 2 * p.q_stride_req; a.q_tok = 2 * p.q_stride_tok; a.q_head = 2 * p.q_stride_head;
   a.kt = static_cast<const uint8_t*>(p.k_tree); a.vt = static_cast<const uint8_t*>(p.v_tree);
   a.t_req = 2 * p.t_stride_req; a.t_tok = 2 * p.t_stride_tok; a.t_head = 2 * p.t_stride_head;
@@ -76,7 +77,7 @@ using namespace seqtree;
 
 extern "C" size_t seq_tree_kv4_attention_workspace_bytes(const seq_tree_kv4_attention_params* p) {
   if (p == nullptr || p->num_kv_heads < 1 || p->num_q_heads < 1 || p->n_tree < 1) return 0;
-  return few_rows(*p) ? kv4_rows_workspace_bytes(*p) : kv4_tiles_workspace_bytes(*p);
+  return few_rows(*p) ? kv4_rows_workspace_bytes(*p) : kv4_tiles_workspace_bytes();
 }
 
 extern "C" int seq_tree_kv4_attention(const seq_tree_kv4_attention_params* p, void* stream) {

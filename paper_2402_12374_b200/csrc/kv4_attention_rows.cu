@@ -161,8 +161,8 @@ __global__ void __launch_bounds__(32 * kRowsWarps, NT == 1 ? 3 : 2) kv4_rows_ker
       if (tt < lu.prefix.steps) {
         const int key = lu.prefix.key_step(tt) * kRowsStep;
         const int32_t* row = a.table + lu.r * a.table_stride;
-        id0 = row[key / a.page_size];
-        id1 = a.page_size == kGranule && key + kGranule < lu.L ? row[key / a.page_size + 1] : id0;
+        id0 = row[key >> a.page_shift];
+        id1 = a.page_size == kGranule && key + kGranule < lu.L ? row[(key >> a.page_shift) + 1] : id0;
         if ((unsigned)id0 >= (unsigned)a.num_pages || (unsigned)id1 >= (unsigned)a.num_pages) {
           dev_flag(a.status, SEQ_DEV_BAD_PAGE);
           id0 = (unsigned)id0 < (unsigned)a.num_pages ? id0 : 0;

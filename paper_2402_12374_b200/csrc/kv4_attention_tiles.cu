@@ -10,9 +10,9 @@
 // Q's channels are stored in that order too, and O's columns are put back when the rows are written.  The tree's 16-bit rows go
 // through the same warps.
 //
-// Two chains of four row warps, each with its own S/P and O in tensor memory, keep the tensor core busy in turn: with kTwo a
-// unit is 256 rows, a chain has a 128-row tile of its own and both use every K/V tile; otherwise a unit is 128 rows, the
-// chains take the key tiles in turns and meet at the unit's end.  One warp each issues a chain's products.
+// A tile of scores is worked on by two threads a row, 64 keys each; there are four groups of 128 such threads, for the halves of
+// even and of odd tiles, and three S/P buffers, so that the next tiles' scores are computed meanwhile.  All add to one
+// accumulator and share the rows' reference maxima, which they settle in the keys' order (see the chains).
 //
 // Every mbarrier wait is bounded; one that runs out raises SEQ_DEV_TIMEOUT and the CTA drains.
 #include "kv4_attention.cuh"
@@ -28,30 +28,30 @@ constexpr int kHalfKeys = 64;       // keys of a ring stage
 constexpr int kStageBytes = kHalfKeys / kGranule * kGranuleBytes;
 constexpr int kTreeTiles = SEQ_MAX_TREE / kTilesStep;
 
-template <bool kTwo>
+constexpr int kStages = 6, kSBufs = 3;
+constexpr uint32_t kTmemS = 128;  // tensor memory: O in columns 0..127, then the S/P buffers
+
 struct TilesSmem {
-  static constexpr int kStages = kTwo ? 3 : 6;
-  uint8_t q[kTwo ? 2 : 1][kTileBytes];  // tiles: 1024-byte aligned
-  uint8_t k[2][kTileBytes];
+  uint8_t q[kTileBytes];  // tiles: 1024-byte aligned
+  uint8_t k[2][kTileBytes];  // [tile parity]
   uint8_t v[2][kTileBytes];
   uint8_t ring[kStages][kStageBytes];
   uint64_t raw_full[kStages], raw_empty[kStages];
-  uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2];  // [tile parity]
-  uint64_t q_full[2], s_full[2], p_full[2], pv_done[2];   // [chain]
-  uint64_t turn[2][4];  // [chain][lane quarter], with kTwo: most of the chain's exponentials of a tile are under way
+  uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2];
+  uint64_t q_full;
+  uint64_t s_full[kSBufs], p_full[kSBufs][2], pv_done[kSBufs][2];  // [S/P buffer][half of its keys]
+  uint64_t settled[4][4];  // [group][lane quarter]: the reference of the quarter's rows is settled for the group's 64 keys
   uint64_t drained[2];
-  float xchg[2][2][kTileM];        // [chain][half]: what the two threads of a row tell each other
-  float2 ml[kTwo ? 1 : 2][kTwo ? 1 : kTileM];  // the chains' (m, l), where they share rows
-  int32_t above[2][2][2][4];       // [step parity][chain][half][lane quarter]: a score is far above its row's reference
-  int32_t last[2];                 // [chain]: this CTA completes the unit
+  float ref[kTileM];       // the rows' reference maximum, handed on in the keys' order
+  float2 ml[4][kTileM];    // [group]: (m, l) of every row
+  int32_t last;            // this CTA completes the unit
   uint32_t bad[4][kTreeTiles][4];  // [segment mod 4]: tree rows whose V is not finite in half precision
   uint32_t tmem_base;
   volatile int abort_flag;
   Kv4Plan plan;
 };
-template <bool kTwo>
-constexpr size_t tiles_smem_bytes() { return sizeof(TilesSmem<kTwo>) + 1024; }
-static_assert(tiles_smem_bytes<true>() <= 227 * 1024 && tiles_smem_bytes<false>() <= 227 * 1024, "one CTA's shared memory");
+constexpr size_t kTilesSmemBytes = sizeof(TilesSmem) + 1024;
+static_assert(kTilesSmemBytes <= 227 * 1024, "one CTA's shared memory");
 
 __device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
   asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
@@ -80,23 +80,24 @@ __device__ __forceinline__ TilesSeg tiles_seg(const Kv4Plan* plan, const Kv4Args
   return s;
 }
 
-template <bool kTwo, bool kBf16>
+template <bool kBf16>
 __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Args a) {
   extern __shared__ uint8_t smem_raw[];
-  using Smem = TilesSmem<kTwo>;
-  constexpr int kStages = Smem::kStages;
-  Smem* sm = reinterpret_cast<Smem*>(smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u));
+  TilesSmem* sm = reinterpret_cast<TilesSmem*>(smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u));
   const int warp = uniform((int)threadIdx.x >> 5), lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
     for (int s = 0; s < kStages; ++s) { mbar_init(&sm->raw_full[s], 1); mbar_init(&sm->raw_empty[s], 4); }
     for (int b = 0; b < 2; ++b) {
-      mbar_init(&sm->k_full[b], 8); mbar_init(&sm->k_empty[b], kTwo ? 2 : 1);
-      mbar_init(&sm->v_full[b], 8); mbar_init(&sm->v_empty[b], kTwo ? 2 : 1);
-      mbar_init(&sm->q_full[b], kTwo ? 8 : 16);
-      mbar_init(&sm->s_full[b], 1); mbar_init(&sm->p_full[b], 8); mbar_init(&sm->pv_done[b], 1);
-      for (int x = 0; x < 4; ++x) mbar_init(&sm->turn[b][x], 2);
+      mbar_init(&sm->k_full[b], 8); mbar_init(&sm->k_empty[b], 1);
+      mbar_init(&sm->v_full[b], 8); mbar_init(&sm->v_empty[b], 1);
       mbar_init(&sm->drained[b], 1);
     }
+    mbar_init(&sm->q_full, 16);
+    for (int b = 0; b < kSBufs; ++b) {
+      mbar_init(&sm->s_full[b], 1);
+      for (int h = 0; h < 2; ++h) { mbar_init(&sm->p_full[b][h], 4); mbar_init(&sm->pv_done[b][h], 1); }
+    }
+    for (int x = 0; x < 16; ++x) mbar_init(&sm->settled[x >> 2][x & 3], 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     sm->abort_flag = 0;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -131,7 +132,7 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
             if (key >= sg.u.L) break;
             const int granules = min(kHalfKeys / kGranule, (sg.u.L - key + kGranule - 1) / kGranule);
             const int st = issued % kStages, w = issued / kStages;
-            const int first = key / a.page_size, last = (key + granules * kGranule - 1) / a.page_size;
+            const int first = key >> a.page_shift, last = (key + granules * kGranule - 1) >> a.page_shift;
             if (r_known != sg.u.r || first < page0 || last >= page0 + 32) {
               r_known = sg.u.r;
               page0 = first;
@@ -167,53 +168,55 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
           for (uint32_t it = 0; it < (1u << 16); ++it)
             if (mbar_try_wait(&sm->raw_full[x % kStages], (x / kStages) & 1)) break;
     } else if (warp < 3) {
-      // ============================ issuer of a chain ============================
-      const int c = warp - 1;
-      const uint32_t tmem_o = tmem + 128u * c, tmem_s = tmem + 256u + 128u * c;
+      // ============================ issuers: S (warp 1), P V (warp 2) ============================
       const uint32_t idesc = (1u << 4) | ((uint32_t)(kTileM >> 4) << 24) | ((uint32_t)(kTilesStep >> 3) << 17);  // fp16, sums fp32, N = 128
       const uint32_t idesc_pv = idesc | (1u << 16);                                                             // V is MN-major
-      int step = 0, done = 0, seg = 0;  // K/V tiles before this segment, this chain's products, segments
+      int step = 0, seg = 0;  // tiles before this segment, segments
       bool ok = true;
       for (int pos = range_lo; pos < range_hi && ok; ++seg) {
         const TilesSeg sg = tiles_seg(&sm->plan, a, pos, range_hi);
-        ok = mbar_wait(sm, &sm->q_full[c], seg & 1, a.status);
-        const uint32_t q_lo = desc_lo(smem_u32(sm->q[kTwo ? c : 0]), 16);
-        bool first = true;
-        for (int i = 0; i < sg.steps && ok; ++i) {
-          const int x = step + i, b = x & 1, w = x >> 1;
-          if (!kTwo && b != c) continue;
-          // S goes where the last P was: its product has completed
-          ok = mbar_wait(sm, &sm->k_full[b], w & 1, a.status) && (done == 0 || mbar_wait(sm, &sm->pv_done[c], (done - 1) & 1, a.status));
-          if (!ok) break;
-          tc_fence_after();
-          if (elect_one()) {
-            mma_qk<kHalfBytes, kHalfBytes>(tmem_s, q_lo, desc_lo(smem_u32(sm->k[b]), 16), idesc);
-            tc_commit(&sm->s_full[c]);
-            tc_commit(&sm->k_empty[b]);
+        if (warp == 1) {
+          ok = mbar_wait(sm, &sm->q_full, seg & 1, a.status);
+          const uint32_t q_lo = desc_lo(smem_u32(sm->q), 16);
+          for (int i = 0; i < sg.steps && ok; ++i) {
+            const int x = step + i, b = x & 1, u = x / kSBufs, sb = x - u * kSBufs;
+            // S goes where the P of three tiles ago was: its product has completed
+            ok = mbar_wait(sm, &sm->k_full[b], (x >> 1) & 1, a.status) && (u == 0 || mbar_wait(sm, &sm->pv_done[sb][1], (u - 1) & 1, a.status));
+            if (!ok) break;
+            tc_fence_after();
+            if (elect_one()) {
+              mma_qk<kHalfBytes, kHalfBytes>(tmem + kTmemS + 128u * sb, q_lo, desc_lo(smem_u32(sm->k[b]), 16), idesc);
+              tc_commit(&sm->s_full[sb]);
+              tc_commit(&sm->k_empty[b]);
+            }
+            __syncwarp();
           }
-          __syncwarp();
-          ok = mbar_wait(sm, &sm->v_full[b], w & 1, a.status) && mbar_wait(sm, &sm->p_full[c], done & 1, a.status);
-          if (!ok) break;
-          tc_fence_after();
-          const uint32_t v_lo = desc_lo(smem_u32(sm->v[b]), kHalfBytes);
-          if (elect_one()) {
-            mma_pv(tmem_o, tmem_s, v_lo, idesc_pv, first ? 0u : 1u);
-            mma_pv(tmem_o, tmem_s + 64u, v_lo + (kHalfKeys * 128 >> 4), idesc_pv, 1u);
-            tc_commit(&sm->pv_done[c]);
-            tc_commit(&sm->v_empty[b]);
+        } else {
+          for (int i = 0; i < sg.steps && ok; ++i) {
+            const int x = step + i, b = x & 1, u = x / kSBufs, sb = x - u * kSBufs;
+            const uint32_t p_at = tmem + kTmemS + 128u * sb, v_lo = desc_lo(smem_u32(sm->v[b]), kHalfBytes);
+            ok = mbar_wait(sm, &sm->v_full[b], (x >> 1) & 1, a.status);
+            for (int h = 0; h < 2 && ok; ++h) {
+              ok = mbar_wait(sm, &sm->p_full[sb][h], u & 1, a.status);
+              if (!ok) break;
+              tc_fence_after();
+              if (elect_one()) {
+                mma_pv(tmem, p_at + 64u * h, v_lo + h * (kHalfKeys * 128 >> 4), idesc_pv, i > 0 || h > 0 ? 1u : 0u);
+                tc_commit(&sm->pv_done[sb][h]);
+                if (h == 1) tc_commit(&sm->v_empty[b]);
+              }
+              __syncwarp();
+            }
           }
-          __syncwarp();
-          first = false;
-          ++done;
         }
         step += sg.steps;
         pos = sg.next;
       }
       if (!ok) {  // what has been issued reads shared and tensor memory
-        if (elect_one()) tc_commit(&sm->drained[c]);
+        if (elect_one()) tc_commit(&sm->drained[warp - 1]);
         __syncwarp();
         for (uint32_t it = 0; it < (1u << 16); ++it)
-          if (mbar_try_wait(&sm->drained[c], 0)) break;
+          if (mbar_try_wait(&sm->drained[warp - 1], 0)) break;
       }
     }
   } else if (warp < kChainWarp) {
@@ -234,44 +237,27 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
         const int key0 = tree ? (t - sg.u.prefix.steps) * kTilesStep : sg.u.prefix.key_step(t) * kTilesStep;
         const int left = (tree ? a.n : sg.u.L) - key0;  // keys of the tile that there are
         const int halves = left > kHalfKeys ? 2 : 1;
-        // The codes of the thread's rows, of K and of V, into registers: the ring's stages are free again before they are unpacked.
-        uint4 code[2][2];
-        uint32_t params[2][2];
-        if (!tree) {
-          if (half < halves) ok = mbar_wait(sm, &sm->raw_full[(taken + half) % kStages], ((taken + half) / kStages) & 1, a.status);
-          __syncwarp();
-          if (!ok) break;
-          const uint32_t granule = smem_u32(sm->ring[(taken + half) % kStages]) + (w8 & 3) * kGranuleBytes;
-#pragma unroll
-          for (int y = 0; y < 2; ++y) {
-            const int row = 8 * y + r8;
-#pragma unroll
-            for (int which = 0; which < 2; ++which) {
-              code[which][y] = make_uint4(0u, 0u, 0u, 0u);
-              params[which][y] = 0;  // a key behind the prefix: zeros
-              if (w8 * kGranule + row < left) {
-                asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(code[which][y].x), "=r"(code[which][y].y), "=r"(code[which][y].z), "=r"(code[which][y].w)
-                             : "r"(granule + which * kGranuleV + row * kCodeBytes + quad * 16) : "memory");
-                asm volatile("ld.shared.u32 %0, [%1];" : "=r"(params[which][y]) : "r"(granule + kGranuleParams + which * (kGranule * 4) + row * 4) : "memory");
-              }
-            }
-          }
-          __syncwarp();
-          if (lane == 0 && half < halves) mbar_arrive(&sm->raw_empty[(taken + half) % kStages]);
-          taken += halves;
-        }
-#pragma unroll
-        for (int which = 0; which < 2; ++which) {
+        if (!tree && half < halves) ok = mbar_wait(sm, &sm->raw_full[(taken + half) % kStages], ((taken + half) / kStages) & 1, a.status);
+        const uint32_t granule = smem_u32(sm->ring[(taken + half) % kStages]) + (w8 & 3) * kGranuleBytes + r8 * kCodeBytes + quad * 16;
+#pragma unroll 1
+        for (int which = 0; which < 2 && ok; ++which) {
           if (w > 0) ok = mbar_wait(sm, which ? &sm->v_empty[b] : &sm->k_empty[b], (w - 1) & 1, a.status);
           __syncwarp();
           if (!ok) break;
           const uint32_t tile = smem_u32(which ? sm->v[b] : sm->k[b]) + tile_half;
           if (!tree) {
-#pragma unroll
+#pragma unroll 1
             for (int y = 0; y < 2; ++y) {
-              const uint4 cd = code[which][y];
-              const int key = w8 * kGranule + 8 * y + r8;
-              const uint32_t scale = __byte_perm(params[which][y], 0u, 0x1010), mid = __byte_perm(params[which][y], 0u, 0x3232);
+              const int row = 8 * y + r8, key = w8 * kGranule + row;
+              uint4 cd = make_uint4(0u, 0u, 0u, 0u);
+              uint32_t params = 0;  // a key behind the prefix: zeros
+              if (key < left) {
+                asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(cd.x), "=r"(cd.y), "=r"(cd.z), "=r"(cd.w)
+                             : "r"(granule + which * kGranuleV + y * (8 * kCodeBytes)) : "memory");
+                asm volatile("ld.shared.u32 %0, [%1];" : "=r"(params)
+                             : "r"(granule - r8 * kCodeBytes - quad * 16 + kGranuleParams + which * (kGranule * 4) + row * 4) : "memory");
+              }
+              const uint32_t scale = __byte_perm(params, 0u, 0x1010), mid = __byte_perm(params, 0u, 0x3232);
               const uint32_t words[4] = {swap ? cd.z : cd.x, swap ? cd.w : cd.y, swap ? cd.x : cd.z, swap ? cd.y : cd.w};
               const uint32_t line = tile + key * 128;
 #pragma unroll
@@ -327,40 +313,28 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
           __syncwarp();
           if (lane == 0) mbar_arrive(which ? &sm->v_full[b] : &sm->k_full[b]);
         }
+        if (!tree) {
+          if (lane == 0 && half < halves) mbar_arrive(&sm->raw_empty[(taken + half) % kStages]);
+          taken += halves;
+        }
       }
       step += sg.steps;
       seg += sg.steps > 0;
       pos = sg.next;
     }
   } else {
-    // ============================ chains: two threads a row, 64 keys (and columns of O) each ============================
+    // ============================ chains: two threads a row, 64 keys each ============================
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsChain));
-    const int c = (warp - kChainWarp) >> 3, half = ((warp - kChainWarp) >> 2) & 1, quarter = warp & 3, row = quarter * 32 + lane;
+    // group 0, 1: the halves of even tiles, 2, 3: of odd ones
+    const int grp = (warp - kChainWarp) >> 2, half = grp & 1, quarter = warp & 3, row = quarter * 32 + lane;
     const uint32_t lane_sel = (uint32_t)(quarter * 32) << 16;
-    const uint32_t tmem_s = tmem + 256u + 128u * c + 64u * half + lane_sel;
-    const int pair_bar = 2 + 4 * c + quarter;
-    // The two warps of a quarter's rows.  A warp that gives up says so here, once, so that both leave: false if either does.
-    auto pair_sync = [&](bool fine) -> bool {
-      uint32_t out;
-      asm volatile(
-          "{\n\t.reg .pred p, q;\n\t"
-          "setp.eq.u32 q, %1, 0;\n\t"
-          "bar.red.or.pred p, %2, 64, q;\n\t"
-          "selp.u32 %0, 0, 1, p;\n\t}"
-          : "=r"(out) : "r"((uint32_t)fine), "r"(pair_bar) : "memory");
-      return out != 0;
-    };
-    // those that write a unit's rows together: the chain's, or all where the chains share them
-    auto rows_sync = [&]() {
-      if (kTwo) asm volatile("bar.sync %0, 256;" ::"r"(10 + c) : "memory");
-      else asm volatile("bar.sync 1, 512;" ::: "memory");
-    };
-    int step = 0, done = 0, seg = 0;  // (segments with steps)
+    auto rows_sync = [&]() { asm volatile("bar.sync 1, 512;" ::: "memory"); };
+    int step = 0, seg = 0;  // tiles before this segment, segments with steps
     bool ok = true;
     for (int pos = range_lo; pos < range_hi;) {
       const TilesSeg sg = tiles_seg(&sm->plan, a, pos, range_hi);
       const int L = sg.u.L, r = sg.u.r;
-      const int rw = sg.u.m * a.row_tile + (kTwo ? c * kTileM : 0) + row;
+      const int rw = sg.u.m * kTileM + row;
       const bool valid = rw < a.rows;
       const int node = min(rw, a.rows - 1) / a.group, h = sg.u.g * a.group + min(rw, a.rows - 1) % a.group;
       const bool warp_live = rw - lane < a.rows;  // (a warp of padding rows only keeps in step)
@@ -368,9 +342,6 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
       float rs = a.scale_log2;
       {
         const uint4* src = reinterpret_cast<const uint4*>(a.q + r * a.q_req + node * a.q_tok + h * a.q_head);
-        // each thread of a row brings its share of the channels: two share a row, or four where the chains do
-        constexpr int kPieces = kTwo ? 8 : 4;
-        const int from = kTwo ? 8 * half : 8 * half + 4 * c;
         float f = 1.f;
         if (kBf16) {
           uint32_t top = 0;
@@ -387,58 +358,50 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
             rs *= __uint_as_float((uint32_t)(127 - up) << 23);
           }
         }
-        const uint32_t line = smem_u32(sm->q[kTwo ? c : 0]) + row * 128 + half * kHalfBytes;
+        // each group brings a quarter of the channels
+        const uint32_t line = smem_u32(sm->q) + row * 128 + (grp >> 1) * kHalfBytes;
 #pragma unroll
-        for (int p = 0; p < kPieces; ++p) {
-          uint4 x = valid ? src[from + p] : make_uint4(0u, 0u, 0u, 0u);
+        for (int p = 0; p < 4; ++p) {
+          uint4 x = valid ? src[4 * grp + p] : make_uint4(0u, 0u, 0u, 0u);
           if (kBf16) {
             x.x = pack2<false>(__uint_as_float(x.x << 16) * f, __uint_as_float(x.x & 0xffff0000u) * f);
             x.y = pack2<false>(__uint_as_float(x.y << 16) * f, __uint_as_float(x.y & 0xffff0000u) * f);
             x.z = pack2<false>(__uint_as_float(x.z << 16) * f, __uint_as_float(x.z & 0xffff0000u) * f);
             x.w = pack2<false>(__uint_as_float(x.w << 16) * f, __uint_as_float(x.w & 0xffff0000u) * f);
           }
-          sts128(line + ((((from + p) & 7) ^ (row & 7)) << 4), __byte_perm(x.x, x.z, 0x5410), __byte_perm(x.x, x.z, 0x7632),
+          sts128(line + (((4 * (grp & 1) + p) ^ (row & 7)) << 4), __byte_perm(x.x, x.z, 0x5410), __byte_perm(x.x, x.z, 0x7632),
                  __byte_perm(x.y, x.w, 0x5410), __byte_perm(x.y, x.w, 0x7632));
         }
         fence_async_smem();
         __syncwarp();
-        if (lane == 0) {
-          if (kTwo) {
-            mbar_arrive(&sm->q_full[c]);
-          } else {
-            mbar_arrive(&sm->q_full[0]);
-            mbar_arrive(&sm->q_full[1]);
-          }
-        }
+        if (lane == 0) mbar_arrive(&sm->q_full);
       }
       const uint32_t* mask_row = kv4_mask_row(a, r, node);
       const int depth = a.window > 0 ? kv4_depth(a, r, node) : 0;
       const int begin = a.window > 0 ? L + depth + 1 - a.window : 0;  // where the row's window begins
 
+      const int latest = __reduce_max_sync(0xffffffffu, begin);
+
       float m_used = -INFINITY, l = 0.f;
-      bool any = false;  // the chain has had a tile
-      for (int i = 0; i < sg.steps && ok; ++i) {
-        const int x = step + i, t = sg.t0 + i;
-        if (!kTwo && (x & 1) != c) continue;
+      for (int i = (step ^ (grp >> 1)) & 1; i < sg.steps; i += 2) {
+        const int x = step + i, u = x / kSBufs, sb = x - u * kSBufs, t = sg.t0 + i;
+        const uint32_t tmem_s = tmem + kTmemS + 128u * sb + 64u * half + lane_sel;
         const bool tree = t >= sg.u.prefix.steps;
         const int key0 = (tree ? t - sg.u.prefix.steps : sg.u.prefix.key_step(t)) * kTilesStep + half * kHalfKeys;
-        uint32_t vis[2];
-#pragma unroll
-        for (int w = 0; w < 2; ++w) {
-          if (tree) vis[w] = kv4_window_word(a, r, L, depth, (key0 >> 5) + w, kv4_mask_word(a, mask_row, node, (key0 >> 5) + w));
-          else vis[w] = bits_below(L - key0 - 32 * w) & (~bits_below(begin - key0 - 32 * w) | bits_below(a.sinks - key0 - 32 * w));
+        uint32_t vis[2] = {0xffffffffu, 0xffffffffu};
+        const bool masked = tree || key0 + kHalfKeys > L || key0 < latest;  // some keys are not there, or not every row's
+        if (masked) {
+#pragma unroll 1
+          for (int w = 0; w < 2; ++w) {
+            uint32_t bits;
+            if (tree) bits = kv4_window_word(a, r, L, depth, (key0 >> 5) + w, kv4_mask_word(a, mask_row, node, (key0 >> 5) + w));
+            else bits = bits_below(L - key0 - 32 * w) & (~bits_below(begin - key0 - 32 * w) | bits_below(a.sinks - key0 - 32 * w));
+            if (w) vis[1] = bits; else vis[0] = bits;
+          }
         }
-        const bool masked = __any_sync(0xffffffffu, (vis[0] & vis[1]) != 0xffffffffu);
-        ok = mbar_wait(sm, &sm->s_full[c], done & 1, a.status);
-        // Chains that work on the same keys would do so in step, the tensor core idle meanwhile: they take turns at the
-        // exponentials, a tile of chain A, one of chain B.  (Neither is ever more than one turn ahead.)
-        if (kTwo && ok && (c == 1 || done > 0)) ok = mbar_wait(sm, &sm->turn[c ^ 1][quarter], (c == 1 ? done : done - 1) & 1, a.status);
-        ok = __all_sync(0xffffffffu, ok);
-        if (!ok) {
-          if (warp_live) pair_sync(false);
-          break;
-        }
-        bool passed = false;
+        ok = mbar_wait(sm, &sm->s_full[sb], u & 1, a.status);
+        __syncwarp();
+        if (!ok) break;
         if (warp_live) {
           tc_fence_after();
           // 32 scores, -inf where masked
@@ -446,7 +409,7 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
             tmem_ld32(tmem_s + 32u * x2, s, 0);
             tc_wait_ld();
 #pragma unroll
-            for (int e = 0; e < 32; ++e) asm volatile("" : "+r"(s[e]));
+            for (int e = 0; e < 32; ++e) asm volatile("" : "+r"(s[e]));  // (nothing of it moves ahead of the wait)
             if (masked) {
               const uint32_t bits = x2 ? vis[1] : vis[0];
 #pragma unroll
@@ -454,238 +417,175 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
                 if (!((bits >> e) & 1u)) s[e] = __float_as_uint(-INFINITY);
             }
           };
-          // The exponentials are taken against the reference as it stands; their sum tells whether that was right (see
-          // tree_attention_stream.cu): the maximum is taken, the reference moved, O rescaled and the pass repeated only then.  The scores
-          // stay in tensor memory until then; the row's two threads share the reference and decide together.
-          bool settle = __any_sync(0xffffffffu, m_used == -INFINITY);
-          float sum;
-          uint32_t packed[2][16];
+          // (Loops that are not unrolled, here and where codes are unpacked: what the warps of an SM run has to stay in its
+          // instruction caches.  Unrolled, a warp spent a third of its time waiting for instructions.)
+          float mx[2] = {-INFINITY, -INFINITY};
 #pragma unroll 1
-          for (;;) {
-            if (settle) {
-              float mx[2] = {-INFINITY, -INFINITY};
-#pragma unroll 1
-              for (int x2 = 0; x2 < 2; ++x2) {
-                uint32_t s[32];
-                scores(x2, s);
+          for (int x2 = 0; x2 < 2; ++x2) {
+            uint32_t s[32];
+            scores(x2, s);
 #pragma unroll
-                for (int e = 0; e < 32; e += 2) mx[(e >> 1) & 1] = max3(mx[(e >> 1) & 1], __uint_as_float(s[e]), __uint_as_float(s[e + 1]));
-              }
-              sm->xchg[c][half][row] = fmaxf(mx[0], mx[1]);
-              ok = pair_sync(true);
-              const float top = fmaxf(fmaxf(mx[0], mx[1]), sm->xchg[c][half ^ 1][row]) * rs;  // rs > 0
-              if (ok) ok = pair_sync(true);  // (read: the next exchange may follow at once)
-              if (!ok) break;
-              const bool move = top > m_used + kRescaleThreshold || (m_used == -INFINITY && top != -INFINITY);
-              if (__any_sync(0xffffffffu, move)) {
-                float alpha = 1.f;
-                if (move) {
-                  alpha = m_used == -INFINITY ? 0.f : ex2(m_used - top);
-                  l *= alpha;
-                  m_used = top;
-                }
-                __syncwarp();
-                if (any) {  // (the product before this S has completed: see the issuer)
-#pragma unroll 1
-                  for (int x2 = 0; x2 < 2; ++x2) {
-                    const uint32_t at = tmem + 128u * c + 64u * half + 32u * x2 + lane_sel;
-                    uint32_t o[32];
-                    tmem_ld32(at, o, 0);
-                    tc_wait_ld();
-#pragma unroll
-                    for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * alpha);
-                    tmem_st32(at, o, 0);
-                  }
-                }
-              }
-            }
-            const float neg_m = m_used == -INFINITY ? 0.f : -m_used;
-            const uint64_t rs2 = pair_of(rs, rs), neg_m2 = pair_of(neg_m, neg_m);
-            uint64_t sums[2] = {pair_of(0.f, 0.f), pair_of(0.f, 0.f)};
-#pragma unroll
-            for (int x2 = 0; x2 < 2; ++x2) {
-              uint32_t s[32];
-              scores(x2, s);
-#pragma unroll
-              for (int e = 0; e < 16; ++e) {
-                float y0, y1;
-                unpair(fma2(pair_of(__uint_as_float(s[2 * e]), __uint_as_float(s[2 * e + 1])), rs2, neg_m2), y0, y1);
-                const float p0 = ex2(y0), p1 = ex2(y1);
-                sums[e & 1] = add2(sums[e & 1], pair_of(p0, p1));
-                packed[x2][e] = pack2<false>(p0, p1);
-              }
-              if (kTwo && x2 == 0 && !passed) {
-                passed = true;
-                if (lane == 0) mbar_arrive(&sm->turn[c][quarter]);
-              }
-            }
-            float s0, s1, s2, s3;
-            unpair(sums[0], s0, s1);
-            unpair(sums[1], s2, s3);
-            sum = (s0 + s1) + (s2 + s3);
-            if (settle) break;
-            settle = __any_sync(0xffffffffu, !(sum <= kRescaleLimit));
-            if (lane == 0) sm->above[done & 1][c][half][quarter] = settle;
-            ok = pair_sync(true);
-            if (!ok) break;
-            settle = settle || sm->above[done & 1][c][half ^ 1][quarter];
-            if (!settle) break;
+            for (int e = 0; e < 32; e += 2) mx[(e >> 1) & 1] = max3(mx[(e >> 1) & 1], __uint_as_float(s[e]), __uint_as_float(s[e + 1]));
           }
-          if (!ok) break;
-          // over this thread's scores
-          tmem_st16(tmem_s, packed[0]);
-          tmem_st16(tmem_s + 16u, packed[1]);
-          l += sum;
+          const float top = fmaxf(mx[0], mx[1]) * rs;  // rs > 0
+          // All groups add to one accumulator, so they share the rows' reference: it is settled 64 keys by 64 keys, in order, before
+          // the exponentials.  It moves only when a score exceeds it by more than the threshold, or with the first score.
+          const int before = 2 * x + half - 1;  // the 64 keys before: of group before & 3
+          float ref = -INFINITY;
+          if (i > 0 || half > 0) {
+            ok = mbar_wait(sm, &sm->settled[before & 3][quarter], (before >> 2) & 1, a.status);
+            __syncwarp();
+            if (!ok) break;
+            ref = sm->ref[row];
+          }
+          const bool move = top > ref + kRescaleThreshold || (ref == -INFINITY && top != -INFINITY);
+          const float now = move ? top : ref;
+          if (__any_sync(0xffffffffu, move) || (i == 0 && half == 0)) {
+            const float alpha = move && ref != -INFINITY ? ex2(ref - top) : 1.f;
+            if (i > 0 || half > 0) {
+              // O may still be taking the keys before
+              const int bx = before >> 1, bu = bx / kSBufs;
+              ok = mbar_wait(sm, &sm->pv_done[bx - bu * kSBufs][before & 1], bu & 1, a.status);
+              __syncwarp();
+              if (!ok) break;
+              tc_fence_after();
+#pragma unroll 1
+              for (int x4 = 0; x4 < 4; ++x4) {
+                uint32_t o[32];
+                tmem_ld32(tmem + 32u * x4 + lane_sel, o, 0);
+                tc_wait_ld();
+#pragma unroll
+                for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * alpha);
+                tmem_st32(tmem + 32u * x4 + lane_sel, o, 0);
+              }
+              tc_wait_st();
+              tc_fence_before();
+            }
+            sm->ref[row] = now;
+            __syncwarp();
+          }
+          if (lane == 0) mbar_arrive(&sm->settled[grp][quarter]);
+          if (now != m_used) {
+            l *= m_used == -INFINITY ? 0.f : ex2(m_used - now);
+            m_used = now;
+          }
+          const float neg_m = now == -INFINITY ? 0.f : -now;
+          const uint64_t rs2 = pair_of(rs, rs), neg_m2 = pair_of(neg_m, neg_m);
+          uint64_t sums[2] = {pair_of(0.f, 0.f), pair_of(0.f, 0.f)};
+#pragma unroll 1
+          for (int x2 = 0; x2 < 2; ++x2) {
+            uint32_t s[32], packed[16];
+            scores(x2, s);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+              float y0, y1;
+              unpair(fma2(pair_of(__uint_as_float(s[2 * e]), __uint_as_float(s[2 * e + 1])), rs2, neg_m2), y0, y1);
+              const float p0 = ex2(y0), p1 = ex2(y1);
+              sums[e & 1] = add2(sums[e & 1], pair_of(p0, p1));
+              packed[e] = pack2<false>(p0, p1);
+            }
+            tmem_st16(tmem_s + 16u * x2, packed);  // over scores that have been read
+          }
+          float s0, s1, s2, s3;
+          unpair(sums[0], s0, s1);
+          unpair(sums[1], s2, s3);
+          l += (s0 + s1) + (s2 + s3);
           tc_wait_st();
           tc_fence_before();
-        } else if (kTwo && lane == 0) {
-          mbar_arrive(&sm->turn[c][quarter]);
+        } else if (lane == 0) {
+          mbar_arrive(&sm->settled[grp][quarter]);
         }
         __syncwarp();
-        if (lane == 0) mbar_arrive(&sm->p_full[c]);
-        any = true;
-        ++done;
+        if (lane == 0) mbar_arrive(&sm->p_full[sb][half]);
       }
-      // ---- the chain's last product
-      if (any && ok) ok = mbar_wait(sm, &sm->pv_done[c], (done - 1) & 1, a.status);
+      // ---- the last product
+      if (sg.steps > 0 && ok) {
+        const int x = step + sg.steps - 1, u = x / kSBufs;
+        ok = mbar_wait(sm, &sm->pv_done[x - u * kSBufs][1], u & 1, a.status);
+      }
       __syncwarp();
       tc_fence_after();
-      if (!ok) any = false;
-      uint32_t poison = 0;
-      for (int i = max(sg.u.prefix.steps - sg.t0, 0); i < sg.steps; ++i) {  // tree rows that are not finite and that the row sees
-        if (!kTwo && ((step + i) & 1) != c) continue;
+      uint32_t poison = 0;  // tree rows that are not finite and that the row sees
+      for (int i = max(sg.u.prefix.steps - sg.t0, 0); i < sg.steps; ++i) {
         const int tile = sg.t0 + i - sg.u.prefix.steps;
-#pragma unroll
-        for (int w = 0; w < 4; ++w) {
-          const uint32_t bad = sm->bad[seg & 3][tile][w];
-          if (bad != 0) poison |= bad & kv4_window_word(a, r, L, depth, 4 * tile + w, kv4_mask_word(a, mask_row, node, 4 * tile + w));
-        }
+        const uint32_t bad = sm->bad[seg & 3][tile][grp];
+        if (bad != 0) poison |= bad & kv4_window_word(a, r, L, depth, 4 * tile + grp, kv4_mask_word(a, mask_row, node, 4 * tile + grp));
       }
       if (poison != 0) l = NAN;
-      // ---- the row's sum: of its two threads, of the two chains where they share it
-      rows_sync();  // (nobody looks at what was exchanged last any more)
-      sm->xchg[c][half][row] = l;
-      if (!kTwo && half == 0) sm->ml[kTwo ? 0 : c][kTwo ? 0 : row].x = any ? m_used : -INFINITY;
+      // ---- the groups' sums, against the reference that O ended in
+      sm->ml[grp][row] = make_float2(m_used, l);
       rows_sync();
-      float M = any ? m_used : -INFINITY, fA = 1.f, fB = 0.f, sum;
-      if (kTwo) {
-        sum = sm->xchg[c][0][row] + sm->xchg[c][1][row];
-      } else {
-        const float mA = sm->ml[0][kTwo ? 0 : row].x, mB = sm->ml[kTwo ? 0 : 1][kTwo ? 0 : row].x;
-        M = fmaxf(mA, mB);
-        fA = mA == -INFINITY ? 0.f : ex2(mA - M);
-        fB = mB == -INFINITY ? 0.f : ex2(mB - M);
-        sum = fmaf(sm->xchg[0][0][row] + sm->xchg[0][1][row], fA, (sm->xchg[1][0][row] + sm->xchg[1][1][row]) * fB);
+      const bool any = sg.steps > 0 && ok;
+      float M = any ? sm->ref[row] : -INFINITY, sum = 0.f;
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        const float2 ml = sm->ml[w][row];
+        sum = fmaf(ml.y, ml.x == -INFINITY ? 0.f : ex2(ml.x - M), sum);
       }
-      // 32 columns of the accumulator, unnormalised; first column 32 * x4
-      auto columns = [&](int x4, float (&o)[32]) {
-        __syncwarp();
-        if (kTwo) {
-          if (any) {
-            tmem_ld32(tmem + 128u * c + lane_sel + 32u * x4, reinterpret_cast<uint32_t*>(o), 0);
-            tc_wait_ld();
-          } else {
+      // The group's 32 columns of O, unnormalised: the row's four threads write a quarter each.
+      float o[32];
+      if (any) {
+        tmem_ld32(tmem + lane_sel + 32u * grp, reinterpret_cast<uint32_t*>(o), 0);
+        tc_wait_ld();
+      } else {
 #pragma unroll
-            for (int e = 0; e < 32; ++e) o[e] = 0.f;
-          }
-        } else {
-          // (an accumulator that nobody wrote may hold anything)
-          tmem_ld32(tmem + lane_sel + 32u * x4, reinterpret_cast<uint32_t*>(o), 0);
-          tc_wait_ld();
-#pragma unroll
-          for (int e = 0; e < 32; ++e) o[e] = fA == 0.f ? 0.f : o[e] * fA;
-#pragma unroll
-          for (int y = 0; y < 2; ++y) {
-            uint32_t b[16];
-            asm volatile(
-                "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
-                : "=r"(b[0]), "=r"(b[1]), "=r"(b[2]), "=r"(b[3]), "=r"(b[4]), "=r"(b[5]), "=r"(b[6]), "=r"(b[7]), "=r"(b[8]), "=r"(b[9]), "=r"(b[10]),
-                  "=r"(b[11]), "=r"(b[12]), "=r"(b[13]), "=r"(b[14]), "=r"(b[15]) : "r"(tmem + 128u + lane_sel + 32u * x4 + 16u * y) : "memory");
-            tc_wait_ld();
-#pragma unroll
-            for (int e = 0; e < 16; ++e) o[16 * y + e] += fB == 0.f ? 0.f : __uint_as_float(b[e]) * fB;
-          }
-        }
-      };
-      constexpr int kRuns = kTwo ? 2 : 1;  // of 32 columns a thread
-      const int first_run = kTwo ? 2 * half : 2 * half + c;
+        for (int e = 0; e < 32; ++e) o[e] = 0.f;
+      }
       bool complete = sg.whole;
-      Kv4Pieces pieces;
       if (!sg.whole) {
         // This CTA's piece goes to the workspace and is counted; the one that counts the last piece adds them all, in the order
         // of their CTAs, and writes the rows.  Nobody waits for anybody.
-        pieces = kv4_pieces(ranges, sg.u);
-        int32_t* const count = a.ws_count + 2 * pieces.first + (kTwo ? c : 0);
-        const int64_t mine = (int64_t)kv4_slot(ranges, blockIdx.x, sg.u.begin) * a.row_tile + (kTwo ? c * kTileM : 0);
-        float4* to = reinterpret_cast<float4*>(a.ws_o + mine * kHeadDim) + row;  // [channel / 4][row]
-#pragma unroll 1
-        for (int run = first_run; run < first_run + kRuns; ++run) {
-          float o[32];
-          columns(run, o);
+        const Kv4Pieces pieces = kv4_pieces(ranges, sg.u);
+        const int64_t mine = (int64_t)kv4_slot(ranges, blockIdx.x, sg.u.begin) * kTileM;
+        float4* to = reinterpret_cast<float4*>(a.ws_o + mine * kHeadDim) + (8 * grp) * kTileM + row;  // [channel / 4][row]
 #pragma unroll
-          for (int e = 0; e < 32; e += 4) to[(int64_t)(8 * run + (e >> 2)) * kTileM] = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
-        }
-        if (half == 0 && (kTwo || c == 0)) a.ws_ml[mine + row] = make_float2(M, sum);
+        for (int e = 0; e < 32; e += 4) to[(e >> 2) * kTileM] = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+        if (grp == 0) a.ws_ml[mine + row] = make_float2(M, sum);
         __threadfence();
         rows_sync();
-        const bool teller = half == 0 && quarter == 0 && lane == 0 && (kTwo || c == 0);
-        if (teller) sm->last[kTwo ? c : 0] = atomicAdd(count, 1) == pieces.last - pieces.first;
+        if (grp == 0 && row == 0) sm->last = atomicAdd(a.ws_count + 2 * pieces.first, 1) == pieces.last - pieces.first;
         rows_sync();
-        complete = sm->last[kTwo ? c : 0] != 0;
+        complete = sm->last != 0;
         if (complete) {
           __threadfence();
           M = -INFINITY;
-          for (int x = pieces.first; x <= pieces.last; ++x)
-            M = fmaxf(M, __ldcg(a.ws_ml + (int64_t)kv4_slot(ranges, x, sg.u.begin) * a.row_tile + (kTwo ? c * kTileM : 0) + row).x);
+          for (int x = pieces.first; x <= pieces.last; ++x) M = fmaxf(M, __ldcg(a.ws_ml + (int64_t)kv4_slot(ranges, x, sg.u.begin) * kTileM + row).x);
           sum = 0.f;
+#pragma unroll
+          for (int e = 0; e < 32; ++e) o[e] = 0.f;
           for (int x = pieces.first; x <= pieces.last; ++x) {
-            const float2 ml = __ldcg(a.ws_ml + (int64_t)kv4_slot(ranges, x, sg.u.begin) * a.row_tile + (kTwo ? c * kTileM : 0) + row);
-            sum = fmaf(ml.y, ml.x == -INFINITY ? 0.f : ex2(ml.x - M), sum);
+            const int64_t at = (int64_t)kv4_slot(ranges, x, sg.u.begin) * kTileM;
+            const float2 ml = __ldcg(a.ws_ml + at + row);
+            const float f = ml.x == -INFINITY ? 0.f : ex2(ml.x - M);
+            sum = fmaf(ml.y, f, sum);
+            const float4* from = reinterpret_cast<const float4*>(a.ws_o + at * kHeadDim) + (8 * grp) * kTileM + row;
+#pragma unroll
+            for (int e = 0; e < 32; e += 4) {
+              const float4 v = __ldcg(from + (e >> 2) * kTileM);
+              o[e] = fmaf(v.x, f, o[e]);
+              o[e + 1] = fmaf(v.y, f, o[e + 1]);
+              o[e + 2] = fmaf(v.z, f, o[e + 2]);
+              o[e + 3] = fmaf(v.w, f, o[e + 3]);
+            }
           }
         }
       }
-      if (complete) {
+      if (complete && valid) {
         const float inv = 1.f / sum;
-        uint8_t* out = a.out + r * a.o_req + node * a.o_tok + h * a.o_head;
-#pragma unroll 1
-        for (int run = first_run; run < first_run + kRuns; ++run) {
-          float o[32];
-          if (sg.whole) {
-            columns(run, o);
-          } else {
+        uint8_t* out = a.out + r * a.o_req + node * a.o_tok + h * a.o_head + 64 * grp;
 #pragma unroll
-            for (int e = 0; e < 32; ++e) o[e] = 0.f;
-            for (int x = pieces.first; x <= pieces.last; ++x) {
-              const int64_t at = (int64_t)kv4_slot(ranges, x, sg.u.begin) * a.row_tile + (kTwo ? c * kTileM : 0);
-              const float mx = __ldcg(a.ws_ml + at + row).x;
-              const float f = mx == -INFINITY ? 0.f : ex2(mx - M);
-              const float4* from = reinterpret_cast<const float4*>(a.ws_o + at * kHeadDim) + row;
-#pragma unroll
-              for (int e = 0; e < 32; e += 4) {
-                const float4 v = __ldcg(from + (int64_t)(8 * run + (e >> 2)) * kTileM);
-                o[e] = fmaf(v.x, f, o[e]);
-                o[e + 1] = fmaf(v.y, f, o[e + 1]);
-                o[e + 2] = fmaf(v.z, f, o[e + 2]);
-                o[e + 3] = fmaf(v.w, f, o[e + 3]);
-              }
-            }
-          }
-          if (valid) {
-#pragma unroll
-            for (int e = 0; e < 32; e += 8) {  // columns 0,2,4,6,1,3,5,7 are channels 0..7
-              uint4 val;
-              val.x = pack2<kBf16>(o[e] * inv, o[e + 2] * inv);
-              val.y = pack2<kBf16>(o[e + 4] * inv, o[e + 6] * inv);
-              val.z = pack2<kBf16>(o[e + 1] * inv, o[e + 3] * inv);
-              val.w = pack2<kBf16>(o[e + 5] * inv, o[e + 7] * inv);
-              *reinterpret_cast<uint4*>(out + 64 * run + 2 * e) = val;
-            }
-          }
+        for (int e = 0; e < 32; e += 8) {  // columns 0,2,4,6,1,3,5,7 are channels 0..7
+          uint4 val;
+          val.x = pack2<kBf16>(o[e] * inv, o[e + 2] * inv);
+          val.y = pack2<kBf16>(o[e + 4] * inv, o[e + 6] * inv);
+          val.z = pack2<kBf16>(o[e + 1] * inv, o[e + 3] * inv);
+          val.w = pack2<kBf16>(o[e + 5] * inv, o[e + 7] * inv);
+          *reinterpret_cast<uint4*>(out + 2 * e) = val;
         }
-        if (valid && half == 0 && (kTwo || c == 0) && a.lse != nullptr) a.lse[((int64_t)r * a.Hq + h) * a.n + node] = (M + log2f(sum)) * kLn2;
+        if (grp == 0 && a.lse != nullptr) a.lse[((int64_t)r * a.Hq + h) * a.n + node] = (M + log2f(sum)) * kLn2;
       }
       tc_fence_before();
-      rows_sync();  // the accumulators are read, the rows are through with Q and with what they exchanged
+      rows_sync();  // the accumulator is read, the rows are through with Q and with what they exchanged
       step += sg.steps;
       seg += sg.steps > 0;
       pos = sg.next;
@@ -700,18 +600,15 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
 }
 
 // ---------------------------------------------------------------- host side ---------------------
-static bool tiles_two(const seq_tree_kv4_attention_params& p) { return p.n_tree * (p.num_q_heads / p.num_kv_heads) > kTileM; }
-
-size_t kv4_tiles_workspace_bytes(const seq_tree_kv4_attention_params& p) {
+size_t kv4_tiles_workspace_bytes() {
   const size_t sms = device_sm_count();
-  return kv4_count_bytes(sms) + 2 * sms * (tiles_two(p) ? 2 : 1) * kTileM * (kHeadDim * sizeof(float) + sizeof(float2));
+  return kv4_count_bytes(sms) + 2 * sms * kTileM * (kHeadDim * sizeof(float) + sizeof(float2));
 }
 
 int launch_kv4_tiles(const seq_tree_kv4_attention_params& p, cudaStream_t stream) {
-  const bool two = tiles_two(p);
   const int sms = device_sm_count();
   Kv4Args a = kv4_args(p);
-  a.row_tile = two ? 2 * kTileM : kTileM;
+  a.row_tile = kTileM;
   a.tiles = (a.rows + a.row_tile - 1) / a.row_tile;
   a.tree_steps = (a.n + kTilesStep - 1) / kTilesStep;
   a.min_steps = 2;
@@ -733,22 +630,18 @@ int launch_kv4_tiles(const seq_tree_kv4_attention_params& p, cudaStream_t stream
   early[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = early;
   cfg.numAttrs = 1;
-  auto launch = [&](auto kernel, int which, size_t smem) -> int {
-    static int done[4][64];
+  cfg.dynamicSmemBytes = kTilesSmemBytes;
+  auto launch = [&](auto kernel, int which) -> int {
+    static int done[2][64];
     const int rc = once_per_device(done[which], [&]() -> int {
-      SEQ_CUDA_OK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+      SEQ_CUDA_OK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kTilesSmemBytes));
       return SEQ_OK;
     });
     if (rc != SEQ_OK) return rc;
-    cfg.dynamicSmemBytes = smem;
     SEQ_CUDA_OK(cudaLaunchKernelEx(&cfg, kernel, a));
     return SEQ_OK;
   };
-  const bool bf16 = p.dtype == SEQ_BF16;
-  int rc;
-  if (two) rc = bf16 ? launch(kv4_tiles_kernel<true, true>, 0, tiles_smem_bytes<true>()) : launch(kv4_tiles_kernel<true, false>, 1, tiles_smem_bytes<true>());
-  else rc = bf16 ? launch(kv4_tiles_kernel<false, true>, 2, tiles_smem_bytes<false>()) : launch(kv4_tiles_kernel<false, false>, 3, tiles_smem_bytes<false>());
-  return rc;
+  return p.dtype == SEQ_BF16 ? launch(kv4_tiles_kernel<true>, 0) : launch(kv4_tiles_kernel<false>, 1);
 }
 
 }  // namespace seqtree
