@@ -10,9 +10,12 @@
 // Q's channels are stored in that order too, and O's columns are put back when the rows are written.  The tree's 16-bit rows go
 // through the same warps.
 //
-// A tile of scores is worked on by two threads a row, 64 keys each; there are four groups of 128 such threads, for the halves of
-// even and of odd tiles, and three S/P buffers, so that the next tiles' scores are computed meanwhile.  All add to one
-// accumulator and share the rows' reference maxima, which they settle in the keys' order (see the chains).
+// A tile of scores is worked on by two threads a row, 64 keys each.  There are four groups of 128 such threads and 512 columns of
+// tensor memory, used in one of two ways:
+//   kTwo (more than 128 rows a kv head)  a unit is 256 rows, two tiles with an S/P buffer, an accumulator and two groups each;
+//       both use every K/V tile, so that the codes are unpacked once for both.  The tiles take turns.
+//   otherwise  a unit is 128 rows with one accumulator and three S/P buffers; two groups have the even key tiles, two the odd ones.
+// Groups that add to one accumulator share the rows' reference maxima, which they settle in the keys' order (see the chains).
 //
 // Every mbarrier wait is bounded; one that runs out raises SEQ_DEV_TIMEOUT and the CTA drains.
 #include "kv4_attention.cuh"
@@ -28,34 +31,57 @@ constexpr int kHalfKeys = 64;       // keys of a ring stage
 constexpr int kStageBytes = kHalfKeys / kGranule * kGranuleBytes;
 constexpr int kTreeTiles = SEQ_MAX_TREE / kTilesStep;
 
-constexpr int kStages = 6, kSBufs = 3;
-constexpr uint32_t kTmemS = 128;  // tensor memory: O in columns 0..127, then the S/P buffers
-
+template <bool kTwo>
 struct TilesSmem {
-  uint8_t q[kTileBytes];  // tiles: 1024-byte aligned
-  uint8_t k[2][kTileBytes];  // [tile parity]
+  static constexpr int kStages = kTwo ? 3 : 6;
+  static constexpr int kSBufs = kTwo ? 2 : 3;
+  uint8_t q[kTwo ? 2 : 1][kTileBytes];  // tiles: 1024-byte aligned
+  uint8_t k[2][kTileBytes];             // [key tile parity]
   uint8_t v[2][kTileBytes];
   uint8_t ring[kStages][kStageBytes];
   uint64_t raw_full[kStages], raw_empty[kStages];
   uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2];
-  uint64_t q_full;
+  uint64_t q_full[2];
   uint64_t s_full[kSBufs], p_full[kSBufs][2], pv_done[kSBufs][2];  // [S/P buffer][half of its keys]
   uint64_t settled[4][4];  // [group][lane quarter]: the reference of the quarter's rows is settled for the group's 64 keys
+  uint64_t turn[2][4];     // [query tile][lane quarter], with kTwo: half of the tile's exponentials are under way
   uint64_t drained[2];
-  float ref[kTileM];       // the rows' reference maximum, handed on in the keys' order
-  float2 ml[4][kTileM];    // [group]: (m, l) of every row
-  int32_t last;            // this CTA completes the unit
-  uint32_t bad[4][kTreeTiles][4];  // [segment mod 4]: tree rows whose V is not finite in half precision
+  float ref[kTwo ? 2 : 1][kTileM];  // the rows' reference maximum, handed on in the keys' order
+  float sum[4][kTileM];             // [group]: the rows' sums
+  int32_t last[2];                  // this CTA completes the unit
+  uint32_t bad[4][kTreeTiles][4];   // [segment mod 4]: tree rows whose V is not finite in half precision
   uint32_t tmem_base;
   volatile int abort_flag;
   Kv4Plan plan;
 };
-constexpr size_t kTilesSmemBytes = sizeof(TilesSmem) + 1024;
-static_assert(kTilesSmemBytes <= 227 * 1024, "one CTA's shared memory");
+template <bool kTwo>
+constexpr size_t tiles_smem_bytes() { return sizeof(TilesSmem<kTwo>) + 1024; }
+static_assert(tiles_smem_bytes<true>() <= 227 * 1024 && tiles_smem_bytes<false>() <= 227 * 1024, "one CTA's shared memory");
 
 __device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
   asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
                ::"r"(smem_u32(dst)), "l"(src), "r"(bytes), "r"(smem_u32(bar)) : "memory");
+}
+// mbar_wait for the many warps of this kernel: a wait that is not over at once sleeps on the barrier (20 us at a time, 1.3 s in
+// all) instead of taking issue slots.
+__device__ __forceinline__ bool mbar_sleep(uint64_t* bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok) : "r"(smem_u32(bar)), "r"(parity), "r"(20000u) : "memory");
+  return ok != 0;
+}
+template <typename Smem>
+__device__ __forceinline__ bool mbar_wait_long(Smem* sm, uint64_t* bar, uint32_t parity, int32_t* dev_status) {
+  for (uint32_t it = 0; it < (1u << 16); ++it) {
+    if (mbar_sleep(bar, parity)) return true;
+    if (sm->abort_flag) return false;
+  }
+  sm->abort_flag = 1;
+  dev_flag(dev_status, SEQ_DEV_TIMEOUT);
+  return false;
 }
 __device__ __forceinline__ void sts128(uint32_t at, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
   asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
@@ -80,19 +106,24 @@ __device__ __forceinline__ TilesSeg tiles_seg(const Kv4Plan* plan, const Kv4Args
   return s;
 }
 
-template <bool kBf16>
+template <bool kTwo, bool kBf16>
 __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Args a) {
   extern __shared__ uint8_t smem_raw[];
-  TilesSmem* sm = reinterpret_cast<TilesSmem*>(smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u));
+  using Smem = TilesSmem<kTwo>;
+  constexpr int kStages = Smem::kStages, kSBufs = Smem::kSBufs;
+  // tensor memory: the accumulators, then the S/P buffers
+  constexpr uint32_t kTmemS = kTwo ? 256 : 128;
+  Smem* sm = reinterpret_cast<Smem*>(smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u));
   const int warp = uniform((int)threadIdx.x >> 5), lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
     for (int s = 0; s < kStages; ++s) { mbar_init(&sm->raw_full[s], 1); mbar_init(&sm->raw_empty[s], 4); }
     for (int b = 0; b < 2; ++b) {
-      mbar_init(&sm->k_full[b], 8); mbar_init(&sm->k_empty[b], 1);
-      mbar_init(&sm->v_full[b], 8); mbar_init(&sm->v_empty[b], 1);
+      mbar_init(&sm->k_full[b], 8); mbar_init(&sm->k_empty[b], kTwo ? 2 : 1);
+      mbar_init(&sm->v_full[b], 8); mbar_init(&sm->v_empty[b], kTwo ? 2 : 1);
+      mbar_init(&sm->q_full[b], kTwo ? 8 : 16);
+      for (int x = 0; x < 4; ++x) mbar_init(&sm->turn[b][x], 2);
       mbar_init(&sm->drained[b], 1);
     }
-    mbar_init(&sm->q_full, 16);
     for (int b = 0; b < kSBufs; ++b) {
       mbar_init(&sm->s_full[b], 1);
       for (int h = 0; h < 2; ++h) { mbar_init(&sm->p_full[b][h], 4); mbar_init(&sm->pv_done[b][h], 1); }
@@ -146,7 +177,7 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
                 }
               }
             }
-            if (w > 0 && !mbar_wait(sm, &sm->raw_empty[st], (w - 1) & 1, a.status)) { ok = false; break; }
+            if (w > 0 && !mbar_wait_long(sm, &sm->raw_empty[st], (w - 1) & 1, a.status)) { ok = false; break; }
             if (lane == 0) mbar_expect_tx(&sm->raw_full[st], granules * kGranuleBytes);
             __syncwarp();
             // lane x: the x-th page's part
@@ -168,40 +199,42 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
           for (uint32_t it = 0; it < (1u << 16); ++it)
             if (mbar_try_wait(&sm->raw_full[x % kStages], (x / kStages) & 1)) break;
     } else if (warp < 3) {
-      // ============================ issuers: S (warp 1), P V (warp 2) ============================
+      // ============================ issuers: one a query tile, or S (warp 1) and P V (warp 2) ============================
       const uint32_t idesc = (1u << 4) | ((uint32_t)(kTileM >> 4) << 24) | ((uint32_t)(kTilesStep >> 3) << 17);  // fp16, sums fp32, N = 128
       const uint32_t idesc_pv = idesc | (1u << 16);                                                             // V is MN-major
-      int step = 0, seg = 0;  // tiles before this segment, segments
+      const int c = warp - 1;
+      const uint32_t tmem_o = kTwo ? tmem + 128u * c : tmem;
+      int step = 0, seg = 0;  // key tiles before this segment, segments
       bool ok = true;
       for (int pos = range_lo; pos < range_hi && ok; ++seg) {
         const TilesSeg sg = tiles_seg(&sm->plan, a, pos, range_hi);
-        if (warp == 1) {
-          ok = mbar_wait(sm, &sm->q_full, seg & 1, a.status);
-          const uint32_t q_lo = desc_lo(smem_u32(sm->q), 16);
-          for (int i = 0; i < sg.steps && ok; ++i) {
-            const int x = step + i, b = x & 1, u = x / kSBufs, sb = x - u * kSBufs;
-            // S goes where the P of three tiles ago was: its product has completed
-            ok = mbar_wait(sm, &sm->k_full[b], (x >> 1) & 1, a.status) && (u == 0 || mbar_wait(sm, &sm->pv_done[sb][1], (u - 1) & 1, a.status));
+        if (kTwo || c == 0) ok = mbar_wait_long(sm, &sm->q_full[c], seg & 1, a.status);
+        const uint32_t q_lo = desc_lo(smem_u32(sm->q[kTwo ? c : 0]), 16);
+        for (int i = 0; i < sg.steps && ok; ++i) {
+          const int x = step + i, b = x & 1, u = kTwo ? x : x / kSBufs, sb = kTwo ? c : x - u * kSBufs;
+          const uint32_t sp = tmem + kTmemS + 128u * sb;
+          if (kTwo || c == 0) {
+            // S goes where an earlier tile's P was: its product has completed
+            ok = mbar_wait_long(sm, &sm->k_full[b], (x >> 1) & 1, a.status) && (u == 0 || mbar_wait_long(sm, &sm->pv_done[sb][1], (u - 1) & 1, a.status));
             if (!ok) break;
             tc_fence_after();
             if (elect_one()) {
-              mma_qk<kHalfBytes, kHalfBytes>(tmem + kTmemS + 128u * sb, q_lo, desc_lo(smem_u32(sm->k[b]), 16), idesc);
+              mma_qk<kHalfBytes, kHalfBytes>(sp, q_lo, desc_lo(smem_u32(sm->k[b]), 16), idesc);
               tc_commit(&sm->s_full[sb]);
               tc_commit(&sm->k_empty[b]);
             }
             __syncwarp();
           }
-        } else {
-          for (int i = 0; i < sg.steps && ok; ++i) {
-            const int x = step + i, b = x & 1, u = x / kSBufs, sb = x - u * kSBufs;
-            const uint32_t p_at = tmem + kTmemS + 128u * sb, v_lo = desc_lo(smem_u32(sm->v[b]), kHalfBytes);
-            ok = mbar_wait(sm, &sm->v_full[b], (x >> 1) & 1, a.status);
+          if (kTwo || c == 1) {
+            const uint32_t v_lo = desc_lo(smem_u32(sm->v[b]), kHalfBytes);
+            ok = mbar_wait_long(sm, &sm->v_full[b], (x >> 1) & 1, a.status);
+#pragma unroll 1
             for (int h = 0; h < 2 && ok; ++h) {
-              ok = mbar_wait(sm, &sm->p_full[sb][h], u & 1, a.status);
+              ok = mbar_wait_long(sm, &sm->p_full[sb][h], u & 1, a.status);
               if (!ok) break;
               tc_fence_after();
               if (elect_one()) {
-                mma_pv(tmem, p_at + 64u * h, v_lo + h * (kHalfKeys * 128 >> 4), idesc_pv, i > 0 || h > 0 ? 1u : 0u);
+                mma_pv(tmem_o, sp + 64u * h, v_lo + h * (kHalfKeys * 128 >> 4), idesc_pv, i > 0 || h > 0 ? 1u : 0u);
                 tc_commit(&sm->pv_done[sb][h]);
                 if (h == 1) tc_commit(&sm->v_empty[b]);
               }
@@ -237,11 +270,11 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
         const int key0 = tree ? (t - sg.u.prefix.steps) * kTilesStep : sg.u.prefix.key_step(t) * kTilesStep;
         const int left = (tree ? a.n : sg.u.L) - key0;  // keys of the tile that there are
         const int halves = left > kHalfKeys ? 2 : 1;
-        if (!tree && half < halves) ok = mbar_wait(sm, &sm->raw_full[(taken + half) % kStages], ((taken + half) / kStages) & 1, a.status);
+        if (!tree && half < halves) ok = mbar_wait_long(sm, &sm->raw_full[(taken + half) % kStages], ((taken + half) / kStages) & 1, a.status);
         const uint32_t granule = smem_u32(sm->ring[(taken + half) % kStages]) + (w8 & 3) * kGranuleBytes + r8 * kCodeBytes + quad * 16;
 #pragma unroll 1
         for (int which = 0; which < 2 && ok; ++which) {
-          if (w > 0) ok = mbar_wait(sm, which ? &sm->v_empty[b] : &sm->k_empty[b], (w - 1) & 1, a.status);
+          if (w > 0) ok = mbar_wait_long(sm, which ? &sm->v_empty[b] : &sm->k_empty[b], (w - 1) & 1, a.status);
           __syncwarp();
           if (!ok) break;
           const uint32_t tile = smem_u32(which ? sm->v[b] : sm->k[b]) + tile_half;
@@ -325,16 +358,22 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
   } else {
     // ============================ chains: two threads a row, 64 keys each ============================
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsChain));
-    // group 0, 1: the halves of even tiles, 2, 3: of odd ones
-    const int grp = (warp - kChainWarp) >> 2, half = grp & 1, quarter = warp & 3, row = quarter * 32 + lane;
+    // groups 0, 1: the halves of the first query tile's keys, or of even key tiles; 2, 3: of the second's, or of odd ones
+    const int grp = (warp - kChainWarp) >> 2, half = grp & 1, c = grp >> 1, quarter = warp & 3, row = quarter * 32 + lane;
+    const int tile = kTwo ? c : 0;  // the query tile, its accumulator
     const uint32_t lane_sel = (uint32_t)(quarter * 32) << 16;
-    auto rows_sync = [&]() { asm volatile("bar.sync 1, 512;" ::: "memory"); };
+    const uint32_t tmem_o = tmem + 128u * tile + lane_sel;
+    // the groups that share a query tile
+    auto rows_sync = [&]() {
+      if (kTwo) asm volatile("bar.sync %0, 256;" ::"r"(1 + c) : "memory");
+      else asm volatile("bar.sync 1, 512;" ::: "memory");
+    };
     int step = 0, seg = 0;  // tiles before this segment, segments with steps
     bool ok = true;
     for (int pos = range_lo; pos < range_hi;) {
       const TilesSeg sg = tiles_seg(&sm->plan, a, pos, range_hi);
       const int L = sg.u.L, r = sg.u.r;
-      const int rw = sg.u.m * kTileM + row;
+      const int rw = sg.u.m * a.row_tile + tile * kTileM + row;
       const bool valid = rw < a.rows;
       const int node = min(rw, a.rows - 1) / a.group, h = sg.u.g * a.group + min(rw, a.rows - 1) % a.group;
       const bool warp_live = rw - lane < a.rows;  // (a warp of padding rows only keeps in step)
@@ -358,23 +397,25 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
             rs *= __uint_as_float((uint32_t)(127 - up) << 23);
           }
         }
-        // each group brings a quarter of the channels
-        const uint32_t line = smem_u32(sm->q) + row * 128 + (grp >> 1) * kHalfBytes;
-#pragma unroll
-        for (int p = 0; p < 4; ++p) {
-          uint4 x = valid ? src[4 * grp + p] : make_uint4(0u, 0u, 0u, 0u);
+        // each group of the tile brings its share of the channels
+        constexpr int kPieces = kTwo ? 8 : 4;
+        const int from = kPieces * (kTwo ? half : grp);
+        const uint32_t line = smem_u32(sm->q[tile]) + row * 128 + (from >> 3) * kHalfBytes;
+#pragma unroll 4
+        for (int p = 0; p < kPieces; ++p) {
+          uint4 x = valid ? src[from + p] : make_uint4(0u, 0u, 0u, 0u);
           if (kBf16) {
             x.x = pack2<false>(__uint_as_float(x.x << 16) * f, __uint_as_float(x.x & 0xffff0000u) * f);
             x.y = pack2<false>(__uint_as_float(x.y << 16) * f, __uint_as_float(x.y & 0xffff0000u) * f);
             x.z = pack2<false>(__uint_as_float(x.z << 16) * f, __uint_as_float(x.z & 0xffff0000u) * f);
             x.w = pack2<false>(__uint_as_float(x.w << 16) * f, __uint_as_float(x.w & 0xffff0000u) * f);
           }
-          sts128(line + (((4 * (grp & 1) + p) ^ (row & 7)) << 4), __byte_perm(x.x, x.z, 0x5410), __byte_perm(x.x, x.z, 0x7632),
+          sts128(line + ((((from + p) & 7) ^ (row & 7)) << 4), __byte_perm(x.x, x.z, 0x5410), __byte_perm(x.x, x.z, 0x7632),
                  __byte_perm(x.y, x.w, 0x5410), __byte_perm(x.y, x.w, 0x7632));
         }
         fence_async_smem();
         __syncwarp();
-        if (lane == 0) mbar_arrive(&sm->q_full);
+        if (lane == 0) mbar_arrive(&sm->q_full[tile]);
       }
       const uint32_t* mask_row = kv4_mask_row(a, r, node);
       const int depth = a.window > 0 ? kv4_depth(a, r, node) : 0;
@@ -383,8 +424,8 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
       const int latest = __reduce_max_sync(0xffffffffu, begin);
 
       float m_used = -INFINITY, l = 0.f;
-      for (int i = (step ^ (grp >> 1)) & 1; i < sg.steps; i += 2) {
-        const int x = step + i, u = x / kSBufs, sb = x - u * kSBufs, t = sg.t0 + i;
+      for (int i = kTwo ? 0 : (step ^ c) & 1; i < sg.steps; i += kTwo ? 1 : 2) {
+        const int x = step + i, u = kTwo ? x : x / kSBufs, sb = kTwo ? c : x - u * kSBufs, t = sg.t0 + i;
         const uint32_t tmem_s = tmem + kTmemS + 128u * sb + 64u * half + lane_sel;
         const bool tree = t >= sg.u.prefix.steps;
         const int key0 = (tree ? t - sg.u.prefix.steps : sg.u.prefix.key_step(t)) * kTilesStep + half * kHalfKeys;
@@ -399,7 +440,7 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
             if (w) vis[1] = bits; else vis[0] = bits;
           }
         }
-        ok = mbar_wait(sm, &sm->s_full[sb], u & 1, a.status);
+        ok = mbar_wait_long(sm, &sm->s_full[sb], u & 1, a.status);
         __syncwarp();
         if (!ok) break;
         if (warp_live) {
@@ -430,13 +471,13 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
           const float top = fmaxf(mx[0], mx[1]) * rs;  // rs > 0
           // All groups add to one accumulator, so they share the rows' reference: it is settled 64 keys by 64 keys, in order, before
           // the exponentials.  It moves only when a score exceeds it by more than the threshold, or with the first score.
-          const int before = 2 * x + half - 1;  // the 64 keys before: of group before & 3
+          const int bx = half ? x : x - 1;  // the 64 keys before are the other half of this key tile
           float ref = -INFINITY;
           if (i > 0 || half > 0) {
-            ok = mbar_wait(sm, &sm->settled[before & 3][quarter], (before >> 2) & 1, a.status);
+            ok = mbar_wait_long(sm, &sm->settled[kTwo ? grp ^ 1 : 2 * (bx & 1) + (half ^ 1)][quarter], kTwo ? bx & 1 : (bx >> 1) & 1, a.status);
             __syncwarp();
             if (!ok) break;
-            ref = sm->ref[row];
+            ref = sm->ref[tile][row];
           }
           const bool move = top > ref + kRescaleThreshold || (ref == -INFINITY && top != -INFINITY);
           const float now = move ? top : ref;
@@ -444,24 +485,24 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
             const float alpha = move && ref != -INFINITY ? ex2(ref - top) : 1.f;
             if (i > 0 || half > 0) {
               // O may still be taking the keys before
-              const int bx = before >> 1, bu = bx / kSBufs;
-              ok = mbar_wait(sm, &sm->pv_done[bx - bu * kSBufs][before & 1], bu & 1, a.status);
+              const int bu = kTwo ? bx : bx / kSBufs;
+              ok = mbar_wait_long(sm, &sm->pv_done[kTwo ? c : bx - bu * kSBufs][half ^ 1], bu & 1, a.status);
               __syncwarp();
               if (!ok) break;
               tc_fence_after();
 #pragma unroll 1
               for (int x4 = 0; x4 < 4; ++x4) {
                 uint32_t o[32];
-                tmem_ld32(tmem + 32u * x4 + lane_sel, o, 0);
+                tmem_ld32(tmem_o + 32u * x4, o, 0);
                 tc_wait_ld();
 #pragma unroll
                 for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * alpha);
-                tmem_st32(tmem + 32u * x4 + lane_sel, o, 0);
+                tmem_st32(tmem_o + 32u * x4, o, 0);
               }
               tc_wait_st();
               tc_fence_before();
             }
-            sm->ref[row] = now;
+            sm->ref[tile][row] = now;
             __syncwarp();
           }
           if (lane == 0) mbar_arrive(&sm->settled[grp][quarter]);
@@ -472,6 +513,13 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
           const float neg_m = now == -INFINITY ? 0.f : -now;
           const uint64_t rs2 = pair_of(rs, rs), neg_m2 = pair_of(neg_m, neg_m);
           uint64_t sums[2] = {pair_of(0.f, 0.f), pair_of(0.f, 0.f)};
+          // Query tiles that work on the same keys would do so in step, the tensor core idle meanwhile: they take turns at the
+          // exponentials, the first tile's, the second's.  (Neither is ever more than one turn ahead.)
+          if (kTwo && (c == 1 || x > 0)) {
+            ok = mbar_wait_long(sm, &sm->turn[c ^ 1][quarter], (c == 1 ? x : x - 1) & 1, a.status);
+            __syncwarp();
+            if (!ok) break;
+          }
 #pragma unroll 1
           for (int x2 = 0; x2 < 2; ++x2) {
             uint32_t s[32], packed[16];
@@ -485,6 +533,7 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
               packed[e] = pack2<false>(p0, p1);
             }
             tmem_st16(tmem_s + 16u * x2, packed);  // over scores that have been read
+            if (kTwo && x2 == 0 && lane == 0) mbar_arrive(&sm->turn[c][quarter]);
           }
           float s0, s1, s2, s3;
           unpair(sums[0], s0, s1);
@@ -492,97 +541,121 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
           l += (s0 + s1) + (s2 + s3);
           tc_wait_st();
           tc_fence_before();
-        } else if (lane == 0) {
-          mbar_arrive(&sm->settled[grp][quarter]);
+        } else {
+          if (kTwo && (c == 1 || x > 0)) ok = mbar_wait_long(sm, &sm->turn[c ^ 1][quarter], (c == 1 ? x : x - 1) & 1, a.status);
+          __syncwarp();
+          if (!ok) break;
+          if (lane == 0) {
+            if (kTwo) mbar_arrive(&sm->turn[c][quarter]);
+            mbar_arrive(&sm->settled[grp][quarter]);
+          }
         }
         __syncwarp();
         if (lane == 0) mbar_arrive(&sm->p_full[sb][half]);
       }
       // ---- the last product
       if (sg.steps > 0 && ok) {
-        const int x = step + sg.steps - 1, u = x / kSBufs;
-        ok = mbar_wait(sm, &sm->pv_done[x - u * kSBufs][1], u & 1, a.status);
+        const int x = step + sg.steps - 1, u = kTwo ? x : x / kSBufs;
+        ok = mbar_wait_long(sm, &sm->pv_done[kTwo ? c : x - u * kSBufs][1], u & 1, a.status);
       }
       __syncwarp();
       tc_fence_after();
-      uint32_t poison = 0;  // tree rows that are not finite and that the row sees
-      for (int i = max(sg.u.prefix.steps - sg.t0, 0); i < sg.steps; ++i) {
-        const int tile = sg.t0 + i - sg.u.prefix.steps;
-        const uint32_t bad = sm->bad[seg & 3][tile][grp];
-        if (bad != 0) poison |= bad & kv4_window_word(a, r, L, depth, 4 * tile + grp, kv4_mask_word(a, mask_row, node, 4 * tile + grp));
-      }
-      if (poison != 0) l = NAN;
-      // ---- the groups' sums, against the reference that O ended in
-      sm->ml[grp][row] = make_float2(m_used, l);
-      rows_sync();
       const bool any = sg.steps > 0 && ok;
-      float M = any ? sm->ref[row] : -INFINITY, sum = 0.f;
-#pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        const float2 ml = sm->ml[w][row];
-        sum = fmaf(ml.y, ml.x == -INFINITY ? 0.f : ex2(ml.x - M), sum);
+      uint32_t poison = 0;  // tree rows that are not finite and that the row sees
+#pragma unroll 1
+      for (int i = max(sg.u.prefix.steps - sg.t0, 0); i < sg.steps; ++i) {
+        const int tt = sg.t0 + i - sg.u.prefix.steps;
+#pragma unroll 1
+        for (int w = 0; w < 4; ++w) {
+          const uint32_t bad = sm->bad[seg & 3][tt][w];
+          if (bad != 0) poison |= bad & kv4_window_word(a, r, L, depth, 4 * tt + w, kv4_mask_word(a, mask_row, node, 4 * tt + w));
+        }
       }
-      // The group's 32 columns of O, unnormalised: the row's four threads write a quarter each.
-      float o[32];
-      if (any) {
-        tmem_ld32(tmem + lane_sel + 32u * grp, reinterpret_cast<uint32_t*>(o), 0);
-        tc_wait_ld();
-      } else {
-#pragma unroll
-        for (int e = 0; e < 32; ++e) o[e] = 0.f;
-      }
+      // ---- the groups' sums, against the reference that O ended in: the last one settled
+      float M = any ? sm->ref[tile][row] : -INFINITY;
+      sm->sum[grp][row] = poison != 0 ? NAN : m_used == -INFINITY ? l : l * ex2(m_used - M);
+      rows_sync();
+      float sum = sm->sum[2 * tile][row] + sm->sum[2 * tile + 1][row];
+      if (!kTwo) sum += sm->sum[2][row] + sm->sum[3][row];
+      // A group writes 64 columns of its tile's O, or 32, 32 at a time.
+      constexpr int kRuns = kTwo ? 2 : 1;
+      const int first_run = kRuns * (kTwo ? half : grp);
       bool complete = sg.whole;
+      Kv4Pieces pieces = {0, 0};
       if (!sg.whole) {
         // This CTA's piece goes to the workspace and is counted; the one that counts the last piece adds them all, in the order
         // of their CTAs, and writes the rows.  Nobody waits for anybody.
-        const Kv4Pieces pieces = kv4_pieces(ranges, sg.u);
-        const int64_t mine = (int64_t)kv4_slot(ranges, blockIdx.x, sg.u.begin) * kTileM;
-        float4* to = reinterpret_cast<float4*>(a.ws_o + mine * kHeadDim) + (8 * grp) * kTileM + row;  // [channel / 4][row]
+        pieces = kv4_pieces(ranges, sg.u);
+        const int64_t mine = (int64_t)kv4_slot(ranges, blockIdx.x, sg.u.begin) * a.row_tile + tile * kTileM;
+#pragma unroll 1
+        for (int run = first_run; run < first_run + kRuns; ++run) {
+          float o[32];
+          tmem_ld32(tmem_o + 32u * run, reinterpret_cast<uint32_t*>(o), 0);
+          tc_wait_ld();
+          float4* to = reinterpret_cast<float4*>(a.ws_o + mine * kHeadDim) + (8 * run) * kTileM + row;  // [channel / 4][row]
 #pragma unroll
-        for (int e = 0; e < 32; e += 4) to[(e >> 2) * kTileM] = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
-        if (grp == 0) a.ws_ml[mine + row] = make_float2(M, sum);
+          for (int e = 0; e < 32; e += 4) to[(e >> 2) * kTileM] = any ? make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]) : make_float4(0.f, 0.f, 0.f, 0.f);
+        }
+        if (half == 0 && (kTwo || c == 0)) a.ws_ml[mine + row] = make_float2(M, sum);
         __threadfence();
         rows_sync();
-        if (grp == 0 && row == 0) sm->last = atomicAdd(a.ws_count + 2 * pieces.first, 1) == pieces.last - pieces.first;
+        if (half == 0 && (kTwo || c == 0) && row == 0) sm->last[tile] = atomicAdd(a.ws_count + 2 * pieces.first + tile, 1) == pieces.last - pieces.first;
         rows_sync();
-        complete = sm->last != 0;
+        complete = sm->last[tile] != 0;
         if (complete) {
           __threadfence();
           M = -INFINITY;
-          for (int x = pieces.first; x <= pieces.last; ++x) M = fmaxf(M, __ldcg(a.ws_ml + (int64_t)kv4_slot(ranges, x, sg.u.begin) * kTileM + row).x);
+          for (int x = pieces.first; x <= pieces.last; ++x)
+            M = fmaxf(M, __ldcg(a.ws_ml + (int64_t)kv4_slot(ranges, x, sg.u.begin) * a.row_tile + tile * kTileM + row).x);
           sum = 0.f;
-#pragma unroll
-          for (int e = 0; e < 32; ++e) o[e] = 0.f;
           for (int x = pieces.first; x <= pieces.last; ++x) {
-            const int64_t at = (int64_t)kv4_slot(ranges, x, sg.u.begin) * kTileM;
-            const float2 ml = __ldcg(a.ws_ml + at + row);
-            const float f = ml.x == -INFINITY ? 0.f : ex2(ml.x - M);
-            sum = fmaf(ml.y, f, sum);
-            const float4* from = reinterpret_cast<const float4*>(a.ws_o + at * kHeadDim) + (8 * grp) * kTileM + row;
-#pragma unroll
-            for (int e = 0; e < 32; e += 4) {
-              const float4 v = __ldcg(from + (e >> 2) * kTileM);
-              o[e] = fmaf(v.x, f, o[e]);
-              o[e + 1] = fmaf(v.y, f, o[e + 1]);
-              o[e + 2] = fmaf(v.z, f, o[e + 2]);
-              o[e + 3] = fmaf(v.w, f, o[e + 3]);
-            }
+            const float2 ml = __ldcg(a.ws_ml + (int64_t)kv4_slot(ranges, x, sg.u.begin) * a.row_tile + tile * kTileM + row);
+            sum = fmaf(ml.y, ml.x == -INFINITY ? 0.f : ex2(ml.x - M), sum);
           }
         }
       }
-      if (complete && valid) {
+      if (complete) {
         const float inv = 1.f / sum;
-        uint8_t* out = a.out + r * a.o_req + node * a.o_tok + h * a.o_head + 64 * grp;
+#pragma unroll 1
+        for (int run = first_run; run < first_run + kRuns; ++run) {
+          float o[32];
+          if (sg.whole) {
+            tmem_ld32(tmem_o + 32u * run, reinterpret_cast<uint32_t*>(o), 0);
+            tc_wait_ld();
+          } else {
 #pragma unroll
-        for (int e = 0; e < 32; e += 8) {  // columns 0,2,4,6,1,3,5,7 are channels 0..7
-          uint4 val;
-          val.x = pack2<kBf16>(o[e] * inv, o[e + 2] * inv);
-          val.y = pack2<kBf16>(o[e + 4] * inv, o[e + 6] * inv);
-          val.z = pack2<kBf16>(o[e + 1] * inv, o[e + 3] * inv);
-          val.w = pack2<kBf16>(o[e + 5] * inv, o[e + 7] * inv);
-          *reinterpret_cast<uint4*>(out + 2 * e) = val;
+            for (int e = 0; e < 32; ++e) o[e] = 0.f;
+#pragma unroll 1
+            for (int x = pieces.first; x <= pieces.last; ++x) {
+              const int64_t at = (int64_t)kv4_slot(ranges, x, sg.u.begin) * a.row_tile + tile * kTileM;
+              const float mx = __ldcg(a.ws_ml + at + row).x;
+              const float f = mx == -INFINITY ? 0.f : ex2(mx - M);
+              const float4* from = reinterpret_cast<const float4*>(a.ws_o + at * kHeadDim) + (8 * run) * kTileM + row;
+#pragma unroll
+              for (int e = 0; e < 32; e += 4) {
+                const float4 v = __ldcg(from + (e >> 2) * kTileM);
+                o[e] = fmaf(v.x, f, o[e]);
+                o[e + 1] = fmaf(v.y, f, o[e + 1]);
+                o[e + 2] = fmaf(v.z, f, o[e + 2]);
+                o[e + 3] = fmaf(v.w, f, o[e + 3]);
+              }
+            }
+          }
+          if (valid) {
+            uint8_t* out = a.out + r * a.o_req + node * a.o_tok + h * a.o_head + 64 * run;
+#pragma unroll
+            for (int e = 0; e < 32; e += 8) {  // columns 0,2,4,6,1,3,5,7 are channels 0..7
+              uint4 val;
+              val.x = pack2<kBf16>(o[e] * inv, o[e + 2] * inv);
+              val.y = pack2<kBf16>(o[e + 4] * inv, o[e + 6] * inv);
+              val.z = pack2<kBf16>(o[e + 1] * inv, o[e + 3] * inv);
+              val.w = pack2<kBf16>(o[e + 5] * inv, o[e + 7] * inv);
+              *reinterpret_cast<uint4*>(out + 2 * e) = val;
+            }
+          }
+          __syncwarp();
         }
-        if (grp == 0 && a.lse != nullptr) a.lse[((int64_t)r * a.Hq + h) * a.n + node] = (M + log2f(sum)) * kLn2;
+        if (valid && half == 0 && (kTwo || c == 0) && a.lse != nullptr) a.lse[((int64_t)r * a.Hq + h) * a.n + node] = (M + log2f(sum)) * kLn2;
       }
       tc_fence_before();
       rows_sync();  // the accumulator is read, the rows are through with Q and with what they exchanged
@@ -600,15 +673,18 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
 }
 
 // ---------------------------------------------------------------- host side ---------------------
-size_t kv4_tiles_workspace_bytes() {
+static bool tiles_two(const seq_tree_kv4_attention_params& p) { return p.n_tree * (p.num_q_heads / p.num_kv_heads) > kTileM; }
+
+size_t kv4_tiles_workspace_bytes(const seq_tree_kv4_attention_params& p) {
   const size_t sms = device_sm_count();
-  return kv4_count_bytes(sms) + 2 * sms * kTileM * (kHeadDim * sizeof(float) + sizeof(float2));
+  return kv4_count_bytes(sms) + 2 * sms * (tiles_two(p) ? 2 : 1) * kTileM * (kHeadDim * sizeof(float) + sizeof(float2));
 }
 
 int launch_kv4_tiles(const seq_tree_kv4_attention_params& p, cudaStream_t stream) {
+  const bool two = tiles_two(p);
   const int sms = device_sm_count();
   Kv4Args a = kv4_args(p);
-  a.row_tile = kTileM;
+  a.row_tile = two ? 2 * kTileM : kTileM;
   a.tiles = (a.rows + a.row_tile - 1) / a.row_tile;
   a.tree_steps = (a.n + kTilesStep - 1) / kTilesStep;
   a.min_steps = 2;
@@ -630,18 +706,20 @@ int launch_kv4_tiles(const seq_tree_kv4_attention_params& p, cudaStream_t stream
   early[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = early;
   cfg.numAttrs = 1;
-  cfg.dynamicSmemBytes = kTilesSmemBytes;
-  auto launch = [&](auto kernel, int which) -> int {
-    static int done[2][64];
+  auto launch = [&](auto kernel, int which, size_t smem) -> int {
+    static int done[4][64];
     const int rc = once_per_device(done[which], [&]() -> int {
-      SEQ_CUDA_OK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kTilesSmemBytes));
+      SEQ_CUDA_OK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
       return SEQ_OK;
     });
     if (rc != SEQ_OK) return rc;
+    cfg.dynamicSmemBytes = smem;
     SEQ_CUDA_OK(cudaLaunchKernelEx(&cfg, kernel, a));
     return SEQ_OK;
   };
-  return p.dtype == SEQ_BF16 ? launch(kv4_tiles_kernel<true>, 0) : launch(kv4_tiles_kernel<false>, 1);
+  const bool bf16 = p.dtype == SEQ_BF16;
+  if (two) return bf16 ? launch(kv4_tiles_kernel<true, true>, 0, tiles_smem_bytes<true>()) : launch(kv4_tiles_kernel<true, false>, 1, tiles_smem_bytes<true>());
+  return bf16 ? launch(kv4_tiles_kernel<false, true>, 2, tiles_smem_bytes<false>()) : launch(kv4_tiles_kernel<false, false>, 3, tiles_smem_bytes<false>());
 }
 
 }  // namespace seqtree
