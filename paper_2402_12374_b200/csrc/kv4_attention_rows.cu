@@ -1,14 +1,16 @@
 // Attention over the 4-bit pages for few query rows: the codes go from shared memory into mma fragments in registers.
 //
 // A warp takes 32 keys at a time, S^T = K Q^T with the keys in the 16-row operand and 8 query rows in the 8-column one, so that
-// a single token's eight grouped heads fill the tile:
-//     S^T  keys x rows:    A = codes less 8 of K, exact in half precision; scale and mid of a key are applied to the fp32 sums,
-//                          scale * (q . (code - 8)) + mid * sum(q)
-//     O^T  channels x rows: A = V^T, the values scale * (code - 8) + mid rounded to half; B = P^T, a movmatrix of S^T's layout
-// A thread's code words hold channels of one key (K) or, two words interleaved, of a pair of keys (V); the contraction's order
-// is free, so neither needs a transposition.  Each warp has a ring of steps in shared memory, filled by bulk copies (a step is
-// two granules, contiguous in a page), its own maxima and sums, and takes every fourth step of the CTA's range; the four meet
-// at the end of each unit.
+// a single token's eight grouped heads fill the tile.  What bounds such a kernel before HBM does is instructions, so codes are not
+// converted at all: four bits at the bottom of a half-precision word are the subnormal number code * 2^-24, four bits above
+// them code * 2^-20, and the tensor core takes subnormals exactly.  One AND makes two operand values, a shift serves four.
+//     S^T  keys x rows:     A = codes of K; q's channels that meet codes of 2^-20 are sixteen times smaller.  With s, m a key's scale and mid,
+//                           s * (q . code) + (m - 8 s) * sum(q) is put together in fp32.
+//     O^T  channels x rows: A = V^T, codes as they are (ldmatrix transposes 16-bit units, four channels of a key); B = P^T, a
+//                           movmatrix of S^T's layout, P = s * probability in half precision; m * probability and -8 P are summed beside it.
+// Scales are divided by a power of two not far from the largest met so far, so that P neither overflows nor becomes subnormal.
+// Each warp has a ring of steps in shared memory, filled by bulk copies (a step is two granules, contiguous in a page), its
+// own maxima and sums, and takes every fourth step of the CTA's range; the four meet at the end of each unit.
 #include "kv4_attention.cuh"
 #include "umma.cuh"
 
@@ -73,49 +75,87 @@ __device__ __forceinline__ void pairs_of_8(uint4 x, uint32_t* out) {
   out[3] = __byte_perm(x.y, x.w, 0x7632);
 }
 
-// A step's scores x (log2 units, -inf where masked) become probabilities of half precision in P^T's layout, against reference
-// maxima that only move when a score exceeds them by more than the threshold.
+// eight 8x8 blocks of 16-bit units in two instructions: thread (g, t) gets unit g of rows 2t, 2t + 1, transposed
+__device__ __forceinline__ void ldmatrix_x4_trans(uint32_t at, uint32_t* r) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
+}
+// Four codes of two words' halves each, as subnormal halves: x[0], x[2] code * 2^-24, x[1], x[3] code * 2^-20
+__device__ __forceinline__ void codes4(uint32_t w, uint32_t* x) {
+  const uint32_t v = w >> 8;
+  x[0] = w & 0x000f000fu;
+  x[1] = w & 0x00f000f0u;
+  x[2] = v & 0x000f000fu;
+  x[3] = v & 0x00f000f0u;
+}
+constexpr float k2p24 = 16777216.f, k2p20 = 1048576.f;
+
+// What a warp knows of its rows 2 t4 and 2 t4 + 1 (of each group of eight)
+template <int NT>
+struct RowsState {
+  float m[NT][2], l[NT][2];    // reference maximum (log2 units), sum of probabilities
+  float pm[NT][2], pr[NT][2];  // sums of mid * probability and of P as rounded, over the thread's keys
+  float o[NT][8][4];           // codes x P; or, once finished(), values x probabilities
+  int e;                       // P holds scale * probability / 2^e
+};
+
+// The reference follows scores that exceed it by more than the threshold, the exponent larger scales.
 template <int NG, int NT>
-__device__ __forceinline__ void softmax_step(float (&x)[NG][NT][4], float (&m)[NT][2], float (&l)[NT][2], float (&o)[NT][8][4], uint32_t (&p)[NG][NT][2]) {
-  bool move = false;
+__device__ __forceinline__ void follow(const float (&x)[NG][NT][4], int e, RowsState<NT>& st) {
+  bool move = e > st.e;
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
+    for (int v = 0; v < 4; ++v)
 #pragma unroll
-      for (int gr = 0; gr < NG; ++gr) move |= x[gr][nt][e] > m[nt][e & 1] + kRescaleThreshold;  // (also the first score: m = -inf)
-  if (__any_sync(0xffffffffu, move)) {
+      for (int gr = 0; gr < NG; ++gr) move |= x[gr][nt][v] > st.m[nt][v & 1] + kRescaleThreshold;  // (also the first score: m = -inf)
+  if (!__any_sync(0xffffffffu, move)) return;
+  const float shrink = e > st.e ? (st.e - e < -126 ? 0.f : __uint_as_float((uint32_t)(127 + st.e - e) << 23)) : 1.f;
+  st.e = max(st.e, e);
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
+  for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        float mx = m[nt][i];
+    for (int i = 0; i < 2; ++i) {
+      float mx = st.m[nt][i];
 #pragma unroll
-        for (int gr = 0; gr < NG; ++gr) mx = max3(mx, x[gr][nt][i], x[gr][nt][i + 2]);
+      for (int gr = 0; gr < NG; ++gr) mx = max3(mx, x[gr][nt][i], x[gr][nt][i + 2]);
 #pragma unroll
-        for (int d = 4; d < 32; d <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
-        const float alpha = m[nt][i] == -INFINITY ? 0.f : ex2(m[nt][i] - mx);
-        m[nt][i] = mx;
-        l[nt][i] *= alpha;
+      for (int d = 4; d < 32; d <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
+      const float alpha = st.m[nt][i] == -INFINITY ? 0.f : ex2(st.m[nt][i] - mx);
+      st.m[nt][i] = mx;
+      st.l[nt][i] *= alpha;
+      st.pm[nt][i] *= alpha;
+      st.pr[nt][i] *= alpha * shrink;
 #pragma unroll
-        for (int mt = 0; mt < 8; ++mt) {
-          o[nt][mt][i] *= alpha;
-          o[nt][mt][i + 2] *= alpha;
-        }
+      for (int mt = 0; mt < 8; ++mt) {
+        st.o[nt][mt][i] *= alpha * shrink;
+        st.o[nt][mt][i + 2] *= alpha * shrink;
       }
-  }
-#pragma unroll
-  for (int nt = 0; nt < NT; ++nt) {
-    const float n0 = m[nt][0] == -INFINITY ? 0.f : m[nt][0], n1 = m[nt][1] == -INFINITY ? 0.f : m[nt][1];
-#pragma unroll
-    for (int gr = 0; gr < NG; ++gr) {
-      const float p0 = ex2(x[gr][nt][0] - n0), p1 = ex2(x[gr][nt][1] - n1), p2 = ex2(x[gr][nt][2] - n0), p3 = ex2(x[gr][nt][3] - n1);
-      l[nt][0] += p0 + p2;
-      l[nt][1] += p1 + p3;
-      p[gr][nt][0] = transpose8x8(pack2<false>(p0, p1));
-      p[gr][nt][1] = transpose8x8(pack2<false>(p2, p3));
     }
-  }
+}
+
+// The sums over the thread's keys become the warp's, and o what it stands for.  O's tile 4 j + k, rows 0..7, 8..15: channels
+// 4 * (16 j + g8) + k, 4 * (16 j + 8 + g8) + k.
+template <int NT>
+__device__ __forceinline__ void finish(RowsState<NT>& st) {
+  const int e = min(max(st.e, -126), 126);
+  const float unit = __uint_as_float((uint32_t)(127 + e) << 23);
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      float pm = st.pm[nt][i], pr = st.pr[nt][i];
+#pragma unroll
+      for (int d = 4; d < 32; d <<= 1) {
+        pm += __shfl_xor_sync(0xffffffffu, pm, d);
+        pr += __shfl_xor_sync(0xffffffffu, pr, d);
+      }
+#pragma unroll
+      for (int mt = 0; mt < 8; ++mt) {
+        const float c = mt & 1 ? k2p20 : k2p24;
+        st.o[nt][mt][i] = fmaf(unit, fmaf(st.o[nt][mt][i], c, -8.f * pr), pm);
+        st.o[nt][mt][i + 2] = fmaf(unit, fmaf(st.o[nt][mt][i + 2], c, -8.f * pr), pm);
+      }
+    }
 }
 
 template <int NT, bool kBf16>
@@ -198,15 +238,17 @@ __global__ void __launch_bounds__(32 * kRowsWarps, NT == 1 ? 3 : 2) kv4_rows_ker
   for (int s = 0; s < kStages; ++s) load_next();
 
   bool ok = true;
-  const int kappa = (g8 & 1) ? 4 + ((g8 >> 1) ^ 1) : g8 >> 1;  // the key in the granule of operand row g8 (row g8 + 8: 8 more)
   for (int pos = range_lo; pos < range_hi;) {
     const Kv4Unit u = kv4_unit<kRowsStep>(&sm->plan, a, pos);
     const int seg_end = min(u.end, range_hi);
     const int row0 = u.m * 8 * NT, live_rows = min(8 * NT, a.rows - row0);
 
     // ---- the unit's rows: q as half precision (bf16 rows scaled by a power of two, exactly), its sum, what it sees
-    uint32_t qf[NT][16];
-    float rs[NT][2], sq[NT][2], m[NT][2], l[NT][2], o[NT][8][4];
+    uint32_t qc[NT][16];
+    float rs[NT][2], sq[NT][2];
+    RowsState<NT> st;
+    st.e = -1000;
+    bool finished = false;
     int node[NT][2], begin[NT][2], depth[NT][2];
     int latest = 0;  // the last begin of a row's window
 #pragma unroll
@@ -217,36 +259,47 @@ __global__ void __launch_bounds__(32 * kRowsWarps, NT == 1 ? 3 : 2) kv4_rows_ker
       uint4 x[4];
 #pragma unroll
       for (int w = 0; w < 4; ++w) x[w] = src[w];
-      float f = 1.f, inv_f = 1.f;
-      if (kBf16) {  // the row's largest magnitude into [2^8, 2^9); a row of zeros, or one that is not finite, as it is
-        uint32_t top = 0;
+      float v[4][8], top = 0.f;
 #pragma unroll
-        for (int w = 0; w < 4; ++w)
+      for (int w = 0; w < 4; ++w) {
+        const uint32_t y[4] = {x[w].x, x[w].y, x[w].z, x[w].w};
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const uint32_t v = i == 0 ? x[w].x : i == 1 ? x[w].y : i == 2 ? x[w].z : x[w].w;
-            top = max(top, max((v << 16) & 0x7fffffffu, v & 0x7fff0000u));
+        for (int i = 0; i < 4; ++i) {
+          if (kBf16) {
+            v[w][2 * i] = __uint_as_float(y[i] << 16);
+            v[w][2 * i + 1] = __uint_as_float(y[i] & 0xffff0000u);
+          } else {
+            const float2 f2 = __half22float2(*reinterpret_cast<const __half2*>(&y[i]));
+            v[w][2 * i] = f2.x;
+            v[w][2 * i + 1] = f2.y;
           }
-        top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-        top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-        const int e = (int)(top >> 23);
-        if (e > 8 && e < 255) {
-          const int up = min(max(8 + 127 - e, -100), 100);
-          f = __uint_as_float((uint32_t)(127 + up) << 23);
-          inv_f = __uint_as_float((uint32_t)(127 - up) << 23);
+          top = max3(top, fabsf(v[w][2 * i]), fabsf(v[w][2 * i + 1]));
         }
+      }
+      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+      // the row's largest magnitude into [2^8, 2^9); a row of zeros, or one that is not finite, as it is
+      const int e = (int)(__float_as_uint(top) >> 23);
+      float f = 1.f, inv_f = 1.f;
+      if (e > 8 && e < 255) {
+        const int up = min(max(8 + 127 - e, -100), 100);
+        f = __uint_as_float((uint32_t)(127 + up) << 23);
+        inv_f = __uint_as_float((uint32_t)(127 - up) << 23);
       }
       float sum = 0.f;
 #pragma unroll
       for (int w = 0; w < 4; ++w) {
-        uint32_t v[4] = {x[w].x, x[w].y, x[w].z, x[w].w};
+        uint32_t y[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          if (kBf16) v[i] = pack2<false>(__uint_as_float(v[i] << 16) * f, __uint_as_float(v[i] & 0xffff0000u) * f);
-          const float2 y = __half22float2(*reinterpret_cast<const __half2*>(&v[i]));
-          sum += y.x + y.y;
+          y[i] = pack2<false>(v[w][2 * i] * f, v[w][2 * i + 1] * f);
+          const float2 z = __half22float2(*reinterpret_cast<const __half2*>(&y[i]));
+          sum += z.x + z.y;
         }
-        pairs_of_8(make_uint4(v[0], v[1], v[2], v[3]), &qf[nt][4 * w]);
+        pairs_of_8(make_uint4(y[0], y[1], y[2], y[3]), &qc[nt][4 * w]);
+        // channels 1, 3, 5, 7 meet codes of 2^-20
+        qc[nt][4 * w + 1] = hmul2_bits(qc[nt][4 * w + 1], 0x2c002c00u);
+        qc[nt][4 * w + 3] = hmul2_bits(qc[nt][4 * w + 3], 0x2c002c00u);
       }
       sum += __shfl_xor_sync(0xffffffffu, sum, 1);
       sum += __shfl_xor_sync(0xffffffffu, sum, 2);
@@ -259,13 +312,13 @@ __global__ void __launch_bounds__(32 * kRowsWarps, NT == 1 ? 3 : 2) kv4_rows_ker
         depth[nt][i] = a.window > 0 ? kv4_depth(a, u.r, node[nt][i]) : 0;
         begin[nt][i] = a.window > 0 ? u.L + depth[nt][i] + 1 - a.window : 0;
         latest = max(latest, begin[nt][i]);
-        m[nt][i] = -INFINITY;
-        l[nt][i] = 0.f;
+        st.m[nt][i] = -INFINITY;
+        st.l[nt][i] = st.pm[nt][i] = st.pr[nt][i] = 0.f;
       }
 #pragma unroll
       for (int mt = 0; mt < 8; ++mt)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) o[nt][mt][e] = 0.f;
+        for (int e2 = 0; e2 < 4; ++e2) st.o[nt][mt][e2] = 0.f;
     }
     latest = __reduce_max_sync(0xffffffffu, latest);
 
@@ -276,88 +329,105 @@ __global__ void __launch_bounds__(32 * kRowsWarps, NT == 1 ? 3 : 2) kv4_rows_ker
         const int stage = used % kStages, key0 = u.prefix.key_step(t) * kRowsStep;
         if (ok) ok = mbar_wait(sm, &sm->full[warp][stage], (used / kStages) & 1, a.status);
         if (!ok) break;
-        const uint32_t st = smem_u32(sm->ring[warp][stage]);
+        const uint32_t at = smem_u32(sm->ring[warp][stage]);
+        const bool ends = key0 + kRowsStep > u.L;
+        // the step's largest scale of V: a lane a key
+        uint32_t vp = lds32(at + (lane >> 4) * kGranuleBytes + kGranuleParams + kGranule * 4 + (lane & 15) * 4);
+        if (ends && key0 + lane >= u.L) vp = 0u;
+        // (the exponent of a half, rounded up; of zero and of subnormals: -14)
+        const int e = __reduce_max_sync(0xffffffffu, (int)((vp >> 10) & 31u)) - 14;
         float x[2][NT][4];
+        float vs[2][2], vm[2][2];  // V's scale and mid of the thread's keys g8, g8 + 8
 #pragma unroll
         for (int gr = 0; gr < 2; ++gr) {
-          const uint32_t k_at = st + gr * kGranuleBytes + kappa * kCodeBytes + t4 * 16;
+          const uint32_t k_at = at + gr * kGranuleBytes + g8 * kCodeBytes + t4 * 16;
           const uint4 ka = lds128(k_at), kb = lds128(k_at + 8 * kCodeBytes);
-          const uint32_t p_at = st + gr * kGranuleBytes + kGranuleParams + kappa * 4;
+          const uint32_t p_at = at + gr * kGranuleBytes + kGranuleParams + g8 * 4;
           const uint32_t pa = lds32(p_at), pb = lds32(p_at + 32);
           float s[NT][4];
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) s[nt][e] = 0.f;
+            for (int v = 0; v < 4; ++v) s[nt][v] = 0.f;
 #pragma unroll
           for (int w = 0; w < 4; ++w) {
             uint32_t a0[4], a1[4];
-            unpack4(w == 0 ? ka.x : w == 1 ? ka.y : w == 2 ? ka.z : ka.w, a0);
-            unpack4(w == 0 ? kb.x : w == 1 ? kb.y : w == 2 ? kb.z : kb.w, a1);
+            codes4(w == 0 ? ka.x : w == 1 ? ka.y : w == 2 ? ka.z : ka.w, a0);
+            codes4(w == 0 ? kb.x : w == 1 ? kb.y : w == 2 ? kb.z : kb.w, a1);
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
-              mma16816(s[nt], a0[0], a1[0], a0[1], a1[1], qf[nt][4 * w], qf[nt][4 * w + 1]);
-              mma16816(s[nt], a0[2], a1[2], a0[3], a1[3], qf[nt][4 * w + 2], qf[nt][4 * w + 3]);
+              mma16816(s[nt], a0[0], a1[0], a0[1], a1[1], qc[nt][4 * w], qc[nt][4 * w + 1]);
+              mma16816(s[nt], a0[2], a1[2], a0[3], a1[3], qc[nt][4 * w + 2], qc[nt][4 * w + 3]);
             }
           }
           const float2 fa = __half22float2(*reinterpret_cast<const __half2*>(&pa)), fb = __half22float2(*reinterpret_cast<const __half2*>(&pb));
+          const float sa = fa.x * k2p24, sb = fb.x * k2p24, ma = fmaf(fa.x, -8.f, fa.y), mb = fmaf(fb.x, -8.f, fb.y);
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-              x[gr][nt][i] = rs[nt][i] * fmaf(fa.x, s[nt][i], fa.y * sq[nt][i]);
-              x[gr][nt][i + 2] = rs[nt][i] * fmaf(fb.x, s[nt][i + 2], fb.y * sq[nt][i]);
+              x[gr][nt][i] = rs[nt][i] * fmaf(sa, s[nt][i], ma * sq[nt][i]);
+              x[gr][nt][i + 2] = rs[nt][i] * fmaf(sb, s[nt][i + 2], mb * sq[nt][i]);
             }
+          uint32_t va = lds32(p_at + kGranule * 4), vb = lds32(p_at + kGranule * 4 + 32);
+          if (ends) {  // what lies behind the prefix may be anything: zeros
+            if (key0 + gr * kGranule + g8 >= u.L) va = 0u;
+            if (key0 + gr * kGranule + g8 + 8 >= u.L) vb = 0u;
+          }
+          const float2 ga = __half22float2(*reinterpret_cast<const __half2*>(&va)), gb = __half22float2(*reinterpret_cast<const __half2*>(&vb));
+          vs[gr][0] = ga.x; vm[gr][0] = ga.y;
+          vs[gr][1] = gb.x; vm[gr][1] = gb.y;
         }
-        const bool ends = key0 + kRowsStep > u.L;
         if (ends || (a.window > 0 && key0 < latest)) {  // some keys are not there, or not every row's
 #pragma unroll
           for (int gr = 0; gr < 2; ++gr)
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              const int j = key0 + gr * kGranule + kappa + 8 * e;
+            for (int v = 0; v < 2; ++v) {
+              const int j = key0 + gr * kGranule + g8 + 8 * v;
 #pragma unroll
               for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                 for (int i = 0; i < 2; ++i)
-                  if (j >= u.L || (j < begin[nt][i] && j >= a.sinks)) x[gr][nt][2 * e + i] = -INFINITY;
+                  if (j >= u.L || (j < begin[nt][i] && j >= a.sinks)) x[gr][nt][2 * v + i] = -INFINITY;
             }
         }
+        follow<2, NT>(x, e, st);
+        const float per_unit = __uint_as_float((uint32_t)(127 - st.e) << 23);  // (-14 <= e <= 17)
         uint32_t pf[2][NT][2];
-        softmax_step<2, NT>(x, m, l, o, pf);
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          const float n0 = st.m[nt][0] == -INFINITY ? 0.f : st.m[nt][0], n1 = st.m[nt][1] == -INFINITY ? 0.f : st.m[nt][1];
+#pragma unroll
+          for (int gr = 0; gr < 2; ++gr)
+#pragma unroll
+            for (int v = 0; v < 2; ++v) {
+              const float p0 = ex2(x[gr][nt][2 * v] - n0), p1 = ex2(x[gr][nt][2 * v + 1] - n1);
+              const float sc = vs[gr][v] * per_unit;
+              const uint32_t packed = pack2<false>(p0 * sc, p1 * sc);
+              const float2 back = __half22float2(*reinterpret_cast<const __half2*>(&packed));
+              st.l[nt][0] += p0;
+              st.l[nt][1] += p1;
+              st.pm[nt][0] = fmaf(p0, vm[gr][v], st.pm[nt][0]);
+              st.pm[nt][1] = fmaf(p1, vm[gr][v], st.pm[nt][1]);
+              st.pr[nt][0] += back.x;
+              st.pr[nt][1] += back.y;
+              pf[gr][nt][v] = transpose8x8(packed);
+            }
+        }
 #pragma unroll
         for (int gr = 0; gr < 2; ++gr) {
-          // the thread's four keys of the granule, in two pairs: operand columns 2 t4, 2 t4 + 1 and eight more
-          const int ja = t4, jb = 4 + (t4 ^ 1);
-          const uint32_t v_at = st + gr * kGranuleBytes + kGranuleV + g8 * 8;
-          const uint32_t q_at = st + gr * kGranuleBytes + kGranuleParams + kGranule * 4;
-          const uint2 wa = lds64(v_at + ja * kCodeBytes), wb = lds64(v_at + jb * kCodeBytes);
-          const uint2 wc = lds64(v_at + (ja + 8) * kCodeBytes), wd = lds64(v_at + (jb + 8) * kCodeBytes);
-          uint32_t pa = lds32(q_at + ja * 4), pb = lds32(q_at + jb * 4), pc = lds32(q_at + ja * 4 + 32), pd = lds32(q_at + jb * 4 + 32);
-          if (ends) {  // what lies behind the prefix may be anything: zeros
-            const int j = key0 + gr * kGranule;
-            pa = j + ja < u.L ? pa : 0u;
-            pb = j + jb < u.L ? pb : 0u;
-            pc = j + ja + 8 < u.L ? pc : 0u;
-            pd = j + jb + 8 < u.L ? pd : 0u;
-          }
-          const uint32_t s_ab = __byte_perm(pa, pb, 0x5410), m_ab = __byte_perm(pa, pb, 0x7632);
-          const uint32_t s_cd = __byte_perm(pc, pd, 0x5410), m_cd = __byte_perm(pc, pd, 0x7632);
+          // lane: a row of the four blocks (keys 0..7 and 8..15 of 16-byte columns 2 c and 2 c + 1)
+          const uint32_t v_at = at + gr * kGranuleBytes + kGranuleV + ((lane & 7) + 8 * ((lane >> 3) & 1)) * kCodeBytes + (lane >> 4) * 16;
 #pragma unroll
-          for (int half = 0; half < 2; ++half) {  // channels 4 half .. 4 half + 3 of the thread's two words
-            const int sel = half ? 0x7632 : 0x5410;
-            uint32_t v0[4], v1[4], v2[4], v3[4];
-            unpack4(__byte_perm(wa.x, wb.x, sel), v0);
-            unpack4(__byte_perm(wa.y, wb.y, sel), v1);
-            unpack4(__byte_perm(wc.x, wd.x, sel), v2);
-            unpack4(__byte_perm(wc.y, wd.y, sel), v3);
+          for (int c = 0; c < 2; ++c) {
+            uint32_t w[4], b[4][4];  // blocks: (column 2c, keys 0..7), (2c, 8..15), (2c + 1, 0..7), (2c + 1, 8..15)
+            ldmatrix_x4_trans(v_at + 32 * c, w);
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
-              const uint32_t b0 = hfma2_bits(v0[c], s_ab, m_ab), b1 = hfma2_bits(v1[c], s_ab, m_ab);
-              const uint32_t b2 = hfma2_bits(v2[c], s_cd, m_cd), b3 = hfma2_bits(v3[c], s_cd, m_cd);
+            for (int y = 0; y < 4; ++y) codes4(w[y], b[y]);
 #pragma unroll
-              for (int nt = 0; nt < NT; ++nt) mma16816(o[nt][4 * half + c], b0, b1, b2, b3, pf[gr][nt][0], pf[gr][nt][1]);
-            }
+            for (int k = 0; k < 4; ++k)
+#pragma unroll
+              for (int nt = 0; nt < NT; ++nt) mma16816(st.o[nt][4 * c + k], b[0][k], b[2][k], b[1][k], b[3][k], pf[gr][nt][0], pf[gr][nt][1]);
           }
         }
         __syncwarp();  // every lane has read the stage
@@ -365,7 +435,11 @@ __global__ void __launch_bounds__(32 * kRowsWarps, NT == 1 ? 3 : 2) kv4_rows_ker
         load_next();
         continue;
       }
-      // ---- 32 rows of the tree, from global memory: 16 at a time
+      // ---- 32 rows of the tree, from global memory: 16 at a time.  (The last steps of a unit: o becomes what it stands for.)
+      if (!finished) {
+        finish(st);
+        finished = true;
+      }
       const int w = t - u.prefix.steps;
       uint32_t seen[NT][2];
 #pragma unroll
@@ -398,8 +472,8 @@ __global__ void __launch_bounds__(32 * kRowsWarps, NT == 1 ? 3 : 2) kv4_rows_ker
           }
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt) {
-            mma16816(s[0][nt], f0[0], f1[0], f0[1], f1[1], qf[nt][4 * c], qf[nt][4 * c + 1]);
-            mma16816(s[0][nt], f0[2], f1[2], f0[3], f1[3], qf[nt][4 * c + 2], qf[nt][4 * c + 3]);
+            mma16816(s[0][nt], f0[0], f1[0], f0[1], f1[1], qc[nt][4 * c], hmul2_bits(qc[nt][4 * c + 1], 0x4c004c00u));
+            mma16816(s[0][nt], f0[2], f1[2], f0[3], f1[3], qc[nt][4 * c + 2], hmul2_bits(qc[nt][4 * c + 3], 0x4c004c00u));
           }
         }
         // V, in pairs of rows (2 t4, 2 t4 + 1 and eight more).  A row with a value that is not finite in half precision counts as zeros, so that
@@ -408,24 +482,20 @@ __global__ void __launch_bounds__(32 * kRowsWarps, NT == 1 ? 3 : 2) kv4_rows_ker
 #pragma unroll
         for (int y = 0; y < 2; ++y) {
           const int j = n0 + 2 * t4 + 8 * y;
-          uint4 x0[2], x1[2];
-#pragma unroll
-          for (int z = 0; z < 2; ++z) {
-            x0[z] = x1[z] = make_uint4(0u, 0u, 0u, 0u);
-            if (j < a.n) x0[z] = reinterpret_cast<const uint4*>(v_rows + j * a.t_tok)[2 * g8 + z];
-            if (j + 1 < a.n) x1[z] = reinterpret_cast<const uint4*>(v_rows + (j + 1) * a.t_tok)[2 * g8 + z];
-          }
           uint32_t big = 0;  // the largest exponents of the two rows
 #pragma unroll
-          for (int z = 0; z < 2; ++z)
+          for (int c = 0; c < 4; ++c) {  // channels 4 * (8 c + g8) and the three behind
+            uint2 x0 = make_uint2(0u, 0u), x1 = make_uint2(0u, 0u);
+            if (j < a.n) x0 = reinterpret_cast<const uint2*>(v_rows + j * a.t_tok)[8 * c + g8];
+            if (j + 1 < a.n) x1 = reinterpret_cast<const uint2*>(v_rows + (j + 1) * a.t_tok)[8 * c + g8];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const uint32_t h0 = to_half2<kBf16>(i == 0 ? x0[z].x : i == 1 ? x0[z].y : i == 2 ? x0[z].z : x0[z].w);
-              const uint32_t h1 = to_half2<kBf16>(i == 0 ? x1[z].x : i == 1 ? x1[z].y : i == 2 ? x1[z].z : x1[z].w);
-              v[y][8 * z + 2 * i] = __byte_perm(h0, h1, 0x5410);
-              v[y][8 * z + 2 * i + 1] = __byte_perm(h0, h1, 0x7632);
-              big = __vmaxu2(big, __vmaxu2(v[y][8 * z + 2 * i] & 0x7c007c00u, v[y][8 * z + 2 * i + 1] & 0x7c007c00u));
+            for (int i = 0; i < 2; ++i) {
+              const uint32_t h0 = to_half2<kBf16>(i ? x0.y : x0.x), h1 = to_half2<kBf16>(i ? x1.y : x1.x);
+              v[y][4 * c + 2 * i] = __byte_perm(h0, h1, 0x5410);
+              v[y][4 * c + 2 * i + 1] = __byte_perm(h0, h1, 0x7632);
+              big = __vmaxu2(big, __vmaxu2(v[y][4 * c + 2 * i] & 0x7c007c00u, v[y][4 * c + 2 * i + 1] & 0x7c007c00u));
             }
+          }
           if ((big & 0xffffu) == 0x7c00u) not_finite |= 1u << (16 * gr + 2 * t4 + 8 * y);
           if ((big >> 16) == 0x7c00u) not_finite |= 2u << (16 * gr + 2 * t4 + 8 * y);
         }
@@ -446,65 +516,86 @@ __global__ void __launch_bounds__(32 * kRowsWarps, NT == 1 ? 3 : 2) kv4_rows_ker
             const bool visible = (seen[nt][e & 1] >> (16 * gr + g8 + 8 * (e >> 1))) & 1u;
             s[0][nt][e] = visible ? s[0][nt][e] * rs[nt][e & 1] : -INFINITY;
           }
-        uint32_t pf[1][NT][2];
-        softmax_step<1, NT>(s, m, l, o, pf);
+        follow<1, NT>(s, st.e, st);
+        uint32_t pf[NT][2];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          const float n0 = st.m[nt][0] == -INFINITY ? 0.f : st.m[nt][0], n1 = st.m[nt][1] == -INFINITY ? 0.f : st.m[nt][1];
+#pragma unroll
+          for (int y = 0; y < 2; ++y) {
+            const float p0 = ex2(s[0][nt][2 * y] - n0), p1 = ex2(s[0][nt][2 * y + 1] - n1);
+            st.l[nt][0] += p0;
+            st.l[nt][1] += p1;
+            pf[nt][y] = transpose8x8(pack2<false>(p0, p1));
+          }
+        }
         if (not_finite != 0) {
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int i = 0; i < 2; ++i)
-              if (seen[nt][i] & not_finite) l[nt][i] = NAN;
+              if (seen[nt][i] & not_finite) st.l[nt][i] = NAN;
         }
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-          for (int mt = 0; mt < 8; ++mt) mma16816(o[nt][mt], v[0][mt], v[0][8 + mt], v[1][mt], v[1][8 + mt], pf[0][nt][0], pf[0][nt][1]);
+          for (int c = 0; c < 2; ++c)
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+              mma16816(st.o[nt][4 * c + k], v[0][8 * c + k], v[0][8 * c + 4 + k], v[1][8 * c + k], v[1][8 * c + 4 + k], pf[nt][0], pf[nt][1]);
       }
     }
 
     // ---- the four warps' rows meet
+    if (!finished) finish(st);
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
+        float l = st.l[nt][i];
 #pragma unroll
-        for (int d = 4; d < 32; d <<= 1) l[nt][i] += __shfl_xor_sync(0xffffffffu, l[nt][i], d);
+        for (int d = 4; d < 32; d <<= 1) l += __shfl_xor_sync(0xffffffffu, l, d);
         const int row = nt * 8 + 2 * t4 + i;
-        if (g8 == 0) sm->ml[warp][row] = make_float2(m[nt][i], l[nt][i]);
-        float4* to = reinterpret_cast<float4*>(&sm->o[warp][row][16 * g8]);
+        if (g8 == 0) sm->ml[warp][row] = make_float2(st.m[nt][i], l);
 #pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          to[c] = make_float4(o[nt][4 * c][i], o[nt][4 * c + 1][i], o[nt][4 * c + 2][i], o[nt][4 * c + 3][i]);
-          to[c + 2] = make_float4(o[nt][4 * c][i + 2], o[nt][4 * c + 1][i + 2], o[nt][4 * c + 2][i + 2], o[nt][4 * c + 3][i + 2]);
+        for (int c = 0; c < 4; ++c) {
+          const int mt = 4 * (c >> 1), v = i + 2 * (c & 1);
+          *reinterpret_cast<float4*>(&sm->o[warp][row][4 * (8 * c + g8)]) = make_float4(st.o[nt][mt][v], st.o[nt][mt + 1][v], st.o[nt][mt + 2][v], st.o[nt][mt + 3][v]);
         }
       }
     __syncthreads();
     const bool whole = pos == u.begin && seg_end == u.end;
-    const int c = threadIdx.x;
-    using T = typename std::conditional<kBf16, __nv_bfloat16, __half>::type;
-    auto write_row = [&](int row, float M, float sum, float acc) {
-      const int rw = row0 + row, nd = rw / a.group, h = u.g * a.group + rw - nd * a.group;
-      reinterpret_cast<T*>(a.out + u.r * a.o_req + nd * a.o_tok + h * a.o_head)[c] = from_float<T>(acc / sum);
-      if (a.lse != nullptr && c == 0) a.lse[((int64_t)u.r * a.Hq + h) * a.n + nd] = (M + log2f(sum)) * kLn2;
-    };
     const int64_t slot = (int64_t)kv4_slot(ranges, blockIdx.x, u.begin) * a.row_tile;
-    for (int row = 0; row < live_rows; ++row) {
-      float M = -INFINITY;
+    // Warp w: rows w, w + 4, ...; a lane has four channels of a row.
+    using T = typename std::conditional<kBf16, __nv_bfloat16, __half>::type;
+    auto write_row = [&](int row, float M, float sum, float4 acc) {
+      const int rw = row0 + row, nd = rw / a.group, h = u.g * a.group + rw - nd * a.group;
+      const float inv = 1.f / sum;
+      *reinterpret_cast<uint2*>(a.out + u.r * a.o_req + nd * a.o_tok + h * a.o_head + 8 * lane) =
+          make_uint2(pack2<kBf16>(acc.x * inv, acc.y * inv), pack2<kBf16>(acc.z * inv, acc.w * inv));
+      if (a.lse != nullptr && lane == 0) a.lse[((int64_t)u.r * a.Hq + h) * a.n + nd] = (M + log2f(sum)) * kLn2;
+    };
+#pragma unroll
+    for (int y = 0; y < 2 * NT; ++y) {
+      const int row = warp + kRowsWarps * y;
+      float M = -INFINITY, sum = 0.f;
+      float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
       for (int w = 0; w < kRowsWarps; ++w) M = fmaxf(M, sm->ml[w][row].x);
-      float sum = 0.f, acc = 0.f;
 #pragma unroll
       for (int w = 0; w < kRowsWarps; ++w) {
         const float2 ml = sm->ml[w][row];
         const float f = ml.x == -INFINITY ? 0.f : ex2(ml.x - M);
+        const float4 v = *reinterpret_cast<const float4*>(&sm->o[w][row][4 * lane]);
         sum = fmaf(ml.y, f, sum);
-        acc = fmaf(sm->o[w][row][c], f, acc);
+        acc.x = fmaf(v.x, f, acc.x); acc.y = fmaf(v.y, f, acc.y); acc.z = fmaf(v.z, f, acc.z); acc.w = fmaf(v.w, f, acc.w);
       }
+      if (row >= live_rows) continue;
       if (whole) {
         write_row(row, M, sum, acc);
       } else {
-        a.ws_o[(slot + row) * kHeadDim + c] = acc;
-        if (c == 0) a.ws_ml[slot + row] = make_float2(M, sum);
+        reinterpret_cast<float4*>(a.ws_o + (slot + row) * kHeadDim)[lane] = acc;
+        if (lane == 0) a.ws_ml[slot + row] = make_float2(M, sum);
       }
     }
     if (!whole) {
@@ -512,20 +603,32 @@ __global__ void __launch_bounds__(32 * kRowsWarps, NT == 1 ? 3 : 2) kv4_rows_ker
       const Kv4Pieces pieces = kv4_pieces(ranges, u);
       __threadfence();
       __syncthreads();
-      if (c == 0) sm->last = atomicAdd(a.ws_count + 2 * pieces.first, 1) == pieces.last - pieces.first;
+      if (threadIdx.x == 0) sm->last = atomicAdd(a.ws_count + 2 * pieces.first, 1) == pieces.last - pieces.first;
       __syncthreads();
       if (sm->last) {
         __threadfence();
-        for (int row = 0; row < live_rows; ++row) {
-          float M = -INFINITY;
-          for (int x = pieces.first; x <= pieces.last; ++x) M = fmaxf(M, __ldcg(a.ws_ml + (int64_t)kv4_slot(ranges, x, u.begin) * a.row_tile + row).x);
-          float sum = 0.f, acc = 0.f;
-          for (int x = pieces.first; x <= pieces.last; ++x) {
-            const int64_t s = (int64_t)kv4_slot(ranges, x, u.begin) * a.row_tile + row;
-            const float2 ml = __ldcg(a.ws_ml + s);
+#pragma unroll
+        for (int y = 0; y < 2 * NT; ++y) {
+          const int row = warp + kRowsWarps * y;
+          if (row >= live_rows) continue;
+          // 32 pieces at a time: a lane looks one's (m, l) up, then all add its rows
+          float M = -INFINITY, sum = 0.f;
+          float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+          for (int p0 = pieces.first; p0 <= pieces.last; p0 += 32) {
+            const int n = min(32, pieces.last - p0 + 1);
+            float2 ml = make_float2(-INFINITY, 0.f);
+            if (lane < n) ml = __ldcg(a.ws_ml + (int64_t)kv4_slot(ranges, p0 + lane, u.begin) * a.row_tile + row);
+            const float now = fmaxf(M, warp_max(ml.x)), old = M == -INFINITY ? 0.f : ex2(M - now);
+            M = now;
             const float f = ml.x == -INFINITY ? 0.f : ex2(ml.x - M);
-            sum = fmaf(ml.y, f, sum);
-            acc = fmaf(__ldcg(a.ws_o + s * kHeadDim + c), f, acc);
+            sum = sum * old + warp_sum(ml.y * f);
+            acc.x *= old; acc.y *= old; acc.z *= old; acc.w *= old;
+#pragma unroll 4
+            for (int p = 0; p < n; ++p) {
+              const float4 v = __ldcg(reinterpret_cast<const float4*>(a.ws_o + ((int64_t)kv4_slot(ranges, p0 + p, u.begin) * a.row_tile + row) * kHeadDim) + lane);
+              const float w = __shfl_sync(0xffffffffu, f, p);
+              acc.x = fmaf(v.x, w, acc.x); acc.y = fmaf(v.y, w, acc.y); acc.z = fmaf(v.z, w, acc.z); acc.w = fmaf(v.w, w, acc.w);
+            }
           }
           write_row(row, M, sum, acc);
         }
