@@ -16,7 +16,7 @@ struct Kv4Args {
   int32_t batch, n, max_len, Hq, Hkv, group, rows;  // rows: n * group
   int32_t window, sinks;
   int32_t num_pages, page_size, page_shift;
-  int32_t row_tile, tiles, tree_steps, ctas, min_steps;
+  int32_t row_tile, tiles, tree_steps, ctas, min_steps, cluster;
   const uint8_t* q; int64_t q_req, q_tok, q_head;  // all strides in bytes
   const uint8_t* kt; const uint8_t* vt; int64_t t_req, t_tok, t_head;
   const uint8_t* pages; int64_t page_stride;

@@ -83,7 +83,8 @@ extern "C" size_t seq_tree_kv4_attention_workspace_bytes(const seq_tree_kv4_atte
 extern "C" int seq_tree_kv4_attention(const seq_tree_kv4_attention_params* p, void* stream) {
   const int rc = check_kv4_attention(p);
   if (rc != SEQ_OK) return rc;
-  if (p->workspace == nullptr || p->workspace_bytes < seq_tree_kv4_attention_workspace_bytes(p)) return SEQ_ERR_WORKSPACE;
-  if (reinterpret_cast<uintptr_t>(p->workspace) % 256 != 0) return SEQ_ERR_INVALID_ARG;
+  const size_t need = seq_tree_kv4_attention_workspace_bytes(p);
+  if (need > 0 && (p->workspace == nullptr || p->workspace_bytes < need)) return SEQ_ERR_WORKSPACE;
+  if (need > 0 && reinterpret_cast<uintptr_t>(p->workspace) % 256 != 0) return SEQ_ERR_INVALID_ARG;
   return few_rows(*p) ? launch_kv4_rows(*p, static_cast<cudaStream_t>(stream)) : launch_kv4_tiles(*p, static_cast<cudaStream_t>(stream));
 }

@@ -136,11 +136,12 @@ def test_a_long_prefix_of_one_request(n, Hq):
 
 
 def test_same_call_same_bits_and_any_workspace_contents():
-    for n in (1, 40):
-        c = Case([900, 30, 411], n, 8, 2, 16, torch.bfloat16)
+    for n, lengths in ((1, [900, 30, 411]), (1, [900, 30, 411] * 40), (40, [900, 30, 411])):
+        c = Case(lengths, n, 8, 2, 16, torch.bfloat16)
         call = c.call()
         a = call.run().clone()
-        call.workspace.fill_(0xFF)
+        if call.workspace is not None:
+            call.workspace.fill_(0xFF)
         call.out.zero_()
         assert torch.equal(a, call.run())
 
@@ -292,8 +293,11 @@ def test_offsets_beyond_32_bits():
 
 
 def test_workspace_that_is_too_small_is_refused():
-    c = Case([45], 1, 8, 1, 16, torch.float16)
-    need = c.call().workspace_bytes_needed
-    call = c.call(workspace=torch.empty(need - 16, dtype=torch.uint8, device="cuda"))
-    with pytest.raises(B.SeqTreeError, match="WORKSPACE"):
-        call.run()
+    for lengths, n in (([45] * 300, 1), ([45], 40)):
+        c = Case(lengths, n, 16, 2, 16, torch.float16)
+        need = c.call().workspace_bytes_needed
+        assert need > 0
+        call = c.call(workspace=torch.empty(need - 16, dtype=torch.uint8, device="cuda"))
+        with pytest.raises(B.SeqTreeError, match="WORKSPACE"):
+            call.run()
+    assert Case([45], 1, 8, 1, 16, torch.float16).call().workspace is None  # a cluster a unit: none is needed
