@@ -12,8 +12,8 @@
 // Each warp has a ring of steps in shared memory, filled by bulk copies (granules are contiguous in a page), its own maxima and
 // sums, and takes every fourth step of the CTA's range; the four meet at the end of each unit.
 //
-// Two ways to cut the work.  Few units: a cluster of CTAs each, steps of 32 keys, the CTAs meet in shared memory; one launch without
-// a workspace.  Many: the ranges of kv4_attention.cuh, equal whatever the requests' lengths are, and steps of 64 keys.
+// Two ways to cut the work.  Few units: a cluster of CTAs each, which meet in shared memory, one launch without a workspace.  Many:
+// the ranges of kv4_attention.cuh, equal whatever the requests' lengths are.
 #include "kv4_attention.cuh"
 #include "umma.cuh"
 
@@ -24,17 +24,19 @@ constexpr int kTreeStep = 32;  // rows of the tree in a step
 constexpr int kRowsCluster = 8;  // CTAs of a cluster, at most
 constexpr float kNoRef = -1e30f;  // a row that has seen no key yet
 
-template <int NT, bool kCluster>
+constexpr int kKeys = 32;    // of a step
+constexpr int kStages = 3;
+constexpr int kBytes = kKeys / kGranule * kGranuleBytes;
+
+template <int NT>
 struct RowsSmem {
-  static constexpr int kKeys = kCluster ? 32 : 64;  // of a step
-  static constexpr int kStages = kCluster ? 3 : 2;
-  static constexpr int kBytes = kKeys / kGranule * kGranuleBytes;
   uint8_t ring[kRowsWarps][kStages][kBytes];
   float o[kRowsWarps][8 * NT][kHeadDim + 4];
   float2 ml[kRowsWarps][8 * NT];
   uint64_t full[kRowsWarps][kStages];
   volatile int abort_flag;
   int32_t last;  // this CTA completes the unit
+  int32_t begin[8 * NT];  // where the rows' windows begin
   Kv4Plan plan;
 };
 
@@ -182,9 +184,7 @@ __device__ __forceinline__ void finish(RowsState<NT>& st) {
 template <int NT, bool kBf16, bool kCluster>
 __global__ void __launch_bounds__(32 * kRowsWarps, NT == 1 ? 3 : 2) kv4_rows_kernel(const Kv4Args a) {
   extern __shared__ __align__(128) uint8_t smem_raw[];
-  using Smem = RowsSmem<NT, kCluster>;
-  constexpr int kKeys = Smem::kKeys, kStages = Smem::kStages, kBytes = Smem::kBytes;
-  Smem* sm = reinterpret_cast<Smem*>(smem_raw);
+  RowsSmem<NT>* sm = reinterpret_cast<RowsSmem<NT>*>(smem_raw);
   const int warp = uniform((int)threadIdx.x >> 5), lane = threadIdx.x & 31, g8 = lane >> 2, t4 = lane & 3;
   if (threadIdx.x == 0) {
     for (int w = 0; w < kRowsWarps; ++w)
@@ -223,62 +223,64 @@ __global__ void __launch_bounds__(32 * kRowsWarps, NT == 1 ? 3 : 2) kv4_rows_ker
     return kv4_unit<kKeys>(&sm->plan, a, pos);
   };
 
-  // ---- the loader: every warp asks for its steps, kStages of them ahead.  A step's keys are in 1, 2 or 4 pages; page numbers are looked up
-  // 32 at a time, a lane each.
+  // ---- the loader: every warp's lane 0 asks for its steps, kStages of them ahead.  Page numbers are looked up 32 steps at a time,
+  // a lane each.
   const uint32_t ring = smem_u32(sm->ring[warp][0]), bars = smem_u32(&sm->full[warp][0]);
-  const int log_pages = max(0, (kKeys == 32 ? 5 : 6) - a.page_shift);     // pages of a step
-  const uint32_t page_part = (uint32_t)min(kKeys, a.page_size) * 136u;    // bytes of the step in a page
   int load_pos = range_lo + warp, load_stage = 0, loaded = 0;
   int lt = 0, lt_end = 0;  // the step of the unit at load_pos, where the unit's prefix (or the range) ends
-  Kv4Unit lu = {};
-  const uint8_t* l_head = nullptr;
-  const int32_t* l_row = nullptr;
-  int id = 0, ids_left = 0, ids_at = 0;
+  int l_unit_end = 0, l_len = 0, l_split = 0, l_gap = 0, l_r = 0, l_g = 0;
+  int id0 = 0, id1 = 0, ids = 32;  // lane x: the pages of the step x steps ahead of where they were looked up, ids steps ago
   auto load_next = [&]() {
     while (lt >= lt_end) {  // (a unit's prefix is through; its tree's steps are read where they are used)
       if (kCluster && lt_end > 0) return;
-      const int from = loaded == 0 ? load_pos : max(load_pos, lu.end + ((warp - (lu.end - range_lo)) & (kRowsWarps - 1)));
+      const int from = loaded == 0 ? load_pos : max(load_pos, l_unit_end + ((warp - (l_unit_end - range_lo)) & (kRowsWarps - 1)));
       if (from >= range_hi) return;
       load_pos = from;
-      lu = unit_at(load_pos);
+      const Kv4Unit lu = unit_at(load_pos);
+      l_unit_end = lu.end; l_len = lu.L; l_split = lu.prefix.split; l_gap = lu.prefix.gap; l_r = lu.r; l_g = lu.g;
       lt = load_pos - lu.begin;
       lt_end = min(lu.prefix.steps, range_hi - lu.begin);
-      l_head = a.pages + (int64_t)lu.g * a.page_size * 136;
-      l_row = a.table + lu.r * a.table_stride;
-      ids_left = 0;
+      ids = 32;
       if (lt >= lt_end) {  // nothing of this unit to load
         if (kCluster) {
           lt = lt_end = 1;
           return;
         }
-        load_pos = lu.end + ((warp - (lu.end - range_lo)) & (kRowsWarps - 1));
+        load_pos = l_unit_end + ((warp - (l_unit_end - range_lo)) & (kRowsWarps - 1));
         lt = lt_end = 0;
       }
     }
-    if (ids_left == 0) {
-      const int ahead = lt + (lane >> log_pages) * kRowsWarps;
-      const int key = lu.prefix.key_step(ahead) * kKeys + ((lane & ((1 << log_pages) - 1)) << a.page_shift);
-      id = 0;
-      if (ahead < lt_end && key < lu.L) {
-        id = l_row[key >> a.page_shift];
-        if ((unsigned)id >= (unsigned)a.num_pages) {
+    if (ids == 32) {
+      const int ahead = lt + lane * kRowsWarps, key = (ahead < l_split ? ahead : ahead + l_gap) * kKeys;
+      id0 = id1 = 0;
+      if (ahead < lt_end) {
+        const int32_t* row = a.table + l_r * a.table_stride + (key >> a.page_shift);
+        id0 = row[0];
+        if (a.page_size == kGranule && key + kGranule < l_len) id1 = row[1];
+        if ((unsigned)id0 >= (unsigned)a.num_pages || (unsigned)id1 >= (unsigned)a.num_pages) {
           dev_flag(a.status, SEQ_DEV_BAD_PAGE);
-          id = 0;
+          if ((unsigned)id0 >= (unsigned)a.num_pages) id0 = 0;
+          if ((unsigned)id1 >= (unsigned)a.num_pages) id1 = 0;
         }
       }
-      ids_at = 0;
-      ids_left = 32 >> log_pages;
+      ids = 0;
     }
-    const int key = lu.prefix.key_step(lt) * kKeys;
-    const int pages = min(1 << log_pages, ((lu.L - key - 1) >> a.page_shift) + 1);
-    const int mine = __shfl_sync(0xffffffffu, id, ids_at + lane);
-    const uint32_t dst = ring + load_stage * kBytes, bar = bars + 8 * load_stage;
-    if (lane == 0) asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(pages * page_part) : "memory");
+    const int p0 = __shfl_sync(0xffffffffu, id0, ids), p1 = __shfl_sync(0xffffffffu, id1, ids);
+    if (lane == 0) {
+      const int key = (lt < l_split ? lt : lt + l_gap) * kKeys;
+      const uint32_t dst = ring + load_stage * kBytes, bar = bars + 8 * load_stage;
+      const uint8_t* head = a.pages + l_g * (a.page_size * 136);  // (1024 heads of 17408 bytes at most)
+      const bool all = a.page_size > kGranule || key + kGranule < l_len;
+      asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(all ? kBytes : kGranuleBytes) : "memory");
+      if (a.page_size > kGranule) {
+        bulk_load(dst, head + p0 * a.page_stride + (key & (a.page_size - 1)) * 136, kBytes, bar);
+      } else {
+        bulk_load(dst, head + p0 * a.page_stride, kGranuleBytes, bar);
+        if (all) bulk_load(dst + kGranuleBytes, head + p1 * a.page_stride, kGranuleBytes, bar);
+      }
+    }
     __syncwarp();
-    if (lane < pages) bulk_load(dst + lane * page_part, l_head + mine * a.page_stride + (key & (a.page_size - 1)) * 136, page_part, bar);
-    __syncwarp();
-    ids_at += 1 << log_pages;
-    --ids_left;
+    ++ids;
     ++loaded;
     load_stage = load_stage + 1 == kStages ? 0 : load_stage + 1;
     lt += kRowsWarps;
@@ -298,7 +300,6 @@ __global__ void __launch_bounds__(32 * kRowsWarps, NT == 1 ? 3 : 2) kv4_rows_ker
     float sq[NT][2];
     RowsState<NT> st;
     st.e = -1000;
-    int node[NT][2], begin[NT][2], depth[NT][2];
     int latest = 0;  // the last begin of a row's window
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
@@ -356,11 +357,11 @@ __global__ void __launch_bounds__(32 * kRowsWarps, NT == 1 ? 3 : 2) kv4_rows_ker
       for (int i = 0; i < 2; ++i) {
         sq[nt][i] = __shfl_sync(0xffffffffu, sum, (2 * t4 + i) * 4);
         st.rs[nt][i] = a.scale_log2 * __shfl_sync(0xffffffffu, inv_f, (2 * t4 + i) * 4);
-        const int rw = min(row0 + nt * 8 + 2 * t4 + i, a.rows - 1);
-        node[nt][i] = rw / a.group;
-        depth[nt][i] = a.window > 0 ? kv4_depth(a, u.r, node[nt][i]) : 0;
-        begin[nt][i] = a.window > 0 ? u.L + depth[nt][i] + 1 - a.window : 0;
-        latest = max(latest, begin[nt][i]);
+        if (a.window > 0) {  // (every warp finds the same)
+          const int begin = u.L + 1 - a.window + kv4_depth(a, u.r, min(row0 + nt * 8 + 2 * t4 + i, a.rows - 1) / a.group);
+          sm->begin[nt * 8 + 2 * t4 + i] = begin;
+          latest = max(latest, begin);
+        }
         st.m[nt][i] = kNoRef;
         st.l[nt][i] = st.pm[nt][i] = st.pr[nt][i] = 0.f;
       }
@@ -370,17 +371,16 @@ __global__ void __launch_bounds__(32 * kRowsWarps, NT == 1 ? 3 : 2) kv4_rows_ker
         for (int e2 = 0; e2 < 4; ++e2) st.o[nt][mt][e2] = 0.f;
     }
     latest = __reduce_max_sync(0xffffffffu, latest);
+    __syncwarp();
 
     int t = pos - u.begin + ((warp - (pos - range_lo)) & (kRowsWarps - 1));
     const int t_end = seg_end - u.begin;
     for (; t < min(u.prefix.steps, t_end); t += kRowsWarps) {
       if (ok) ok = mbar_wait(sm, &sm->full[warp][stage], phase, a.status);
       if (!ok) break;
-      const int step_key = u.prefix.key_step(t) * kKeys;
-#pragma unroll 1
-      for (int key0 = step_key; key0 < min(step_key + kKeys, u.L); key0 += 32) {
-      const uint32_t at = ring + stage * kBytes + (key0 - step_key) * 136;
-      const bool ends = key0 + 32 > u.L;
+      const int key0 = u.prefix.key_step(t) * kKeys;
+      const uint32_t at = ring + stage * kBytes;
+      const bool ends = key0 + kKeys > u.L;
       // the step's largest scale of V, a lane a key: the exponent of a half, rounded up (of zero and of subnormals: -14)
       uint32_t vp = lds32(at + (lane >> 4) * kGranuleBytes + kGranuleParams + kGranule * 4 + (lane & 15) * 4);
       if (ends && key0 + lane >= u.L) vp = 0u;
@@ -427,7 +427,7 @@ __global__ void __launch_bounds__(32 * kRowsWarps, NT == 1 ? 3 : 2) kv4_rows_ker
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
               for (int i = 0; i < 2; ++i)
-                if (j >= u.L || (j < begin[nt][i] && j >= a.sinks)) x[gr][nt][2 * v + i] = -INFINITY;
+                if (j >= u.L || (latest > 0 && j < sm->begin[nt * 8 + 2 * t4 + i] && j >= a.sinks)) x[gr][nt][2 * v + i] = -INFINITY;
           }
       }
       follow<2, NT>(x, y, e, st);
@@ -472,7 +472,6 @@ __global__ void __launch_bounds__(32 * kRowsWarps, NT == 1 ? 3 : 2) kv4_rows_ker
             for (int nt = 0; nt < NT; ++nt) mma16816(st.o[nt][4 * c + k], b[0][k], b[2][k], b[1][k], b[3][k], pf[gr][nt][0], pf[gr][nt][1]);
         }
       }
-      }
       __syncwarp();  // every lane has read the stage
       ++used;
       if (++stage == kStages) { stage = 0; phase ^= 1; }
@@ -488,35 +487,39 @@ __global__ void __launch_bounds__(32 * kRowsWarps, NT == 1 ? 3 : 2) kv4_rows_ker
 #pragma unroll 1
       for (int gr = 0; gr < 2 && 32 * w + 16 * gr < a.n; ++gr) {
         const int n0 = 32 * w + 16 * gr;
-        // everything is asked for before anything is used
         uint4 kx[2][4];
         uint2 vx[2][2][4];
 #pragma unroll
-        for (int z = 0; z < 2; ++z) {
-          const int j = n0 + g8 + 8 * z;
+        for (int z = 0; z < 2; ++z)
 #pragma unroll
           for (int c = 0; c < 4; ++c) {
+            const int j = n0 + g8 + 8 * z;
             kx[z][c] = make_uint4(0u, 0u, 0u, 0u);
             if (j < a.n) kx[z][c] = reinterpret_cast<const uint4*>(k_rows + j * a.t_tok)[4 * t4 + c];
           }
-          // V in pairs of rows (2 t4, 2 t4 + 1 and eight more), channels 4 * (8 c + g8) and the three behind
+        // V in pairs of rows (2 t4, 2 t4 + 1 and eight more), channels 4 * (8 c + g8) and the three behind.  A cluster asks for it before anything
+        // is used, where latency counts; the ranges do without the registers.
+        auto load_v = [&]() {
 #pragma unroll
-          for (int y = 0; y < 2; ++y) {
-            const int jv = n0 + 2 * t4 + 8 * z + y;
+          for (int z = 0; z < 2; ++z)
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
-              vx[z][y][c] = make_uint2(0u, 0u);
-              if (jv < a.n) vx[z][y][c] = reinterpret_cast<const uint2*>(v_rows + jv * a.t_tok)[8 * c + g8];
-            }
-          }
-        }
+            for (int y = 0; y < 2; ++y)
+#pragma unroll
+              for (int c = 0; c < 4; ++c) {
+                const int j = n0 + 2 * t4 + 8 * z + y;
+                vx[z][y][c] = make_uint2(0u, 0u);
+                if (j < a.n) vx[z][y][c] = reinterpret_cast<const uint2*>(v_rows + j * a.t_tok)[8 * c + g8];
+              }
+        };
+        if (kCluster) load_v();
         uint32_t seen[NT][2];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
-            const uint32_t bits = kv4_mask_word(a, kv4_mask_row(a, u.r, node[nt][i]), node[nt][i], w);
-            seen[nt][i] = kv4_window_word(a, u.r, u.L, depth[nt][i], w, bits);
+            const int node = min(row0 + nt * 8 + 2 * t4 + i, a.rows - 1) / a.group;
+            const uint32_t bits = kv4_mask_word(a, kv4_mask_row(a, u.r, node), node, w);
+            seen[nt][i] = kv4_window_word(a, u.r, u.L, a.window > 0 ? sm->begin[nt * 8 + 2 * t4 + i] + a.window - 1 - u.L : 0, w, bits);
           }
         float s[1][NT][4], y[1][NT][4];
 #pragma unroll
@@ -535,6 +538,7 @@ __global__ void __launch_bounds__(32 * kRowsWarps, NT == 1 ? 3 : 2) kv4_rows_ker
             mma16816(s[0][nt], f[0][2], f[1][2], f[0][3], f[1][3], qc[nt][4 * c + 2], hmul2_bits(qc[nt][4 * c + 3], 0x4c004c00u));
           }
         }
+        if (!kCluster) load_v();
         // A row of V with a value that is not finite in half precision counts as zeros, so that it stays out of the rows that do not see
         // it; those that do become NaN.
         uint32_t v[2][16], not_finite = 0;
@@ -784,7 +788,7 @@ int launch_kv4_rows(const seq_tree_kv4_attention_params& p, cudaStream_t stream)
     attr[1].val.clusterDim.x = a.cluster; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
     cfg.numAttrs = 2;
   } else {
-    const int64_t most = (int64_t)a.batch * a.Hkv * a.tiles * ((p.max_len + 63) / 64 + 1 + a.tree_steps);
+    const int64_t most = (int64_t)a.batch * a.Hkv * a.tiles * ((p.max_len + kKeys - 1) / kKeys + 1 + a.tree_steps);
     if (most > 0x7fffffff) return SEQ_ERR_UNSUPPORTED;
     const int64_t want = (most + a.min_steps - 1) / a.min_steps;
     a.ctas = want < rows_ctas(nt) ? (int)want : rows_ctas(nt);
@@ -806,12 +810,11 @@ int launch_kv4_rows(const seq_tree_kv4_attention_params& p, cudaStream_t stream)
     SEQ_CUDA_OK(cudaLaunchKernelEx(&cfg, kernel, a));
     return SEQ_OK;
   };
+  constexpr size_t s1 = sizeof(RowsSmem<1>), s2 = sizeof(RowsSmem<2>);
   if (a.cluster != 0) {
-    constexpr size_t s1 = sizeof(RowsSmem<1, true>), s2 = sizeof(RowsSmem<2, true>);
     if (nt == 1) return bf16 ? launch(kv4_rows_kernel<1, true, true>, 0, s1) : launch(kv4_rows_kernel<1, false, true>, 1, s1);
     return bf16 ? launch(kv4_rows_kernel<2, true, true>, 2, s2) : launch(kv4_rows_kernel<2, false, true>, 3, s2);
   }
-  constexpr size_t s1 = sizeof(RowsSmem<1, false>), s2 = sizeof(RowsSmem<2, false>);
   if (nt == 1) return bf16 ? launch(kv4_rows_kernel<1, true, false>, 4, s1) : launch(kv4_rows_kernel<1, false, false>, 5, s1);
   return bf16 ? launch(kv4_rows_kernel<2, true, false>, 6, s2) : launch(kv4_rows_kernel<2, false, false>, 7, s2);
 }
