@@ -587,8 +587,8 @@ int seq_tree_kv4_read(const seq_tree_kv4_append_params* p, void* stream);
  *   pages        device, 16-byte aligned (fork, compact): plane x of page p is page_bytes bytes (a multiple of 16) at
  *                p*page_stride_bytes + x*plane_stride_bytes, x < num_planes (a pool of all layers: one plane; a pool per
  *                layer: a plane each)
- *   workspace    seq_tree_pages_workspace_bytes(p) bytes, 16-byte aligned, device (fork, compact); contents undefined; two
- *                calls that can run at the same time need one each.
+ *   workspace    seq_tree_pages_workspace_bytes(p) bytes, 16-byte aligned, device; contents undefined; two calls that can run
+ *                at the same time need one each.
  * Table entries outside [0, num_pages) that a call meets raise SEQ_DEV_BAD_PAGE and count as no page (compact leaves -1); a
  * page_count outside [0, max_pages] raises SEQ_DEV_BAD_SLOT and the slot is left alone; a ref_count below what is
  * given up, or negative, raises SEQ_DEV_BAD_SLOT and counts as 0.  Returns SEQ_OK, SEQ_ERR_INVALID_ARG, SEQ_ERR_WORKSPACE or

@@ -672,7 +672,14 @@ def _pages_params(page_table, page_count, ref_count, page_size, table_out, count
     return p
 
 
-def _pages_pool(p, pool, planes: bool, workspace):
+def _pages_workspace(p, workspace, like):
+    if workspace is None:
+        workspace = like.new_empty(load().seq_tree_pages_workspace_bytes(C.byref(p)) // 4)
+    p.workspace, p.workspace_bytes = _dev(workspace, "workspace"), workspace.numel() * workspace.element_size()
+    return workspace  # (until the call is enqueued)
+
+
+def _pages_pool(p, pool, planes: bool):
     """pool [pages, ...] (planes: [planes, pages, ...]) of any type, a page contiguous."""
     if not planes:
         pool = pool.unsqueeze(0)
@@ -683,18 +690,15 @@ def _pages_pool(p, pool, planes: bool, workspace):
     p.pages, p.num_planes, p.page_bytes = _dev(pool, "pool"), pool.shape[0], one.numel() * e
     p.page_stride_bytes = pool.stride(1) * e if pool.shape[1] > 1 else p.page_bytes
     p.plane_stride_bytes = pool.stride(0) * e if pool.shape[0] > 1 else p.page_stride_bytes * p.num_pages
-    if workspace is None:
-        workspace = torch.empty(load().seq_tree_pages_workspace_bytes(C.byref(p)), dtype=torch.uint8, device=pool.device)
-    p.workspace, p.workspace_bytes = _dev(workspace, "workspace"), workspace.numel() * workspace.element_size()
-    return workspace
 
 
 def seq_tree_pages_resize(page_table, page_count, ref_count, tokens, page_size: int, *, table_out=None, count_out=None, refs_out=None,
-                          dev_status=None, stream=None):
+                          workspace=None, dev_status=None, stream=None):
     """Slot r holds ceil(tokens[r] / page_size) pages afterwards (0: freed, negative: left alone).  In place, or into
     table_out, count_out, refs_out (all of them)."""
     p = _pages_params(page_table, page_count, ref_count, page_size, table_out, count_out, refs_out, dev_status)
     p.tokens = _per_slot(tokens, p.slots, "tokens")
+    workspace = _pages_workspace(p, workspace, page_count)
     _check("seq_tree_pages_resize", load().seq_tree_pages_resize(C.byref(p), _stream(stream)))
 
 
@@ -705,7 +709,8 @@ def seq_tree_pages_fork(pool, page_table, page_count, ref_count, lengths, source
     p = _pages_params(page_table, page_count, ref_count, page_size, table_out, count_out, refs_out, dev_status)
     p.lengths, p.source = _per_slot(lengths, p.slots, "lengths"), _per_slot(source, p.slots, "source")
     p.lengths_out = p.lengths if lengths_out is None else _per_slot(lengths_out, p.slots, "lengths_out")
-    workspace = _pages_pool(p, pool, planes, workspace)
+    _pages_pool(p, pool, planes)
+    workspace = _pages_workspace(p, workspace, page_count)
     _check("seq_tree_pages_fork", load().seq_tree_pages_fork(C.byref(p), _stream(stream)))
 
 
@@ -715,7 +720,8 @@ def seq_tree_pages_compact(pool, page_table, page_count, ref_count, *, table_out
     many they are.  In place, or (tables and counts) into table_out, refs_out."""
     p = _pages_params(page_table, page_count, ref_count, 1, table_out, None, refs_out, dev_status)
     p.live = _dev(live, "live", torch.int32)
-    workspace = _pages_pool(p, pool, planes, workspace)
+    _pages_pool(p, pool, planes)
+    workspace = _pages_workspace(p, workspace, page_count)
     _check("seq_tree_pages_compact", load().seq_tree_pages_compact(C.byref(p), _stream(stream)))
 
 

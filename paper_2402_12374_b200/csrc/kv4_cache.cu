@@ -1,8 +1,9 @@
 // seq_tree_kv4_append, seq_tree_kv4_read: rows of 16 bits to and from the 4-bit pages (the format: include/seq_tree.h).
 //
-// Half a warp has a row (128 channels, 16 bytes a lane): minimum and maximum by four shuffles, the codes of a lane's eight
-// channels are one 32-bit word, the row's 64 bytes one store.  A half-warp walks 16 consecutive rows of one (layer, request,
-// kv head, K or V), four of them in flight, with the 16 page numbers (and path entries) looked up at once, a lane each.
+// Half a warp has a row (128 channels, 16 bytes a lane): its maximum and minimum as one packed pair (max, -min) by four shuffles, the
+// codes of a lane's eight channels are one 32-bit word, the row's 64 bytes one store.  A half-warp walks 16 consecutive rows of
+// one (layer, request, kv head, K or V) with the 16 page numbers (and path entries) looked up at once, a lane each; the append has
+// four rows in flight, the read, whose loads are smaller, eight.
 // Bound by HBM for prompts, by latency for paths.  Blocks are in the order (16-row chunk, layer, request, heads), so those behind a
 // request's count, which have nothing to do, come last.
 #include "kv4.cuh"
@@ -11,7 +12,6 @@ namespace seqtree {
 
 constexpr int kRowThreads = 256;
 constexpr int kChunkRows = 16;
-constexpr int kRowsInFlight = 4;
 constexpr float kLargest = 65504.f;  // of half precision
 
 struct RowsArgs {
@@ -41,26 +41,51 @@ __device__ __forceinline__ void widen8(uint4 x, float* v) {
   }
 }
 
-// The eight codes of a lane's channels.  Quotients are taken as products with the reciprocal (off by less than 2e-6 at +-8);
-// one that lies so near the middle between two codes that this could decide is divided.
+// (a, b) -> (max, max), NaN if either is one
+template <typename T>
+__device__ __forceinline__ uint32_t max_pair(uint32_t a, uint32_t b) {
+  uint32_t d;
+  if (std::is_same<T, __nv_bfloat16>::value) asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+  else asm("max.NaN.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+  return d;
+}
+// The largest of a lane's eight channels and the largest of their negatives, as a pair
+template <typename T>
+__device__ __forceinline__ uint32_t extremes(uint4 x) {
+  const uint32_t hi = max_pair<T>(max_pair<T>(x.x, x.y), max_pair<T>(x.z, x.w));
+  const uint32_t n = 0x80008000u;
+  const uint32_t lo = max_pair<T>(max_pair<T>(x.x ^ n, x.y ^ n), max_pair<T>(x.z ^ n, x.w ^ n));
+  return max_pair<T>(__byte_perm(hi, lo, 0x5410), __byte_perm(hi, lo, 0x7632));
+}
+
+// The eight codes of a lane's channels.  Quotients are taken as products with the reciprocal (off by less than 3e-6 at +-8); where
+// one lies so near the middle between two codes that this could decide, they are divided.
 __device__ __forceinline__ uint32_t quantise8(const float* v, float scale, float mid) {
-  const float inv = scale > 0.f ? __fdiv_rn(1.f, scale) : 0.f;
-  uint32_t word = 0;
-  bool near = false;
-  float y[8];
+  constexpr float kMagic = 12582920.f;  // 1.5 * 2^23 + 8: adding it rounds to a whole number, even in the middle, 8 more in the last bits
+  float inv;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(scale));
+  inv = scale > 0.f ? inv : 0.f;
+  float off = 0.f;
+  float c[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    y[i] = fminf(fmaxf((v[i] - mid) * inv, -8.f), 7.f);
-    const float r = (y[i] + 12582920.f) - 12582920.f;  // to the nearest whole number, even in the middle (1.5 * 2^23 + 8)
-    near |= fabsf(y[i] - r) > 0.499995f;
+    const float d = v[i] - mid;
+    c[i] = fmaf(d, inv, kMagic);
+    off = fmaxf(off, fabsf(fmaf(d, inv, kMagic - c[i])));
+    c[i] = fminf(fmaxf(c[i], kMagic - 8.f), kMagic + 7.f);
   }
-  if (near) {
+  if (off > 0.499995f) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) y[i] = scale > 0.f ? fminf(fmaxf(__fdiv_rn(v[i] - mid, scale), -8.f), 7.f) : 0.f;
+    for (int i = 0; i < 8; ++i) c[i] = fminf(fmaxf(scale > 0.f ? __fdiv_rn(v[i] - mid, scale) : 0.f, -8.f), 7.f) + kMagic;
   }
+  // the last bits of each, four apart; what else the numbers hold is the same and taken off
+  uint32_t word = 0, rest = 0;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) word |= (__float_as_uint(y[i] + 12582920.f) & 15u) << (4 * i);
-  return word;
+  for (int i = 7; i >= 0; --i) {
+    word = word * 16u + __float_as_uint(c[i]);
+    rest = rest * 16u + 0x4b400000u;
+  }
+  return word - rest;
 }
 
 // How many rows of request r there are; -1: none, for a reason that is told once per call
@@ -121,6 +146,7 @@ __global__ void __launch_bounds__(kRowThreads) kv4_rows_copy_kernel(const RowsAr
   const uint8_t* rows = (which ? a.v : a.k) + l * a.s_layer + r * a.s_req + g * a.s_head + 16 * lane;
   uint8_t* pool = a.pages + l * a.layer_stride + (int64_t)g * a.page_size * 136;
   const int rows_here = min(kChunkRows, m - i0);
+  constexpr int kRowsInFlight = kAppend ? 4 : 8;
   for (int j0 = 0; j0 < rows_here; j0 += kRowsInFlight) {
     uint4 x[kRowsInFlight];
     uint8_t* at[kRowsInFlight];  // the row's codes; the row's (scale, mid) at `params`
@@ -147,20 +173,19 @@ __global__ void __launch_bounds__(kRowThreads) kv4_rows_copy_kernel(const RowsAr
       if (kAppend) {
         float v[8];
         widen8<T>(x[u], v);
-        bool fine = true;
-        float lo = v[0], hi = v[0];
+        uint32_t both = extremes<T>(x[u]);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          fine &= fabsf(v[i]) <= kLargest;  // (false for a NaN)
-          lo = fminf(lo, v[i]);
-          hi = fmaxf(hi, v[i]);
+        for (int o = 8; o > 0; o >>= 1) both = max_pair<T>(both, __shfl_xor_sync(half, both, o, 16));
+        float hi, lo;
+        if (std::is_same<T, __nv_bfloat16>::value) {
+          hi = __uint_as_float(both << 16);
+          lo = -__uint_as_float(both & 0xffff0000u);
+        } else {
+          const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&both));
+          hi = f.x;
+          lo = -f.y;
         }
-#pragma unroll
-        for (int o = 8; o > 0; o >>= 1) {
-          lo = fminf(lo, __shfl_xor_sync(half, lo, o, 16));
-          hi = fmaxf(hi, __shfl_xor_sync(half, hi, o, 16));
-        }
-        fine = __all_sync(half, fine);
+        const bool fine = fabsf(hi) <= kLargest && fabsf(lo) <= kLargest;  // (false for a NaN)
         // halves, so that the difference cannot overflow; it is exact in fp32 but for magnitudes far apart
         __half2 sm = __floats2half2_rn(__fdiv_rn(hi * 0.5f - lo * 0.5f, 7.5f), 0.f);
         sm.y = __float2half_rn(__low2float(sm) * 8.f + lo);

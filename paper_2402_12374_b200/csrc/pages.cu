@@ -1,7 +1,7 @@
 // seq_tree_pages_resize, _fork, _compact: the page tables of a paged cache (include/seq_tree.h states what they do).
 //
-// Which page goes where is a chain of counts over all slots and all pages, so one cluster of 16 CTAs plans a call: each CTA
-// owns a sixteenth of the pages, counts its free (or held) ones, reads the other CTAs' counts from their shared memory, and
+// Which page goes where is a chain of counts over all slots and all pages, so one cluster of up to 16 CTAs plans a call: each CTA
+// owns a share of the pages, counts its free (or held) ones, reads the other CTAs' counts from their shared memory, and
 // from then on knows the number of every page in its share among all of them.  No order of atomics enters a result: counts
 // are sums, and a page's rank says who gets it.  What is only moved - rows of the table, contents of pages - goes over the
 // whole device: further clusters of the planning launch copy the table's rows, a second launch behind it the pages.
@@ -10,9 +10,11 @@
 
 namespace seqtree {
 
-constexpr int kPlanCtas = 16;
+constexpr int kPlanCtas = 16;           // CTAs that plan, at most
+constexpr int kPagesPerCta = 4096;      // ... one for each so many pages
 constexpr int kPlanThreads = 1024;
 constexpr int kMoveThreads = 256;
+constexpr int kInFlight = 16;  // loads of a lane before the first is used
 constexpr int kSlotsPerThread = SEQ_MAX_SLOTS / kPlanThreads;
 
 struct PagesArgs {
@@ -23,13 +25,18 @@ struct PagesArgs {
   int32_t* count_out; int32_t* refs_out; int32_t* lengths_out;
   const int32_t* tokens; const int32_t* source;
   int32_t* live;
-  int32_t* ws;  // fork, compact: [0] how many pages move, then from[], to[] (fork: slots each, compact: num_pages each), map[num_pages] (compact)
+  int32_t* ws;  // resize: free pages in order; fork, compact: [0] how many pages move, then from[], to[] (fork: slots each, compact: num_pages each), map[num_pages] (compact)
   int32_t* status;
 };
 
 __device__ __forceinline__ uint32_t cluster_rank() {
   uint32_t r;
   asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ uint32_t cluster_size() {
+  uint32_t r;
+  asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
   return r;
 }
 // Also orders the CTAs' global memory accesses: what one wrote before it, every other one reads behind it.
@@ -47,7 +54,7 @@ __device__ __forceinline__ int peer_word(const int* p, uint32_t cta) {
 struct PlanSmem {
   int32_t before[SEQ_MAX_SLOTS + 1];  // pages that the slots before need
   int32_t source[SEQ_MAX_SLOTS];      // fork: a slot's source, -1 for none, and the source's length
-  int32_t length[SEQ_MAX_SLOTS];
+  int32_t length[SEQ_MAX_SLOTS];      // (resize: the pages a slot holds)
   int32_t warp_sum[kPlanThreads / 32];
   int32_t total;
   int32_t mine;  // what this CTA counted; read by the others
@@ -86,7 +93,7 @@ __device__ __forceinline__ void cluster_count(PlanSmem* sm, uint32_t rank, int m
   if (threadIdx.x == 0) sm->mine = mine;
   cluster_sync();
   if (threadIdx.x < 32) {
-    const int v = threadIdx.x < kPlanCtas ? peer_word(&sm->mine, threadIdx.x) : 0;
+    const int v = threadIdx.x < cluster_size() ? peer_word(&sm->mine, threadIdx.x) : 0;
     const int before = __reduce_add_sync(0xffffffffu, threadIdx.x < rank ? v : 0);
     const int all = __reduce_add_sync(0xffffffffu, v);
     if (threadIdx.x == 0) { sm->base = before; sm->all = all; }
@@ -109,7 +116,7 @@ __device__ __forceinline__ int ceil_pages(int tokens, int page_size) { return to
 // One CTA's share of the pages, a multiple of four (16-byte loads; only the last share's end is ragged)
 struct Share { int lo, hi; };
 __device__ __forceinline__ Share share_of(int num_pages, uint32_t rank) {
-  const int per = ((num_pages + kPlanCtas - 1) / kPlanCtas + 3) & ~3;
+  const int ctas = cluster_size(), per = ((num_pages + ctas - 1) / ctas + 3) & ~3;
   const int64_t lo = (int64_t)per * rank;
   return {(int)min(lo, (int64_t)num_pages), (int)min(lo + per, (int64_t)num_pages)};
 }
@@ -152,8 +159,8 @@ __device__ __forceinline__ int fork_source(const PagesArgs& a, int r, bool tell)
 template <int kMode>
 __device__ void copy_rows(const PagesArgs& a) {
   const int lane = threadIdx.x & 31;
-  const int warps = (gridDim.x - kPlanCtas) * (kPlanThreads / 32);
-  for (int r = (blockIdx.x - kPlanCtas) * (kPlanThreads / 32) + (threadIdx.x >> 5); r < a.slots; r += warps) {
+  const int ctas = gridDim.x - cluster_size(), cta = blockIdx.x - cluster_size();  // (a slot's neighbours go to other CTAs)
+  for (int r = (threadIdx.x >> 5) * ctas + cta; r < a.slots; r += ctas * (kPlanThreads / 32)) {
     int have, want;
     if (kMode == 0) {
       wanted_of(a, r, have, want, false);
@@ -164,8 +171,14 @@ __device__ void copy_rows(const PagesArgs& a) {
     const int keep = min(have, want), end = max(have, want);
     const int32_t* from = a.table + r * a.table_stride;
     int32_t* to = a.table_out + r * a.table_out_stride;
-#pragma unroll 8
-    for (int i = lane; i < keep; i += 32) to[i] = from[i];
+    for (int i0 = lane; i0 < keep; i0 += 32 * kInFlight) {
+      int v[kInFlight];
+#pragma unroll
+      for (int y = 0; y < kInFlight; ++y) v[y] = i0 + 32 * y < keep ? from[i0 + 32 * y] : 0;
+#pragma unroll
+      for (int y = 0; y < kInFlight; ++y)
+        if (i0 + 32 * y < keep) to[i0 + 32 * y] = v[y];
+    }
     for (int i = end + lane; i < a.max_pages; i += 32) to[i] = -1;
   }
 }
@@ -177,31 +190,96 @@ __device__ __forceinline__ void copy_refs(const PagesArgs& a, Share s) {
     const int n4 = (s.hi - s.lo) >> 2;
     const int4* from = reinterpret_cast<const int4*>(a.refs + s.lo);
     int4* to = reinterpret_cast<int4*>(a.refs_out + s.lo);
-#pragma unroll 4
-    for (int i = threadIdx.x; i < n4; i += kPlanThreads) to[i] = from[i];
+    for (int i0 = threadIdx.x; i0 < n4; i0 += 8 * kPlanThreads) {
+      int4 v[8];
+#pragma unroll
+      for (int y = 0; y < 8; ++y)
+        if (i0 + y * kPlanThreads < n4) v[y] = from[i0 + y * kPlanThreads];
+#pragma unroll
+      for (int y = 0; y < 8; ++y)
+        if (i0 + y * kPlanThreads < n4) to[i0 + y * kPlanThreads] = v[y];
+    }
     for (int i = s.lo + 4 * n4 + threadIdx.x; i < s.hi; i += kPlanThreads) a.refs_out[i] = a.refs[i];
   } else {
     for (int i = s.lo + threadIdx.x; i < s.hi; i += kPlanThreads) a.refs_out[i] = a.refs[i];
   }
 }
 
-// Calls take(rank, page) for the pages of this CTA's share with free(refs_out[page]), in order, until `limit` of all CTAs'
-// are told.  The threads' pages are neighbours, so that a scan of their counts numbers them.
-template <typename Free, typename Take>
-__device__ __forceinline__ void number_pages(PlanSmem* sm, uint32_t rank, Share s, const int32_t* refs, int limit_or_all, Free is_free, Take take, int& total) {
-  int mine = 0;
-  for (int i = s.lo + threadIdx.x; i < s.hi; i += kPlanThreads) mine += is_free(__ldcg(refs + i));
-  block_scan(sm, mine);
+// Calls visit(i, v) for a warp's run of pages [lo, hi): a lane has four neighbours i .. i + 3 at a time (i >= hi
+// for lanes behind the end), v their counts.  Four loads of a lane are in flight before the first is used.
+template <typename Visit>
+__device__ __forceinline__ void for_run(const int32_t* refs, int lo, int hi, Visit visit) {
+  constexpr int kBatch = 4;
+  const int lane = threadIdx.x & 31;
+  const bool aligned = ((reinterpret_cast<uintptr_t>(refs) | (uintptr_t)lo << 2) & 15) == 0;  // (i - lo is a multiple of four)
+  for (int i0 = lo; i0 < hi; i0 += 128 * kBatch) {
+    int4 v[kBatch];
+#pragma unroll
+    for (int y = 0; y < kBatch; ++y) {
+      const int i = i0 + 128 * y + 4 * lane;
+      v[y] = make_int4(0, 0, 0, 0);
+      if (aligned && i + 4 <= hi) {
+        v[y] = __ldcg(reinterpret_cast<const int4*>(refs + i));
+      } else {
+        if (i < hi) v[y].x = __ldcg(refs + i);
+        if (i + 1 < hi) v[y].y = __ldcg(refs + i + 1);
+        if (i + 2 < hi) v[y].z = __ldcg(refs + i + 2);
+        if (i + 3 < hi) v[y].w = __ldcg(refs + i + 3);
+      }
+    }
+#pragma unroll
+    for (int y = 0; y < kBatch; ++y)
+      if (i0 + 128 * y < hi) visit(i0 + 128 * y + 4 * lane, v[y]);
+  }
+}
+
+// Calls take(number, page) for the pages of this CTA's share that chosen(page, refs[page]) holds for: their numbers among all CTAs',
+// in order, below `limit`.  A warp has a run of neighbours; a lane's pages, four at a time, have numbers in a row.
+template <typename Chosen, typename Take>
+__device__ __forceinline__ void number_pages(PlanSmem* sm, uint32_t rank, Share s, const int32_t* refs, int limit, Chosen chosen, Take take, int& total) {
+  const int warps = kPlanThreads / 32, lane = threadIdx.x & 31;
+  const int per = ((s.hi - s.lo + warps - 1) / warps + 3) & ~3;
+  const int lo = min(s.lo + (int)(threadIdx.x >> 5) * per, s.hi), hi = min(lo + per, s.hi);
+  auto bits = [&](int i, int4 v) -> int {
+    return (int)(i < hi && chosen(i, v.x)) | (int)(i + 1 < hi && chosen(i + 1, v.y)) << 1 | (int)(i + 2 < hi && chosen(i + 2, v.z)) << 2 |
+           (int)(i + 3 < hi && chosen(i + 3, v.w)) << 3;
+  };
+  // (what was chosen is kept where 64 bits hold it: up to 2048 pages a warp)
+  int mine = 0, turn = 0;
+  uint64_t kept = 0;
+  for_run(refs, lo, hi, [&](int i, int4 v) {
+    const int b = bits(i, v);
+    mine += __popc(b);
+    kept |= turn < 16 ? (uint64_t)b << (4 * turn) : 0ull;
+    ++turn;
+  });
+  const int before = block_scan(sm, mine);
   cluster_count(sm, rank, sm->total);
   total = sm->all;
-  const int limit = min(limit_or_all, total);
-  int base = sm->base;
-  for (int i0 = s.lo; i0 < s.hi && base < limit; i0 += kPlanThreads) {
-    const int i = i0 + threadIdx.x;
-    const int f = i < s.hi && is_free(__ldcg(refs + i));
-    const int at = base + block_scan(sm, f);
-    if (f && at < limit) take(at, i);
-    base += sm->total;
+  int at = sm->base + __shfl_sync(0xffffffffu, before, 0);  // of the warp's first page
+  const int found = __reduce_add_sync(0xffffffffu, mine);
+  if (found == 0 || at >= limit) return;
+  auto number = [&](int i, int b) {
+    const int n = __popc(b);
+    int incl = n;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const int u = __shfl_up_sync(0xffffffffu, incl, d);
+      if (lane >= d) incl += u;
+    }
+    int k = at + incl - n;
+    at += __shfl_sync(0xffffffffu, incl, 31);
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if ((b >> e) & 1) {
+        if (k < limit) take(k, i + e);
+        ++k;
+      }
+  };
+  if (turn <= 16) {
+    for (int y = 0; y < turn; ++y) number(lo + 128 * y + 4 * lane, (int)(kept >> (4 * y)) & 15);
+  } else {
+    for_run(refs, lo, hi, [&](int i, int4 v) { number(i, bits(i, v)); });
   }
 }
 
@@ -210,7 +288,7 @@ __global__ void __launch_bounds__(kPlanThreads, 1) pages_resize_kernel(const Pag
   PlanSmem* sm = &smem;
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  if (blockIdx.x >= kPlanCtas) {
+  if (blockIdx.x >= cluster_size()) {
     copy_rows<0>(a);
     return;
   }
@@ -221,14 +299,23 @@ __global__ void __launch_bounds__(kPlanThreads, 1) pages_resize_kernel(const Pag
 
   // What is given up.  A warp a slot.
   const int lane = threadIdx.x & 31;
-  for (int r = rank * (kPlanThreads / 32) + (threadIdx.x >> 5); r < a.slots; r += kPlanCtas * (kPlanThreads / 32)) {
+  const uint32_t ctas = cluster_size();
+  for (int r = (threadIdx.x >> 5) * ctas + rank; r < a.slots; r += ctas * (kPlanThreads / 32)) {
     int have, want;
     wanted_of(a, r, have, want, lane == 0);
-    for (int i = want + lane; i < have; i += 32) {
-      const int page = a.table[r * a.table_stride + i];
-      a.table_out[r * a.table_out_stride + i] = -1;
-      if (page < 0 || page >= a.num_pages) dev_flag(a.status, SEQ_DEV_BAD_PAGE);
-      else atomicSub(a.refs_out + page, 1);
+    const int32_t* row = a.table + r * a.table_stride;
+    int32_t* out = a.table_out + r * a.table_out_stride;
+    for (int i0 = want + lane; i0 < have; i0 += 32 * kInFlight) {
+      int page[kInFlight];
+#pragma unroll
+      for (int y = 0; y < kInFlight; ++y) page[y] = i0 + 32 * y < have ? row[i0 + 32 * y] : 0;
+#pragma unroll
+      for (int y = 0; y < kInFlight; ++y) {
+        if (i0 + 32 * y >= have) break;
+        out[i0 + 32 * y] = -1;
+        if (page[y] < 0 || page[y] >= a.num_pages) dev_flag(a.status, SEQ_DEV_BAD_PAGE);
+        else atomicSub(a.refs_out + page[y], 1);
+      }
     }
   }
   // Meanwhile, every CTA for itself: how many pages the slots before each one need
@@ -241,6 +328,7 @@ __global__ void __launch_bounds__(kPlanThreads, 1) pages_resize_kernel(const Pag
     if (first + j < a.slots) {
       wanted_of(a, first + j, have, want, false);
       need[j] = max(want - have, 0);
+      sm->length[first + j] = have;  // (kept: in place, the counts change below)
     }
     sum += need[j];
   }
@@ -253,27 +341,27 @@ __global__ void __launch_bounds__(kPlanThreads, 1) pages_resize_kernel(const Pag
   if (threadIdx.x == 0) sm->before[a.slots] = sm->total;
   cluster_sync();
 
-  // a reference too many was given up
-  for (int i = share.lo + threadIdx.x; i < share.hi; i += kPlanThreads)
-    if (__ldcg(a.refs_out + i) < 0) {
-      dev_flag(a.status, SEQ_DEV_BAD_SLOT);
-      a.refs_out[i] = 0;
-    }
-  __syncthreads();
-
   // The free pages, lowest first: number k goes to the slot whose growth holds it, if that fits as a whole.
   const int needed = sm->before[a.slots];
   int free_pages = 0;
-  const auto give = [&](int k, int page) {
-    const int r = slot_of(sm, a.slots, k);
-    if (sm->before[r + 1] > sm->all) return;
-    a.table_out[r * a.table_out_stride + a.count[r] + k - sm->before[r]] = page;
-    a.refs_out[page] = 1;
+  const auto is_free = [&](int page, int v) -> bool {
+    if (v < 0) {  // a reference too many was given up
+      dev_flag(a.status, SEQ_DEV_BAD_SLOT);
+      a.refs_out[page] = 0;
+    }
+    return v <= 0;
   };
-  number_pages(sm, rank, share, a.refs_out, needed, [](int v) { return v <= 0; }, give, free_pages);
-  cluster_sync();  // nobody looks at an old count any more (in place they are overwritten now)
+  number_pages(sm, rank, share, a.refs_out, needed, is_free, [&](int k, int page) { a.ws[k] = page; }, free_pages);
+  cluster_sync();  // the list is there
+  for (int k = rank * kPlanThreads + threadIdx.x; k < min(needed, free_pages); k += ctas * kPlanThreads) {
+    const int r = slot_of(sm, a.slots, k);
+    if (sm->before[r + 1] > free_pages) continue;
+    const int page = __ldcg(a.ws + k);
+    a.table_out[r * a.table_out_stride + sm->length[r] + k - sm->before[r]] = page;
+    a.refs_out[page] = 1;
+  }
   // the slots' counts, and what is not there for those that do not grow
-  for (int r = rank * kPlanThreads + threadIdx.x; r < a.slots; r += kPlanCtas * kPlanThreads) {
+  for (int r = rank * kPlanThreads + threadIdx.x; r < a.slots; r += ctas * kPlanThreads) {
     int have, want;
     const bool sound = wanted_of(a, r, have, want, false);
     const bool grows = want > have;
@@ -292,7 +380,7 @@ __global__ void __launch_bounds__(kPlanThreads, 1) pages_fork_kernel(const Pages
   PlanSmem* sm = &smem;
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  if (blockIdx.x >= kPlanCtas) {
+  if (blockIdx.x >= cluster_size()) {
     copy_rows<1>(a);
     return;
   }
@@ -336,30 +424,35 @@ __global__ void __launch_bounds__(kPlanThreads, 1) pages_fork_kernel(const Pages
     to[k] = page;
     a.table_out[r * a.table_out_stride + full] = page;
   };
-  number_pages(sm, rank, share, a.refs_out, needed, [](int v) { return v <= 0; }, give, free_pages);
+  number_pages(sm, rank, share, a.refs_out, needed, [](int, int v) { return v <= 0; }, give, free_pages);
   const int given = min(needed, free_pages);
   if (rank == 0 && threadIdx.x == 0) a.ws[0] = given;
   cluster_sync();  // every free page is numbered: from here on counts change
-  for (int k = rank * kPlanThreads + threadIdx.x; k < given; k += kPlanCtas * kPlanThreads) a.refs_out[__ldcg(to + k)] = 1;
+  const uint32_t ctas = cluster_size();
+  for (int k = rank * kPlanThreads + threadIdx.x; k < given; k += ctas * kPlanThreads) a.refs_out[__ldcg(to + k)] = 1;
   // The forks' rows, a warp each
   const int lane = threadIdx.x & 31;
-  for (int r = rank * (kPlanThreads / 32) + (threadIdx.x >> 5); r < a.slots; r += kPlanCtas * (kPlanThreads / 32)) {
+  for (int r = (threadIdx.x >> 5) * ctas + rank; r < a.slots; r += ctas * (kPlanThreads / 32)) {
     const int s = sm->source[r], n = sm->length[r];
     const bool copied = sm->before[r + 1] > sm->before[r];
     const bool fits = s >= 0 && (!copied || sm->before[r + 1] <= free_pages);
     if (s >= 0) {
       const int full = fits ? n / a.page_size : 0, held = fits ? full + copied : 0;
       int32_t* row = a.table_out + r * a.table_out_stride;
-      for (int i = lane; i < a.max_pages; i += 32) {
-        if (i < full) {
-          const int page = a.table[s * a.table_stride + i];
-          row[i] = page;
-          if (page < 0 || page >= a.num_pages) dev_flag(a.status, SEQ_DEV_BAD_PAGE);
-          else atomicAdd(a.refs_out + page, 1);
-        } else if (i >= held) {
-          row[i] = -1;
+      const int32_t* from_row = a.table + s * a.table_stride;
+      for (int i0 = lane; i0 < full; i0 += 32 * kInFlight) {
+        int page[kInFlight];
+#pragma unroll
+        for (int y = 0; y < kInFlight; ++y) page[y] = i0 + 32 * y < full ? from_row[i0 + 32 * y] : 0;
+#pragma unroll
+        for (int y = 0; y < kInFlight; ++y) {
+          if (i0 + 32 * y >= full) break;
+          row[i0 + 32 * y] = page[y];
+          if (page[y] < 0 || page[y] >= a.num_pages) dev_flag(a.status, SEQ_DEV_BAD_PAGE);
+          else atomicAdd(a.refs_out + page[y], 1);
         }
       }
+      for (int i = held + lane; i < a.max_pages; i += 32) row[i] = -1;
       if (!fits && lane == 0) dev_flag(a.status, SEQ_DEV_NO_PAGES);
       if (lane == 0) {
         if (fits || a.count_out != a.count) a.count_out[r] = held;
@@ -395,8 +488,8 @@ __global__ void __launch_bounds__(kPlanThreads, 1) pages_compact_kernel(const Pa
   // far = held pages from `live` on, holes = free ones below it: as many of the one as of the other
   const Share below = {min(share.lo, live), min(share.hi, live)}, above = {max(share.lo, live), max(share.hi, live)};
   int holes = 0, far = 0;
-  number_pages(sm, rank, below, a.refs, 0x7fffffff, [](int v) { return v <= 0; }, [&](int k, int page) { to[k] = page; }, holes);
-  number_pages(sm, rank, above, a.refs, 0x7fffffff, [](int v) { return v > 0; }, [&](int k, int page) { from[k] = page; }, far);
+  number_pages(sm, rank, share, a.refs, 0x7fffffff, [&](int page, int v) { return page < live && v <= 0; }, [&](int k, int page) { to[k] = page; }, holes);
+  number_pages(sm, rank, share, a.refs, 0x7fffffff, [&](int page, int v) { return page >= live && v > 0; }, [&](int k, int page) { from[k] = page; }, far);
   if (rank == 0 && threadIdx.x == 0) {
     a.ws[0] = far;
     if (a.live != nullptr) *a.live = live;
@@ -415,7 +508,7 @@ __global__ void __launch_bounds__(kPlanThreads, 1) pages_compact_kernel(const Pa
       if (a.refs_out != a.refs || a.refs[i] < 0) a.refs_out[i] = 0;
     }
   cluster_sync();  // (in place: what is moved below was free above)
-  for (int k = rank * kPlanThreads + threadIdx.x; k < far; k += kPlanCtas * kPlanThreads) {
+  for (int k = rank * kPlanThreads + threadIdx.x; k < far; k += cluster_size() * kPlanThreads) {
     const int p = __ldcg(from + k), q = __ldcg(to + k);
     const int v = a.refs[p];
     map[p] = q;
@@ -504,9 +597,11 @@ static int check_pool(const seq_tree_pages_params* p) {
   if (p->page_bytes < 16 || p->page_bytes % 16 != 0 || p->page_stride_bytes < p->page_bytes || p->page_stride_bytes % 16 != 0) return SEQ_ERR_INVALID_ARG;
   if (p->num_planes > 1 && (p->plane_stride_bytes < p->page_bytes || p->plane_stride_bytes % 16 != 0)) return SEQ_ERR_INVALID_ARG;
   if (p->page_bytes / kMoveChunk > (1 << 24)) return SEQ_ERR_INVALID_ARG;
-  if (p->workspace == nullptr || p->workspace_bytes < seq_tree_pages_workspace_bytes(p)) return SEQ_ERR_WORKSPACE;
-  if (reinterpret_cast<uintptr_t>(p->workspace) % 16 != 0) return SEQ_ERR_INVALID_ARG;
   return SEQ_OK;
+}
+static int check_workspace(const seq_tree_pages_params* p) {
+  if (p->workspace == nullptr || p->workspace_bytes < seq_tree_pages_workspace_bytes(p)) return SEQ_ERR_WORKSPACE;
+  return reinterpret_cast<uintptr_t>(p->workspace) % 16 != 0 ? SEQ_ERR_INVALID_ARG : SEQ_OK;
 }
 
 static PagesArgs pages_args(const seq_tree_pages_params* p) {
@@ -527,19 +622,23 @@ static int launch_plan(Kernel kernel, int* done, const seq_tree_pages_params* p,
     return SEQ_OK;
   });
   if (rc != SEQ_OK) return rc;
-  // clusters that copy the table: one for every 64 Ki entries, no more than there is room for beside the plan
+  // A cluster plans: a CTA for every kPagesPerCta pages or table entries (exchanges between CTAs cost more than a few loads), a power of two.
+  int ctas = 1;
+  const int64_t entries = (int64_t)p->slots * p->max_pages;
+  while (ctas < kPlanCtas && (int64_t)ctas * kPagesPerCta < (p->num_pages > entries ? p->num_pages : entries)) ctas *= 2;
+  // CTAs that copy the table, in clusters of the same size: one for every 8 Ki entries, up to 96
   int copiers = 0;
   if (rows_are_copied) {
-    const int64_t want = ((int64_t)p->slots * p->max_pages + 65535) / 65536;
-    copiers = (int)(want < 6 ? want : 6);
+    const int64_t want = (entries + 8191) / 8192;
+    copiers = (int)((want < 96 ? want : 96) + ctas - 1) / ctas;
   }
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(kPlanCtas * (1 + copiers));
+  cfg.gridDim = dim3(ctas * (1 + copiers));
   cfg.blockDim = dim3(kPlanThreads);
   cfg.stream = static_cast<cudaStream_t>(stream);
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = kPlanCtas; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+  attr[0].val.clusterDim.x = ctas; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
   attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
@@ -585,10 +684,12 @@ extern "C" size_t seq_tree_pages_workspace_bytes(const seq_tree_pages_params* p)
 }
 
 extern "C" int seq_tree_pages_resize(const seq_tree_pages_params* p, void* stream) {
-  const int rc = check_pages(p);
+  int rc = check_pages(p);
   if (rc != SEQ_OK) return rc;
   if (p->tokens == nullptr || p->count_out == nullptr || p->page_size < 1) return SEQ_ERR_INVALID_ARG;
   if ((p->count_out == p->page_count) != (p->table_out == p->page_table)) return SEQ_ERR_INVALID_ARG;
+  rc = check_workspace(p);
+  if (rc != SEQ_OK) return rc;
   static int done[64];
   return launch_plan(pages_resize_kernel, done, p, p->table_out != p->page_table, stream);
 }
@@ -600,6 +701,7 @@ extern "C" int seq_tree_pages_fork(const seq_tree_pages_params* p, void* stream)
   const bool in_place = p->table_out == p->page_table;
   if ((p->count_out == p->page_count) != in_place || (p->lengths_out == p->lengths) != in_place) return SEQ_ERR_INVALID_ARG;
   rc = check_pool(p);
+  if (rc == SEQ_OK) rc = check_workspace(p);
   if (rc != SEQ_OK) return rc;
   static int done[64];
   rc = launch_plan(pages_fork_kernel, done, p, p->table_out != p->page_table, stream);
@@ -611,6 +713,7 @@ extern "C" int seq_tree_pages_compact(const seq_tree_pages_params* p, void* stre
   int rc = check_pages(p);
   if (rc != SEQ_OK) return rc;
   rc = check_pool(p);
+  if (rc == SEQ_OK) rc = check_workspace(p);
   if (rc != SEQ_OK) return rc;
   static int done[64];
   rc = launch_plan(pages_compact_kernel, done, p, false, stream);

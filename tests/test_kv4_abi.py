@@ -137,11 +137,13 @@ def test_pages_calls_refuse_what_each_needs(lib):
         assert lib.seq_tree_pages_resize(C.byref(pages(**bad)), None) == B.SEQ_ERR_INVALID_ARG
     for bad in (dict(source=None), dict(lengths=None), dict(lengths_out=None), dict(count_out=None), dict(page_size=0), dict(lengths_out=FAKE + 4096)):
         assert lib.seq_tree_pages_fork(C.byref(pages(**bad)), None) == B.SEQ_ERR_INVALID_ARG
+    need = lib.seq_tree_pages_workspace_bytes(C.byref(pages()))
+    for bad in (dict(workspace=None), dict(workspace_bytes=need - 1)):
+        assert lib.seq_tree_pages_resize(C.byref(pages(**bad)), None) == B.SEQ_ERR_WORKSPACE
     for fn in (lib.seq_tree_pages_fork, lib.seq_tree_pages_compact):
         for bad in (dict(pages=None), dict(pages=FAKE + 8), dict(num_planes=0), dict(page_bytes=0), dict(page_bytes=24), dict(page_stride_bytes=4080),
                     dict(page_stride_bytes=4104), dict(num_planes=2, plane_stride_bytes=16), dict(workspace=FAKE + 4)):
             assert fn(C.byref(pages(**bad)), None) == B.SEQ_ERR_INVALID_ARG, bad
-        need = lib.seq_tree_pages_workspace_bytes(C.byref(pages()))
         for bad in (dict(workspace=None), dict(workspace_bytes=need - 1)):
             assert fn(C.byref(pages(**bad)), None) == B.SEQ_ERR_WORKSPACE
     for fn in (lib.seq_tree_pages_resize, lib.seq_tree_pages_fork, lib.seq_tree_pages_compact):
