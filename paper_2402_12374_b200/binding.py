@@ -514,28 +514,32 @@ class PagesParams(C.Structure):
     ]
 
 
-def _kv4_pool(pool, what: str):
-    """(layers, kv heads, page size, page stride, layer stride) of a pool uint8 [pages, heads, page_size * 136] or
-    [pages, layers, heads, page_size * 136]: a head's part contiguous, the heads of a page one behind the other."""
-    if pool.dim() == 3:
-        pool = pool.unsqueeze(1)
-    if pool.dim() != 4 or pool.dtype is not torch.uint8:
-        raise ValueError(f"{what} must be uint8 [pages, heads, page_size * 136] or [pages, layers, heads, page_size * 136]")
-    _, layers, heads, part = pool.shape
-    page, layer, head, one = pool.stride()
-    if part % 136 or one != 1 or (heads > 1 and head != part):
-        raise ValueError(f"{what}: page_size * 136 bytes a head, contiguous over heads")
-    return layers, heads, part // 136, page if pool.shape[0] > 1 else layers * heads * part, layer if layers > 1 else heads * part
+def _kv4_pool(pool):
+    """(layers, kv heads, page size, page stride, layer stride, pages) of a pool uint8 [pages, heads, page_size * 136] or [pages, layers,
+    heads, page_size * 136]: a head's part contiguous, the heads of a page one behind the other."""
+    shape, strides = pool.shape, pool.stride()
+    n = len(shape)
+    if (n != 3 and n != 4) or pool.dtype is not torch.uint8:
+        raise ValueError("pool must be uint8 [pages, heads, page_size * 136] or [pages, layers, heads, page_size * 136]")
+    pages, layers, heads, part = shape[0], 1 if n == 3 else shape[1], shape[-2], shape[-1]
+    if part % 136 or strides[-1] != 1 or (heads > 1 and strides[-2] != part):
+        raise ValueError("pool: page_size * 136 bytes a head, contiguous over heads")
+    return layers, heads, part // 136, strides[0] if pages > 1 else layers * heads * part, strides[1] if layers > 1 else heads * part, pages
 
 
 def _table(page_table):
-    if page_table.dim() != 2 or page_table.stride(1) != 1:
+    """(address, entries between rows, rows, entries of a row)"""
+    slots, most = page_table.shape
+    row, one = page_table.stride()
+    if one != 1:
         raise ValueError("page_table must be [slots, max_pages] with contiguous rows")
-    return _dev(page_table, "page_table", torch.int32), page_table.stride(0) if page_table.shape[0] > 1 else page_table.shape[1]
+    return _dev(page_table, "page_table", torch.int32), row if slots > 1 else most, slots, most
 
 
 def _per_slot(t, slots: int, name: str):
-    if t is not None and (t.shape != (slots,) or not t.is_contiguous()):
+    if t is None:
+        return None
+    if t.dim() != 1 or t.shape[0] != slots or (t.stride(0) != 1 and slots > 1):
         raise ValueError(f"{name} must be [{slots}], contiguous")
     return _dev(t, name, torch.int32)
 
@@ -553,7 +557,7 @@ class KV4AttentionCall:
         if q.dtype not in (torch.float16, torch.bfloat16) or k_tree.dtype != q.dtype or v_tree.dtype != q.dtype:
             raise ValueError("q, k_tree, v_tree must share one of float16/bfloat16")
         R, n, Hq, d = q.shape
-        layers, Hkv, page_size, page_stride, _ = _kv4_pool(pool, "pool")
+        layers, Hkv, page_size, page_stride, _, pages = _kv4_pool(pool)
         if layers != 1:
             raise ValueError("pool must be one layer's: pool[:, layer]")
         if k_tree.shape != (R, n, Hkv, d) or v_tree.shape != k_tree.shape:
@@ -578,9 +582,8 @@ class KV4AttentionCall:
         p.q, p.q_stride_req, p.q_stride_tok, p.q_stride_head = _dev(q, "q"), *q.stride()[:3]
         p.k_tree, p.v_tree = _dev(k_tree, "k_tree"), _dev(v_tree, "v_tree")
         p.t_stride_req, p.t_stride_tok, p.t_stride_head = k_tree.stride()[:3]
-        p.pages, p.page_stride_bytes, p.num_pages, p.page_size = _dev(pool, "pool"), page_stride, pool.shape[0], page_size
-        p.page_table, p.table_stride = _table(page_table)
-        p.max_pages = page_table.shape[1]
+        p.pages, p.page_stride_bytes, p.num_pages, p.page_size = _dev(pool, "pool"), page_stride, pages, page_size
+        p.page_table, p.table_stride, _, p.max_pages = _table(page_table)
         p.lengths = _per_slot(lengths, R, "lengths")
         if mask_bits is not None:
             if mask_bits.stride(-1) != 1 or mask_bits.shape[-2] != n or (mask_bits.dim() == 3 and mask_bits.shape[0] != R) or mask_bits.dim() not in (2, 3):
@@ -616,21 +619,22 @@ def seq_tree_kv4_attention(q, k_tree, v_tree, pool, page_table, lengths, **kw):
 
 
 def _kv4_rows(k, v, pool, page_table, lengths, count, dev_status, what):
-    layers, Hkv, page_size, page_stride, layer_stride = _kv4_pool(pool, "pool")
-    if k.dim() == 4:
-        k, v = k.unsqueeze(0), v.unsqueeze(0)
-    if k.dim() != 5 or k.shape != v.shape or k.stride() != v.stride() or k.dtype != v.dtype or k.stride(4) != 1:
+    layers, heads, page_size, page_stride, layer_stride, pages = _kv4_pool(pool)
+    shape, strides, dtype = k.shape, k.stride(), k.dtype
+    if len(shape) == 4:
+        shape, strides = (1, *shape), (0, *strides)
+    if len(shape) != 5 or v.shape != k.shape or v.stride() != k.stride() or strides[4] != 1:
         raise ValueError(f"{what} must be [layers, requests, rows, kv heads, head_dim] (layers optional) with the same strides, rows contiguous")
-    if k.dtype not in (torch.float16, torch.bfloat16):
+    if (dtype is not torch.float16 and dtype is not torch.bfloat16) or v.dtype is not dtype:
         raise ValueError(f"{what} must be float16 or bfloat16")
-    if k.shape[0] != layers or k.shape[3] != Hkv or page_table.shape[0] != k.shape[1]:
+    table, table_stride, slots, max_pages = _table(page_table)
+    R = shape[1]
+    if shape[0] != layers or shape[3] != heads or slots != R:
         raise ValueError(f"{what}: layers and kv heads as in the pool, one row of page_table per request")
-    sl, sr, st, sh, _ = k.stride()
-    table, table_stride = _table(page_table)
-    R = k.shape[1]
-    return Kv4AppendParams(layers, R, k.shape[2], Hkv, k.shape[4], _DTYPES[k.dtype], _dev(k, "k"), _dev(v, "v"), sl, sr, st, sh,
-                           _dev(pool, "pool"), page_stride, layer_stride, pool.shape[0], page_size, table, table_stride, page_table.shape[1],
-                           _per_slot(lengths, R, "lengths"), _per_slot(count, R, "count"), None, 0, None, _dev(dev_status, "dev_status", torch.int32))
+    return Kv4AppendParams(layers, R, shape[2], heads, shape[4], SEQ_F16 if dtype is torch.float16 else SEQ_BF16, _dev(k, "k"), _dev(v, "v"),
+                           strides[0], strides[1], strides[2], strides[3], _dev(pool, "pool"), page_stride, layer_stride, pages, page_size,
+                           table, table_stride, max_pages, _per_slot(lengths, R, "lengths"), _per_slot(count, R, "count"), None, 0, None,
+                           _dev(dev_status, "dev_status", torch.int32))
 
 
 def seq_tree_kv4_append(k, v, pool, page_table, lengths, *, count=None, path=None, new_lengths=None, dev_status=None, stream=None):
@@ -655,21 +659,18 @@ def seq_tree_kv4_read(pool, page_table, k_out, v_out, *, start=None, count=None,
 
 
 def _pages_params(page_table, page_count, ref_count, page_size, table_out, count_out, refs_out, dev_status):
-    slots = page_table.shape[0]
-    table, table_stride = _table(page_table)
-    out, out_stride = (table, table_stride) if table_out is None else _table(table_out)
-    if table_out is not None and table_out.shape != page_table.shape:
-        raise ValueError("table_out must be like page_table")
-    if ref_count.dim() != 1 or not ref_count.is_contiguous() or (refs_out is not None and (refs_out.shape != ref_count.shape or not refs_out.is_contiguous())):
-        raise ValueError("ref_count and refs_out must be [pages], contiguous")
-    p = PagesParams()
-    p.slots, p.max_pages, p.num_pages, p.page_size = slots, page_table.shape[1], ref_count.shape[0], page_size
-    p.page_table, p.table_stride, p.table_out, p.table_out_stride = table, table_stride, out, out_stride
-    p.page_count, p.ref_count = _per_slot(page_count, slots, "page_count"), _dev(ref_count, "ref_count", torch.int32)
-    p.count_out = p.page_count if count_out is None else _per_slot(count_out, slots, "count_out")
-    p.refs_out = p.ref_count if refs_out is None else _dev(refs_out, "refs_out", torch.int32)
-    p.dev_status = _dev(dev_status, "dev_status", torch.int32)
-    return p
+    table, table_stride, slots, max_pages = _table(page_table)
+    out, out_stride = table, table_stride
+    if table_out is not None:
+        out, out_stride, s, m = _table(table_out)
+        if s != slots or m != max_pages:
+            raise ValueError("table_out must be like page_table")
+    pages = ref_count.shape[0]
+    count, refs = _per_slot(page_count, slots, "page_count"), _per_slot(ref_count, pages, "ref_count")
+    return PagesParams(slots, max_pages, pages, page_size, table, table_stride, count, refs, None, out, out_stride,
+                       count if count_out is None else _per_slot(count_out, slots, "count_out"),
+                       refs if refs_out is None else _per_slot(refs_out, pages, "refs_out"), None, None, None, None, 0, 0, 0, 0, None, None, 0,
+                       _dev(dev_status, "dev_status", torch.int32))
 
 
 def _pages_workspace(p, workspace, like):
@@ -681,15 +682,19 @@ def _pages_workspace(p, workspace, like):
 
 def _pages_pool(p, pool, planes: bool):
     """pool [pages, ...] (planes: [planes, pages, ...]) of any type, a page contiguous."""
-    if not planes:
-        pool = pool.unsqueeze(0)
-    one = pool[0, 0]
-    if pool.dim() < 3 or not one.is_contiguous() or pool.shape[1] != p.num_pages:
-        raise ValueError("pool must be [pages, ...] ([planes, pages, ...] with planes=True), as many pages as ref_count, each contiguous")
-    e = pool.element_size()
-    p.pages, p.num_planes, p.page_bytes = _dev(pool, "pool"), pool.shape[0], one.numel() * e
-    p.page_stride_bytes = pool.stride(1) * e if pool.shape[1] > 1 else p.page_bytes
-    p.plane_stride_bytes = pool.stride(0) * e if pool.shape[0] > 1 else p.page_stride_bytes * p.num_pages
+    shape, strides, e = pool.shape, pool.stride(), pool.element_size()
+    at = 1 if planes else 0  # the dimension of the pages
+    size = 1
+    for n, s in zip(reversed(shape[at + 1:]), reversed(strides[at + 1:])):
+        if n > 1 and s != size:
+            raise ValueError("pool: a page must be contiguous")
+        size *= n
+    if len(shape) < at + 2 or shape[at] != p.num_pages:
+        raise ValueError("pool must be [pages, ...] ([planes, pages, ...] with planes=True), as many pages as ref_count")
+    p.pages, p.page_bytes = _dev(pool, "pool"), size * e
+    p.page_stride_bytes = strides[at] * e if shape[at] > 1 else size * e
+    p.num_planes = shape[0] if planes else 1
+    p.plane_stride_bytes = strides[0] * e if planes and shape[0] > 1 else p.page_stride_bytes * p.num_pages
 
 
 def seq_tree_pages_resize(page_table, page_count, ref_count, tokens, page_size: int, *, table_out=None, count_out=None, refs_out=None,
