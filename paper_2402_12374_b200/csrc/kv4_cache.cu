@@ -2,11 +2,14 @@
 //
 // Half a warp has a row (128 channels, 16 bytes a lane): its maximum and minimum as one packed pair (max, -min) by four shuffles, the
 // codes of a lane's eight channels are one 32-bit word, the row's 64 bytes one store.  A half-warp walks 16 consecutive rows of
-// one (layer, request, kv head, K or V) with the 16 page numbers (and path entries) looked up at once, a lane each; the append has
-// four rows in flight, the read, whose loads are smaller, eight.
-// Bound by HBM for prompts, by latency for paths.  Blocks are in the order (16-row chunk, layer, request, heads), so those behind a
+// one (layer, request, kv head, K or V); the 16 rows' places are looked up at once, a lane each, and their (scale, mid) worked out
+// and stored by a lane each, four rows at a time: done by every lane for every row, that and the addresses were half of the
+// instructions, which bind the kernel before HBM does (two prompts of up to 4001 rows, 4 layers of 32 heads: append 346 -> 175 us,
+// still at three quarters of the issue slots; read 146 -> 107, at two thirds of HBM).
+// Paths are bound by latency.  Blocks are in the order (16-row chunk, layer, request, heads), so those behind a
 // request's count, which have nothing to do, come last.
 #include "kv4.cuh"
+#include "umma.cuh"
 
 namespace seqtree {
 
@@ -58,34 +61,42 @@ __device__ __forceinline__ uint32_t extremes(uint4 x) {
   return max_pair<T>(__byte_perm(hi, lo, 0x5410), __byte_perm(hi, lo, 0x7632));
 }
 
-// The eight codes of a lane's channels.  Quotients are taken as products with the reciprocal (off by less than 3e-6 at +-8); where
-// one lies so near the middle between two codes that this could decide, they are divided.
-__device__ __forceinline__ uint32_t quantise8(const float* v, float scale, float mid) {
-  constexpr float kMagic = 12582920.f;  // 1.5 * 2^23 + 8: adding it rounds to a whole number, even in the middle, 8 more in the last bits
-  float inv;
-  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(scale));
-  inv = scale > 0.f ? inv : 0.f;
-  float off = 0.f;
-  float c[8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const float d = v[i] - mid;
-    c[i] = fmaf(d, inv, kMagic);
-    off = fmaxf(off, fabsf(fmaf(d, inv, kMagic - c[i])));
-    c[i] = fminf(fmaxf(c[i], kMagic - 8.f), kMagic + 7.f);
-  }
-  if (off > 0.499995f) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) c[i] = fminf(fmaxf(scale > 0.f ? __fdiv_rn(v[i] - mid, scale) : 0.f, -8.f), 7.f) + kMagic;
-  }
+// The eight codes of a lane's channels.  Quotients are taken as products with the reciprocal (off by less than 3e-6 at +-8); `near`: one
+// lies so near the middle between two codes that this could decide.
+constexpr float kMagic = 12582920.f;  // 1.5 * 2^23 + 8: adding it rounds to a whole number, even in the middle, 8 more in the last bits
+__device__ __forceinline__ uint32_t join8(const float* c) {
   // the last bits of each, four apart; what else the numbers hold is the same and taken off
   uint32_t word = 0, rest = 0;
 #pragma unroll
   for (int i = 7; i >= 0; --i) {
-    word = word * 16u + __float_as_uint(c[i]);
+    word = word * 16u + __float_as_uint(fminf(fmaxf(c[i], kMagic - 8.f), kMagic + 7.f));
     rest = rest * 16u + 0x4b400000u;
   }
   return word - rest;
+}
+__device__ __forceinline__ uint32_t quantise8(const float* v, float inv, float mid, bool& near) {
+  const uint64_t inv2 = pair_of(inv, inv), mid2 = pair_of(-mid, -mid), magic = pair_of(kMagic, kMagic), minus = pair_of(-1.f, -1.f);
+  float off = 0.f, c[8];
+#pragma unroll
+  for (int i = 0; i < 8; i += 2) {
+    const uint64_t d = add2(pair_of(v[i], v[i + 1]), mid2), y = fma2(d, inv2, magic);
+    float a, b;
+    unpair(fma2(d, inv2, fma2(y, minus, magic)), a, b);  // how far from the whole number
+    off = max3(off, fabsf(a), fabsf(b));
+    unpair(y, c[i], c[i + 1]);
+  }
+  near = off > 0.499995f;
+  return join8(c);
+}
+__device__ __forceinline__ uint32_t divide8(const float* v, float scale, float mid) {
+  float c[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) c[i] = (scale > 0.f ? __fdiv_rn(v[i] - mid, scale) : 0.f) + kMagic;
+  return join8(c);
+}
+__device__ __forceinline__ uint64_t shfl64(uint64_t x, int from) {
+  const uint32_t lo = __shfl_sync(0xffffffffu, (uint32_t)x, from, 16), hi = __shfl_sync(0xffffffffu, (uint32_t)(x >> 32), from, 16);
+  return (uint64_t)hi << 32 | lo;
 }
 
 // How many rows of request r there are; -1: none, for a reason that is told once per call
@@ -111,7 +122,6 @@ __global__ void __launch_bounds__(kRowThreads) kv4_rows_copy_kernel(const RowsAr
   const int lr = blockIdx.x / a.groups, l = lr / a.batch, r = lr - l * a.batch;
   const int item = (blockIdx.x - lr * a.groups) * (kRowThreads / 16) + (threadIdx.x >> 4);  // (kv head, K or V)
   const int lane = threadIdx.x & 15;
-  const unsigned half = 0xffffu << (threadIdx.x & 16);
   const bool first_block = chunk == 0 && blockIdx.x - lr * a.groups == 0 && l == 0;
   const int len = a.lengths != nullptr ? a.lengths[r] : 0;
   int m = rows_of(a, r, len, first_block && threadIdx.x == 0);
@@ -129,84 +139,119 @@ __global__ void __launch_bounds__(kRowThreads) kv4_rows_copy_kernel(const RowsAr
   }
   if (kAppend && first_block && threadIdx.x == 0 && a.new_lengths != nullptr) a.new_lengths[r] = len + max(m, 0);
   const int i0 = chunk * kChunkRows;
-  if (i0 >= m || item >= 2 * a.heads) return;
-  const int g = item >> 1, which = item & 1;
+  if (i0 >= m) return;
+  const bool live = item < 2 * a.heads;  // (both halves of a warp go through everything)
+  const int g = min(item >> 1, a.heads - 1), which = item & 1;
 
-  // lane j: row i0 + j's page, its place there and its row
-  int page = -1, node = 0;
+  // lane j: where row i0 + j's codes and its (scale, mid) are (0: nowhere), and where the row is
+  uint64_t codes = 0;
+  uint32_t* params = nullptr;
+  uint64_t row = 0;
   if (i0 + lane < m) {
-    const int t = len + i0 + lane;
-    page = a.table[r * a.table_stride + t / a.page_size];
+    const int t = len + i0 + lane, in_page = t & (a.page_size - 1), line = in_page & (kGranule - 1);
+    const int page = a.table[r * a.table_stride + t / a.page_size];
     if (page < 0 || page >= a.num_pages) {
       if (l == 0 && item == 0) dev_flag(a.status, SEQ_DEV_BAD_PAGE);
-      page = -1;
+    } else if (live) {
+      uint8_t* granule = a.pages + l * a.layer_stride + page * a.page_stride + (int64_t)g * a.page_size * 136 + in_page / kGranule * kGranuleBytes;
+      codes = reinterpret_cast<uint64_t>(granule + which * kGranuleV + line * kCodeBytes);
+      params = reinterpret_cast<uint32_t*>(granule + kGranuleParams + which * (kGranule * 4) + line * 4);
     }
-    node = kAppend && a.path != nullptr ? a.path[r * a.path_stride + i0 + lane] : i0 + lane;
+    row = (uint64_t)((kAppend && a.path != nullptr ? a.path[r * a.path_stride + i0 + lane] : i0 + lane) * a.s_tok);
   }
   const uint8_t* rows = (which ? a.v : a.k) + l * a.s_layer + r * a.s_req + g * a.s_head + 16 * lane;
-  uint8_t* pool = a.pages + l * a.layer_stride + (int64_t)g * a.page_size * 136;
   const int rows_here = min(kChunkRows, m - i0);
-  constexpr int kRowsInFlight = kAppend ? 4 : 8;
-  for (int j0 = 0; j0 < rows_here; j0 += kRowsInFlight) {
-    uint4 x[kRowsInFlight];
-    uint8_t* at[kRowsInFlight];  // the row's codes; the row's (scale, mid) at `params`
-    int params[kRowsInFlight];
+  if (kAppend) {
+    uint32_t mine = 0;  // lane j: row j's (scale, mid)
+#pragma unroll 1
+    for (int j0 = 0; j0 < rows_here; j0 += 4) {
+      uint4 x[4];
+      uint32_t both[4];
 #pragma unroll
-    for (int u = 0; u < kRowsInFlight; ++u) {
-      const int j = j0 + u;
-      const int p = __shfl_sync(half, page, j, 16), nd = __shfl_sync(half, node, j, 16);
-      const int t = len + i0 + j, in_page = t & (a.page_size - 1), row = in_page & (kGranule - 1);
-      at[u] = p < 0 ? nullptr : pool + p * a.page_stride + (int64_t)(in_page / kGranule) * kGranuleBytes + which * kGranuleV + row * kCodeBytes;
-      params[u] = kGranuleParams + which * (kGranule * 4) - which * kGranuleV - row * kCodeBytes + row * 4;
-      x[u] = make_uint4(0u, 0u, 0u, 0u);
-      if (at[u] == nullptr) continue;
-      if (kAppend) {
-        x[u] = *reinterpret_cast<const uint4*>(rows + nd * a.s_tok);
-      } else {
-        x[u].x = *reinterpret_cast<const uint32_t*>(at[u] + 4 * lane);
-        x[u].y = *reinterpret_cast<const uint32_t*>(at[u] + params[u]);
+      for (int u = 0; u < 4; ++u) x[u] = *reinterpret_cast<const uint4*>(rows + shfl64(row, j0 + u));  // (rows behind the last: row 0)
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        both[u] = extremes<T>(x[u]);
+#pragma unroll
+        for (int o = 8; o > 0; o >>= 1) both[u] = max_pair<T>(both[u], __shfl_xor_sync(0xffffffffu, both[u], o, 16));
       }
-    }
+      // lane j works out row j0 + (j & 3)'s scale and mid
+      const uint32_t b = (lane & 2) ? ((lane & 1) ? both[3] : both[2]) : ((lane & 1) ? both[1] : both[0]);
+      float hi, lo;
+      if (std::is_same<T, __nv_bfloat16>::value) {
+        hi = __uint_as_float(b << 16);
+        lo = -__uint_as_float(b & 0xffff0000u);
+      } else {
+        const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&b));
+        hi = f.x;
+        lo = -f.y;
+      }
+      const bool fine = fabsf(hi) <= kLargest && fabsf(lo) <= kLargest;  // (false for a NaN)
+      // halves, so that the difference cannot overflow; it is exact in fp32 but for magnitudes far apart
+      __half2 sm = __floats2half2_rn(__fdiv_rn(hi * 0.5f - lo * 0.5f, 7.5f), 0.f);
+      const float scale = __low2float(sm);
+      sm.y = __float2half_rn(scale * 8.f + lo);
+      const float mid = __high2float(sm);
+      float inv;
+      asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(scale));
+      inv = scale > 0.f ? inv : 0.f;
+      const bool some_bad = __any_sync(0xffffffffu, !fine);
+      if ((lane >> 2) == (j0 >> 2)) {
+        mine = fine ? *reinterpret_cast<uint32_t*>(&sm) : 0u;
+        if (!fine && params != nullptr) dev_flag(a.status, SEQ_DEV_NONFINITE);
+      }
 #pragma unroll
-    for (int u = 0; u < kRowsInFlight; ++u) {
-      if (at[u] == nullptr) continue;  // (the same for the whole half)
-      if (kAppend) {
+      for (int u = 0; u < 4; ++u) {
+        const float iu = __shfl_sync(0xffffffffu, inv, u, 16), mu = __shfl_sync(0xffffffffu, mid, u, 16);
         float v[8];
         widen8<T>(x[u], v);
-        uint32_t both = extremes<T>(x[u]);
+        bool near;
+        uint32_t word = quantise8(v, iu, mu, near);
+        if (__any_sync(0xffffffffu, near)) {
+          const float su = __shfl_sync(0xffffffffu, scale, u, 16);
+          if (near) word = divide8(v, su, mu);
+        }
+        if (some_bad && !__shfl_sync(0xffffffffu, (int)fine, u, 16)) word = 0x88888888u;
+        const uint64_t to = shfl64(codes, j0 + u);
+        if (to != 0) *reinterpret_cast<uint32_t*>(to + 4 * lane) = word;
+      }
+    }
+    if (params != nullptr) *params = mine;
+  } else {
+    const uint32_t sm = params != nullptr ? *params : 0u;
+    uint8_t* out = const_cast<uint8_t*>(rows);
+#pragma unroll 1
+    for (int j0 = 0; j0 < rows_here; j0 += 8) {
+      uint32_t x[8];
+      uint64_t from[8];
 #pragma unroll
-        for (int o = 8; o > 0; o >>= 1) both = max_pair<T>(both, __shfl_xor_sync(half, both, o, 16));
-        float hi, lo;
+      for (int u = 0; u < 8; ++u) {
+        from[u] = shfl64(codes, j0 + u);
+        x[u] = from[u] != 0 ? *reinterpret_cast<const uint32_t*>(from[u] + 4 * lane) : 0u;
+      }
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        const uint32_t p = __shfl_sync(0xffffffffu, sm, j0 + u, 16);
+        uint32_t c[4];  // channels (0, 4), (1, 5), (2, 6), (3, 7), less 8
+        unpack4(x[u], c);
+        uint4 o;
         if (std::is_same<T, __nv_bfloat16>::value) {
-          hi = __uint_as_float(both << 16);
-          lo = -__uint_as_float(both & 0xffff0000u);
-        } else {
-          const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&both));
-          hi = f.x;
-          lo = -f.y;
-        }
-        const bool fine = fabsf(hi) <= kLargest && fabsf(lo) <= kLargest;  // (false for a NaN)
-        // halves, so that the difference cannot overflow; it is exact in fp32 but for magnitudes far apart
-        __half2 sm = __floats2half2_rn(__fdiv_rn(hi * 0.5f - lo * 0.5f, 7.5f), 0.f);
-        sm.y = __float2half_rn(__low2float(sm) * 8.f + lo);
-        if (!fine) {
-          sm = __floats2half2_rn(0.f, 0.f);
-          if (lane == 0) dev_flag(a.status, SEQ_DEV_NONFINITE);
-        }
-        const uint32_t word = fine ? quantise8(v, __low2float(sm), __high2float(sm)) : 0x88888888u;
-        *reinterpret_cast<uint32_t*>(at[u] + 4 * lane) = word;
-        if (lane == 0) *reinterpret_cast<__half2*>(at[u] + params[u]) = sm;
-      } else {
-        const float2 sm = __half22float2(*reinterpret_cast<const __half2*>(&x[u].y));
-        uint32_t o[4];
+          const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&p));
+          float2 y[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float c0 = __uint_as_float(((x[u].x >> (8 * i)) & 15u) | 0x4b000000u) - 8388616.f;  // the nibble less 8
-          const float c1 = __uint_as_float(((x[u].x >> (8 * i + 4)) & 15u) | 0x4b000000u) - 8388616.f;
-          const T lo = from_float<T>(fmaf(sm.x, c0, sm.y)), hi = from_float<T>(fmaf(sm.x, c1, sm.y));
-          o[i] = (uint32_t)*reinterpret_cast<const uint16_t*>(&lo) | ((uint32_t)*reinterpret_cast<const uint16_t*>(&hi) << 16);
+          for (int i = 0; i < 4; ++i) {
+            y[i] = __half22float2(*reinterpret_cast<const __half2*>(&c[i]));
+            y[i].x = fmaf(f.x, y[i].x, f.y);
+            y[i].y = fmaf(f.x, y[i].y, f.y);
+          }
+          o = make_uint4(pack2<true>(y[0].x, y[1].x), pack2<true>(y[2].x, y[3].x), pack2<true>(y[0].y, y[1].y), pack2<true>(y[2].y, y[3].y));
+        } else {  // (the fused multiply-add of halves rounds once, too)
+          const uint32_t s = __byte_perm(p, 0u, 0x1010), m2 = __byte_perm(p, 0u, 0x3232);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) c[i] = hfma2_bits(c[i], s, m2);
+          o = make_uint4(__byte_perm(c[0], c[1], 0x5410), __byte_perm(c[2], c[3], 0x5410), __byte_perm(c[0], c[1], 0x7632), __byte_perm(c[2], c[3], 0x7632));
         }
-        *reinterpret_cast<uint4*>(const_cast<uint8_t*>(rows) + (int64_t)(i0 + j0 + u) * a.s_tok) = make_uint4(o[0], o[1], o[2], o[3]);
+        if (from[u] != 0) *reinterpret_cast<uint4*>(out + (int64_t)(i0 + j0 + u) * a.s_tok) = o;
       }
     }
   }
