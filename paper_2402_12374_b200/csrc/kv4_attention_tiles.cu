@@ -23,10 +23,10 @@
 
 namespace seqtree {
 
-constexpr int kTilesThreads = 896;  // warps: loader, two issuers, one idle; eight that unpack; 16 for the chains
+constexpr int kTilesThreads = 896;  // warps: loader, two issuers, one idle; four that unpack K, four V; 16 for the chains
 constexpr int kUnpackWarp = 4, kChainWarp = 12;
 constexpr int kTilesStep = 128;     // keys
-constexpr int kRegsIssue = 40, kRegsChain = 80;  // 128 * 40 + 256 * 72 + 512 * 80 = 896 * 72
+constexpr int kRegsIssue = 24, kRegsUnpack = 48, kRegsChain = 96;  // 128 * 24 + 256 * 48 + 512 * 96 = 896 * 72
 constexpr int kHalfKeys = 64;       // keys of a ring stage
 constexpr int kStageBytes = kHalfKeys / kGranule * kGranuleBytes;
 constexpr int kTreeTiles = SEQ_MAX_TREE / kTilesStep;
@@ -62,29 +62,15 @@ __device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t b
   asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
                ::"r"(smem_u32(dst)), "l"(src), "r"(bytes), "r"(smem_u32(bar)) : "memory");
 }
-// mbar_wait for the many warps of this kernel: a wait that is not over at once sleeps on the barrier (20 us at a time, 1.3 s in
-// all) instead of taking issue slots.
-__device__ __forceinline__ bool mbar_sleep(uint64_t* bar, uint32_t parity) {
-  uint32_t ok;
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
-      "selp.u32 %0, 1, 0, p;\n\t}"
-      : "=r"(ok) : "r"(smem_u32(bar)), "r"(parity), "r"(20000u) : "memory");
-  return ok != 0;
-}
-template <typename Smem>
-__device__ __forceinline__ bool mbar_wait_long(Smem* sm, uint64_t* bar, uint32_t parity, int32_t* dev_status) {
-  for (uint32_t it = 0; it < (1u << 16); ++it) {
-    if (mbar_sleep(bar, parity)) return true;
-    if (sm->abort_flag) return false;
-  }
-  sm->abort_flag = 1;
-  dev_flag(dev_status, SEQ_DEV_TIMEOUT);
-  return false;
-}
 __device__ __forceinline__ void sts128(uint32_t at, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
   asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
+// 16 consecutive fp32 columns of this thread's tensor-memory lane
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
+        "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]) : "r"(taddr) : "memory");
 }
 __device__ __forceinline__ uint32_t bits_below(int x) { return x <= 0 ? 0u : (x >= 32 ? 0xffffffffu : (1u << x) - 1u); }
 
@@ -116,10 +102,10 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
   Smem* sm = reinterpret_cast<Smem*>(smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u));
   const int warp = uniform((int)threadIdx.x >> 5), lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
-    for (int s = 0; s < kStages; ++s) { mbar_init(&sm->raw_full[s], 1); mbar_init(&sm->raw_empty[s], 4); }
+    for (int s = 0; s < kStages; ++s) { mbar_init(&sm->raw_full[s], 1); mbar_init(&sm->raw_empty[s], 8); }
     for (int b = 0; b < 2; ++b) {
-      mbar_init(&sm->k_full[b], 8); mbar_init(&sm->k_empty[b], kTwo ? 2 : 1);
-      mbar_init(&sm->v_full[b], 8); mbar_init(&sm->v_empty[b], kTwo ? 2 : 1);
+      mbar_init(&sm->k_full[b], 4); mbar_init(&sm->k_empty[b], kTwo ? 2 : 1);
+      mbar_init(&sm->v_full[b], 4); mbar_init(&sm->v_empty[b], kTwo ? 2 : 1);
       mbar_init(&sm->q_full[b], kTwo ? 8 : 16);
       for (int x = 0; x < 4; ++x) mbar_init(&sm->turn[b][x], 2);
       mbar_init(&sm->drained[b], 1);
@@ -177,7 +163,7 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
                 }
               }
             }
-            if (w > 0 && !mbar_wait_long(sm, &sm->raw_empty[st], (w - 1) & 1, a.status)) { ok = false; break; }
+            if (w > 0 && !mbar_wait(sm, &sm->raw_empty[st], (w - 1) & 1, a.status)) { ok = false; break; }
             if (lane == 0) mbar_expect_tx(&sm->raw_full[st], granules * kGranuleBytes);
             __syncwarp();
             // lane x: the x-th page's part
@@ -208,14 +194,14 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
       bool ok = true;
       for (int pos = range_lo; pos < range_hi && ok; ++seg) {
         const TilesSeg sg = tiles_seg(&sm->plan, a, pos, range_hi);
-        if (kTwo || c == 0) ok = mbar_wait_long(sm, &sm->q_full[c], seg & 1, a.status);
+        if (kTwo || c == 0) ok = mbar_wait(sm, &sm->q_full[c], seg & 1, a.status);
         const uint32_t q_lo = desc_lo(smem_u32(sm->q[kTwo ? c : 0]), 16);
         for (int i = 0; i < sg.steps && ok; ++i) {
           const int x = step + i, b = x & 1, u = kTwo ? x : x / kSBufs, sb = kTwo ? c : x - u * kSBufs;
           const uint32_t sp = tmem + kTmemS + 128u * sb;
           if (kTwo || c == 0) {
             // S goes where an earlier tile's P was: its product has completed
-            ok = mbar_wait_long(sm, &sm->k_full[b], (x >> 1) & 1, a.status) && (u == 0 || mbar_wait_long(sm, &sm->pv_done[sb][1], (u - 1) & 1, a.status));
+            ok = mbar_wait(sm, &sm->k_full[b], (x >> 1) & 1, a.status) && (u == 0 || mbar_wait(sm, &sm->pv_done[sb][1], (u - 1) & 1, a.status));
             if (!ok) break;
             tc_fence_after();
             if (elect_one()) {
@@ -227,10 +213,10 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
           }
           if (kTwo || c == 1) {
             const uint32_t v_lo = desc_lo(smem_u32(sm->v[b]), kHalfBytes);
-            ok = mbar_wait_long(sm, &sm->v_full[b], (x >> 1) & 1, a.status);
+            ok = mbar_wait(sm, &sm->v_full[b], (x >> 1) & 1, a.status);
 #pragma unroll 1
             for (int h = 0; h < 2 && ok; ++h) {
-              ok = mbar_wait_long(sm, &sm->p_full[sb][h], u & 1, a.status);
+              ok = mbar_wait(sm, &sm->p_full[sb][h], u & 1, a.status);
               if (!ok) break;
               tc_fence_after();
               if (elect_one()) {
@@ -253,15 +239,19 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
       }
     }
   } else if (warp < kChainWarp) {
-    // ============================ codes, and the tree's rows, to half-precision tiles: 16 rows a warp ============================
-    const int w8 = warp - kUnpackWarp, quad = lane & 3, r8 = lane >> 2;
-    const int half = w8 >> 2;
+    // ============================ codes, and the tree's rows, to half-precision tiles: 32 rows of K or of V a warp ============================
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsUnpack));
+    const int which = (warp - kUnpackWarp) >> 2, w4 = warp & 3, quad = lane & 3, r8 = lane >> 2;
+    uint64_t* const full = which ? sm->v_full : sm->k_full;
+    uint64_t* const empty = which ? sm->v_empty : sm->k_empty;
     int step = 0, taken = 0, seg = 0;  // (segments with steps)
     bool ok = true;
     // A thread's 32 channels of a row are four 16-byte pieces.  Quads 2, 3 write to the tile's second half, 16 KiB on, that is, to the same
-    // banks: they go through their pieces in another order.
-    const uint32_t piece0 = (quad & 1) * 4, swap = quad >= 2 ? 2u : 0u;
-    const uint32_t tile_half = (quad >> 1) * kHalfBytes;
+    // banks: they go through their pieces in another order.  (A thread's rows are alike modulo 8: the pieces' places are the same.)
+    const uint32_t swap = quad >= 2 ? 2u : 0u;
+    uint32_t place[4];
+#pragma unroll
+    for (int p = 0; p < 4; ++p) place[p] = (quad >> 1) * kHalfBytes + r8 * 128 + ((((quad & 1) * 4 + (p ^ swap)) ^ r8) << 4);
     for (int pos = range_lo; pos < range_hi && ok;) {
       const TilesSeg sg = tiles_seg(&sm->plan, a, pos, range_hi);
       for (int i = 0; i < sg.steps && ok; ++i) {
@@ -269,87 +259,91 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
         const bool tree = t >= sg.u.prefix.steps;
         const int key0 = tree ? (t - sg.u.prefix.steps) * kTilesStep : sg.u.prefix.key_step(t) * kTilesStep;
         const int left = (tree ? a.n : sg.u.L) - key0;  // keys of the tile that there are
-        const int halves = left > kHalfKeys ? 2 : 1;
-        if (!tree && half < halves) ok = mbar_wait_long(sm, &sm->raw_full[(taken + half) % kStages], ((taken + half) / kStages) & 1, a.status);
-        const uint32_t granule = smem_u32(sm->ring[(taken + half) % kStages]) + (w8 & 3) * kGranuleBytes + r8 * kCodeBytes + quad * 16;
+        if (w > 0) ok = mbar_wait(sm, &empty[b], (w - 1) & 1, a.status);
+        const uint32_t tile = smem_u32(which ? sm->v[b] : sm->k[b]);
+        if (!tree) {
 #pragma unroll 1
-        for (int which = 0; which < 2 && ok; ++which) {
-          if (w > 0) ok = mbar_wait_long(sm, which ? &sm->v_empty[b] : &sm->k_empty[b], (w - 1) & 1, a.status);
-          __syncwarp();
-          if (!ok) break;
-          const uint32_t tile = smem_u32(which ? sm->v[b] : sm->k[b]) + tile_half;
-          if (!tree) {
-#pragma unroll 1
+          for (int h = 0; h < 2 && ok; ++h) {
+            const int st = taken % kStages;
+            if (h * kHalfKeys < left) ok = mbar_wait(sm, &sm->raw_full[st], (taken / kStages) & 1, a.status);
+            __syncwarp();
+            if (!ok) break;
+            const uint32_t granule = smem_u32(sm->ring[st]) + w4 * kGranuleBytes;
+            uint4 cd[2];
+            uint32_t params[2];
+#pragma unroll
             for (int y = 0; y < 2; ++y) {
-              const int row = 8 * y + r8, key = w8 * kGranule + row;
-              uint4 cd = make_uint4(0u, 0u, 0u, 0u);
-              uint32_t params = 0;  // a key behind the prefix: zeros
-              if (key < left) {
-                asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(cd.x), "=r"(cd.y), "=r"(cd.z), "=r"(cd.w)
-                             : "r"(granule + which * kGranuleV + y * (8 * kCodeBytes)) : "memory");
-                asm volatile("ld.shared.u32 %0, [%1];" : "=r"(params)
-                             : "r"(granule - r8 * kCodeBytes - quad * 16 + kGranuleParams + which * (kGranule * 4) + row * 4) : "memory");
+              cd[y] = make_uint4(0u, 0u, 0u, 0u);
+              params[y] = 0;  // a key behind the prefix: zeros
+              if (h * kHalfKeys + w4 * kGranule + 8 * y + r8 < left) {
+                asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(cd[y].x), "=r"(cd[y].y), "=r"(cd[y].z), "=r"(cd[y].w)
+                             : "r"(granule + which * kGranuleV + (8 * y + r8) * kCodeBytes + quad * 16));
+                asm volatile("ld.shared.u32 %0, [%1];" : "=r"(params[y]) : "r"(granule + kGranuleParams + which * (kGranule * 4) + (8 * y + r8) * 4));
               }
-              const uint32_t scale = __byte_perm(params, 0u, 0x1010), mid = __byte_perm(params, 0u, 0x3232);
-              const uint32_t words[4] = {swap ? cd.z : cd.x, swap ? cd.w : cd.y, swap ? cd.x : cd.z, swap ? cd.y : cd.w};
-              const uint32_t line = tile + key * 128;
+            }
+#pragma unroll
+            for (int y = 0; y < 2; ++y) {
+              const uint32_t scale = __byte_perm(params[y], 0u, 0x1010), mid = __byte_perm(params[y], 0u, 0x3232);
+              const uint32_t words[4] = {swap ? cd[y].z : cd[y].x, swap ? cd[y].w : cd[y].y, swap ? cd[y].x : cd[y].z, swap ? cd[y].y : cd[y].w};
+              const uint32_t line = tile + (h * kHalfKeys + w4 * kGranule + 8 * y) * 128;
 #pragma unroll
               for (int p = 0; p < 4; ++p) {
                 uint32_t v[4];
                 unpack4(words[p], v);
-                sts128(line + (((piece0 + (p ^ swap)) ^ (key & 7)) << 4), hfma2_bits(v[0], scale, mid), hfma2_bits(v[1], scale, mid),
-                       hfma2_bits(v[2], scale, mid), hfma2_bits(v[3], scale, mid));
+                sts128(line + place[p], hfma2_bits(v[0], scale, mid), hfma2_bits(v[1], scale, mid), hfma2_bits(v[2], scale, mid), hfma2_bits(v[3], scale, mid));
               }
             }
-          } else {
-            uint32_t bad = 0;  // of the warp's 16 rows
-            const uint8_t* rows = (which ? a.vt : a.kt) + sg.u.r * a.t_req + sg.u.g * a.t_head + quad * 64;
-#pragma unroll 1
-            for (int y = 0; y < 2; ++y) {
-              const int key = w8 * 16 + 8 * y + r8;
-              uint4 in[4];
-#pragma unroll
-              for (int p = 0; p < 4; ++p) {
-                in[p] = make_uint4(0u, 0u, 0u, 0u);
-                if (key < left) in[p] = reinterpret_cast<const uint4*>(rows + (int64_t)(key0 + key) * a.t_tok)[p ^ swap];
-              }
-              uint32_t big = 0;
-#pragma unroll
-              for (int p = 0; p < 4; ++p) {
-                if (kBf16) {
-                  in[p].x = pack2<false>(__uint_as_float(in[p].x << 16), __uint_as_float(in[p].x & 0xffff0000u));
-                  in[p].y = pack2<false>(__uint_as_float(in[p].y << 16), __uint_as_float(in[p].y & 0xffff0000u));
-                  in[p].z = pack2<false>(__uint_as_float(in[p].z << 16), __uint_as_float(in[p].z & 0xffff0000u));
-                  in[p].w = pack2<false>(__uint_as_float(in[p].w << 16), __uint_as_float(in[p].w & 0xffff0000u));
-                }
-                big = __vmaxu2(__vmaxu2(big, in[p].x & 0x7c007c00u), __vmaxu2(in[p].y & 0x7c007c00u, __vmaxu2(in[p].z & 0x7c007c00u, in[p].w & 0x7c007c00u)));
-              }
-              uint32_t keep = 0xffffffffu;
-              if (which == 1) {
-                // a row of V that is not finite counts as zeros, so that it stays out of the rows that do not see it; those
-                // that do become NaN when they are written
-                const uint32_t b4 = __ballot_sync(0xffffffffu, (big & 0xffffu) == 0x7c00u || (big >> 16) == 0x7c00u);
-                if ((b4 >> (lane & 28)) & 15u) keep = 0u;
-#pragma unroll
-                for (int z = 0; z < 8; ++z) bad |= (b4 >> (4 * z)) & 15u ? 1u << (8 * y + z) : 0u;
-              }
-              const uint32_t line = tile + key * 128;
-#pragma unroll
-              for (int p = 0; p < 4; ++p)
-                sts128(line + (((piece0 + (p ^ swap)) ^ (key & 7)) << 4), __byte_perm(in[p].x, in[p].z, 0x5410) & keep, __byte_perm(in[p].x, in[p].z, 0x7632) & keep,
-                       __byte_perm(in[p].y, in[p].w, 0x5410) & keep, __byte_perm(in[p].y, in[p].w, 0x7632) & keep);
+            if (h * kHalfKeys < left) {
+              __syncwarp();
+              if (lane == 0) mbar_arrive(&sm->raw_empty[st]);
+              ++taken;
             }
-            // (four segments' words: this warp is two tiles ahead of the rows that look at them, at most)
-            if (which == 1 && lane == 0) reinterpret_cast<uint16_t*>(sm->bad[seg & 3][key0 / kTilesStep])[w8] = (uint16_t)bad;
           }
-          fence_async_smem();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(which ? &sm->v_full[b] : &sm->k_full[b]);
+        } else if (ok) {
+          uint32_t bad = 0;  // of the warp's 32 rows
+          const uint8_t* rows = (which ? a.vt : a.kt) + sg.u.r * a.t_req + sg.u.g * a.t_head + quad * 64;
+#pragma unroll 1
+          for (int y = 0; y < 4; ++y) {
+            const int key = w4 * 32 + 8 * y + r8;
+            uint4 in[4];
+#pragma unroll
+            for (int p = 0; p < 4; ++p) {
+              in[p] = make_uint4(0u, 0u, 0u, 0u);
+              if (key < left) in[p] = reinterpret_cast<const uint4*>(rows + (int64_t)(key0 + key) * a.t_tok)[p ^ swap];
+            }
+            uint32_t big = 0;
+#pragma unroll
+            for (int p = 0; p < 4; ++p) {
+              if (kBf16) {
+                in[p].x = pack2<false>(__uint_as_float(in[p].x << 16), __uint_as_float(in[p].x & 0xffff0000u));
+                in[p].y = pack2<false>(__uint_as_float(in[p].y << 16), __uint_as_float(in[p].y & 0xffff0000u));
+                in[p].z = pack2<false>(__uint_as_float(in[p].z << 16), __uint_as_float(in[p].z & 0xffff0000u));
+                in[p].w = pack2<false>(__uint_as_float(in[p].w << 16), __uint_as_float(in[p].w & 0xffff0000u));
+              }
+              big = __vmaxu2(__vmaxu2(big, in[p].x & 0x7c007c00u), __vmaxu2(in[p].y & 0x7c007c00u, __vmaxu2(in[p].z & 0x7c007c00u, in[p].w & 0x7c007c00u)));
+            }
+            uint32_t keep = 0xffffffffu;
+            if (which == 1) {
+              // a row of V that is not finite counts as zeros, so that it stays out of the rows that do not see it; those
+              // that do become NaN when they are written
+              const uint32_t b4 = __ballot_sync(0xffffffffu, (big & 0xffffu) == 0x7c00u || (big >> 16) == 0x7c00u);
+              if ((b4 >> (lane & 28)) & 15u) keep = 0u;
+#pragma unroll 1
+              for (int z = 0; z < 8; ++z) bad |= (b4 >> (4 * z)) & 15u ? 1u << (8 * y + z) : 0u;
+            }
+            const uint32_t line = tile + (w4 * 32 + 8 * y) * 128;
+#pragma unroll
+            for (int p = 0; p < 4; ++p)
+              sts128(line + place[p], __byte_perm(in[p].x, in[p].z, 0x5410) & keep, __byte_perm(in[p].x, in[p].z, 0x7632) & keep,
+                     __byte_perm(in[p].y, in[p].w, 0x5410) & keep, __byte_perm(in[p].y, in[p].w, 0x7632) & keep);
+          }
+          // (four segments' words: this warp is two tiles ahead of the rows that look at them, at most)
+          if (which == 1 && lane == 0) sm->bad[seg & 3][key0 / kTilesStep][w4] = bad;
         }
-        if (!tree) {
-          if (lane == 0 && half < halves) mbar_arrive(&sm->raw_empty[(taken + half) % kStages]);
-          taken += halves;
-        }
+        if (!ok) break;
+        fence_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&full[b]);
       }
       step += sg.steps;
       seg += sg.steps > 0;
@@ -440,41 +434,34 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
             if (w) vis[1] = bits; else vis[0] = bits;
           }
         }
-        ok = mbar_wait_long(sm, &sm->s_full[sb], u & 1, a.status);
+        ok = mbar_wait(sm, &sm->s_full[sb], u & 1, a.status);
         __syncwarp();
         if (!ok) break;
         if (warp_live) {
           tc_fence_after();
-          // 32 scores, -inf where masked
-          auto scores = [&](int x2, uint32_t (&s)[32]) {
-            tmem_ld32(tmem_s + 32u * x2, s, 0);
-            tc_wait_ld();
+          uint32_t s[64];
+          tmem_ld32(tmem_s, s, 0);
+          tmem_ld32(tmem_s + 32u, s, 32);
+          tc_wait_ld();
 #pragma unroll
-            for (int e = 0; e < 32; ++e) asm volatile("" : "+r"(s[e]));  // (nothing of it moves ahead of the wait)
-            if (masked) {
-              const uint32_t bits = x2 ? vis[1] : vis[0];
+          for (int e = 0; e < 64; ++e) asm volatile("" : "+r"(s[e]));  // (nothing of it moves ahead of the wait)
+          if (masked) {
 #pragma unroll
-              for (int e = 0; e < 32; ++e)
-                if (!((bits >> e) & 1u)) s[e] = __float_as_uint(-INFINITY);
-            }
-          };
-          // (Loops that are not unrolled, here and where codes are unpacked: what the warps of an SM run has to stay in its
-          // instruction caches.  Unrolled, a warp spent a third of its time waiting for instructions.)
-          float mx[2] = {-INFINITY, -INFINITY};
-#pragma unroll 1
-          for (int x2 = 0; x2 < 2; ++x2) {
-            uint32_t s[32];
-            scores(x2, s);
-#pragma unroll
-            for (int e = 0; e < 32; e += 2) mx[(e >> 1) & 1] = max3(mx[(e >> 1) & 1], __uint_as_float(s[e]), __uint_as_float(s[e + 1]));
+            for (int e = 0; e < 64; ++e)
+              if (!((vis[e >> 5] >> (e & 31)) & 1u)) s[e] = __float_as_uint(-INFINITY);
           }
+          float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+          for (int e = 0; e < 64; e += 2) mx[(e >> 1) & 3] = max3(mx[(e >> 1) & 3], __uint_as_float(s[e]), __uint_as_float(s[e + 1]));
+          mx[0] = fmaxf(mx[0], mx[2]);
+          mx[1] = fmaxf(mx[1], mx[3]);
           const float top = fmaxf(mx[0], mx[1]) * rs;  // rs > 0
           // All groups add to one accumulator, so they share the rows' reference: it is settled 64 keys by 64 keys, in order, before
           // the exponentials.  It moves only when a score exceeds it by more than the threshold, or with the first score.
           const int bx = half ? x : x - 1;  // the 64 keys before are the other half of this key tile
           float ref = -INFINITY;
           if (i > 0 || half > 0) {
-            ok = mbar_wait_long(sm, &sm->settled[kTwo ? grp ^ 1 : 2 * (bx & 1) + (half ^ 1)][quarter], kTwo ? bx & 1 : (bx >> 1) & 1, a.status);
+            ok = mbar_wait(sm, &sm->settled[kTwo ? grp ^ 1 : 2 * (bx & 1) + (half ^ 1)][quarter], kTwo ? bx & 1 : (bx >> 1) & 1, a.status);
             __syncwarp();
             if (!ok) break;
             ref = sm->ref[tile][row];
@@ -486,18 +473,18 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
             if (i > 0 || half > 0) {
               // O may still be taking the keys before
               const int bu = kTwo ? bx : bx / kSBufs;
-              ok = mbar_wait_long(sm, &sm->pv_done[kTwo ? c : bx - bu * kSBufs][half ^ 1], bu & 1, a.status);
+              ok = mbar_wait(sm, &sm->pv_done[kTwo ? c : bx - bu * kSBufs][half ^ 1], bu & 1, a.status);
               __syncwarp();
               if (!ok) break;
               tc_fence_after();
 #pragma unroll 1
-              for (int x4 = 0; x4 < 4; ++x4) {
-                uint32_t o[32];
-                tmem_ld32(tmem_o + 32u * x4, o, 0);
+              for (int x8 = 0; x8 < 8; ++x8) {
+                uint32_t o[16];
+                tmem_ld16(tmem_o + 16u * x8, o);
                 tc_wait_ld();
 #pragma unroll
-                for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * alpha);
-                tmem_st32(tmem_o + 32u * x4, o, 0);
+                for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * alpha);
+                tmem_st16(tmem_o + 16u * x8, o);
               }
               tc_wait_st();
               tc_fence_before();
@@ -516,18 +503,17 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
           // Query tiles that work on the same keys would do so in step, the tensor core idle meanwhile: they take turns at the
           // exponentials, the first tile's, the second's.  (Neither is ever more than one turn ahead.)
           if (kTwo && (c == 1 || x > 0)) {
-            ok = mbar_wait_long(sm, &sm->turn[c ^ 1][quarter], (c == 1 ? x : x - 1) & 1, a.status);
+            ok = mbar_wait(sm, &sm->turn[c ^ 1][quarter], (c == 1 ? x : x - 1) & 1, a.status);
             __syncwarp();
             if (!ok) break;
           }
-#pragma unroll 1
+#pragma unroll
           for (int x2 = 0; x2 < 2; ++x2) {
-            uint32_t s[32], packed[16];
-            scores(x2, s);
+            uint32_t packed[16];
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
               float y0, y1;
-              unpair(fma2(pair_of(__uint_as_float(s[2 * e]), __uint_as_float(s[2 * e + 1])), rs2, neg_m2), y0, y1);
+              unpair(fma2(pair_of(__uint_as_float(s[32 * x2 + 2 * e]), __uint_as_float(s[32 * x2 + 2 * e + 1])), rs2, neg_m2), y0, y1);
               const float p0 = ex2(y0), p1 = ex2(y1);
               sums[e & 1] = add2(sums[e & 1], pair_of(p0, p1));
               packed[e] = pack2<false>(p0, p1);
@@ -542,7 +528,7 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
           tc_wait_st();
           tc_fence_before();
         } else {
-          if (kTwo && (c == 1 || x > 0)) ok = mbar_wait_long(sm, &sm->turn[c ^ 1][quarter], (c == 1 ? x : x - 1) & 1, a.status);
+          if (kTwo && (c == 1 || x > 0)) ok = mbar_wait(sm, &sm->turn[c ^ 1][quarter], (c == 1 ? x : x - 1) & 1, a.status);
           __syncwarp();
           if (!ok) break;
           if (lane == 0) {
@@ -556,7 +542,7 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
       // ---- the last product
       if (sg.steps > 0 && ok) {
         const int x = step + sg.steps - 1, u = kTwo ? x : x / kSBufs;
-        ok = mbar_wait_long(sm, &sm->pv_done[kTwo ? c : x - u * kSBufs][1], u & 1, a.status);
+        ok = mbar_wait(sm, &sm->pv_done[kTwo ? c : x - u * kSBufs][1], u & 1, a.status);
       }
       __syncwarp();
       tc_fence_after();
