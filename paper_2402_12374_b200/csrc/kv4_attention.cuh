@@ -163,7 +163,7 @@ __device__ __forceinline__ uint32_t kv4_window_word(const Kv4Args& a, int r, int
 
 size_t kv4_rows_workspace_bytes(const seq_tree_kv4_attention_params& p);
 int launch_kv4_rows(const seq_tree_kv4_attention_params& p, cudaStream_t stream);
-size_t kv4_tiles_workspace_bytes(const seq_tree_kv4_attention_params& p);
+size_t kv4_tiles_workspace_bytes();
 int launch_kv4_tiles(const seq_tree_kv4_attention_params& p, cudaStream_t stream);
 // Arguments that do not depend on the kernel
 Kv4Args kv4_args(const seq_tree_kv4_attention_params& p);

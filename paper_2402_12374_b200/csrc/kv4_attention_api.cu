@@ -77,7 +77,7 @@ using namespace seqtree;
 
 extern "C" size_t seq_tree_kv4_attention_workspace_bytes(const seq_tree_kv4_attention_params* p) {
   if (p == nullptr || p->num_kv_heads < 1 || p->num_q_heads < 1 || p->n_tree < 1) return 0;
-  return few_rows(*p) ? kv4_rows_workspace_bytes(*p) : kv4_tiles_workspace_bytes(*p);
+  return few_rows(*p) ? kv4_rows_workspace_bytes(*p) : kv4_tiles_workspace_bytes();
 }
 
 extern "C" int seq_tree_kv4_attention(const seq_tree_kv4_attention_params* p, void* stream) {

@@ -10,12 +10,14 @@
 // Q's channels are stored in that order too, and O's columns are put back when the rows are written.  The tree's 16-bit rows go
 // through the same warps.
 //
-// A tile of scores is worked on by two threads a row, 64 keys each.  There are four groups of 128 such threads and 512 columns of
-// tensor memory, used in one of two ways:
-//   kTwo (more than 128 rows a kv head)  a unit is 256 rows, two tiles with an S/P buffer, an accumulator and two groups each;
-//       both use every K/V tile, so that the codes are unpacked once for both.  The tiles take turns.
-//   otherwise  a unit is 128 rows with one accumulator and three S/P buffers; two groups have the even key tiles, two the odd ones.
-// Groups that add to one accumulator share the rows' reference maxima, which they settle in the keys' order (see the chains).
+// Two groups of 128 threads, a thread a row, have the even and the odd key tiles, three S/P buffers let the next tiles' scores be
+// computed meanwhile.  Both add to one accumulator and share the rows' reference maxima, which they settle in the keys' order (see
+// the groups).
+//
+// What bounds it: instruction issue.  A tile costs an SM's scheduler about 600 instructions to unpack K and V, 550 for its part of the
+// 128 x 128 exponentials, and as many again for waits, addresses and hand-overs; loops that are not unrolled, as what the
+// warps run has to stay in the instruction caches.  Two tiles of 128 rows that shared the unpacked keys had one S buffer each and
+// spent the time they saved on waiting for products (768 nodes on 4096 tokens of 64/8 heads: 204 us).
 //
 // Every mbarrier wait is bounded; one that runs out raises SEQ_DEV_TIMEOUT and the CTA drains.
 #include "kv4_attention.cuh"
@@ -23,40 +25,38 @@
 
 namespace seqtree {
 
-constexpr int kTilesThreads = 896;  // warps: loader, two issuers, one idle; four that unpack K, four V; 16 for the chains
-constexpr int kUnpackWarp = 4, kChainWarp = 12;
+constexpr int kTilesThreads = 640;  // warps: loader, two issuers, one idle; four that unpack K, four V; two groups of four for the rows
+constexpr int kUnpackWarp = 4, kGroupWarp = 12, kGroups = 2, kSBufs = 3;
 constexpr int kTilesStep = 128;     // keys
-constexpr int kRegsIssue = 24, kRegsUnpack = 48, kRegsChain = 96;  // 128 * 24 + 256 * 48 + 512 * 96 = 896 * 72
+constexpr int kRegsIssue = 40, kRegsUnpack = 56, kRegsGroup = 160;  // 128 * 40 + 256 * 56 + 256 * 160 <= 640 * 96
 constexpr int kHalfKeys = 64;       // keys of a ring stage
 constexpr int kStageBytes = kHalfKeys / kGranule * kGranuleBytes;
 constexpr int kTreeTiles = SEQ_MAX_TREE / kTilesStep;
 
-template <bool kTwo>
+constexpr int kStages = 6;
+constexpr uint32_t kTmemS = 128;  // tensor memory: O in columns 0..127, then the S/P buffers
+
 struct TilesSmem {
-  static constexpr int kStages = kTwo ? 3 : 6;
-  static constexpr int kSBufs = kTwo ? 2 : 3;
-  uint8_t q[kTwo ? 2 : 1][kTileBytes];  // tiles: 1024-byte aligned
-  uint8_t k[2][kTileBytes];             // [key tile parity]
+  uint8_t q[kTileBytes];     // tiles: 1024-byte aligned
+  uint8_t k[2][kTileBytes];  // [key tile parity]
   uint8_t v[2][kTileBytes];
   uint8_t ring[kStages][kStageBytes];
   uint64_t raw_full[kStages], raw_empty[kStages];
   uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2];
-  uint64_t q_full[2];
-  uint64_t s_full[kSBufs], p_full[kSBufs][2], pv_done[kSBufs][2];  // [S/P buffer][half of its keys]
-  uint64_t settled[4][4];  // [group][lane quarter]: the reference of the quarter's rows is settled for the group's 64 keys
-  uint64_t turn[2][4];     // [query tile][lane quarter], with kTwo: half of the tile's exponentials are under way
+  uint64_t q_full;
+  uint64_t s_full[kSBufs], p_full[kSBufs], pv_done[kSBufs];
+  uint64_t settled[kGroups][4];  // [group][lane quarter]: the reference of the quarter's rows is settled for the group's tile
   uint64_t drained[2];
-  float ref[kTwo ? 2 : 1][kTileM];  // the rows' reference maximum, handed on in the keys' order
-  float sum[4][kTileM];             // [group]: the rows' sums
-  int32_t last[2];                  // this CTA completes the unit
-  uint32_t bad[4][kTreeTiles][4];   // [segment mod 4]: tree rows whose V is not finite in half precision
+  float ref[kTileM];             // the rows' reference maximum, handed on in the keys' order
+  float sum[kGroups][kTileM];
+  int32_t last;                  // this CTA completes the unit
+  uint32_t bad[4][kTreeTiles][4];  // [segment mod 4]: tree rows whose V is not finite in half precision
   uint32_t tmem_base;
   volatile int abort_flag;
   Kv4Plan plan;
 };
-template <bool kTwo>
-constexpr size_t tiles_smem_bytes() { return sizeof(TilesSmem<kTwo>) + 1024; }
-static_assert(tiles_smem_bytes<true>() <= 227 * 1024 && tiles_smem_bytes<false>() <= 227 * 1024, "one CTA's shared memory");
+constexpr size_t kTilesSmemBytes = sizeof(TilesSmem) + 1024;
+static_assert(kTilesSmemBytes <= 227 * 1024, "one CTA's shared memory");
 
 __device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
   asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
@@ -65,12 +65,22 @@ __device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t b
 __device__ __forceinline__ void sts128(uint32_t at, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
   asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
 }
-// 16 consecutive fp32 columns of this thread's tensor-memory lane
-__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16]) {
+#define SEQ_R16(a, o) \
+  "=r"(a[o]), "=r"(a[o + 1]), "=r"(a[o + 2]), "=r"(a[o + 3]), "=r"(a[o + 4]), "=r"(a[o + 5]), "=r"(a[o + 6]), "=r"(a[o + 7]), "=r"(a[o + 8]), \
+  "=r"(a[o + 9]), "=r"(a[o + 10]), "=r"(a[o + 11]), "=r"(a[o + 12]), "=r"(a[o + 13]), "=r"(a[o + 14]), "=r"(a[o + 15])
+// Consecutive fp32 columns of this thread's tensor-memory lane, there when it returns
+__device__ __forceinline__ void tmem_get16(uint32_t taddr, uint32_t (&r)[16]) {
   asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
-      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
-        "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]) : "r"(taddr) : "memory");
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n\t"
+      "tcgen05.wait::ld.sync.aligned;"
+      : SEQ_R16(r, 0) : "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void tmem_get64(uint32_t taddr, uint32_t (&r)[64]) {
+  tmem_ld32(taddr, r, 0);
+  tmem_ld32(taddr + 32u, r, 32);
+  tc_wait_ld();
+#pragma unroll
+  for (int e = 0; e < 64; ++e) asm volatile("" : "+r"(r[e]));  // (nothing of it moves ahead of the wait)
 }
 __device__ __forceinline__ uint32_t bits_below(int x) { return x <= 0 ? 0u : (x >= 32 ? 0xffffffffu : (1u << x) - 1u); }
 
@@ -92,29 +102,21 @@ __device__ __forceinline__ TilesSeg tiles_seg(const Kv4Plan* plan, const Kv4Args
   return s;
 }
 
-template <bool kTwo, bool kBf16>
+template <bool kBf16>
 __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Args a) {
   extern __shared__ uint8_t smem_raw[];
-  using Smem = TilesSmem<kTwo>;
-  constexpr int kStages = Smem::kStages, kSBufs = Smem::kSBufs;
-  // tensor memory: the accumulators, then the S/P buffers
-  constexpr uint32_t kTmemS = kTwo ? 256 : 128;
-  Smem* sm = reinterpret_cast<Smem*>(smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u));
+  TilesSmem* sm = reinterpret_cast<TilesSmem*>(smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u));
   const int warp = uniform((int)threadIdx.x >> 5), lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
     for (int s = 0; s < kStages; ++s) { mbar_init(&sm->raw_full[s], 1); mbar_init(&sm->raw_empty[s], 8); }
     for (int b = 0; b < 2; ++b) {
-      mbar_init(&sm->k_full[b], 4); mbar_init(&sm->k_empty[b], kTwo ? 2 : 1);
-      mbar_init(&sm->v_full[b], 4); mbar_init(&sm->v_empty[b], kTwo ? 2 : 1);
-      mbar_init(&sm->q_full[b], kTwo ? 8 : 16);
-      for (int x = 0; x < 4; ++x) mbar_init(&sm->turn[b][x], 2);
+      mbar_init(&sm->k_full[b], 4); mbar_init(&sm->k_empty[b], 1);
+      mbar_init(&sm->v_full[b], 4); mbar_init(&sm->v_empty[b], 1);
       mbar_init(&sm->drained[b], 1);
     }
-    for (int b = 0; b < kSBufs; ++b) {
-      mbar_init(&sm->s_full[b], 1);
-      for (int h = 0; h < 2; ++h) { mbar_init(&sm->p_full[b][h], 4); mbar_init(&sm->pv_done[b][h], 1); }
-    }
-    for (int x = 0; x < 16; ++x) mbar_init(&sm->settled[x >> 2][x & 3], 1);
+    mbar_init(&sm->q_full, 4 * kGroups);
+    for (int b = 0; b < kSBufs; ++b) { mbar_init(&sm->s_full[b], 1); mbar_init(&sm->p_full[b], 4); mbar_init(&sm->pv_done[b], 1); }
+    for (int x = 0; x < 4 * kGroups; ++x) mbar_init(&sm->settled[x >> 2][x & 3], 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     sm->abort_flag = 0;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -185,23 +187,21 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
           for (uint32_t it = 0; it < (1u << 16); ++it)
             if (mbar_try_wait(&sm->raw_full[x % kStages], (x / kStages) & 1)) break;
     } else if (warp < 3) {
-      // ============================ issuers: one a query tile, or S (warp 1) and P V (warp 2) ============================
+      // ============================ issuers: S (warp 1), P V (warp 2) ============================
       const uint32_t idesc = (1u << 4) | ((uint32_t)(kTileM >> 4) << 24) | ((uint32_t)(kTilesStep >> 3) << 17);  // fp16, sums fp32, N = 128
       const uint32_t idesc_pv = idesc | (1u << 16);                                                             // V is MN-major
-      const int c = warp - 1;
-      const uint32_t tmem_o = kTwo ? tmem + 128u * c : tmem;
-      int step = 0, seg = 0;  // key tiles before this segment, segments
+      const uint32_t q_lo = desc_lo(smem_u32(sm->q), 16);
+      int step = 0, seg = 0, sb = 0, u = 0;  // key tiles before this segment, segments, the next tile's buffer and how often that was used
       bool ok = true;
       for (int pos = range_lo; pos < range_hi && ok; ++seg) {
         const TilesSeg sg = tiles_seg(&sm->plan, a, pos, range_hi);
-        if (kTwo || c == 0) ok = mbar_wait(sm, &sm->q_full[c], seg & 1, a.status);
-        const uint32_t q_lo = desc_lo(smem_u32(sm->q[kTwo ? c : 0]), 16);
+        if (warp == 1) ok = mbar_wait(sm, &sm->q_full, seg & 1, a.status);
         for (int i = 0; i < sg.steps && ok; ++i) {
-          const int x = step + i, b = x & 1, u = kTwo ? x : x / kSBufs, sb = kTwo ? c : x - u * kSBufs;
+          const int x = step + i, b = x & 1;
           const uint32_t sp = tmem + kTmemS + 128u * sb;
-          if (kTwo || c == 0) {
-            // S goes where an earlier tile's P was: its product has completed
-            ok = mbar_wait(sm, &sm->k_full[b], (x >> 1) & 1, a.status) && (u == 0 || mbar_wait(sm, &sm->pv_done[sb][1], (u - 1) & 1, a.status));
+          if (warp == 1) {
+            // S goes where the P of three tiles ago was: its product has completed
+            ok = mbar_wait(sm, &sm->k_full[b], (x >> 1) & 1, a.status) && (u == 0 || mbar_wait(sm, &sm->pv_done[sb], (u - 1) & 1, a.status));
             if (!ok) break;
             tc_fence_after();
             if (elect_one()) {
@@ -209,24 +209,20 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
               tc_commit(&sm->s_full[sb]);
               tc_commit(&sm->k_empty[b]);
             }
-            __syncwarp();
-          }
-          if (kTwo || c == 1) {
+          } else {
             const uint32_t v_lo = desc_lo(smem_u32(sm->v[b]), kHalfBytes);
-            ok = mbar_wait(sm, &sm->v_full[b], (x >> 1) & 1, a.status);
-#pragma unroll 1
-            for (int h = 0; h < 2 && ok; ++h) {
-              ok = mbar_wait(sm, &sm->p_full[sb][h], u & 1, a.status);
-              if (!ok) break;
-              tc_fence_after();
-              if (elect_one()) {
-                mma_pv(tmem_o, sp + 64u * h, v_lo + h * (kHalfKeys * 128 >> 4), idesc_pv, i > 0 || h > 0 ? 1u : 0u);
-                tc_commit(&sm->pv_done[sb][h]);
-                if (h == 1) tc_commit(&sm->v_empty[b]);
-              }
-              __syncwarp();
+            ok = mbar_wait(sm, &sm->v_full[b], (x >> 1) & 1, a.status) && mbar_wait(sm, &sm->p_full[sb], u & 1, a.status);
+            if (!ok) break;
+            tc_fence_after();
+            if (elect_one()) {  // (P of each half of the keys is where its scores were)
+              mma_pv(tmem, sp, v_lo, idesc_pv, i > 0 ? 1u : 0u);
+              mma_pv(tmem, sp + 64u, v_lo + (kHalfKeys * 128 >> 4), idesc_pv, 1u);
+              tc_commit(&sm->pv_done[sb]);
+              tc_commit(&sm->v_empty[b]);
             }
           }
+          __syncwarp();
+          if (++sb == kSBufs) { sb = 0; ++u; }
         }
         step += sg.steps;
         pos = sg.next;
@@ -238,7 +234,7 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
           if (mbar_try_wait(&sm->drained[warp - 1], 0)) break;
       }
     }
-  } else if (warp < kChainWarp) {
+  } else if (warp < kGroupWarp) {
     // ============================ codes, and the tree's rows, to half-precision tiles: 32 rows of K or of V a warp ============================
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsUnpack));
     const int which = (warp - kUnpackWarp) >> 2, w4 = warp & 3, quad = lane & 3, r8 = lane >> 2;
@@ -350,24 +346,19 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
       pos = sg.next;
     }
   } else {
-    // ============================ chains: two threads a row, 64 keys each ============================
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsChain));
-    // groups 0, 1: the halves of the first query tile's keys, or of even key tiles; 2, 3: of the second's, or of odd ones
-    const int grp = (warp - kChainWarp) >> 2, half = grp & 1, c = grp >> 1, quarter = warp & 3, row = quarter * 32 + lane;
-    const int tile = kTwo ? c : 0;  // the query tile, its accumulator
+    // ============================ groups: one thread a row ============================
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsGroup));
+    const int grp = (warp - kGroupWarp) >> 2;  // even or odd tiles
+    const int quarter = warp & 3, row = quarter * 32 + lane;
     const uint32_t lane_sel = (uint32_t)(quarter * 32) << 16;
-    const uint32_t tmem_o = tmem + 128u * tile + lane_sel;
-    // the groups that share a query tile
-    auto rows_sync = [&]() {
-      if (kTwo) asm volatile("bar.sync %0, 256;" ::"r"(1 + c) : "memory");
-      else asm volatile("bar.sync 1, 512;" ::: "memory");
-    };
-    int step = 0, seg = 0;  // tiles before this segment, segments with steps
+    const uint32_t tmem_o = tmem + lane_sel;
+    auto rows_sync = [&]() { asm volatile("bar.sync 1, 256;" ::: "memory"); };
+    int step = 0, seg = 0, own = 0;  // key tiles before this segment, segments with steps, tiles of this group
     bool ok = true;
     for (int pos = range_lo; pos < range_hi;) {
       const TilesSeg sg = tiles_seg(&sm->plan, a, pos, range_hi);
       const int L = sg.u.L, r = sg.u.r;
-      const int rw = sg.u.m * a.row_tile + tile * kTileM + row;
+      const int rw = sg.u.m * kTileM + row;
       const bool valid = rw < a.rows;
       const int node = min(rw, a.rows - 1) / a.group, h = sg.u.g * a.group + min(rw, a.rows - 1) % a.group;
       const bool warp_live = rw - lane < a.rows;  // (a warp of padding rows only keeps in step)
@@ -391,97 +382,92 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
             rs *= __uint_as_float((uint32_t)(127 - up) << 23);
           }
         }
-        // each group of the tile brings its share of the channels
-        constexpr int kPieces = kTwo ? 8 : 4;
-        const int from = kPieces * (kTwo ? half : grp);
-        const uint32_t line = smem_u32(sm->q[tile]) + row * 128 + (from >> 3) * kHalfBytes;
-#pragma unroll 4
-        for (int p = 0; p < kPieces; ++p) {
-          uint4 x = valid ? src[from + p] : make_uint4(0u, 0u, 0u, 0u);
+        // each group brings every other piece of eight channels
+        const uint32_t line = smem_u32(sm->q) + row * 128;
+#pragma unroll 2
+        for (int p = grp; p < 16; p += kGroups) {
+          uint4 x = valid ? src[p] : make_uint4(0u, 0u, 0u, 0u);
           if (kBf16) {
             x.x = pack2<false>(__uint_as_float(x.x << 16) * f, __uint_as_float(x.x & 0xffff0000u) * f);
             x.y = pack2<false>(__uint_as_float(x.y << 16) * f, __uint_as_float(x.y & 0xffff0000u) * f);
             x.z = pack2<false>(__uint_as_float(x.z << 16) * f, __uint_as_float(x.z & 0xffff0000u) * f);
             x.w = pack2<false>(__uint_as_float(x.w << 16) * f, __uint_as_float(x.w & 0xffff0000u) * f);
           }
-          sts128(line + ((((from + p) & 7) ^ (row & 7)) << 4), __byte_perm(x.x, x.z, 0x5410), __byte_perm(x.x, x.z, 0x7632),
+          sts128(line + (p >> 3) * kHalfBytes + (((p & 7) ^ (row & 7)) << 4), __byte_perm(x.x, x.z, 0x5410), __byte_perm(x.x, x.z, 0x7632),
                  __byte_perm(x.y, x.w, 0x5410), __byte_perm(x.y, x.w, 0x7632));
         }
         fence_async_smem();
         __syncwarp();
-        if (lane == 0) mbar_arrive(&sm->q_full[tile]);
+        if (lane == 0) mbar_arrive(&sm->q_full);
       }
       const uint32_t* mask_row = kv4_mask_row(a, r, node);
       const int depth = a.window > 0 ? kv4_depth(a, r, node) : 0;
       const int begin = a.window > 0 ? L + depth + 1 - a.window : 0;  // where the row's window begins
-
       const int latest = __reduce_max_sync(0xffffffffu, begin);
 
       float m_used = -INFINITY, l = 0.f;
-      for (int i = kTwo ? 0 : (step ^ c) & 1; i < sg.steps; i += kTwo ? 1 : 2) {
-        const int x = step + i, u = kTwo ? x : x / kSBufs, sb = kTwo ? c : x - u * kSBufs, t = sg.t0 + i;
-        const uint32_t tmem_s = tmem + kTmemS + 128u * sb + 64u * half + lane_sel;
+      for (int i = (grp ^ step) & 1; i < sg.steps; i += kGroups, ++own) {
+        const int t = sg.t0 + i, x = step + i, u = x / kSBufs, sb = x - u * kSBufs;
+        const uint32_t tmem_s = tmem + kTmemS + 128u * sb + lane_sel;
         const bool tree = t >= sg.u.prefix.steps;
-        const int key0 = (tree ? t - sg.u.prefix.steps : sg.u.prefix.key_step(t)) * kTilesStep + half * kHalfKeys;
-        uint32_t vis[2] = {0xffffffffu, 0xffffffffu};
-        const bool masked = tree || key0 + kHalfKeys > L || key0 < latest;  // some keys are not there, or not every row's
-        if (masked) {
+        const int key0 = (tree ? t - sg.u.prefix.steps : sg.u.prefix.key_step(t)) * kTilesStep;
+        const bool masked = tree || key0 + kTilesStep > L || key0 < latest;  // some keys are not there, or not every row's
+        auto hide = [&](int half, uint32_t (&s)[64]) {  // masked scores become -inf
 #pragma unroll 1
           for (int w = 0; w < 2; ++w) {
+            const int k = key0 + 64 * half + 32 * w;
             uint32_t bits;
-            if (tree) bits = kv4_window_word(a, r, L, depth, (key0 >> 5) + w, kv4_mask_word(a, mask_row, node, (key0 >> 5) + w));
-            else bits = bits_below(L - key0 - 32 * w) & (~bits_below(begin - key0 - 32 * w) | bits_below(a.sinks - key0 - 32 * w));
-            if (w) vis[1] = bits; else vis[0] = bits;
+            if (tree) bits = kv4_window_word(a, r, L, depth, k >> 5, kv4_mask_word(a, mask_row, node, k >> 5));
+            else bits = bits_below(L - k) & (~bits_below(begin - k) | bits_below(a.sinks - k));
+            if (w == 0) {
+#pragma unroll
+              for (int e = 0; e < 32; ++e)
+                if (!((bits >> e) & 1u)) s[e] = __float_as_uint(-INFINITY);
+            } else {
+#pragma unroll
+              for (int e = 0; e < 32; ++e)
+                if (!((bits >> e) & 1u)) s[32 + e] = __float_as_uint(-INFINITY);
+            }
           }
-        }
+        };
         ok = mbar_wait(sm, &sm->s_full[sb], u & 1, a.status);
         __syncwarp();
         if (!ok) break;
         if (warp_live) {
           tc_fence_after();
           uint32_t s[64];
-          tmem_ld32(tmem_s, s, 0);
-          tmem_ld32(tmem_s + 32u, s, 32);
-          tc_wait_ld();
-#pragma unroll
-          for (int e = 0; e < 64; ++e) asm volatile("" : "+r"(s[e]));  // (nothing of it moves ahead of the wait)
-          if (masked) {
-#pragma unroll
-            for (int e = 0; e < 64; ++e)
-              if (!((vis[e >> 5] >> (e & 31)) & 1u)) s[e] = __float_as_uint(-INFINITY);
-          }
           float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll 1
+          for (int half = 0; half < 2; ++half) {  // (the second half's scores stay in registers)
+            tmem_get64(tmem_s + 64u * half, s);
+            if (masked) hide(half, s);
 #pragma unroll
-          for (int e = 0; e < 64; e += 2) mx[(e >> 1) & 3] = max3(mx[(e >> 1) & 3], __uint_as_float(s[e]), __uint_as_float(s[e + 1]));
-          mx[0] = fmaxf(mx[0], mx[2]);
-          mx[1] = fmaxf(mx[1], mx[3]);
-          const float top = fmaxf(mx[0], mx[1]) * rs;  // rs > 0
-          // All groups add to one accumulator, so they share the rows' reference: it is settled 64 keys by 64 keys, in order, before
-          // the exponentials.  It moves only when a score exceeds it by more than the threshold, or with the first score.
-          const int bx = half ? x : x - 1;  // the 64 keys before are the other half of this key tile
+            for (int e = 0; e < 64; e += 2) mx[(e >> 1) & 3] = max3(mx[(e >> 1) & 3], __uint_as_float(s[e]), __uint_as_float(s[e + 1]));
+          }
+          const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * rs;  // rs > 0
+          // All groups add to one accumulator, so they share the rows' reference: it is settled tile by tile, in order, before the
+          // exponentials.  It moves only when a score exceeds it by more than the threshold, or with the first score.
           float ref = -INFINITY;
-          if (i > 0 || half > 0) {
-            ok = mbar_wait(sm, &sm->settled[kTwo ? grp ^ 1 : 2 * (bx & 1) + (half ^ 1)][quarter], kTwo ? bx & 1 : (bx >> 1) & 1, a.status);
+          if (i > 0) {
+            ok = mbar_wait(sm, &sm->settled[grp ^ 1][quarter], (own - (grp == 0)) & 1, a.status);
             __syncwarp();
             if (!ok) break;
-            ref = sm->ref[tile][row];
+            ref = sm->ref[row];
           }
           const bool move = top > ref + kRescaleThreshold || (ref == -INFINITY && top != -INFINITY);
           const float now = move ? top : ref;
-          if (__any_sync(0xffffffffu, move) || (i == 0 && half == 0)) {
+          if (__any_sync(0xffffffffu, move) || i == 0) {
             const float alpha = move && ref != -INFINITY ? ex2(ref - top) : 1.f;
-            if (i > 0 || half > 0) {
-              // O may still be taking the keys before
-              const int bu = kTwo ? bx : bx / kSBufs;
-              ok = mbar_wait(sm, &sm->pv_done[kTwo ? c : bx - bu * kSBufs][half ^ 1], bu & 1, a.status);
+            if (i > 0) {
+              // O may still be taking the tile before
+              ok = mbar_wait(sm, &sm->pv_done[sb == 0 ? kSBufs - 1 : sb - 1], (u - (sb == 0)) & 1, a.status);
               __syncwarp();
               if (!ok) break;
               tc_fence_after();
 #pragma unroll 1
               for (int x8 = 0; x8 < 8; ++x8) {
                 uint32_t o[16];
-                tmem_ld16(tmem_o + 16u * x8, o);
-                tc_wait_ld();
+                tmem_get16(tmem_o + 16u * x8, o);
 #pragma unroll
                 for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * alpha);
                 tmem_st16(tmem_o + 16u * x8, o);
@@ -489,7 +475,7 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
               tc_wait_st();
               tc_fence_before();
             }
-            sm->ref[tile][row] = now;
+            sm->ref[row] = now;
             __syncwarp();
           }
           if (lane == 0) mbar_arrive(&sm->settled[grp][quarter]);
@@ -500,26 +486,22 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
           const float neg_m = now == -INFINITY ? 0.f : -now;
           const uint64_t rs2 = pair_of(rs, rs), neg_m2 = pair_of(neg_m, neg_m);
           uint64_t sums[2] = {pair_of(0.f, 0.f), pair_of(0.f, 0.f)};
-          // Query tiles that work on the same keys would do so in step, the tensor core idle meanwhile: they take turns at the
-          // exponentials, the first tile's, the second's.  (Neither is ever more than one turn ahead.)
-          if (kTwo && (c == 1 || x > 0)) {
-            ok = mbar_wait(sm, &sm->turn[c ^ 1][quarter], (c == 1 ? x : x - 1) & 1, a.status);
-            __syncwarp();
-            if (!ok) break;
-          }
+#pragma unroll 1
+          for (int half = 1; half >= 0; --half) {
+            if (half == 0) {
+              tmem_get64(tmem_s, s);
+              if (masked) hide(0, s);
+            }
+            uint32_t packed[32];
 #pragma unroll
-          for (int x2 = 0; x2 < 2; ++x2) {
-            uint32_t packed[16];
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
+            for (int e = 0; e < 32; ++e) {
               float y0, y1;
-              unpair(fma2(pair_of(__uint_as_float(s[32 * x2 + 2 * e]), __uint_as_float(s[32 * x2 + 2 * e + 1])), rs2, neg_m2), y0, y1);
+              unpair(fma2(pair_of(__uint_as_float(s[2 * e]), __uint_as_float(s[2 * e + 1])), rs2, neg_m2), y0, y1);
               const float p0 = ex2(y0), p1 = ex2(y1);
               sums[e & 1] = add2(sums[e & 1], pair_of(p0, p1));
               packed[e] = pack2<false>(p0, p1);
             }
-            tmem_st16(tmem_s + 16u * x2, packed);  // over scores that have been read
-            if (kTwo && x2 == 0 && lane == 0) mbar_arrive(&sm->turn[c][quarter]);
+            tmem_st32(tmem_s + 64u * half, packed, 0);  // over scores that have been read
           }
           float s0, s1, s2, s3;
           unpair(sums[0], s0, s1);
@@ -527,22 +509,16 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
           l += (s0 + s1) + (s2 + s3);
           tc_wait_st();
           tc_fence_before();
-        } else {
-          if (kTwo && (c == 1 || x > 0)) ok = mbar_wait(sm, &sm->turn[c ^ 1][quarter], (c == 1 ? x : x - 1) & 1, a.status);
-          __syncwarp();
-          if (!ok) break;
-          if (lane == 0) {
-            if (kTwo) mbar_arrive(&sm->turn[c][quarter]);
-            mbar_arrive(&sm->settled[grp][quarter]);
-          }
+        } else if (lane == 0) {
+          mbar_arrive(&sm->settled[grp][quarter]);
         }
         __syncwarp();
-        if (lane == 0) mbar_arrive(&sm->p_full[sb][half]);
+        if (lane == 0) mbar_arrive(&sm->p_full[sb]);
       }
       // ---- the last product
       if (sg.steps > 0 && ok) {
-        const int x = step + sg.steps - 1, u = kTwo ? x : x / kSBufs;
-        ok = mbar_wait(sm, &sm->pv_done[kTwo ? c : x - u * kSBufs][1], u & 1, a.status);
+        const int x = step + sg.steps - 1, u = x / kSBufs;
+        ok = mbar_wait(sm, &sm->pv_done[x - u * kSBufs], u & 1, a.status);
       }
       __syncwarp();
       tc_fence_after();
@@ -558,44 +534,38 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
         }
       }
       // ---- the groups' sums, against the reference that O ended in: the last one settled
-      float M = any ? sm->ref[tile][row] : -INFINITY;
+      float M = any ? sm->ref[row] : -INFINITY;
       sm->sum[grp][row] = poison != 0 ? NAN : m_used == -INFINITY ? l : l * ex2(m_used - M);
       rows_sync();
-      float sum = sm->sum[2 * tile][row] + sm->sum[2 * tile + 1][row];
-      if (!kTwo) sum += sm->sum[2][row] + sm->sum[3][row];
-      // A group writes 64 columns of its tile's O, or 32, 32 at a time.
-      constexpr int kRuns = kTwo ? 2 : 1;
-      const int first_run = kRuns * (kTwo ? half : grp);
+      float sum = sm->sum[0][row] + sm->sum[1][row];
       bool complete = sg.whole;
       Kv4Pieces pieces = {0, 0};
       if (!sg.whole) {
         // This CTA's piece goes to the workspace and is counted; the one that counts the last piece adds them all, in the order
         // of their CTAs, and writes the rows.  Nobody waits for anybody.
         pieces = kv4_pieces(ranges, sg.u);
-        const int64_t mine = (int64_t)kv4_slot(ranges, blockIdx.x, sg.u.begin) * a.row_tile + tile * kTileM;
+        const int64_t mine = (int64_t)kv4_slot(ranges, blockIdx.x, sg.u.begin) * kTileM;
 #pragma unroll 1
-        for (int run = first_run; run < first_run + kRuns; ++run) {
-          float o[32];
-          tmem_ld32(tmem_o + 32u * run, reinterpret_cast<uint32_t*>(o), 0);
-          tc_wait_ld();
-          float4* to = reinterpret_cast<float4*>(a.ws_o + mine * kHeadDim) + (8 * run) * kTileM + row;  // [channel / 4][row]
+        for (int run = grp; run < 8; run += kGroups) {  // 16 columns of O, unnormalised
+          uint32_t o[16];
+          tmem_get16(tmem_o + 16u * run, o);
+          uint4* to = reinterpret_cast<uint4*>(a.ws_o + mine * kHeadDim) + (4 * run) * kTileM + row;  // [channel / 4][row]
 #pragma unroll
-          for (int e = 0; e < 32; e += 4) to[(e >> 2) * kTileM] = any ? make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]) : make_float4(0.f, 0.f, 0.f, 0.f);
+          for (int e = 0; e < 16; e += 4) to[(e >> 2) * kTileM] = any ? make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]) : make_uint4(0u, 0u, 0u, 0u);
         }
-        if (half == 0 && (kTwo || c == 0)) a.ws_ml[mine + row] = make_float2(M, sum);
+        if (grp == 0) a.ws_ml[mine + row] = make_float2(M, sum);
         __threadfence();
         rows_sync();
-        if (half == 0 && (kTwo || c == 0) && row == 0) sm->last[tile] = atomicAdd(a.ws_count + 2 * pieces.first + tile, 1) == pieces.last - pieces.first;
+        if (grp == 0 && row == 0) sm->last = atomicAdd(a.ws_count + 2 * pieces.first, 1) == pieces.last - pieces.first;
         rows_sync();
-        complete = sm->last[tile] != 0;
+        complete = sm->last != 0;
         if (complete) {
           __threadfence();
           M = -INFINITY;
-          for (int x = pieces.first; x <= pieces.last; ++x)
-            M = fmaxf(M, __ldcg(a.ws_ml + (int64_t)kv4_slot(ranges, x, sg.u.begin) * a.row_tile + tile * kTileM + row).x);
+          for (int x = pieces.first; x <= pieces.last; ++x) M = fmaxf(M, __ldcg(a.ws_ml + (int64_t)kv4_slot(ranges, x, sg.u.begin) * kTileM + row).x);
           sum = 0.f;
           for (int x = pieces.first; x <= pieces.last; ++x) {
-            const float2 ml = __ldcg(a.ws_ml + (int64_t)kv4_slot(ranges, x, sg.u.begin) * a.row_tile + tile * kTileM + row);
+            const float2 ml = __ldcg(a.ws_ml + (int64_t)kv4_slot(ranges, x, sg.u.begin) * kTileM + row);
             sum = fmaf(ml.y, ml.x == -INFINITY ? 0.f : ex2(ml.x - M), sum);
           }
         }
@@ -603,45 +573,46 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
       if (complete) {
         const float inv = 1.f / sum;
 #pragma unroll 1
-        for (int run = first_run; run < first_run + kRuns; ++run) {
-          float o[32];
+        for (int run = grp; run < 8; run += kGroups) {
+          uint32_t o[16];
           if (sg.whole) {
-            tmem_ld32(tmem_o + 32u * run, reinterpret_cast<uint32_t*>(o), 0);
-            tc_wait_ld();
+            tmem_get16(tmem_o + 16u * run, o);
           } else {
+            float acc[16];
 #pragma unroll
-            for (int e = 0; e < 32; ++e) o[e] = 0.f;
+            for (int e = 0; e < 16; ++e) acc[e] = 0.f;
 #pragma unroll 1
             for (int x = pieces.first; x <= pieces.last; ++x) {
-              const int64_t at = (int64_t)kv4_slot(ranges, x, sg.u.begin) * a.row_tile + tile * kTileM;
+              const int64_t at = (int64_t)kv4_slot(ranges, x, sg.u.begin) * kTileM;
               const float mx = __ldcg(a.ws_ml + at + row).x;
               const float f = mx == -INFINITY ? 0.f : ex2(mx - M);
-              const float4* from = reinterpret_cast<const float4*>(a.ws_o + at * kHeadDim) + (8 * run) * kTileM + row;
+              const float4* from = reinterpret_cast<const float4*>(a.ws_o + at * kHeadDim) + (4 * run) * kTileM + row;
 #pragma unroll
-              for (int e = 0; e < 32; e += 4) {
+              for (int e = 0; e < 16; e += 4) {
                 const float4 v = __ldcg(from + (e >> 2) * kTileM);
-                o[e] = fmaf(v.x, f, o[e]);
-                o[e + 1] = fmaf(v.y, f, o[e + 1]);
-                o[e + 2] = fmaf(v.z, f, o[e + 2]);
-                o[e + 3] = fmaf(v.w, f, o[e + 3]);
+                acc[e] = fmaf(v.x, f, acc[e]);
+                acc[e + 1] = fmaf(v.y, f, acc[e + 1]);
+                acc[e + 2] = fmaf(v.z, f, acc[e + 2]);
+                acc[e + 3] = fmaf(v.w, f, acc[e + 3]);
               }
             }
+#pragma unroll
+            for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(acc[e]);
           }
           if (valid) {
-            uint8_t* out = a.out + r * a.o_req + node * a.o_tok + h * a.o_head + 64 * run;
+            uint8_t* out = a.out + r * a.o_req + node * a.o_tok + h * a.o_head + 32 * run;
 #pragma unroll
-            for (int e = 0; e < 32; e += 8) {  // columns 0,2,4,6,1,3,5,7 are channels 0..7
-              uint4 val;
-              val.x = pack2<kBf16>(o[e] * inv, o[e + 2] * inv);
-              val.y = pack2<kBf16>(o[e + 4] * inv, o[e + 6] * inv);
-              val.z = pack2<kBf16>(o[e + 1] * inv, o[e + 3] * inv);
-              val.w = pack2<kBf16>(o[e + 5] * inv, o[e + 7] * inv);
-              *reinterpret_cast<uint4*>(out + 2 * e) = val;
+            for (int e = 0; e < 16; e += 8) {  // columns 0,2,4,6,1,3,5,7 are channels 0..7
+              float y[8];
+#pragma unroll
+              for (int z = 0; z < 8; ++z) y[z] = __uint_as_float(o[e + z]) * inv;
+              *reinterpret_cast<uint4*>(out + 2 * e) =
+                  make_uint4(pack2<kBf16>(y[0], y[2]), pack2<kBf16>(y[4], y[6]), pack2<kBf16>(y[1], y[3]), pack2<kBf16>(y[5], y[7]));
             }
           }
           __syncwarp();
         }
-        if (valid && half == 0 && (kTwo || c == 0) && a.lse != nullptr) a.lse[((int64_t)r * a.Hq + h) * a.n + node] = (M + log2f(sum)) * kLn2;
+        if (valid && grp == 0 && a.lse != nullptr) a.lse[((int64_t)r * a.Hq + h) * a.n + node] = (M + log2f(sum)) * kLn2;
       }
       tc_fence_before();
       rows_sync();  // the accumulator is read, the rows are through with Q and with what they exchanged
@@ -659,19 +630,16 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
 }
 
 // ---------------------------------------------------------------- host side ---------------------
-static bool tiles_two(const seq_tree_kv4_attention_params& p) { return p.n_tree * (p.num_q_heads / p.num_kv_heads) > kTileM; }
-
-size_t kv4_tiles_workspace_bytes(const seq_tree_kv4_attention_params& p) {
+size_t kv4_tiles_workspace_bytes() {
   const size_t sms = device_sm_count();
-  return kv4_count_bytes(sms) + 2 * sms * (tiles_two(p) ? 2 : 1) * kTileM * (kHeadDim * sizeof(float) + sizeof(float2));
+  return kv4_count_bytes(sms) + 2 * sms * kTileM * (kHeadDim * sizeof(float) + sizeof(float2));
 }
 
 int launch_kv4_tiles(const seq_tree_kv4_attention_params& p, cudaStream_t stream) {
-  const bool two = tiles_two(p);
   const int sms = device_sm_count();
   Kv4Args a = kv4_args(p);
-  a.row_tile = two ? 2 * kTileM : kTileM;
-  a.tiles = (a.rows + a.row_tile - 1) / a.row_tile;
+  a.row_tile = kTileM;
+  a.tiles = (a.rows + kTileM - 1) / kTileM;
   a.tree_steps = (a.n + kTilesStep - 1) / kTilesStep;
   a.min_steps = 2;
   const int64_t most = (int64_t)a.batch * a.Hkv * a.tiles * ((p.max_len + kTilesStep - 1) / kTilesStep + 1 + a.tree_steps);
@@ -680,32 +648,30 @@ int launch_kv4_tiles(const seq_tree_kv4_attention_params& p, cudaStream_t stream
   a.ctas = want < sms ? (int)want : sms;
   a.ws_count = static_cast<int32_t*>(p.workspace);
   a.ws_o = reinterpret_cast<float*>(static_cast<uint8_t*>(p.workspace) + kv4_count_bytes(sms));
-  a.ws_ml = reinterpret_cast<float2*>(a.ws_o + (size_t)2 * sms * a.row_tile * kHeadDim);
+  a.ws_ml = reinterpret_cast<float2*>(a.ws_o + (size_t)2 * sms * kTileM * kHeadDim);
   const int rc0 = launch_kv4_zero(a, stream);
   if (rc0 != SEQ_OK) return rc0;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(a.ctas);
   cfg.blockDim = dim3(kTilesThreads);
+  cfg.dynamicSmemBytes = kTilesSmemBytes;
   cfg.stream = stream;
   cudaLaunchAttribute early[1];
   early[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   early[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = early;
   cfg.numAttrs = 1;
-  auto launch = [&](auto kernel, int which, size_t smem) -> int {
-    static int done[4][64];
+  auto launch = [&](auto kernel, int which) -> int {
+    static int done[2][64];
     const int rc = once_per_device(done[which], [&]() -> int {
-      SEQ_CUDA_OK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+      SEQ_CUDA_OK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kTilesSmemBytes));
       return SEQ_OK;
     });
     if (rc != SEQ_OK) return rc;
-    cfg.dynamicSmemBytes = smem;
     SEQ_CUDA_OK(cudaLaunchKernelEx(&cfg, kernel, a));
     return SEQ_OK;
   };
-  const bool bf16 = p.dtype == SEQ_BF16;
-  if (two) return bf16 ? launch(kv4_tiles_kernel<true, true>, 0, tiles_smem_bytes<true>()) : launch(kv4_tiles_kernel<true, false>, 1, tiles_smem_bytes<true>());
-  return bf16 ? launch(kv4_tiles_kernel<false, true>, 2, tiles_smem_bytes<false>()) : launch(kv4_tiles_kernel<false, false>, 3, tiles_smem_bytes<false>());
+  return p.dtype == SEQ_BF16 ? launch(kv4_tiles_kernel<true>, 0) : launch(kv4_tiles_kernel<false>, 1);
 }
 
 }  // namespace seqtree
