@@ -4,8 +4,7 @@
 // A unit is (request, kv head, tile of query rows); a row is a (node, head in group) pair.  A unit's keys come in steps: those of the prefix that
 // some row can see (the sinks, then the window: the steps in between are left out), then the tree's.  The steps of all
 // units are laid end to end and cut into equal ranges, one a CTA, whatever lengths the requests have.  A unit inside one range is
-// finished there; the pieces of one that is cut go to the workspace, and the CTA that leaves the last of them adds them in the
-// order of their CTAs.
+// finished there; the pieces of one that is cut go to the workspace, and a second kernel adds them, in the order of their CTAs.
 #pragma once
 
 #include "kv4.cuh"
@@ -25,7 +24,7 @@ struct Kv4Args {
   const uint32_t* mask; int32_t mask_wpr; int64_t mask_req;
   uint8_t* out; int64_t o_req, o_tok, o_head;
   float* lse;
-  int32_t* ws_count;  // [2 * ctas] pieces left of a unit that begins in the CTA's range: zero when the kernel starts
+  int4* ws_cut;       // [ctas] the unit that begins in the CTA's range and is cut: (unit or -1, its first piece's slot, its last CTA)
   float2* ws_ml;      // [2 * ctas][row_tile] (m, l): reference maximum (log2 units) and sum of a piece
   float* ws_o;        // [2 * ctas][row_tile][128] its unnormalised rows
   float scale_log2;
@@ -87,12 +86,16 @@ __device__ __forceinline__ void kv4_plan(Kv4Plan* plan, const Kv4Args& a) {
 
 // The ranges: no more than one for every min_steps steps.
 struct Kv4Ranges {
-  int32_t total, ctas;
-  __device__ __forceinline__ int lo(int c) const { return (int)((int64_t)total * c / ctas); }
+  int32_t total, ctas, base, extra;  // base positions each, one more in the first `extra`
+  __device__ __forceinline__ int lo(int c) const { return c * base + min(c, extra); }
+  __device__ __forceinline__ int at(int pos) const {  // the CTA that has pos
+    const int longer = extra * (base + 1);
+    return pos < longer ? pos / (base + 1) : extra + (pos - longer) / base;
+  }
 };
 __device__ __forceinline__ Kv4Ranges kv4_ranges(const Kv4Plan* plan, const Kv4Args& a) {
-  const int total = plan->start[a.batch];
-  return {total, max(1, min(a.ctas, (total + a.min_steps - 1) / a.min_steps))};
+  const int total = plan->start[a.batch], ctas = max(1, min(a.ctas, (total + a.min_steps - 1) / a.min_steps));
+  return {total, ctas, total / ctas, total % ctas};
 }
 
 struct Kv4Unit {
@@ -119,17 +122,11 @@ __device__ __forceinline__ Kv4Unit kv4_unit(const Kv4Plan* plan, const Kv4Args& 
   return u;
 }
 // Where CTA c leaves its piece of a unit that begins at `begin`: the piece that opens its range, or the one that closes it.
-__device__ __forceinline__ int kv4_slot(const Kv4Ranges& ranges, int c, int begin) { return 2 * c + (max(begin, ranges.lo(c)) == ranges.lo(c) ? 0 : 1); }
+__device__ __forceinline__ int kv4_slot(const Kv4Ranges& ranges, int c, int begin) { return 2 * c + (begin <= ranges.lo(c) ? 0 : 1); }
 
-// The CTAs whose ranges hold a unit's steps
-struct Kv4Pieces { int32_t first, last; };
-__device__ __forceinline__ Kv4Pieces kv4_pieces(const Kv4Ranges& ranges, const Kv4Unit& u) {
-  Kv4Pieces p;
-  p.first = blockIdx.x;
-  while (ranges.lo(p.first) > u.begin) --p.first;
-  p.last = blockIdx.x;
-  while (p.last + 1 < ranges.ctas && ranges.lo(p.last + 1) < u.end) ++p.last;
-  return p;
+// The unit that a CTA's last segment begins and that goes on behind its range (the merge's later pieces are in slots 2 c)
+__device__ __forceinline__ int4 kv4_cut(const Kv4Args& a, const Kv4Ranges& ranges, const Kv4Unit& u) {
+  return make_int4((u.r * a.Hkv + u.g) * a.tiles + u.m, kv4_slot(ranges, blockIdx.x, u.begin), ranges.at(u.end - 1), 0);
 }
 
 __device__ __forceinline__ const uint32_t* kv4_mask_row(const Kv4Args& a, int r, int node) {
@@ -167,8 +164,14 @@ size_t kv4_tiles_workspace_bytes();
 int launch_kv4_tiles(const seq_tree_kv4_attention_params& p, cudaStream_t stream);
 // Arguments that do not depend on the kernel
 Kv4Args kv4_args(const seq_tree_kv4_attention_params& p);
-// Zeroes the counts
-int launch_kv4_zero(const Kv4Args& a, cudaStream_t stream);
-inline size_t kv4_count_bytes(size_t ctas) { return (2 * ctas * sizeof(int32_t) + 255) & ~(size_t)255; }
+// Adds the pieces of the units that are cut.  tiles: which kernel left them.
+int launch_kv4_merge(const Kv4Args& a, bool bf16, bool tiles, cudaStream_t stream);
+// The workspace's parts: ws_o, ws_ml, ws_cut
+inline size_t kv4_ranges_bytes(size_t ctas, size_t row_tile) { return ctas * (2 * row_tile * (kHeadDim * sizeof(float) + sizeof(float2)) + sizeof(int4)); }
+inline void kv4_ranges_place(Kv4Args& a, size_t ctas, void* workspace) {
+  a.ws_o = static_cast<float*>(workspace);
+  a.ws_ml = reinterpret_cast<float2*>(a.ws_o + 2 * ctas * a.row_tile * kHeadDim);
+  a.ws_cut = reinterpret_cast<int4*>(a.ws_ml + 2 * ctas * a.row_tile);
+}
 
 }  // namespace seqtree

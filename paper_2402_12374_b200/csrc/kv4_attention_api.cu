@@ -1,28 +1,77 @@
 // seq_tree_kv4_attention: checks and the choice of kernel.
 #include "kv4_attention.cuh"
+#include "umma.cuh"
 
 namespace seqtree {
 
-// A kernel of one's own, not a memset: it is scheduled under the tail of the launch before and lets the attention's set-up run
-// under itself.
-__global__ void kv4_zero_kernel(int32_t* words, int n) {
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+// The pieces of the units that are cut.  A CTA has some rows of one unit (16 of the tiles kernel's, whose pieces are [channel / 4][row], 8 of the
+// other's, [row][channel]), a thread eight channels of a row, or twice eight; four pieces are on their way at once.
+// The launch behind it is not let in early: its CTAs took the places that these leave first and were spread unevenly (32 requests of 8192
+// tokens, launch after launch: 54 us, 74 with it).
+template <bool kBf16, bool kTiles>
+__global__ void __launch_bounds__(128) kv4_merge_kernel(const Kv4Args a) {
+  constexpr int kRows = kTiles ? 16 : 8, kSets = kTiles ? 2 : 1;
+  const int slices = a.row_tile / kRows, c = blockIdx.x / slices;
+  const int x = threadIdx.x & 15, y = threadIdx.x >> 4;
+  const int row = (blockIdx.x - c * slices) * kRows + (kTiles ? x : y), set = kTiles ? y : x;
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  for (int i = threadIdx.x; i < n; i += blockDim.x) words[i] = 0;
+  const int4 cut = a.ws_cut[c];
+  const int rg = cut.x / a.tiles, rw = (cut.x - rg * a.tiles) * a.row_tile + row;
+  if (cut.x < 0 || rw >= a.rows) return;
+  const int pieces = cut.z - c + 1;
+  auto piece = [&](int p) -> int64_t { return (int64_t)(p == 0 ? cut.y : 2 * (c + p)) * a.row_tile; };
+  float M = -INFINITY, sum = 0.f;
+#pragma unroll 4
+  for (int p = 0; p < pieces; ++p) M = fmaxf(M, a.ws_ml[piece(p) + row].x);
+  float o[kSets][8];
+#pragma unroll
+  for (int s = 0; s < kSets; ++s)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) o[s][e] = 0.f;
+#pragma unroll 4
+  for (int p = 0; p < pieces; ++p) {
+    const float2 ml = a.ws_ml[piece(p) + row];
+    const float4* from = reinterpret_cast<const float4*>(a.ws_o + piece(p) * kHeadDim);
+    const float f = ml.x == -INFINITY ? 0.f : ex2(ml.x - M);
+    sum = fmaf(ml.y, f, sum);
+#pragma unroll
+    for (int s = 0; s < kSets; ++s)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int quad = 2 * (set + 8 * s) + e;
+        const float4 v = from[kTiles ? quad * a.row_tile + row : row * (kHeadDim / 4) + quad];
+        o[s][4 * e] = fmaf(v.x, f, o[s][4 * e]);
+        o[s][4 * e + 1] = fmaf(v.y, f, o[s][4 * e + 1]);
+        o[s][4 * e + 2] = fmaf(v.z, f, o[s][4 * e + 2]);
+        o[s][4 * e + 3] = fmaf(v.w, f, o[s][4 * e + 3]);
+      }
+  }
+  const float inv = 1.f / sum;
+  const int r = rg / a.Hkv, nd = rw / a.group, h = (rg - r * a.Hkv) * a.group + rw - nd * a.group;
+  uint8_t* out = a.out + r * a.o_req + nd * a.o_tok + h * a.o_head;
+#pragma unroll
+  for (int s = 0; s < kSets; ++s) {
+    float z[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) z[e] = o[s][kTiles ? ((e & 3) << 1) + (e >> 2) : e] * inv;  // (the tiles' columns are channels 0,4,1,5,2,6,3,7)
+    *reinterpret_cast<uint4*>(out + 16 * (set + 8 * s)) = make_uint4(pack2<kBf16>(z[0], z[1]), pack2<kBf16>(z[2], z[3]), pack2<kBf16>(z[4], z[5]), pack2<kBf16>(z[6], z[7]));
+  }
+  if (a.lse != nullptr && set == 0) a.lse[((int64_t)r * a.Hq + h) * a.n + nd] = (M + log2f(sum)) * kLn2;
 }
 
-int launch_kv4_zero(const Kv4Args& a, cudaStream_t stream) {
+int launch_kv4_merge(const Kv4Args& a, bool bf16, bool tiles, cudaStream_t stream) {
   if (a.ctas < 2) return SEQ_OK;  // nothing is cut
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(1);
-  cfg.blockDim = dim3(512);
+  cfg.gridDim = dim3((a.ctas - 1) * (a.row_tile / (tiles ? 16 : 8)));  // (nothing that begins in the last range is)
+  cfg.blockDim = dim3(128);
   cfg.stream = stream;
   cudaLaunchAttribute early[1];
   early[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   early[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = early;
   cfg.numAttrs = 1;
-  SEQ_CUDA_OK(cudaLaunchKernelEx(&cfg, kv4_zero_kernel, a.ws_count, 2 * a.ctas));
+  SEQ_CUDA_OK(cudaLaunchKernelEx(&cfg, bf16 ? (tiles ? kv4_merge_kernel<true, true> : kv4_merge_kernel<true, false>)
+                                            : (tiles ? kv4_merge_kernel<false, true> : kv4_merge_kernel<false, false>), a));
   return SEQ_OK;
 }
 

@@ -35,7 +35,6 @@ struct RowsSmem {
   float2 ml[kRowsWarps][8 * NT];
   uint64_t full[kRowsWarps][kStages];
   volatile int abort_flag;
-  int32_t last;  // this CTA completes the unit
   int32_t begin[8 * NT];  // where the rows' windows begin
   Kv4Plan plan;
 };
@@ -195,7 +194,7 @@ __global__ void __launch_bounds__(32 * kRowsWarps, NT == 1 ? 3 : 2) kv4_rows_ker
   }
   asm volatile("griddepcontrol.wait;" ::: "memory");
   // The CTA's range of positions: of all units', or of its cluster's unit, which starts at 0.
-  Kv4Ranges ranges = {0, 1};
+  Kv4Ranges ranges = {0, 1, 0, 0};
   Kv4Unit own = {};
   int range_lo, range_hi;
   if (kCluster) {
@@ -214,6 +213,7 @@ __global__ void __launch_bounds__(32 * kRowsWarps, NT == 1 ? 3 : 2) kv4_rows_ker
   } else {
     kv4_plan<kKeys, 32 * kRowsWarps>(&sm->plan, a);
     ranges = kv4_ranges(&sm->plan, a);
+    if (threadIdx.x == 0) a.ws_cut[blockIdx.x] = make_int4(-1, 0, 0, 0);
     if ((int)blockIdx.x >= ranges.ctas || ranges.total == 0) return;
     range_lo = ranges.lo(blockIdx.x);
     range_hi = ranges.lo(blockIdx.x + 1);
@@ -685,45 +685,7 @@ __global__ void __launch_bounds__(32 * kRowsWarps, NT == 1 ? 3 : 2) kv4_rows_ker
       rows_cluster_sync();  // nobody's rows are read any more
       break;
     }
-    if (!whole) {
-      // The piece is counted; the CTA that counts the last one adds them all, in the order of their CTAs.  Nobody waits.
-      const Kv4Pieces pieces = kv4_pieces(ranges, u);
-      __threadfence();
-      __syncthreads();
-      if (threadIdx.x == 0) sm->last = atomicAdd(a.ws_count + 2 * pieces.first, 1) == pieces.last - pieces.first;
-      __syncthreads();
-      if (sm->last) {
-        __threadfence();
-#pragma unroll 1
-        for (int row = warp; row < live_rows; row += kRowsWarps) {
-          // 32 pieces at a time: a lane looks one's (m, l) up, then all add its rows
-          float M = -INFINITY, sum = 0.f;
-          float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-          for (int p0 = pieces.first; p0 <= pieces.last; p0 += 32) {
-            const int n = min(32, pieces.last - p0 + 1);
-            float2 ml = make_float2(-INFINITY, 0.f);
-            int at = 0;
-            if (lane < n) {
-              at = kv4_slot(ranges, p0 + lane, u.begin) * a.row_tile + row;
-              ml = __ldcg(a.ws_ml + at);
-            }
-            const float now = fmaxf(M, warp_max(ml.x)), old = M == -INFINITY ? 0.f : ex2(M - now);
-            M = now;
-            const float f = ml.x == -INFINITY ? 0.f : ex2(ml.x - M);
-            sum = sum * old + warp_sum(ml.y * f);
-            acc.x *= old; acc.y *= old; acc.z *= old; acc.w *= old;
-#pragma unroll 4
-            for (int p = 0; p < n; ++p) {
-              const int64_t from = __shfl_sync(0xffffffffu, at, p);
-              const float4 v = __ldcg(reinterpret_cast<const float4*>(a.ws_o + from * kHeadDim) + lane);
-              const float w = __shfl_sync(0xffffffffu, f, p);
-              acc.x = fmaf(v.x, w, acc.x); acc.y = fmaf(v.y, w, acc.y); acc.z = fmaf(v.z, w, acc.z); acc.w = fmaf(v.w, w, acc.w);
-            }
-          }
-          write_row(row, M, sum, acc);
-        }
-      }
-    }
+    if (threadIdx.x == 0 && seg_end < u.end && pos == u.begin) a.ws_cut[blockIdx.x] = kv4_cut(a, ranges, u);
     __syncthreads();
     pos = seg_end;
   }
@@ -762,7 +724,7 @@ static int rows_cluster(const seq_tree_kv4_attention_params& p) {
 size_t kv4_rows_workspace_bytes(const seq_tree_kv4_attention_params& p) {
   if (rows_cluster(p) != 0) return 0;
   const int nt = rows_nt(p);
-  return kv4_count_bytes(rows_ctas(nt)) + (size_t)2 * rows_ctas(nt) * 8 * nt * (kHeadDim * sizeof(float) + sizeof(float2));
+  return kv4_ranges_bytes(rows_ctas(nt), 8 * nt);
 }
 
 int launch_kv4_rows(const seq_tree_kv4_attention_params& p, cudaStream_t stream) {
@@ -792,12 +754,8 @@ int launch_kv4_rows(const seq_tree_kv4_attention_params& p, cudaStream_t stream)
     if (most > 0x7fffffff) return SEQ_ERR_UNSUPPORTED;
     const int64_t want = (most + a.min_steps - 1) / a.min_steps;
     a.ctas = want < rows_ctas(nt) ? (int)want : rows_ctas(nt);
-    a.ws_count = static_cast<int32_t*>(p.workspace);
-    a.ws_o = reinterpret_cast<float*>(static_cast<uint8_t*>(p.workspace) + kv4_count_bytes(rows_ctas(nt)));
-    a.ws_ml = reinterpret_cast<float2*>(a.ws_o + (size_t)2 * rows_ctas(nt) * a.row_tile * kHeadDim);
+    kv4_ranges_place(a, rows_ctas(nt), p.workspace);
     cfg.gridDim = dim3(a.ctas);
-    const int rc = launch_kv4_zero(a, stream);
-    if (rc != SEQ_OK) return rc;
   }
   auto launch = [&](auto kernel, int which, size_t smem) -> int {
     static int done[8][64];
@@ -815,8 +773,10 @@ int launch_kv4_rows(const seq_tree_kv4_attention_params& p, cudaStream_t stream)
     if (nt == 1) return bf16 ? launch(kv4_rows_kernel<1, true, true>, 0, s1) : launch(kv4_rows_kernel<1, false, true>, 1, s1);
     return bf16 ? launch(kv4_rows_kernel<2, true, true>, 2, s2) : launch(kv4_rows_kernel<2, false, true>, 3, s2);
   }
-  if (nt == 1) return bf16 ? launch(kv4_rows_kernel<1, true, false>, 4, s1) : launch(kv4_rows_kernel<1, false, false>, 5, s1);
-  return bf16 ? launch(kv4_rows_kernel<2, true, false>, 6, s2) : launch(kv4_rows_kernel<2, false, false>, 7, s2);
+  int rc;
+  if (nt == 1) rc = bf16 ? launch(kv4_rows_kernel<1, true, false>, 4, s1) : launch(kv4_rows_kernel<1, false, false>, 5, s1);
+  else rc = bf16 ? launch(kv4_rows_kernel<2, true, false>, 6, s2) : launch(kv4_rows_kernel<2, false, false>, 7, s2);
+  return rc != SEQ_OK ? rc : launch_kv4_merge(a, bf16, false, stream);
 }
 
 }  // namespace seqtree

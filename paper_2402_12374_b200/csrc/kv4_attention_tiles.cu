@@ -49,7 +49,7 @@ struct TilesSmem {
   uint64_t drained[2];
   float ref[kTileM];             // the rows' reference maximum, handed on in the keys' order
   float sum[kGroups][kTileM];
-  int32_t last;                  // this CTA completes the unit
+  uint32_t top[kGroups][kTileM]; // q's largest magnitudes
   uint32_t bad[4][kTreeTiles][4];  // [segment mod 4]: tree rows whose V is not finite in half precision
   uint32_t tmem_base;
   volatile int abort_flag;
@@ -133,6 +133,14 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
   const uint32_t tmem = uniform(sm->tmem_base);
   const Kv4Ranges ranges = kv4_ranges(&sm->plan, a);
   const bool works = (int)blockIdx.x < ranges.ctas && ranges.total > 0;
+  if (warp == 3 && lane == 0 && (int)blockIdx.x < a.ctas) {
+    int4 cut = make_int4(-1, 0, 0, 0);
+    if (works) {
+      const Kv4Unit u = kv4_unit<kTilesStep>(&sm->plan, a, ranges.lo(blockIdx.x + 1) - 1);
+      if (u.begin >= ranges.lo(blockIdx.x) && u.end > ranges.lo(blockIdx.x + 1)) cut = kv4_cut(a, ranges, u);
+    }
+    a.ws_cut[blockIdx.x] = cut;
+  }
   const int range_lo = works ? ranges.lo(blockIdx.x) : 0, range_hi = works ? ranges.lo(blockIdx.x + 1) : 0;
 
   if (warp < 4) {
@@ -365,36 +373,36 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
       // ---- q: half precision (a bfloat16 row scaled by a power of two, exactly), channels in the codes' order
       float rs = a.scale_log2;
       {
-        const uint4* src = reinterpret_cast<const uint4*>(a.q + r * a.q_req + node * a.q_tok + h * a.q_head);
+        // each group brings every other piece of eight channels
+        const uint4* src = reinterpret_cast<const uint4*>(a.q + r * a.q_req + node * a.q_tok + h * a.q_head) + grp;
+        uint4 x[8];
+#pragma unroll
+        for (int p = 0; p < 8; ++p) x[p] = valid ? src[p * kGroups] : make_uint4(0u, 0u, 0u, 0u);
         float f = 1.f;
         if (kBf16) {
           uint32_t top = 0;
-#pragma unroll 4
-          for (int p = 0; p < 16; ++p) {
-            const uint4 x = src[p];
-            top = max(max(top, max((x.x << 16) & 0x7fffffffu, x.x & 0x7fff0000u)), max((x.y << 16) & 0x7fffffffu, x.y & 0x7fff0000u));
-            top = max(max(top, max((x.z << 16) & 0x7fffffffu, x.z & 0x7fff0000u)), max((x.w << 16) & 0x7fffffffu, x.w & 0x7fff0000u));
-          }
-          const int e = (int)(top >> 23);
+#pragma unroll
+          for (int p = 0; p < 8; ++p) top = __vmaxu2(__vmaxu2(top, __vmaxu2(x[p].x & 0x7fff7fffu, x[p].y & 0x7fff7fffu)), __vmaxu2(x[p].z & 0x7fff7fffu, x[p].w & 0x7fff7fffu));
+          sm->top[grp][row] = top = max(top & 0xffffu, top >> 16);
+          rows_sync();
+          const int e = (int)(max(top, sm->top[grp ^ 1][row]) >> 7);
           if (e > 8 && e < 255) {  // the largest magnitude into [2^8, 2^9)
             const int up = min(max(8 + 127 - e, -100), 100);
             f = __uint_as_float((uint32_t)(127 + up) << 23);
             rs *= __uint_as_float((uint32_t)(127 - up) << 23);
           }
         }
-        // each group brings every other piece of eight channels
         const uint32_t line = smem_u32(sm->q) + row * 128;
-#pragma unroll 2
-        for (int p = grp; p < 16; p += kGroups) {
-          uint4 x = valid ? src[p] : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+        for (int p = 0; p < 8; ++p) {
           if (kBf16) {
-            x.x = pack2<false>(__uint_as_float(x.x << 16) * f, __uint_as_float(x.x & 0xffff0000u) * f);
-            x.y = pack2<false>(__uint_as_float(x.y << 16) * f, __uint_as_float(x.y & 0xffff0000u) * f);
-            x.z = pack2<false>(__uint_as_float(x.z << 16) * f, __uint_as_float(x.z & 0xffff0000u) * f);
-            x.w = pack2<false>(__uint_as_float(x.w << 16) * f, __uint_as_float(x.w & 0xffff0000u) * f);
+            x[p].x = pack2<false>(__uint_as_float(x[p].x << 16) * f, __uint_as_float(x[p].x & 0xffff0000u) * f);
+            x[p].y = pack2<false>(__uint_as_float(x[p].y << 16) * f, __uint_as_float(x[p].y & 0xffff0000u) * f);
+            x[p].z = pack2<false>(__uint_as_float(x[p].z << 16) * f, __uint_as_float(x[p].z & 0xffff0000u) * f);
+            x[p].w = pack2<false>(__uint_as_float(x[p].w << 16) * f, __uint_as_float(x[p].w & 0xffff0000u) * f);
           }
-          sts128(line + (p >> 3) * kHalfBytes + (((p & 7) ^ (row & 7)) << 4), __byte_perm(x.x, x.z, 0x5410), __byte_perm(x.x, x.z, 0x7632),
-                 __byte_perm(x.y, x.w, 0x5410), __byte_perm(x.y, x.w, 0x7632));
+          sts128(line + (p >> 2) * kHalfBytes + ((((p & 3) * kGroups + grp) ^ (row & 7)) << 4), __byte_perm(x[p].x, x[p].z, 0x5410), __byte_perm(x[p].x, x[p].z, 0x7632),
+                 __byte_perm(x[p].y, x[p].w, 0x5410), __byte_perm(x[p].y, x[p].w, 0x7632));
         }
         fence_async_smem();
         __syncwarp();
@@ -534,83 +542,30 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
         }
       }
       // ---- the groups' sums, against the reference that O ended in: the last one settled
-      float M = any ? sm->ref[row] : -INFINITY;
+      const float M = any ? sm->ref[row] : -INFINITY;
       sm->sum[grp][row] = poison != 0 ? NAN : m_used == -INFINITY ? l : l * ex2(m_used - M);
       rows_sync();
-      float sum = sm->sum[0][row] + sm->sum[1][row];
-      bool complete = sg.whole;
-      Kv4Pieces pieces = {0, 0};
-      if (!sg.whole) {
-        // This CTA's piece goes to the workspace and is counted; the one that counts the last piece adds them all, in the order
-        // of their CTAs, and writes the rows.  Nobody waits for anybody.
-        pieces = kv4_pieces(ranges, sg.u);
+      const float sum = sm->sum[0][row] + sm->sum[1][row];
+      uint32_t o[64];
+      tmem_get64(tmem_o + 64u * grp, o);
+      if (!sg.whole) {  // a piece, unnormalised
         const int64_t mine = (int64_t)kv4_slot(ranges, blockIdx.x, sg.u.begin) * kTileM;
-#pragma unroll 1
-        for (int run = grp; run < 8; run += kGroups) {  // 16 columns of O, unnormalised
-          uint32_t o[16];
-          tmem_get16(tmem_o + 16u * run, o);
-          uint4* to = reinterpret_cast<uint4*>(a.ws_o + mine * kHeadDim) + (4 * run) * kTileM + row;  // [channel / 4][row]
+        uint4* to = reinterpret_cast<uint4*>(a.ws_o + mine * kHeadDim) + 16 * grp * kTileM + row;  // [channel / 4][row]
 #pragma unroll
-          for (int e = 0; e < 16; e += 4) to[(e >> 2) * kTileM] = any ? make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]) : make_uint4(0u, 0u, 0u, 0u);
-        }
+        for (int e = 0; e < 64; e += 4) to[(e >> 2) * kTileM] = any ? make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]) : make_uint4(0u, 0u, 0u, 0u);
         if (grp == 0) a.ws_ml[mine + row] = make_float2(M, sum);
-        __threadfence();
-        rows_sync();
-        if (grp == 0 && row == 0) sm->last = atomicAdd(a.ws_count + 2 * pieces.first, 1) == pieces.last - pieces.first;
-        rows_sync();
-        complete = sm->last != 0;
-        if (complete) {
-          __threadfence();
-          M = -INFINITY;
-          for (int x = pieces.first; x <= pieces.last; ++x) M = fmaxf(M, __ldcg(a.ws_ml + (int64_t)kv4_slot(ranges, x, sg.u.begin) * kTileM + row).x);
-          sum = 0.f;
-          for (int x = pieces.first; x <= pieces.last; ++x) {
-            const float2 ml = __ldcg(a.ws_ml + (int64_t)kv4_slot(ranges, x, sg.u.begin) * kTileM + row);
-            sum = fmaf(ml.y, ml.x == -INFINITY ? 0.f : ex2(ml.x - M), sum);
-          }
-        }
-      }
-      if (complete) {
+      } else {
         const float inv = 1.f / sum;
-#pragma unroll 1
-        for (int run = grp; run < 8; run += kGroups) {
-          uint32_t o[16];
-          if (sg.whole) {
-            tmem_get16(tmem_o + 16u * run, o);
-          } else {
-            float acc[16];
+        if (valid) {
+          uint8_t* out = a.out + r * a.o_req + node * a.o_tok + h * a.o_head + 128 * grp;
 #pragma unroll
-            for (int e = 0; e < 16; ++e) acc[e] = 0.f;
-#pragma unroll 1
-            for (int x = pieces.first; x <= pieces.last; ++x) {
-              const int64_t at = (int64_t)kv4_slot(ranges, x, sg.u.begin) * kTileM;
-              const float mx = __ldcg(a.ws_ml + at + row).x;
-              const float f = mx == -INFINITY ? 0.f : ex2(mx - M);
-              const float4* from = reinterpret_cast<const float4*>(a.ws_o + at * kHeadDim) + (4 * run) * kTileM + row;
+          for (int e = 0; e < 64; e += 8) {  // columns 0,2,4,6,1,3,5,7 are channels 0..7
+            float y[8];
 #pragma unroll
-              for (int e = 0; e < 16; e += 4) {
-                const float4 v = __ldcg(from + (e >> 2) * kTileM);
-                acc[e] = fmaf(v.x, f, acc[e]);
-                acc[e + 1] = fmaf(v.y, f, acc[e + 1]);
-                acc[e + 2] = fmaf(v.z, f, acc[e + 2]);
-                acc[e + 3] = fmaf(v.w, f, acc[e + 3]);
-              }
-            }
-#pragma unroll
-            for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(acc[e]);
+            for (int z = 0; z < 8; ++z) y[z] = __uint_as_float(o[e + z]) * inv;
+            *reinterpret_cast<uint4*>(out + 2 * e) =
+                make_uint4(pack2<kBf16>(y[0], y[2]), pack2<kBf16>(y[4], y[6]), pack2<kBf16>(y[1], y[3]), pack2<kBf16>(y[5], y[7]));
           }
-          if (valid) {
-            uint8_t* out = a.out + r * a.o_req + node * a.o_tok + h * a.o_head + 32 * run;
-#pragma unroll
-            for (int e = 0; e < 16; e += 8) {  // columns 0,2,4,6,1,3,5,7 are channels 0..7
-              float y[8];
-#pragma unroll
-              for (int z = 0; z < 8; ++z) y[z] = __uint_as_float(o[e + z]) * inv;
-              *reinterpret_cast<uint4*>(out + 2 * e) =
-                  make_uint4(pack2<kBf16>(y[0], y[2]), pack2<kBf16>(y[4], y[6]), pack2<kBf16>(y[1], y[3]), pack2<kBf16>(y[5], y[7]));
-            }
-          }
-          __syncwarp();
         }
         if (valid && grp == 0 && a.lse != nullptr) a.lse[((int64_t)r * a.Hq + h) * a.n + node] = (M + log2f(sum)) * kLn2;
       }
@@ -632,7 +587,7 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
 // ---------------------------------------------------------------- host side ---------------------
 size_t kv4_tiles_workspace_bytes() {
   const size_t sms = device_sm_count();
-  return kv4_count_bytes(sms) + 2 * sms * kTileM * (kHeadDim * sizeof(float) + sizeof(float2));
+  return kv4_ranges_bytes(sms, kTileM);
 }
 
 int launch_kv4_tiles(const seq_tree_kv4_attention_params& p, cudaStream_t stream) {
@@ -646,11 +601,7 @@ int launch_kv4_tiles(const seq_tree_kv4_attention_params& p, cudaStream_t stream
   if (most > 0x7fffffff) return SEQ_ERR_UNSUPPORTED;
   const int64_t want = (most + a.min_steps - 1) / a.min_steps;
   a.ctas = want < sms ? (int)want : sms;
-  a.ws_count = static_cast<int32_t*>(p.workspace);
-  a.ws_o = reinterpret_cast<float*>(static_cast<uint8_t*>(p.workspace) + kv4_count_bytes(sms));
-  a.ws_ml = reinterpret_cast<float2*>(a.ws_o + (size_t)2 * sms * kTileM * kHeadDim);
-  const int rc0 = launch_kv4_zero(a, stream);
-  if (rc0 != SEQ_OK) return rc0;
+  kv4_ranges_place(a, sms, p.workspace);
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(a.ctas);
   cfg.blockDim = dim3(kTilesThreads);
@@ -671,7 +622,9 @@ int launch_kv4_tiles(const seq_tree_kv4_attention_params& p, cudaStream_t stream
     SEQ_CUDA_OK(cudaLaunchKernelEx(&cfg, kernel, a));
     return SEQ_OK;
   };
-  return p.dtype == SEQ_BF16 ? launch(kv4_tiles_kernel<true>, 0) : launch(kv4_tiles_kernel<false>, 1);
+  const bool bf16 = p.dtype == SEQ_BF16;
+  const int rc = bf16 ? launch(kv4_tiles_kernel<true>, 0) : launch(kv4_tiles_kernel<false>, 1);
+  return rc != SEQ_OK ? rc : launch_kv4_merge(a, bf16, true, stream);
 }
 
 }  // namespace seqtree
