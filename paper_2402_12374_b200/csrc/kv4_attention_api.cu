@@ -96,8 +96,13 @@ Kv4Args kv4_args(const seq_tree_kv4_attention_params& p) {
   return a;
 }
 
-// The kernel in registers takes 16 query rows of a kv head at a time, the tensor-core one 128.
-static bool few_rows(const seq_tree_kv4_attention_params& p) { return p.n_tree * (p.num_q_heads / p.num_kv_heads) <= 16; }
+// The kernel in registers takes 16 query rows of a kv head at a time, the tensor-core one 128 and some 20 us for its start and its last
+// pieces.  So few rows are the former's, and whatever its clusters cut to a few dozen steps (bf16, 64/8 heads, 6 nodes on 4096 tokens:
+// 14 us against 28; 64 nodes of 32/32 heads on 1024: 17 against 24).  With ranges it is ahead to two tiles of rows (32 rows of 32 heads, four
+// requests of 2048: 32 us against 38; 48 rows: 65 against 39).
+static bool few_rows(const seq_tree_kv4_attention_params& p) {
+  return p.n_tree * (p.num_q_heads / p.num_kv_heads) <= 32 || kv4_rows_cluster(p) != 0;
+}
 
 static int check_kv4_attention(const seq_tree_kv4_attention_params* p) {
   if (p == nullptr || p->q == nullptr || p->k_tree == nullptr || p->v_tree == nullptr || p->pages == nullptr || p->page_table == nullptr ||

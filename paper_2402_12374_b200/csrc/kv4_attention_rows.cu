@@ -711,7 +711,7 @@ static int rows_steps(const seq_tree_kv4_attention_params& p) {
   return (L + 31) / 32 + (p.n_tree + kTreeStep - 1) / kTreeStep;
 }
 // CTAs of a unit's cluster, 0 for ranges.
-static int rows_cluster(const seq_tree_kv4_attention_params& p) {
+int kv4_rows_cluster(const seq_tree_kv4_attention_params& p) {
   const int64_t units = rows_units(p);
   const int steps = rows_steps(p);
   int c = 1;
@@ -722,7 +722,7 @@ static int rows_cluster(const seq_tree_kv4_attention_params& p) {
 }
 
 size_t kv4_rows_workspace_bytes(const seq_tree_kv4_attention_params& p) {
-  if (rows_cluster(p) != 0) return 0;
+  if (kv4_rows_cluster(p) != 0) return 0;
   const int nt = rows_nt(p);
   return kv4_ranges_bytes(rows_ctas(nt), 8 * nt);
 }
@@ -734,7 +734,7 @@ int launch_kv4_rows(const seq_tree_kv4_attention_params& p, cudaStream_t stream)
   a.tiles = (a.rows + a.row_tile - 1) / a.row_tile;
   a.tree_steps = (a.n + kTreeStep - 1) / kTreeStep;
   a.min_steps = kRowsWarps;
-  a.cluster = rows_cluster(p);
+  a.cluster = kv4_rows_cluster(p);
   const bool bf16 = p.dtype == SEQ_BF16;
   cudaLaunchConfig_t cfg = {};
   cfg.blockDim = dim3(32 * kRowsWarps);

@@ -7,6 +7,15 @@ from paper_2402_12374_b200 import binding as B
 from tests import kv4_util as U
 
 pytestmark = pytest.mark.gpu
+ROOM = 0  # tokens that a page table has room for, at least
+
+
+@pytest.fixture(autouse=True, params=["tight", "roomy"])
+def room(request):
+    """The lengths' bound chooses the kernel: with room for 40000 tokens no cluster takes the few rows, nor small trees."""
+    global ROOM
+    ROOM = 40000 if request.param == "roomy" else 0
+    return request.param
 
 
 class Case:
@@ -17,7 +26,7 @@ class Case:
         self.lengths, self.n, self.Hq, self.Hkv, self.page, self.dt = list(lengths), n, Hq, Hkv, page, dt
         R = len(lengths)
         self.count = [-(-max(L, 0) // page) for L in lengths]
-        most = max(1, max(self.count))
+        most = max(1, max(self.count), -(-ROOM // page))
         pages = sum(self.count) + 2
         self.pool = U.random_pool(pages, layers, Hkv, page, rng)
         self.table = np.full((R, most), 10 ** 6, dtype=np.int32)  # (what is behind the last page is not read)
@@ -292,12 +301,13 @@ def test_offsets_beyond_32_bits():
         U.check_attention(out[0], None, c.reference(0), c.dt, False)
 
 
-def test_workspace_that_is_too_small_is_refused():
-    for lengths, n in (([45] * 300, 1), ([45], 40)):
+def test_workspace_that_is_too_small_is_refused(room):
+    for lengths, n in (([45] * 300, 1), ([45], 400)):
         c = Case(lengths, n, 16, 2, 16, torch.float16)
         need = c.call().workspace_bytes_needed
         assert need > 0
         call = c.call(workspace=torch.empty(need - 16, dtype=torch.uint8, device="cuda"))
         with pytest.raises(B.SeqTreeError, match="WORKSPACE"):
             call.run()
-    assert Case([45], 1, 8, 1, 16, torch.float16).call().workspace is None  # a cluster a unit: none is needed
+    if room == "tight":
+        assert Case([45], 1, 8, 1, 16, torch.float16).call().workspace is None  # a cluster a unit: none is needed
