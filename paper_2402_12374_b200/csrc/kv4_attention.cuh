@@ -145,12 +145,14 @@ __device__ __forceinline__ int kv4_depth(const Kv4Args& a, int r, int node) {
   const uint32_t* row = kv4_mask_row(a, r, node);
   if (row == nullptr) return node;
   int c = 0;
+#pragma unroll 1
   for (int w = 0; w < (a.n + 31) >> 5; ++w) c += __popc(kv4_mask_word(a, row, node, w));
   return max(c - 1, 0);
 }
 // ... with the window: rows a of the tree at L + depth(a)
 __device__ __forceinline__ uint32_t kv4_window_word(const Kv4Args& a, int r, int L, int depth, int w, uint32_t bits) {
   if (a.window == 0 || depth < a.window) return bits;  // (no ancestor is further away than the root)
+#pragma unroll 1
   for (uint32_t left = bits; left != 0; left &= left - 1) {
     const int b = __ffs(left) - 1, d = kv4_depth(a, r, 32 * w + b);
     if (d <= depth - a.window && L + d >= a.sinks) bits &= ~(1u << b);

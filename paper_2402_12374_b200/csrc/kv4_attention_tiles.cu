@@ -58,6 +58,18 @@ struct TilesSmem {
 constexpr size_t kTilesSmemBytes = sizeof(TilesSmem) + 1024;
 static_assert(kTilesSmemBytes <= 227 * 1024, "one CTA's shared memory");
 
+// mbar_wait, rolled: what the warps run has to stay in the instruction caches
+__device__ __forceinline__ bool kv4_wait(TilesSmem* sm, uint64_t* bar, uint32_t parity, int32_t* status) {
+#pragma unroll 1
+  for (uint32_t it = 0; it < kSpinLimit; ++it) {
+    if (mbar_try_wait(bar, parity)) return true;
+    if ((it & 1023u) == 1023u && sm->abort_flag) return false;
+  }
+  sm->abort_flag = 1;
+  dev_flag(status, SEQ_DEV_TIMEOUT);
+  return false;
+}
+
 __device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
   asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
                ::"r"(smem_u32(dst)), "l"(src), "r"(bytes), "r"(smem_u32(bar)) : "memory");
@@ -74,6 +86,12 @@ __device__ __forceinline__ void tmem_get16(uint32_t taddr, uint32_t (&r)[16]) {
       "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n\t"
       "tcgen05.wait::ld.sync.aligned;"
       : SEQ_R16(r, 0) : "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void tmem_get32(uint32_t taddr, uint32_t (&r)[32]) {
+  tmem_ld32(taddr, r, 0);
+  tc_wait_ld();
+#pragma unroll
+  for (int e = 0; e < 32; ++e) asm volatile("" : "+r"(r[e]));  // (nothing of it moves ahead of the wait)
 }
 __device__ __forceinline__ void tmem_get64(uint32_t taddr, uint32_t (&r)[64]) {
   tmem_ld32(taddr, r, 0);
@@ -173,7 +191,7 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
                 }
               }
             }
-            if (w > 0 && !mbar_wait(sm, &sm->raw_empty[st], (w - 1) & 1, a.status)) { ok = false; break; }
+            if (w > 0 && !kv4_wait(sm, &sm->raw_empty[st], (w - 1) & 1, a.status)) { ok = false; break; }
             if (lane == 0) mbar_expect_tx(&sm->raw_full[st], granules * kGranuleBytes);
             __syncwarp();
             // lane x: the x-th page's part
@@ -199,17 +217,17 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
       const uint32_t idesc = (1u << 4) | ((uint32_t)(kTileM >> 4) << 24) | ((uint32_t)(kTilesStep >> 3) << 17);  // fp16, sums fp32, N = 128
       const uint32_t idesc_pv = idesc | (1u << 16);                                                             // V is MN-major
       const uint32_t q_lo = desc_lo(smem_u32(sm->q), 16);
-      int step = 0, seg = 0, sb = 0, u = 0;  // key tiles before this segment, segments, the next tile's buffer and how often that was used
+      int step = 0, seg = 0, sb = 0, u = 0;  // key tiles before this segment, segments with steps, the next tile's buffer and how often that was used
       bool ok = true;
-      for (int pos = range_lo; pos < range_hi && ok; ++seg) {
+      for (int pos = range_lo; pos < range_hi && ok;) {
         const TilesSeg sg = tiles_seg(&sm->plan, a, pos, range_hi);
-        if (warp == 1) ok = mbar_wait(sm, &sm->q_full, seg & 1, a.status);
+        if (warp == 1 && sg.steps > 0) ok = kv4_wait(sm, &sm->q_full, seg & 1, a.status);
         for (int i = 0; i < sg.steps && ok; ++i) {
           const int x = step + i, b = x & 1;
           const uint32_t sp = tmem + kTmemS + 128u * sb;
           if (warp == 1) {
             // S goes where the P of three tiles ago was: its product has completed
-            ok = mbar_wait(sm, &sm->k_full[b], (x >> 1) & 1, a.status) && (u == 0 || mbar_wait(sm, &sm->pv_done[sb], (u - 1) & 1, a.status));
+            ok = kv4_wait(sm, &sm->k_full[b], (x >> 1) & 1, a.status) && (u == 0 || kv4_wait(sm, &sm->pv_done[sb], (u - 1) & 1, a.status));
             if (!ok) break;
             tc_fence_after();
             if (elect_one()) {
@@ -219,7 +237,7 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
             }
           } else {
             const uint32_t v_lo = desc_lo(smem_u32(sm->v[b]), kHalfBytes);
-            ok = mbar_wait(sm, &sm->v_full[b], (x >> 1) & 1, a.status) && mbar_wait(sm, &sm->p_full[sb], u & 1, a.status);
+            ok = kv4_wait(sm, &sm->v_full[b], (x >> 1) & 1, a.status) && kv4_wait(sm, &sm->p_full[sb], u & 1, a.status);
             if (!ok) break;
             tc_fence_after();
             if (elect_one()) {  // (P of each half of the keys is where its scores were)
@@ -233,6 +251,7 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
           if (++sb == kSBufs) { sb = 0; ++u; }
         }
         step += sg.steps;
+        seg += sg.steps > 0;
         pos = sg.next;
       }
       if (!ok) {  // what has been issued reads shared and tensor memory
@@ -263,13 +282,13 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
         const bool tree = t >= sg.u.prefix.steps;
         const int key0 = tree ? (t - sg.u.prefix.steps) * kTilesStep : sg.u.prefix.key_step(t) * kTilesStep;
         const int left = (tree ? a.n : sg.u.L) - key0;  // keys of the tile that there are
-        if (w > 0) ok = mbar_wait(sm, &empty[b], (w - 1) & 1, a.status);
+        if (w > 0) ok = kv4_wait(sm, &empty[b], (w - 1) & 1, a.status);
         const uint32_t tile = smem_u32(which ? sm->v[b] : sm->k[b]);
         if (!tree) {
 #pragma unroll 1
           for (int h = 0; h < 2 && ok; ++h) {
             const int st = taken % kStages;
-            if (h * kHalfKeys < left) ok = mbar_wait(sm, &sm->raw_full[st], (taken / kStages) & 1, a.status);
+            if (h * kHalfKeys < left) ok = kv4_wait(sm, &sm->raw_full[st], (taken / kStages) & 1, a.status);
             __syncwarp();
             if (!ok) break;
             const uint32_t granule = smem_u32(sm->ring[st]) + w4 * kGranuleBytes;
@@ -363,101 +382,180 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
     auto rows_sync = [&]() { asm volatile("bar.sync 1, 256;" ::: "memory"); };
     int step = 0, seg = 0, own = 0;  // key tiles before this segment, segments with steps, tiles of this group
     bool ok = true;
-    for (int pos = range_lo; pos < range_hi;) {
-      const TilesSeg sg = tiles_seg(&sm->plan, a, pos, range_hi);
-      const int L = sg.u.L, r = sg.u.r;
-      const int rw = sg.u.m * kTileM + row;
-      const bool valid = rw < a.rows;
-      const int node = min(rw, a.rows - 1) / a.group, h = sg.u.g * a.group + min(rw, a.rows - 1) % a.group;
-      const bool warp_live = rw - lane < a.rows;  // (a warp of padding rows only keeps in step)
-      // ---- q: half precision (a bfloat16 row scaled by a power of two, exactly), channels in the codes' order
-      float rs = a.scale_log2;
-      {
-        // each group brings every other piece of eight channels
-        const uint4* src = reinterpret_cast<const uint4*>(a.q + r * a.q_req + node * a.q_tok + h * a.q_head) + grp;
-        uint4 x[8];
+    // The thread's row of a segment
+    struct Row {
+      TilesSeg sg;
+      int node, h, depth, begin, latest;  // (begin: where the row's window begins)
+      float rs;
+      bool valid, warp_live;              // a warp of padding rows only keeps in step
+      const uint32_t* mask;
+    };
+    Row cur;
+    bool have = false;
+    float m_used = -INFINITY, l = 0.f;
+    for (int pos = range_lo;;) {
+      // ---- the next segment's rows; its first scores are computed while the last segment's results are written
+      Row next;
+      const bool more = pos < range_hi;
+      if (more) {
+        next.sg = tiles_seg(&sm->plan, a, pos, range_hi);
+        const int r = next.sg.u.r, rw = next.sg.u.m * kTileM + row;
+        const int node = next.node = min(rw, a.rows - 1) / a.group, h = next.h = next.sg.u.g * a.group + min(rw, a.rows - 1) % a.group;
+        const bool valid = next.valid = rw < a.rows;
+        next.warp_live = rw - lane < a.rows;
+        // q: half precision (a bfloat16 row scaled by a power of two, exactly), channels in the codes' order
+        float rs = a.scale_log2;
+        if (next.sg.steps > 0) {
+          // each group brings every other piece of eight channels
+          const uint4* src = reinterpret_cast<const uint4*>(a.q + r * a.q_req + node * a.q_tok + h * a.q_head) + grp;
+          uint4 x[8];
 #pragma unroll
-        for (int p = 0; p < 8; ++p) x[p] = valid ? src[p * kGroups] : make_uint4(0u, 0u, 0u, 0u);
-        float f = 1.f;
-        if (kBf16) {
-          uint32_t top = 0;
-#pragma unroll
-          for (int p = 0; p < 8; ++p) top = __vmaxu2(__vmaxu2(top, __vmaxu2(x[p].x & 0x7fff7fffu, x[p].y & 0x7fff7fffu)), __vmaxu2(x[p].z & 0x7fff7fffu, x[p].w & 0x7fff7fffu));
-          sm->top[grp][row] = top = max(top & 0xffffu, top >> 16);
-          rows_sync();
-          const int e = (int)(max(top, sm->top[grp ^ 1][row]) >> 7);
-          if (e > 8 && e < 255) {  // the largest magnitude into [2^8, 2^9)
-            const int up = min(max(8 + 127 - e, -100), 100);
-            f = __uint_as_float((uint32_t)(127 + up) << 23);
-            rs *= __uint_as_float((uint32_t)(127 - up) << 23);
-          }
-        }
-        const uint32_t line = smem_u32(sm->q) + row * 128;
-#pragma unroll
-        for (int p = 0; p < 8; ++p) {
+          for (int p = 0; p < 8; ++p) x[p] = valid ? src[p * kGroups] : make_uint4(0u, 0u, 0u, 0u);
+          float f = 1.f;
           if (kBf16) {
-            x[p].x = pack2<false>(__uint_as_float(x[p].x << 16) * f, __uint_as_float(x[p].x & 0xffff0000u) * f);
-            x[p].y = pack2<false>(__uint_as_float(x[p].y << 16) * f, __uint_as_float(x[p].y & 0xffff0000u) * f);
-            x[p].z = pack2<false>(__uint_as_float(x[p].z << 16) * f, __uint_as_float(x[p].z & 0xffff0000u) * f);
-            x[p].w = pack2<false>(__uint_as_float(x[p].w << 16) * f, __uint_as_float(x[p].w & 0xffff0000u) * f);
+            uint32_t top = 0;
+#pragma unroll
+            for (int p = 0; p < 8; ++p) top = __vmaxu2(__vmaxu2(top, __vmaxu2(x[p].x & 0x7fff7fffu, x[p].y & 0x7fff7fffu)), __vmaxu2(x[p].z & 0x7fff7fffu, x[p].w & 0x7fff7fffu));
+            sm->top[grp][row] = top = max(top & 0xffffu, top >> 16);
+            rows_sync();
+            const int e = (int)(max(top, sm->top[grp ^ 1][row]) >> 7);
+            if (e > 8 && e < 255) {  // the largest magnitude into [2^8, 2^9)
+              const int up = min(max(8 + 127 - e, -100), 100);
+              f = __uint_as_float((uint32_t)(127 + up) << 23);
+              rs *= __uint_as_float((uint32_t)(127 - up) << 23);
+            }
           }
-          sts128(line + (p >> 2) * kHalfBytes + ((((p & 3) * kGroups + grp) ^ (row & 7)) << 4), __byte_perm(x[p].x, x[p].z, 0x5410), __byte_perm(x[p].x, x[p].z, 0x7632),
-                 __byte_perm(x[p].y, x[p].w, 0x5410), __byte_perm(x[p].y, x[p].w, 0x7632));
+          if (have && cur.sg.steps > 0) {  // the scores of the segment before are complete
+            const int x = step - 1, u = x / kSBufs;
+            ok = kv4_wait(sm, &sm->s_full[x - u * kSBufs], u & 1, a.status);
+            __syncwarp();
+          }
+          const uint32_t line = smem_u32(sm->q) + row * 128;
+#pragma unroll
+          for (int p = 0; p < 8; ++p) {
+            if (kBf16) {
+              x[p].x = pack2<false>(__uint_as_float(x[p].x << 16) * f, __uint_as_float(x[p].x & 0xffff0000u) * f);
+              x[p].y = pack2<false>(__uint_as_float(x[p].y << 16) * f, __uint_as_float(x[p].y & 0xffff0000u) * f);
+              x[p].z = pack2<false>(__uint_as_float(x[p].z << 16) * f, __uint_as_float(x[p].z & 0xffff0000u) * f);
+              x[p].w = pack2<false>(__uint_as_float(x[p].w << 16) * f, __uint_as_float(x[p].w & 0xffff0000u) * f);
+            }
+            sts128(line + (p >> 2) * kHalfBytes + ((((p & 3) * kGroups + grp) ^ (row & 7)) << 4), __byte_perm(x[p].x, x[p].z, 0x5410), __byte_perm(x[p].x, x[p].z, 0x7632),
+                   __byte_perm(x[p].y, x[p].w, 0x5410), __byte_perm(x[p].y, x[p].w, 0x7632));
+          }
+          fence_async_smem();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&sm->q_full);
         }
-        fence_async_smem();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&sm->q_full);
+        next.rs = rs;
+        next.mask = kv4_mask_row(a, r, node);
+        next.depth = a.window > 0 ? kv4_depth(a, r, node) : 0;
+        next.begin = a.window > 0 ? next.sg.u.L + next.depth + 1 - a.window : 0;
+        next.latest = __reduce_max_sync(0xffffffffu, next.begin);
+        pos = next.sg.next;
       }
-      const uint32_t* mask_row = kv4_mask_row(a, r, node);
-      const int depth = a.window > 0 ? kv4_depth(a, r, node) : 0;
-      const int begin = a.window > 0 ? L + depth + 1 - a.window : 0;  // where the row's window begins
-      const int latest = __reduce_max_sync(0xffffffffu, begin);
-
-      float m_used = -INFINITY, l = 0.f;
+      if (have) {
+        const TilesSeg& sg = cur.sg;
+        const int L = sg.u.L, r = sg.u.r, node = cur.node, h = cur.h, depth = cur.depth;
+        const uint32_t* mask_row = cur.mask;
+        const bool valid = cur.valid;
+        // ---- the last product
+        if (sg.steps > 0 && ok) {
+          const int x = step - 1, u = x / kSBufs;
+          ok = kv4_wait(sm, &sm->pv_done[x - u * kSBufs], u & 1, a.status);
+        }
+        __syncwarp();
+        tc_fence_after();
+        const bool any = sg.steps > 0 && ok;
+        uint32_t poison = 0;  // tree rows that are not finite and that the row sees
+#pragma unroll 1
+        for (int i = max(sg.u.prefix.steps - sg.t0, 0); i < sg.steps; ++i) {
+          const int tt = sg.t0 + i - sg.u.prefix.steps;
+#pragma unroll 1
+          for (int w = 0; w < 4; ++w) {
+            const uint32_t bad = sm->bad[(seg - 1) & 3][tt][w];
+            if (bad != 0) poison |= bad & kv4_window_word(a, r, L, depth, 4 * tt + w, kv4_mask_word(a, mask_row, node, 4 * tt + w));
+          }
+        }
+        // ---- the groups' sums, against the reference that O ended in: the last one settled
+        const float M = any ? sm->ref[row] : -INFINITY;
+        sm->sum[grp][row] = poison != 0 ? NAN : m_used == -INFINITY ? l : l * ex2(m_used - M);
+        rows_sync();
+        const float sum = sm->sum[0][row] + sm->sum[1][row];
+        uint32_t o[64];
+        tmem_get64(tmem_o + 64u * grp, o);
+        tc_fence_before();
+        rows_sync();  // the accumulator is read, the rows are through with what they exchanged
+        if (!sg.whole) {  // a piece, unnormalised
+          const int64_t mine = (int64_t)kv4_slot(ranges, blockIdx.x, sg.u.begin) * kTileM;
+          uint4* to = reinterpret_cast<uint4*>(a.ws_o + mine * kHeadDim) + 16 * grp * kTileM + row;  // [channel / 4][row]
+#pragma unroll
+          for (int e = 0; e < 64; e += 4) to[(e >> 2) * kTileM] = any ? make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]) : make_uint4(0u, 0u, 0u, 0u);
+          if (grp == 0) a.ws_ml[mine + row] = make_float2(M, sum);
+        } else {
+          const float inv = 1.f / sum;
+          if (valid) {
+            uint8_t* out = a.out + r * a.o_req + node * a.o_tok + h * a.o_head + 128 * grp;
+#pragma unroll
+            for (int e = 0; e < 64; e += 8) {  // columns 0,2,4,6,1,3,5,7 are channels 0..7
+              float y[8];
+#pragma unroll
+              for (int z = 0; z < 8; ++z) y[z] = __uint_as_float(o[e + z]) * inv;
+              *reinterpret_cast<uint4*>(out + 2 * e) =
+                  make_uint4(pack2<kBf16>(y[0], y[2]), pack2<kBf16>(y[4], y[6]), pack2<kBf16>(y[1], y[3]), pack2<kBf16>(y[5], y[7]));
+            }
+          }
+          if (valid && grp == 0 && a.lse != nullptr) a.lse[((int64_t)r * a.Hq + h) * a.n + node] = (M + log2f(sum)) * kLn2;
+        }
+      }
+      if (!more) break;
+      cur = next;
+      have = true;
+      const TilesSeg& sg = cur.sg;
+      const int L = sg.u.L, r = sg.u.r, node = cur.node, depth = cur.depth, begin = cur.begin, latest = cur.latest;
+      const uint32_t* mask_row = cur.mask;
+      const float rs = cur.rs;
+      const bool warp_live = cur.warp_live;
+      m_used = -INFINITY;
+      l = 0.f;
       for (int i = (grp ^ step) & 1; i < sg.steps; i += kGroups, ++own) {
         const int t = sg.t0 + i, x = step + i, u = x / kSBufs, sb = x - u * kSBufs;
         const uint32_t tmem_s = tmem + kTmemS + 128u * sb + lane_sel;
         const bool tree = t >= sg.u.prefix.steps;
         const int key0 = (tree ? t - sg.u.prefix.steps : sg.u.prefix.key_step(t)) * kTilesStep;
         const bool masked = tree || key0 + kTilesStep > L || key0 < latest;  // some keys are not there, or not every row's
-        auto hide = [&](int half, uint32_t (&s)[64]) {  // masked scores become -inf
-#pragma unroll 1
-          for (int w = 0; w < 2; ++w) {
-            const int k = key0 + 64 * half + 32 * w;
-            uint32_t bits;
-            if (tree) bits = kv4_window_word(a, r, L, depth, k >> 5, kv4_mask_word(a, mask_row, node, k >> 5));
-            else bits = bits_below(L - k) & (~bits_below(begin - k) | bits_below(a.sinks - k));
-            if (w == 0) {
+        auto hide = [&](int c, uint32_t (&s)[32]) {  // masked scores become -inf
+          const int k = key0 + 32 * c;
+          uint32_t bits;
+          if (tree) bits = kv4_window_word(a, r, L, depth, k >> 5, kv4_mask_word(a, mask_row, node, k >> 5));
+          else bits = bits_below(L - k) & (~bits_below(begin - k) | bits_below(a.sinks - k));
 #pragma unroll
-              for (int e = 0; e < 32; ++e)
-                if (!((bits >> e) & 1u)) s[e] = __float_as_uint(-INFINITY);
-            } else {
-#pragma unroll
-              for (int e = 0; e < 32; ++e)
-                if (!((bits >> e) & 1u)) s[32 + e] = __float_as_uint(-INFINITY);
-            }
-          }
+          for (int e = 0; e < 32; ++e)
+            if (!((bits >> e) & 1u)) s[e] = __float_as_uint(-INFINITY);
         };
-        ok = mbar_wait(sm, &sm->s_full[sb], u & 1, a.status);
+        ok = kv4_wait(sm, &sm->s_full[sb], u & 1, a.status);
         __syncwarp();
         if (!ok) break;
         if (warp_live) {
           tc_fence_after();
-          uint32_t s[64];
+          uint32_t s[32];
           float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll 1
-          for (int half = 0; half < 2; ++half) {  // (the second half's scores stay in registers)
-            tmem_get64(tmem_s + 64u * half, s);
-            if (masked) hide(half, s);
+          for (int c = 0; c < 4; ++c) {
+            tmem_get32(tmem_s + 32u * c, s);
+            if (masked) {
+              hide(c, s);
+              tmem_st32(tmem_s + 32u * c, s, 0);
+            }
 #pragma unroll
-            for (int e = 0; e < 64; e += 2) mx[(e >> 1) & 3] = max3(mx[(e >> 1) & 3], __uint_as_float(s[e]), __uint_as_float(s[e + 1]));
+            for (int e = 0; e < 32; e += 2) mx[(e >> 1) & 3] = max3(mx[(e >> 1) & 3], __uint_as_float(s[e]), __uint_as_float(s[e + 1]));
           }
+          if (masked) tc_wait_st();
           const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * rs;  // rs > 0
           // All groups add to one accumulator, so they share the rows' reference: it is settled tile by tile, in order, before the
           // exponentials.  It moves only when a score exceeds it by more than the threshold, or with the first score.
           float ref = -INFINITY;
           if (i > 0) {
-            ok = mbar_wait(sm, &sm->settled[grp ^ 1][quarter], (own - (grp == 0)) & 1, a.status);
+            ok = kv4_wait(sm, &sm->settled[grp ^ 1][quarter], (own - (grp == 0)) & 1, a.status);
             __syncwarp();
             if (!ok) break;
             ref = sm->ref[row];
@@ -468,7 +566,7 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
             const float alpha = move && ref != -INFINITY ? ex2(ref - top) : 1.f;
             if (i > 0) {
               // O may still be taking the tile before
-              ok = mbar_wait(sm, &sm->pv_done[sb == 0 ? kSBufs - 1 : sb - 1], (u - (sb == 0)) & 1, a.status);
+              ok = kv4_wait(sm, &sm->pv_done[sb == 0 ? kSBufs - 1 : sb - 1], (u - (sb == 0)) & 1, a.status);
               __syncwarp();
               if (!ok) break;
               tc_fence_after();
@@ -495,21 +593,18 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
           const uint64_t rs2 = pair_of(rs, rs), neg_m2 = pair_of(neg_m, neg_m);
           uint64_t sums[2] = {pair_of(0.f, 0.f), pair_of(0.f, 0.f)};
 #pragma unroll 1
-          for (int half = 1; half >= 0; --half) {
-            if (half == 0) {
-              tmem_get64(tmem_s, s);
-              if (masked) hide(0, s);
-            }
-            uint32_t packed[32];
+          for (int c = 0; c < 4; ++c) {
+            tmem_get32(tmem_s + 32u * c, s);
+            uint32_t packed[16];
 #pragma unroll
-            for (int e = 0; e < 32; ++e) {
+            for (int e = 0; e < 16; ++e) {
               float y0, y1;
               unpair(fma2(pair_of(__uint_as_float(s[2 * e]), __uint_as_float(s[2 * e + 1])), rs2, neg_m2), y0, y1);
               const float p0 = ex2(y0), p1 = ex2(y1);
               sums[e & 1] = add2(sums[e & 1], pair_of(p0, p1));
               packed[e] = pack2<false>(p0, p1);
             }
-            tmem_st32(tmem_s + 64u * half, packed, 0);  // over scores that have been read
+            tmem_st16(tmem_s + 64u * (c >> 1) + 16u * (c & 1), packed);  // over scores that have been read
           }
           float s0, s1, s2, s3;
           unpair(sums[0], s0, s1);
@@ -523,57 +618,8 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
         __syncwarp();
         if (lane == 0) mbar_arrive(&sm->p_full[sb]);
       }
-      // ---- the last product
-      if (sg.steps > 0 && ok) {
-        const int x = step + sg.steps - 1, u = x / kSBufs;
-        ok = mbar_wait(sm, &sm->pv_done[x - u * kSBufs], u & 1, a.status);
-      }
-      __syncwarp();
-      tc_fence_after();
-      const bool any = sg.steps > 0 && ok;
-      uint32_t poison = 0;  // tree rows that are not finite and that the row sees
-#pragma unroll 1
-      for (int i = max(sg.u.prefix.steps - sg.t0, 0); i < sg.steps; ++i) {
-        const int tt = sg.t0 + i - sg.u.prefix.steps;
-#pragma unroll 1
-        for (int w = 0; w < 4; ++w) {
-          const uint32_t bad = sm->bad[seg & 3][tt][w];
-          if (bad != 0) poison |= bad & kv4_window_word(a, r, L, depth, 4 * tt + w, kv4_mask_word(a, mask_row, node, 4 * tt + w));
-        }
-      }
-      // ---- the groups' sums, against the reference that O ended in: the last one settled
-      const float M = any ? sm->ref[row] : -INFINITY;
-      sm->sum[grp][row] = poison != 0 ? NAN : m_used == -INFINITY ? l : l * ex2(m_used - M);
-      rows_sync();
-      const float sum = sm->sum[0][row] + sm->sum[1][row];
-      uint32_t o[64];
-      tmem_get64(tmem_o + 64u * grp, o);
-      if (!sg.whole) {  // a piece, unnormalised
-        const int64_t mine = (int64_t)kv4_slot(ranges, blockIdx.x, sg.u.begin) * kTileM;
-        uint4* to = reinterpret_cast<uint4*>(a.ws_o + mine * kHeadDim) + 16 * grp * kTileM + row;  // [channel / 4][row]
-#pragma unroll
-        for (int e = 0; e < 64; e += 4) to[(e >> 2) * kTileM] = any ? make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]) : make_uint4(0u, 0u, 0u, 0u);
-        if (grp == 0) a.ws_ml[mine + row] = make_float2(M, sum);
-      } else {
-        const float inv = 1.f / sum;
-        if (valid) {
-          uint8_t* out = a.out + r * a.o_req + node * a.o_tok + h * a.o_head + 128 * grp;
-#pragma unroll
-          for (int e = 0; e < 64; e += 8) {  // columns 0,2,4,6,1,3,5,7 are channels 0..7
-            float y[8];
-#pragma unroll
-            for (int z = 0; z < 8; ++z) y[z] = __uint_as_float(o[e + z]) * inv;
-            *reinterpret_cast<uint4*>(out + 2 * e) =
-                make_uint4(pack2<kBf16>(y[0], y[2]), pack2<kBf16>(y[4], y[6]), pack2<kBf16>(y[1], y[3]), pack2<kBf16>(y[5], y[7]));
-          }
-        }
-        if (valid && grp == 0 && a.lse != nullptr) a.lse[((int64_t)r * a.Hq + h) * a.n + node] = (M + log2f(sum)) * kLn2;
-      }
-      tc_fence_before();
-      rows_sync();  // the accumulator is read, the rows are through with Q and with what they exchanged
       step += sg.steps;
       seg += sg.steps > 0;
-      pos = sg.next;
     }
   }
   tc_fence_before();
