@@ -11,11 +11,17 @@
 
 namespace seqtree {
 
+constexpr int kKv4TreeSteps = SEQ_MAX_TREE / 32;  // steps of the tree, at most
+
 struct Kv4Args {
   int32_t batch, n, max_len, Hq, Hkv, group, rows;  // rows: n * group
   int32_t window, sinks;
   int32_t num_pages, page_size, page_shift;
-  int32_t row_tile, tiles, tree_steps, ctas, min_steps, cluster;
+  int32_t row_tile, tiles, ctas, min_steps, cluster;
+  int32_t unit_cost;   // positions at a unit's start that stand for what a unit costs
+  int32_t tree_steps;  // of the last tile of rows; a tile has those up to its last node
+  int32_t tree_from[kKv4TreeSteps];  // the first tile with more than k steps of the tree
+  int32_t tree_total;  // the tree's steps of all tiles
   const uint8_t* q; int64_t q_req, q_tok, q_head;  // all strides in bytes
   const uint8_t* kt; const uint8_t* vt; int64_t t_req, t_tok, t_head;
   const uint8_t* pages; int64_t page_stride;
@@ -54,6 +60,10 @@ __device__ __forceinline__ Kv4Prefix kv4_prefix(const Kv4Args& a, int L) {
 // Request r's prefix; -1: idle
 __device__ __forceinline__ int kv4_len(const Kv4Args& a, int r) { return min(max(a.lengths[r], -1), a.max_len); }
 
+// Positions of a request
+template <int kStep>
+__device__ __forceinline__ int kv4_positions(const Kv4Args& a, int L) { return a.Hkv * (a.tiles * (a.unit_cost + kv4_prefix<kStep>(a, L).steps) + a.tree_total); }
+
 // Every thread of the CTA calls it; the plan is there behind the next barrier that it ends with.
 template <int kStep, int kThreads>
 __device__ __forceinline__ void kv4_plan(Kv4Plan* plan, const Kv4Args& a) {
@@ -63,7 +73,7 @@ __device__ __forceinline__ void kv4_plan(Kv4Plan* plan, const Kv4Args& a) {
   for (int j = first; j < first + per && j < a.batch; ++j) {
     const int L = kv4_len(a, j);
     if (blockIdx.x == 0 && a.lengths[j] > a.max_len) dev_flag(a.status, SEQ_DEV_BAD_LENGTH);
-    if (L >= 0) sum += a.Hkv * a.tiles * (kv4_prefix<kStep>(a, L).steps + a.tree_steps);
+    if (L >= 0) sum += kv4_positions<kStep>(a, L);
   }
   int incl = sum;
 #pragma unroll
@@ -78,7 +88,7 @@ __device__ __forceinline__ void kv4_plan(Kv4Plan* plan, const Kv4Args& a) {
   for (int j = first; j < first + per && j < a.batch; ++j) {
     plan->start[j] = at;
     const int L = kv4_len(a, j);
-    if (L >= 0) at += a.Hkv * a.tiles * (kv4_prefix<kStep>(a, L).steps + a.tree_steps);
+    if (L >= 0) at += kv4_positions<kStep>(a, L);
     if (j == a.batch - 1) plan->start[a.batch] = at;
   }
   __syncthreads();
@@ -114,10 +124,21 @@ __device__ __forceinline__ Kv4Unit kv4_unit(const Kv4Plan* plan, const Kv4Args& 
   u.r = lo;
   u.L = max(kv4_len(a, lo), 0);
   u.prefix = kv4_prefix<kStep>(a, u.L);
-  const int steps = u.prefix.steps + a.tree_steps, rem = pos - plan->start[lo], x = rem / steps;
-  u.g = x / a.tiles;
-  u.m = x - u.g * a.tiles;
-  u.begin = pos - (rem - x * steps);
+  const int fixed = a.unit_cost + u.prefix.steps, head = a.tiles * fixed + a.tree_total;
+  int rem = pos - plan->start[lo];
+  u.g = rem / head;
+  rem -= u.g * head;
+  // tiles [tree_from[k], tree_from[k + 1]) have k + 1 steps of the tree
+  int k = 0, at = 0;
+#pragma unroll 1
+  for (; k + 1 < a.tree_steps; ++k) {
+    const int next = at + (a.tree_from[k + 1] - a.tree_from[k]) * (fixed + k + 1);
+    if (rem < next) break;
+    at = next;
+  }
+  const int steps = fixed + k + 1, x = (rem - at) / steps;
+  u.m = a.tree_from[k] + x;
+  u.begin = pos - (rem - at - x * steps);
   u.end = u.begin + steps;
   return u;
 }
@@ -166,8 +187,8 @@ size_t kv4_rows_workspace_bytes(const seq_tree_kv4_attention_params& p);
 int launch_kv4_rows(const seq_tree_kv4_attention_params& p, cudaStream_t stream);
 size_t kv4_tiles_workspace_bytes();
 int launch_kv4_tiles(const seq_tree_kv4_attention_params& p, cudaStream_t stream);
-// Arguments that do not depend on the kernel
-Kv4Args kv4_args(const seq_tree_kv4_attention_params& p);
+// Arguments, for tiles of so many query rows and steps of so many keys of the tree
+Kv4Args kv4_args(const seq_tree_kv4_attention_params& p, int row_tile, int step);
 // Adds the pieces of the units that are cut.  tiles: which kernel left them.
 int launch_kv4_merge(const Kv4Args& a, bool bf16, bool tiles, cudaStream_t stream);
 // The workspace's parts: ws_o, ws_ml, ws_cut

@@ -206,7 +206,7 @@ __global__ void __launch_bounds__(32 * kRowsWarps, NT == 1 ? 3 : 2) kv4_rows_ker
     if (a.lengths[own.r] > a.max_len && threadIdx.x == 0) dev_flag(a.status, SEQ_DEV_BAD_LENGTH);
     if (own.L < 0) return;  // (the whole cluster)
     own.prefix = kv4_prefix<kKeys>(a, own.L);
-    own.end = own.prefix.steps + a.tree_steps;
+    own.end = own.prefix.steps + (min(a.n, ((own.m + 1) * a.row_tile + a.group - 1) / a.group) + kTreeStep - 1) / kTreeStep;
     range_lo = own.end * rank / a.cluster;
     range_hi = own.end * (rank + 1) / a.cluster;
     __syncthreads();
@@ -729,10 +729,7 @@ size_t kv4_rows_workspace_bytes(const seq_tree_kv4_attention_params& p) {
 
 int launch_kv4_rows(const seq_tree_kv4_attention_params& p, cudaStream_t stream) {
   const int nt = rows_nt(p);
-  Kv4Args a = kv4_args(p);
-  a.row_tile = 8 * nt;
-  a.tiles = (a.rows + a.row_tile - 1) / a.row_tile;
-  a.tree_steps = (a.n + kTreeStep - 1) / kTreeStep;
+  Kv4Args a = kv4_args(p, 8 * nt, kTreeStep);
   a.min_steps = kRowsWarps;
   a.cluster = kv4_rows_cluster(p);
   const bool bf16 = p.dtype == SEQ_BF16;

@@ -34,6 +34,7 @@ constexpr int kStageBytes = kHalfKeys / kGranule * kGranuleBytes;
 constexpr int kTreeTiles = SEQ_MAX_TREE / kTilesStep;
 
 constexpr int kStages = 6;
+constexpr int kUnitCost = 2;  // steps
 constexpr uint32_t kTmemS = 128;  // tensor memory: O in columns 0..127, then the S/P buffers
 
 struct TilesSmem {
@@ -102,21 +103,19 @@ __device__ __forceinline__ void tmem_get64(uint32_t taddr, uint32_t (&r)[64]) {
 }
 __device__ __forceinline__ uint32_t bits_below(int x) { return x <= 0 ? 0u : (x >= 32 ? 0xffffffffu : (1u << x) - 1u); }
 
-// The steps of a unit that fall into a CTA's range.  Steps of the tree behind the unit's last node are nobody's.
+// The steps of a unit that fall into a CTA's range: none, if that is only what stands for its cost
 struct TilesSeg {
   Kv4Unit u;
-  int32_t end, next, t0, steps;  // positions [pos, end), the next segment, first step, how many steps there are to do
+  int32_t next, t0, steps;  // the next segment's position, first step, how many
   bool whole;
 };
 __device__ __forceinline__ TilesSeg tiles_seg(const Kv4Plan* plan, const Kv4Args& a, int pos, int range_hi) {
   TilesSeg s;
   s.u = kv4_unit<kTilesStep>(plan, a, pos);
-  s.end = s.next = min(s.u.end, range_hi);
-  s.whole = pos == s.u.begin && s.end == s.u.end;
-  const int nodes = min(a.n, ((s.u.m + 1) * a.row_tile + a.group - 1) / a.group);
-  const int live_end = s.u.begin + s.u.prefix.steps + (nodes + kTilesStep - 1) / kTilesStep;
-  s.t0 = pos - s.u.begin;
-  s.steps = max(min(s.end, live_end) - pos, 0);
+  s.next = min(s.u.end, range_hi);
+  s.whole = pos == s.u.begin && s.next == s.u.end;
+  s.t0 = max(pos - s.u.begin - a.unit_cost, 0);
+  s.steps = max(s.next - s.u.begin - a.unit_cost, 0) - s.t0;
   return s;
 }
 
@@ -481,22 +480,20 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
         sm->sum[grp][row] = poison != 0 ? NAN : m_used == -INFINITY ? l : l * ex2(m_used - M);
         rows_sync();
         const float sum = sm->sum[0][row] + sm->sum[1][row];
-        uint32_t o[64];
-        tmem_get64(tmem_o + 64u * grp, o);
-        tc_fence_before();
-        rows_sync();  // the accumulator is read, the rows are through with what they exchanged
-        if (!sg.whole) {  // a piece, unnormalised
-          const int64_t mine = (int64_t)kv4_slot(ranges, blockIdx.x, sg.u.begin) * kTileM;
-          uint4* to = reinterpret_cast<uint4*>(a.ws_o + mine * kHeadDim) + 16 * grp * kTileM + row;  // [channel / 4][row]
+        const float inv = 1.f / sum;
+        const int64_t mine = (int64_t)kv4_slot(ranges, blockIdx.x, sg.u.begin) * kTileM;
+#pragma unroll 1
+        for (int c = grp; c < 4; c += kGroups) {  // 32 columns
+          uint32_t o[32];
+          tmem_get32(tmem_o + 32u * c, o);
+          if (!sg.whole) {  // a piece, unnormalised
+            uint4* to = reinterpret_cast<uint4*>(a.ws_o + mine * kHeadDim) + 8 * c * kTileM + row;  // [channel / 4][row]
 #pragma unroll
-          for (int e = 0; e < 64; e += 4) to[(e >> 2) * kTileM] = any ? make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]) : make_uint4(0u, 0u, 0u, 0u);
-          if (grp == 0) a.ws_ml[mine + row] = make_float2(M, sum);
-        } else {
-          const float inv = 1.f / sum;
-          if (valid) {
-            uint8_t* out = a.out + r * a.o_req + node * a.o_tok + h * a.o_head + 128 * grp;
+            for (int e = 0; e < 32; e += 4) to[(e >> 2) * kTileM] = any ? make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]) : make_uint4(0u, 0u, 0u, 0u);
+          } else if (valid) {
+            uint8_t* out = a.out + r * a.o_req + node * a.o_tok + h * a.o_head + 64 * c;
 #pragma unroll
-            for (int e = 0; e < 64; e += 8) {  // columns 0,2,4,6,1,3,5,7 are channels 0..7
+            for (int e = 0; e < 32; e += 8) {  // columns 0,2,4,6,1,3,5,7 are channels 0..7
               float y[8];
 #pragma unroll
               for (int z = 0; z < 8; ++z) y[z] = __uint_as_float(o[e + z]) * inv;
@@ -504,7 +501,13 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
                   make_uint4(pack2<kBf16>(y[0], y[2]), pack2<kBf16>(y[4], y[6]), pack2<kBf16>(y[1], y[3]), pack2<kBf16>(y[5], y[7]));
             }
           }
-          if (valid && grp == 0 && a.lse != nullptr) a.lse[((int64_t)r * a.Hq + h) * a.n + node] = (M + log2f(sum)) * kLn2;
+          __syncwarp();
+        }
+        tc_fence_before();
+        rows_sync();  // the accumulator is read, the rows are through with what they exchanged
+        if (grp == 0) {
+          if (!sg.whole) a.ws_ml[mine + row] = make_float2(M, sum);
+          else if (valid && a.lse != nullptr) a.lse[((int64_t)r * a.Hq + h) * a.n + node] = (M + log2f(sum)) * kLn2;
         }
       }
       if (!more) break;
@@ -638,12 +641,10 @@ size_t kv4_tiles_workspace_bytes() {
 
 int launch_kv4_tiles(const seq_tree_kv4_attention_params& p, cudaStream_t stream) {
   const int sms = device_sm_count();
-  Kv4Args a = kv4_args(p);
-  a.row_tile = kTileM;
-  a.tiles = (a.rows + kTileM - 1) / kTileM;
-  a.tree_steps = (a.n + kTilesStep - 1) / kTilesStep;
-  a.min_steps = 2;
-  const int64_t most = (int64_t)a.batch * a.Hkv * a.tiles * ((p.max_len + kTilesStep - 1) / kTilesStep + 1 + a.tree_steps);
+  Kv4Args a = kv4_args(p, kTileM, kTilesStep);
+  a.unit_cost = kUnitCost;
+  a.min_steps = 2 + kUnitCost;
+  const int64_t most = (int64_t)a.batch * a.Hkv * a.tiles * ((p.max_len + kTilesStep - 1) / kTilesStep + 1 + a.unit_cost + a.tree_steps);
   if (most > 0x7fffffff) return SEQ_ERR_UNSUPPORTED;
   const int64_t want = (most + a.min_steps - 1) / a.min_steps;
   a.ctas = want < sms ? (int)want : sms;
