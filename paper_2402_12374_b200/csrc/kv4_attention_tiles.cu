@@ -350,8 +350,9 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
               // that do become NaN when they are written
               const uint32_t b4 = __ballot_sync(0xffffffffu, (big & 0xffffu) == 0x7c00u || (big >> 16) == 0x7c00u);
               if ((b4 >> (lane & 28)) & 15u) keep = 0u;
+              if (b4 != 0)
 #pragma unroll 1
-              for (int z = 0; z < 8; ++z) bad |= (b4 >> (4 * z)) & 15u ? 1u << (8 * y + z) : 0u;
+                for (int z = 0; z < 8; ++z) bad |= (b4 >> (4 * z)) & 15u ? 1u << (8 * y + z) : 0u;
             }
             const uint32_t line = tile + (w4 * 32 + 8 * y) * 128;
 #pragma unroll
