@@ -456,24 +456,26 @@ int seq_tree_kv_commit(const seq_tree_kv_commit_params* p, void* stream);
  *   sinks    below `sinks` (0 and more; not read without a window): the first tokens that stay visible.
  * depth(i) is the number of i's ancestors, the set bits of its mask row less one; a node always sees itself.
  * n_tree = 1 is a plain decoding step of one token.
- *   q, out           element (r,i,h,c) at r*stride_req + i*stride_tok + h*stride_head + c, f16 or bf16
+ *   q, out           element (r,i,h,c) at r*stride_req + i*stride_tok + h*stride_head + c, f16 or bf16 (a stride of 0 repeats q's or the
+ *                    tree's rows; of out it is refused)
  *   k_tree, v_tree   element (r,i,g,c) at r*t_stride_req + i*t_stride_tok + g*t_stride_head + c, the same type.  Rows that a
  *                    node does not see may hold anything; one that it does see with an inf or NaN among its values (or a
  *                    magnitude above 65504) makes the node's whole output row NaN.
  *   pages            device, 16-byte aligned: kv head g of page p starts at p*page_stride_bytes + g*page_size*136
- *   max_len          the largest length a request can have: sizes the launch; <= max_pages * page_size.  A longer one raises
- *                    SEQ_DEV_BAD_LENGTH and is cut.
+ *   max_len          the largest length a request can have: sizes the launch and chooses the kernel, so a bound far above the
+ *                    lengths costs time; <= max_pages * page_size.  A longer length raises SEQ_DEV_BAD_LENGTH and is cut.
  *   mask_bits        nullable: ancestor words as seq_tree_mask_from_parents writes them, request r's at
  *                    r*mask_stride_req (words; 0: one tree for all).  NULL: node i sees the nodes 0..i (a chain).
  *   lse              nullable, [batch][num_q_heads][n_tree] fp32 natural-log sum-exp.
- *   workspace        seq_tree_kv4_attention_workspace_bytes(p) bytes, 256-byte aligned, device, contents undefined before
- *                    and after: the pieces of work that several CTAs share.  Two calls that can run at the same time
- *                    need one each.
- * All rows 16-byte aligned, head_dim 128, SEQ_F16 or SEQ_BF16.  Products run in half precision with fp32 sums: q enters
- * exactly (scaled by a power of two per row), a key's codes exactly or as its value rounded to half, V and the probabilities rounded to
- * half (2^-12 of the value); tree rows of bf16 as half as well.  Softmax and sums are fp32.  The same call on the same
- * inputs returns the same bits.  Returns SEQ_OK, SEQ_ERR_INVALID_ARG, SEQ_ERR_UNSUPPORTED (head_dim, dtype, page size),
- * SEQ_ERR_WORKSPACE or SEQ_ERR_CUDA.
+ *   workspace        seq_tree_kv4_attention_workspace_bytes(p) bytes (0 where little work is cut within clusters; then it may be
+ *                    NULL), 256-byte aligned, device, contents undefined before and after: the pieces of work that several
+ *                    CTAs share.  Two calls that can run at the same time need one each.
+ * All rows 16-byte aligned, head_dim 128, SEQ_F16 or SEQ_BF16.  Products run in half precision with fp32 sums.  q enters
+ * exactly (a bf16 row scaled by a power of two); tree rows of bf16 are rounded to half.  Where a kv head has few rows, the pages' codes
+ * enter exactly, keys' scales and mids are applied in fp32, and a value's scale times its probability is rounded to half; in
+ * tiles of many rows a key's and a value's number, scale * (code - 8) + mid, and its probability are each rounded to half (2^-11
+ * of the number).  Softmax and sums are fp32.  The same call on the same inputs returns the same bits.  Returns SEQ_OK,
+ * SEQ_ERR_INVALID_ARG, SEQ_ERR_UNSUPPORTED (head_dim, dtype, page size, 2^31 tiles of work), SEQ_ERR_WORKSPACE or SEQ_ERR_CUDA.
  */
 typedef struct {
   int32_t batch, n_tree, max_len, num_q_heads, num_kv_heads, head_dim;

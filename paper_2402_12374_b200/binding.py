@@ -186,6 +186,21 @@ def _stream(stream) -> int:
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
+def _here(*tensors) -> int:
+    """The current device, where the launch goes: the tensors have to be there."""
+    device = _raw_device()
+    for t in tensors:
+        if t is not None and t.get_device() != device:
+            raise ValueError(f"a tensor lives on cuda:{t.get_device()}, the current device is cuda:{device}")
+    return device
+
+
+def _hold(tensor, stream) -> None:
+    """A tensor of the binding's own that a call on ``stream`` uses: its memory is not given to another stream before that."""
+    if stream is not None:
+        tensor.record_stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(_stream(stream), device=tensor.device))
+
+
 def _check(fn: str, code: int) -> None:
     if code != SEQ_OK:
         raise SeqTreeError(fn, code)
@@ -562,7 +577,8 @@ class KV4AttentionCall:
             raise ValueError("pool must be one layer's: pool[:, layer]")
         if k_tree.shape != (R, n, Hkv, d) or v_tree.shape != k_tree.shape:
             raise ValueError("k_tree and v_tree must be [requests, nodes, kv heads, head_dim], the heads those of the pool")
-        if out is None:
+        given = out is not None
+        if not given:
             out = torch.empty_like(q)
         if out.shape != q.shape or out.dtype != q.dtype:
             raise ValueError("out must be like q")
@@ -597,18 +613,27 @@ class KV4AttentionCall:
         p.lse = _dev(lse, "lse", torch.float32)
         p.dev_status = _dev(dev_status, "dev_status", torch.int32)
         need = load().seq_tree_kv4_attention_workspace_bytes(C.byref(p))
+        self._own = [] if given else [out]
         if workspace is None and need:
             workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+            self._own.append(workspace)
         if workspace is not None:
             p.workspace, p.workspace_bytes = _dev(workspace, "workspace"), workspace.numel() * workspace.element_size()
         self.params, self.out, self.lse, self.workspace, self.workspace_bytes_needed = p, out, lse, workspace, need
         self._ref, self._fn = C.byref(p), load().seq_tree_kv4_attention
         self._keep = (q, k_tree, v_tree, pool, page_table, lengths, mask_bits, out, lse, workspace, dev_status)
+        self._device = _here(*self._keep)
 
     def run(self, stream=None):
-        rc = self._fn(self._ref, _raw_stream(_raw_device()) if stream is None else _stream(stream))
+        device = _raw_device()
+        if device != self._device:
+            raise ValueError(f"the call's tensors live on cuda:{self._device}, the current device is cuda:{device}")
+        rc = self._fn(self._ref, _raw_stream(device) if stream is None else _stream(stream))
         if rc:
             _check("seq_tree_kv4_attention", rc)
+        if stream is not None:
+            for t in self._own:
+                _hold(t, stream)
         return self.out
 
 
@@ -647,6 +672,7 @@ def seq_tree_kv4_append(k, v, pool, page_table, lengths, *, count=None, path=Non
             raise ValueError("path must be [requests, rows] with contiguous rows")
         p.path, p.path_stride = _dev(path, "path", torch.int32), path.stride(0) if p.batch > 1 else path.shape[1]
     p.new_lengths = _per_slot(new_lengths, p.batch, "new_lengths")
+    _here(k, v, pool, page_table, lengths, count, path, new_lengths, dev_status)
     _check("seq_tree_kv4_append", load().seq_tree_kv4_append(C.byref(p), _stream(stream)))
 
 
@@ -654,6 +680,7 @@ def seq_tree_kv4_read(pool, page_table, k_out, v_out, *, start=None, count=None,
     """Tokens start[r] (0 without it) .. start[r] + count[r] - 1 of each request as 16-bit rows into k_out, v_out [layers, R, rows,
     Hkv, 128] (layers optional); rows from count[r] on are left as they are."""
     p = _kv4_rows(k_out, v_out, pool, page_table, start, count, dev_status, "k_out and v_out")
+    _here(k_out, v_out, pool, page_table, start, count, dev_status)
     _check("seq_tree_kv4_read", load().seq_tree_kv4_read(C.byref(p), _stream(stream)))
     return k_out, v_out
 
@@ -704,7 +731,9 @@ def seq_tree_pages_resize(page_table, page_count, ref_count, tokens, page_size: 
     p = _pages_params(page_table, page_count, ref_count, page_size, table_out, count_out, refs_out, dev_status)
     p.tokens = _per_slot(tokens, p.slots, "tokens")
     workspace = _pages_workspace(p, workspace, page_count)
+    _here(page_table, page_count, ref_count, tokens, table_out, count_out, refs_out, workspace, dev_status)
     _check("seq_tree_pages_resize", load().seq_tree_pages_resize(C.byref(p), _stream(stream)))
+    _hold(workspace, stream)
 
 
 def seq_tree_pages_fork(pool, page_table, page_count, ref_count, lengths, source, page_size: int, *, table_out=None, count_out=None,
@@ -716,7 +745,9 @@ def seq_tree_pages_fork(pool, page_table, page_count, ref_count, lengths, source
     p.lengths_out = p.lengths if lengths_out is None else _per_slot(lengths_out, p.slots, "lengths_out")
     _pages_pool(p, pool, planes)
     workspace = _pages_workspace(p, workspace, page_count)
+    _here(pool, page_table, page_count, ref_count, lengths, source, table_out, count_out, refs_out, lengths_out, workspace, dev_status)
     _check("seq_tree_pages_fork", load().seq_tree_pages_fork(C.byref(p), _stream(stream)))
+    _hold(workspace, stream)
 
 
 def seq_tree_pages_compact(pool, page_table, page_count, ref_count, *, table_out=None, refs_out=None, live=None, planes: bool = False,
@@ -727,7 +758,9 @@ def seq_tree_pages_compact(pool, page_table, page_count, ref_count, *, table_out
     p.live = _dev(live, "live", torch.int32)
     _pages_pool(p, pool, planes)
     workspace = _pages_workspace(p, workspace, page_count)
+    _here(pool, page_table, page_count, ref_count, table_out, refs_out, live, workspace, dev_status)
     _check("seq_tree_pages_compact", load().seq_tree_pages_compact(C.byref(p), _stream(stream)))
+    _hold(workspace, stream)
 
 
 class TreeBuildParams(C.Structure):

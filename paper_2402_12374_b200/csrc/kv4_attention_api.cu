@@ -130,6 +130,8 @@ static int check_kv4_attention(const seq_tree_kv4_attention_params* p) {
   for (int64_t s : {p->q_stride_req, p->q_stride_tok, p->q_stride_head, p->t_stride_req, p->t_stride_tok, p->t_stride_head, p->o_stride_req,
                     p->o_stride_tok, p->o_stride_head})
     if (s < 0 || s % 8 != 0) return SEQ_ERR_INVALID_ARG;
+  if ((p->batch > 1 && p->o_stride_req == 0) || (p->n_tree > 1 && p->o_stride_tok == 0) || (p->num_q_heads > 1 && p->o_stride_head == 0))
+    return SEQ_ERR_INVALID_ARG;  // rows of out over one another
   if (p->mask_bits != nullptr && (p->mask_words_per_row < (p->n_tree + 31) / 32 || p->mask_stride_req < 0)) return SEQ_ERR_INVALID_ARG;
   return SEQ_OK;
 }

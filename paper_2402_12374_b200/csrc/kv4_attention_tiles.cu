@@ -12,12 +12,17 @@
 //
 // Two groups of 128 threads, a thread a row, have the even and the odd key tiles, three S/P buffers let the next tiles' scores be
 // computed meanwhile.  Both add to one accumulator and share the rows' reference maxima, which they settle in the keys' order (see
-// the groups).
+// the groups).  A group reads a tile's scores twice, 32 at a time, for the maximum and for the exponentials: the second reading costs
+// less than the registers and the code that keep them.  While a segment's results are written the next one's Q is in place already
+// and its first scores are computed.
 //
-// What bounds it: instruction issue.  A tile costs an SM's scheduler about 600 instructions to unpack K and V, 550 for its part of the
-// 128 x 128 exponentials, and as many again for waits, addresses and hand-overs; loops that are not unrolled, as what the
-// warps run has to stay in the instruction caches.  Two tiles of 128 rows that shared the unpacked keys had one S buffer each and
-// spent the time they saved on waiting for products (768 nodes on 4096 tokens of 64/8 heads: 204 us).
+// What bounds it: instructions, 1650 a scheduler and key tile (600 to unpack K and V, 500 for the 128 x 128 scores, the rest
+// waits, hand-overs, the tree's tiles and the segments' ends), of which 0.61 are issued a cycle; and that they have to be in the
+// instruction caches: five warps of a scheduler run four different loops.  So loops are rolled and there is one copy of each: a
+// third of the code less gave 203 -> 188 us (768 nodes on 4096 tokens of 64/8 heads, 64 us at the tensor cores' rate; 175 now).
+// Without effect or slower, for that reason or another: three groups (182 us against 180), sixteen unpacking warps (185), 16 scores
+// at a time (186 against 181), the ancestor words fetched ahead (181 against 171), 16 rows of the tree in flight (70b 168 against
+// 171, 64 nodes of 32/32 heads 63 against 59), and two tiles of 128 rows that shared the unpacked keys.
 //
 // Every mbarrier wait is bounded; one that runs out raises SEQ_DEV_TIMEOUT and the CTA drains.
 #include "kv4_attention.cuh"
@@ -34,7 +39,7 @@ constexpr int kStageBytes = kHalfKeys / kGranule * kGranuleBytes;
 constexpr int kTreeTiles = SEQ_MAX_TREE / kTilesStep;
 
 constexpr int kStages = 6;
-constexpr int kUnitCost = 2;  // steps
+constexpr int kUnitCost = 2;  // steps that a unit's start and end take (0, 1, 2, 3: 172.7, 172.4, 171.5, 171.7 us)
 constexpr uint32_t kTmemS = 128;  // tensor memory: O in columns 0..127, then the S/P buffers
 
 struct TilesSmem {

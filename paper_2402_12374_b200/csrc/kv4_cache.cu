@@ -320,5 +320,8 @@ extern "C" int seq_tree_kv4_read(const seq_tree_kv4_append_params* p, void* stre
   const int rc = check_rows(p);
   if (rc != SEQ_OK) return rc;
   if (p->path != nullptr || p->new_lengths != nullptr) return SEQ_ERR_INVALID_ARG;
+  if ((p->num_layers > 1 && p->stride_layer == 0) || (p->batch > 1 && p->stride_req == 0) || (p->n_rows > 1 && p->stride_tok == 0) ||
+      (p->num_kv_heads > 1 && p->stride_head == 0))
+    return SEQ_ERR_INVALID_ARG;  // rows over one another
   return launch_rows<false>(p, stream);
 }

@@ -311,3 +311,39 @@ def test_workspace_that_is_too_small_is_refused(room):
             call.run()
     if room == "tight":
         assert Case([45], 1, 8, 1, 16, torch.float16).call().workspace is None  # a cluster a unit: none is needed
+
+
+def test_memory_of_a_call_on_another_stream_is_not_handed_out(room):
+    """The workspace and out of a call on a stream of its own outlive the call object until that stream is through."""
+    c = Case([300, 20, 411] * 12, 1, 8, 2, 16, torch.float16, seed=3) if room == "roomy" else Case([300, 20] * 30, 20, 8, 2, 16, torch.float16, seed=3)
+    want = c.call().run().clone()
+    q, kt, vt, pool, table = c.q.cuda(), c.kt.cuda(), c.vt.cuda(), c.pool_dev[:, 0], torch.from_numpy(c.table).cuda()
+    lengths = torch.tensor(c.lengths, dtype=torch.int32, device="cuda")
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(50_000_000)
+    call = B.KV4AttentionCall(q, kt, vt, pool, table, lengths, mask_bits=c.mask)
+    need, held = call.workspace_bytes_needed, set(t.data_ptr() for t in (call.out, call.workspace) if t is not None)
+    out = call.run(stream=side)
+    del call
+    others = [torch.empty(max(need, 1), dtype=torch.uint8, device="cuda") for _ in range(4)]
+    assert need > 0 and not held & set(t.data_ptr() for t in others)
+    side.synchronize()
+    assert torch.equal(out, want)
+
+
+def test_tensors_of_another_device_are_refused(monkeypatch):
+    """The launch goes to the current device."""
+    c = Case([45], 1, 8, 1, 16, torch.float16)
+    call = c.call()
+    one = torch.zeros(1, dtype=torch.int32, device="cuda")
+    rows = torch.zeros(1, 1, 2, 1, 128, dtype=torch.float16, device="cuda")
+    table = torch.from_numpy(c.table).cuda()
+    refs = torch.zeros(c.pool.shape[0], dtype=torch.int32, device="cuda")
+    monkeypatch.setattr(B, "_raw_device", lambda: 1)
+    for f in (call.run, c.call, lambda: B.seq_tree_kv4_append(rows, rows, c.pool_dev, table, one), lambda: B.seq_tree_kv4_read(c.pool_dev, table, rows, rows),
+              lambda: B.seq_tree_pages_resize(table, one, refs, one, 16), lambda: B.seq_tree_pages_compact(c.pool_dev, table, one, refs),
+              lambda: B.seq_tree_pages_fork(c.pool_dev, table, one, refs, one, one, 16)):
+        with pytest.raises(ValueError, match="current device"):
+            f()

@@ -53,13 +53,16 @@ def attention(**kw):
     return p
 
 
+ROOMY = dict(max_pages=4000, table_stride=4000, max_len=60000)  # more than clusters take
+
+
 @pytest.mark.parametrize("bad", [dict(q=None), dict(k_tree=None), dict(v_tree=None), dict(pages=None), dict(page_table=None), dict(lengths=None),
                                  dict(out=None), dict(batch=0), dict(batch=1025), dict(n_tree=0), dict(n_tree=1025), dict(max_len=-1), dict(max_len=113),
                                  dict(num_kv_heads=5), dict(num_kv_heads=0), dict(num_q_heads=0), dict(window=-1), dict(sinks=-1), dict(num_pages=0),
                                  dict(max_pages=0), dict(table_stride=6), dict(page_stride_bytes=8 * 16 * 136 - 16), dict(page_stride_bytes=8 * 16 * 136 + 8),
                                  dict(q=FAKE + 2), dict(pages=FAKE + 8), dict(out=FAKE + 4), dict(q_stride_head=129), dict(o_stride_tok=-128),
                                  dict(t_stride_req=4), dict(mask_words_per_row=0), dict(mask_stride_req=-1), dict(softmax_scale=float("nan")),
-                                 dict(softmax_scale=float("inf")), dict(workspace=FAKE + 16)])
+                                 dict(softmax_scale=float("inf")), dict(workspace=FAKE + 16, **ROOMY)])
 def test_attention_refuses(lib, bad):
     assert lib.seq_tree_kv4_attention(C.byref(attention(**bad)), None) == B.SEQ_ERR_INVALID_ARG
 
@@ -69,8 +72,17 @@ def test_attention_does_not_support(lib, bad):
     assert lib.seq_tree_kv4_attention(C.byref(attention(**bad)), None) == B.SEQ_ERR_UNSUPPORTED
 
 
+@pytest.mark.parametrize("bad", [dict(o_stride_req=0), dict(o_stride_tok=0), dict(o_stride_head=0)])
+def test_attention_refuses_rows_of_out_over_one_another(lib, bad):
+    assert lib.seq_tree_kv4_attention(C.byref(attention(**bad)), None) == B.SEQ_ERR_INVALID_ARG
+
+
 def test_attention_needs_its_workspace(lib):
-    assert lib.seq_tree_kv4_attention(C.byref(attention(workspace=None)), None) == B.SEQ_ERR_WORKSPACE
+    for n in (1, 4, 16):  # one tile of rows, two, tensor-core tiles
+        need = lib.seq_tree_kv4_attention_workspace_bytes(C.byref(attention(n_tree=n, **ROOMY)))
+        for bad in (dict(workspace=None), dict(workspace_bytes=need - 1)):
+            assert need > 0 and lib.seq_tree_kv4_attention(C.byref(attention(n_tree=n, **ROOMY, **bad)), None) == B.SEQ_ERR_WORKSPACE
+    assert lib.seq_tree_kv4_attention_workspace_bytes(C.byref(attention())) == 0  # clusters
     assert lib.seq_tree_kv4_attention(None, None) == B.SEQ_ERR_INVALID_ARG
     assert lib.seq_tree_kv4_attention_workspace_bytes(None) == 0
     assert lib.seq_tree_kv4_attention_workspace_bytes(C.byref(attention(num_kv_heads=0))) == 0
@@ -103,7 +115,7 @@ def test_append_and_read_refuse(lib, bad):
 def test_append_and_read_refuse_what_is_not_theirs(lib):
     for bad in (dict(lengths=None), dict(new_lengths=FAKE), dict(path=FAKE, path_stride=15)):
         assert lib.seq_tree_kv4_append(C.byref(rows(**bad)), None) == B.SEQ_ERR_INVALID_ARG
-    for bad in (dict(path=FAKE, path_stride=16), dict(new_lengths=FAKE + 16)):
+    for bad in (dict(path=FAKE, path_stride=16), dict(new_lengths=FAKE + 16), dict(stride_layer=0), dict(stride_req=0), dict(stride_tok=0), dict(stride_head=0)):
         assert lib.seq_tree_kv4_read(C.byref(rows(**bad)), None) == B.SEQ_ERR_INVALID_ARG
     for bad in (dict(head_dim=96), dict(dtype=B.SEQ_F32), dict(page_size=24)):
         for fn in (lib.seq_tree_kv4_append, lib.seq_tree_kv4_read):
