@@ -5,8 +5,12 @@
 //     O += P V    128x128x128, P from tensor memory, V from shared memory
 //
 // What is special is where K and V come from.  Bulk copies bring granules (16 tokens, 2176 bytes) of 4-bit codes into a ring;
-// four warps turn them into half-precision tiles in the layout that the tensor core reads (128-byte swizzle): scale * (code - 8) +
-// mid, one rounding.  Eight channels leave a code word in the order 0,4,1,5,2,6,3,7 (two nibbles of a 32-bit word per instruction);
+// eight warps turn them into half-precision tiles in the layout that the tensor core reads (128-byte swizzle).  For bfloat16 rows
+// a tile holds scale * (code - 8) + mid, one rounding, an eighth of out's.  For half-precision rows it holds code - 8, and the
+// scales and mids are applied in fp32: a score is s * (q . code) + m * sum(q), P is scale * probability (the rows' reference counts the
+// tile's largest scale, so that it fits), and the sum of m * probability is added to all channels of O.  One rounding instead of three,
+// 3.0e-4 instead of 4.6e-4 of the output (2.1e-4 are out's own), and scores as exact as fp32 is, for 20 % of the time (64 nodes of
+// 32/32 heads over a window of 4096: 59 -> 71 us).  Eight channels leave a code word in the order 0,4,1,5,2,6,3,7 (two nibbles of a 32-bit word per instruction);
 // Q's channels are stored in that order too, and O's columns are put back when the rows are written.  The tree's 16-bit rows go
 // through the same warps.
 //
@@ -38,11 +42,13 @@ constexpr int kHalfKeys = 64;       // keys of a ring stage
 constexpr int kStageBytes = kHalfKeys / kGranule * kGranuleBytes;
 constexpr int kTreeTiles = SEQ_MAX_TREE / kTilesStep;
 
-constexpr int kStages = 6;
+constexpr int kParamTiles = 5;  // tiles of scales and mids: one is written again behind the scores that follow its own three tiles later
 constexpr int kUnitCost = 2;  // steps that a unit's start and end take (0, 1, 2, 3: 172.7, 172.4, 171.5, 171.7 us)
 constexpr uint32_t kTmemS = 128;  // tensor memory: O in columns 0..127, then the S/P buffers
 
+template <bool kExact>
 struct TilesSmem {
+  static constexpr int kStages = kExact ? 5 : 6;
   uint8_t q[kTileBytes];     // tiles: 1024-byte aligned
   uint8_t k[2][kTileBytes];  // [key tile parity]
   uint8_t v[2][kTileBytes];
@@ -60,12 +66,19 @@ struct TilesSmem {
   uint32_t tmem_base;
   volatile int abort_flag;
   Kv4Plan plan;
+  // exact codes: scales and mids of the tiles' keys and values (two keys' scales, their mids), the largest scale's bits of 32 values, the
+  // rows' sums of q, and of mid * probability
+  float4 key_params[kExact ? kParamTiles : 1][kTilesStep / 2], value_params[kExact ? kParamTiles : 1][kTilesStep / 2];
+  int4 largest[kExact ? kParamTiles : 1];
+  float q_sum[kExact ? kGroups : 1][kTileM], mids[kExact ? kGroups : 1][kTileM];
 };
-constexpr size_t kTilesSmemBytes = sizeof(TilesSmem) + 1024;
-static_assert(kTilesSmemBytes <= 227 * 1024, "one CTA's shared memory");
+template <bool kExact>
+constexpr size_t kTilesSmemBytes = sizeof(TilesSmem<kExact>) + 1024;
+static_assert(kTilesSmemBytes<false> <= 227 * 1024 && kTilesSmemBytes<true> <= 227 * 1024, "one CTA's shared memory");
 
 // mbar_wait, rolled: what the warps run has to stay in the instruction caches
-__device__ __forceinline__ bool kv4_wait(TilesSmem* sm, uint64_t* bar, uint32_t parity, int32_t* status) {
+template <typename Smem>
+__device__ __forceinline__ bool kv4_wait(Smem* sm, uint64_t* bar, uint32_t parity, int32_t* status) {
 #pragma unroll 1
   for (uint32_t it = 0; it < kSpinLimit; ++it) {
     if (mbar_try_wait(bar, parity)) return true;
@@ -126,8 +139,12 @@ __device__ __forceinline__ TilesSeg tiles_seg(const Kv4Plan* plan, const Kv4Args
 
 template <bool kBf16>
 __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Args a) {
+  // Half-precision rows: codes enter as they are, see the head.  (For bfloat16 ones out's rounding is 8 times as coarse as a value's.)
+  constexpr bool kExact = !kBf16;
+  using Smem = TilesSmem<kExact>;
+  constexpr int kStages = Smem::kStages;
   extern __shared__ uint8_t smem_raw[];
-  TilesSmem* sm = reinterpret_cast<TilesSmem*>(smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u));
+  Smem* sm = reinterpret_cast<Smem*>(smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u));
   const int warp = uniform((int)threadIdx.x >> 5), lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
     for (int s = 0; s < kStages; ++s) { mbar_init(&sm->raw_full[s], 1); mbar_init(&sm->raw_empty[s], 8); }
@@ -288,6 +305,8 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
         const int left = (tree ? a.n : sg.u.L) - key0;  // keys of the tile that there are
         if (w > 0) ok = kv4_wait(sm, &empty[b], (w - 1) & 1, a.status);
         const uint32_t tile = smem_u32(which ? sm->v[b] : sm->k[b]);
+        const int slot = kExact ? x % kParamTiles : 0;
+        uint32_t largest = 0;  // exact codes: the warps of K leave the scales and mids of both, as they are ahead
         if (!tree) {
 #pragma unroll 1
           for (int h = 0; h < 2 && ok; ++h) {
@@ -313,11 +332,24 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
               const uint32_t scale = __byte_perm(params[y], 0u, 0x1010), mid = __byte_perm(params[y], 0u, 0x3232);
               const uint32_t words[4] = {swap ? cd[y].z : cd[y].x, swap ? cd[y].w : cd[y].y, swap ? cd[y].x : cd[y].z, swap ? cd[y].y : cd[y].w};
               const uint32_t line = tile + (h * kHalfKeys + w4 * kGranule + 8 * y) * 128;
+              if (kExact && which == 0) {
+                const int key = h * kHalfKeys + w4 * kGranule + 8 * y + r8;
+                uint32_t values = 0;
+                if (key < left) asm volatile("ld.shared.u32 %0, [%1];" : "=r"(values) : "r"(granule + kGranuleParams + kGranule * 4 + (8 * y + r8) * 4));
+                largest = max(largest, values & 0x7fffu);
+                const float2 sm2 = __half22float2(*reinterpret_cast<const __half2*>(quad == 0 ? &params[y] : &values));
+                float* to = reinterpret_cast<float*>(quad == 0 ? sm->key_params[slot] : sm->value_params[slot]) + 4 * (key >> 1) + (key & 1);
+                if (quad < 2) {
+                  to[0] = sm2.x;
+                  to[2] = sm2.y;
+                }
+              }
 #pragma unroll
               for (int p = 0; p < 4; ++p) {
                 uint32_t v[4];
                 unpack4(words[p], v);
-                sts128(line + place[p], hfma2_bits(v[0], scale, mid), hfma2_bits(v[1], scale, mid), hfma2_bits(v[2], scale, mid), hfma2_bits(v[3], scale, mid));
+                if (kExact) sts128(line + place[p], v[0], v[1], v[2], v[3]);
+                else sts128(line + place[p], hfma2_bits(v[0], scale, mid), hfma2_bits(v[1], scale, mid), hfma2_bits(v[2], scale, mid), hfma2_bits(v[3], scale, mid));
               }
             }
             if (h * kHalfKeys < left) {
@@ -327,6 +359,16 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
             }
           }
         } else if (ok) {
+          if (kExact && which == 0) {  // (the tree's rows are what they are)
+            largest = 0x3c00u;
+            const int at = 4 * (w4 * 16 + (lane >> 1)) + (lane & 1);
+            float* to = reinterpret_cast<float*>(sm->key_params[slot]) + at;
+            to[0] = 1.f;
+            to[2] = 0.f;
+            to = reinterpret_cast<float*>(sm->value_params[slot]) + at;
+            to[0] = 1.f;
+            to[2] = 0.f;
+          }
           uint32_t bad = 0;  // of the warp's 32 rows
           const uint8_t* rows = (which ? a.vt : a.kt) + sg.u.r * a.t_req + sg.u.g * a.t_head + quad * 64;
 #pragma unroll 1
@@ -369,6 +411,10 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
           if (which == 1 && lane == 0) sm->bad[seg & 3][key0 / kTilesStep][w4] = bad;
         }
         if (!ok) break;
+        if (kExact && which == 0) {
+          largest = __reduce_max_sync(0xffffffffu, largest);
+          if (lane == 0) reinterpret_cast<int*>(&sm->largest[slot])[w4] = (int)largest;
+        }
         fence_async_smem();
         __syncwarp();
         if (lane == 0) mbar_arrive(&full[b]);
@@ -391,13 +437,13 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
     struct Row {
       TilesSeg sg;
       int node, h, depth, begin, latest;  // (begin: where the row's window begins)
-      float rs;
+      float rs, q_sum;
       bool valid, warp_live;              // a warp of padding rows only keeps in step
       const uint32_t* mask;
     };
     Row cur;
     bool have = false;
-    float m_used = -INFINITY, l = 0.f;
+    float m_used = -INFINITY, l = 0.f, mids = 0.f;
     for (int pos = range_lo;;) {
       // ---- the next segment's rows; its first scores are computed while the last segment's results are written
       Row next;
@@ -429,6 +475,21 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
               f = __uint_as_float((uint32_t)(127 + up) << 23);
               rs *= __uint_as_float((uint32_t)(127 - up) << 23);
             }
+          }
+          if (kExact) {
+            float sum = 0.f;
+#pragma unroll
+            for (int p = 0; p < 8; ++p) {
+              const uint32_t y[4] = {x[p].x, x[p].y, x[p].z, x[p].w};
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                const float2 two = __half22float2(*reinterpret_cast<const __half2*>(&y[e]));
+                sum += two.x + two.y;
+              }
+            }
+            sm->q_sum[grp][row] = sum;
+            rows_sync();
+            next.q_sum = sm->q_sum[0][row] + sm->q_sum[1][row];
           }
           if (have && cur.sg.steps > 0) {  // the scores of the segment before are complete
             const int x = step - 1, u = x / kSBufs;
@@ -484,14 +545,20 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
         // ---- the groups' sums, against the reference that O ended in: the last one settled
         const float M = any ? sm->ref[row] : -INFINITY;
         sm->sum[grp][row] = poison != 0 ? NAN : m_used == -INFINITY ? l : l * ex2(m_used - M);
+        if (kExact) sm->mids[grp][row] = m_used == -INFINITY ? 0.f : mids * ex2(m_used - M);
         rows_sync();
         const float sum = sm->sum[0][row] + sm->sum[1][row];
+        const float all_mids = kExact ? sm->mids[0][row] + sm->mids[1][row] : 0.f;
         const float inv = 1.f / sum;
         const int64_t mine = (int64_t)kv4_slot(ranges, blockIdx.x, sg.u.begin) * kTileM;
 #pragma unroll 1
         for (int c = grp; c < 4; c += kGroups) {  // 32 columns
           uint32_t o[32];
           tmem_get32(tmem_o + 32u * c, o);
+          if (kExact) {
+#pragma unroll
+            for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) + all_mids);
+          }
           if (!sg.whole) {  // a piece, unnormalised
             uint4* to = reinterpret_cast<uint4*>(a.ws_o + mine * kHeadDim) + 8 * c * kTileM + row;  // [channel / 4][row]
 #pragma unroll
@@ -525,10 +592,11 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
       const float rs = cur.rs;
       const bool warp_live = cur.warp_live;
       m_used = -INFINITY;
-      l = 0.f;
+      l = mids = 0.f;
       for (int i = (grp ^ step) & 1; i < sg.steps; i += kGroups, ++own) {
         const int t = sg.t0 + i, x = step + i, u = x / kSBufs, sb = x - u * kSBufs;
         const uint32_t tmem_s = tmem + kTmemS + 128u * sb + lane_sel;
+        const int slot = kExact ? x % kParamTiles : 0;
         const bool tree = t >= sg.u.prefix.steps;
         const int key0 = (tree ? t - sg.u.prefix.steps : sg.u.prefix.key_step(t)) * kTilesStep;
         const bool masked = tree || key0 + kTilesStep > L || key0 < latest;  // some keys are not there, or not every row's
@@ -551,15 +619,28 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
 #pragma unroll 1
           for (int c = 0; c < 4; ++c) {
             tmem_get32(tmem_s + 32u * c, s);
-            if (masked) {
-              hide(c, s);
-              tmem_st32(tmem_s + 32u * c, s, 0);
+            if (kExact) {
+              const uint64_t q_sum2 = pair_of(cur.q_sum, cur.q_sum);
+#pragma unroll
+              for (int e = 0; e < 16; ++e) {
+                const float4 kp = sm->key_params[slot][16 * c + e];
+                float y0, y1;
+                unpair(fma2(pair_of(__uint_as_float(s[2 * e]), __uint_as_float(s[2 * e + 1])), pair_of(kp.x, kp.y), mul2(pair_of(kp.z, kp.w), q_sum2)), y0, y1);
+                s[2 * e] = __float_as_uint(y0);
+                s[2 * e + 1] = __float_as_uint(y1);
+              }
             }
+            if (masked) hide(c, s);
+            if (masked || kExact) tmem_st32(tmem_s + 32u * c, s, 0);
 #pragma unroll
             for (int e = 0; e < 32; e += 2) mx[(e >> 1) & 3] = max3(mx[(e >> 1) & 3], __uint_as_float(s[e]), __uint_as_float(s[e + 1]));
           }
-          if (masked) tc_wait_st();
-          const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * rs;  // rs > 0
+          if (masked || kExact) tc_wait_st();
+          float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * rs;  // rs > 0
+          if (kExact) {  // scale * probability is what is rounded: the reference counts the tile's largest scale
+            const int4 big = sm->largest[slot];
+            top += (float)((max(max(big.x, big.y), max(big.z, big.w)) >> 10) - 15);
+          }
           // All groups add to one accumulator, so they share the rows' reference: it is settled tile by tile, in order, before the
           // exponentials.  It moves only when a score exceeds it by more than the threshold, or with the first score.
           float ref = -INFINITY;
@@ -595,12 +676,14 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
           }
           if (lane == 0) mbar_arrive(&sm->settled[grp][quarter]);
           if (now != m_used) {
-            l *= m_used == -INFINITY ? 0.f : ex2(m_used - now);
+            const float f = m_used == -INFINITY ? 0.f : ex2(m_used - now);
+            l *= f;
+            mids *= f;
             m_used = now;
           }
           const float neg_m = now == -INFINITY ? 0.f : -now;
           const uint64_t rs2 = pair_of(rs, rs), neg_m2 = pair_of(neg_m, neg_m);
-          uint64_t sums[2] = {pair_of(0.f, 0.f), pair_of(0.f, 0.f)};
+          uint64_t sums[2] = {pair_of(0.f, 0.f), pair_of(0.f, 0.f)}, mids2 = pair_of(0.f, 0.f);
 #pragma unroll 1
           for (int c = 0; c < 4; ++c) {
             tmem_get32(tmem_s + 32u * c, s);
@@ -609,8 +692,14 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
             for (int e = 0; e < 16; ++e) {
               float y0, y1;
               unpair(fma2(pair_of(__uint_as_float(s[2 * e]), __uint_as_float(s[2 * e + 1])), rs2, neg_m2), y0, y1);
-              const float p0 = ex2(y0), p1 = ex2(y1);
+              float p0 = ex2(y0), p1 = ex2(y1);
               sums[e & 1] = add2(sums[e & 1], pair_of(p0, p1));
+              if (kExact) {
+                const float4 vp = sm->value_params[slot][16 * c + e];
+                const uint64_t p = pair_of(p0, p1);
+                mids2 = fma2(p, pair_of(vp.z, vp.w), mids2);
+                unpair(mul2(p, pair_of(vp.x, vp.y)), p0, p1);
+              }
               packed[e] = pack2<false>(p0, p1);
             }
             tmem_st16(tmem_s + 64u * (c >> 1) + 16u * (c & 1), packed);  // over scores that have been read
@@ -619,6 +708,10 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
           unpair(sums[0], s0, s1);
           unpair(sums[1], s2, s3);
           l += (s0 + s1) + (s2 + s3);
+          if (kExact) {
+            unpair(mids2, s0, s1);
+            mids += s0 + s1;
+          }
           tc_wait_st();
           tc_fence_before();
         } else if (lane == 0) {
@@ -658,25 +751,25 @@ int launch_kv4_tiles(const seq_tree_kv4_attention_params& p, cudaStream_t stream
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(a.ctas);
   cfg.blockDim = dim3(kTilesThreads);
-  cfg.dynamicSmemBytes = kTilesSmemBytes;
   cfg.stream = stream;
   cudaLaunchAttribute early[1];
   early[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   early[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = early;
   cfg.numAttrs = 1;
-  auto launch = [&](auto kernel, int which) -> int {
+  auto launch = [&](auto kernel, int which, size_t smem) -> int {
     static int done[2][64];
     const int rc = once_per_device(done[which], [&]() -> int {
-      SEQ_CUDA_OK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kTilesSmemBytes));
+      SEQ_CUDA_OK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
       return SEQ_OK;
     });
     if (rc != SEQ_OK) return rc;
+    cfg.dynamicSmemBytes = smem;
     SEQ_CUDA_OK(cudaLaunchKernelEx(&cfg, kernel, a));
     return SEQ_OK;
   };
   const bool bf16 = p.dtype == SEQ_BF16;
-  const int rc = bf16 ? launch(kv4_tiles_kernel<true>, 0) : launch(kv4_tiles_kernel<false>, 1);
+  const int rc = bf16 ? launch(kv4_tiles_kernel<true>, 0, kTilesSmemBytes<false>) : launch(kv4_tiles_kernel<false>, 1, kTilesSmemBytes<true>);
   return rc != SEQ_OK ? rc : launch_kv4_merge(a, bf16, true, stream);
 }
 

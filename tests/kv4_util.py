@@ -126,10 +126,13 @@ def attention(q, kt, vt, k, v, seen, scale=None, window=0, sinks=0):
 def check_attention(got, got_lse, ref, dt, exact_keys):
     """Roundings: the output's, half a step; V's and P's to half precision; a key's value to half precision in 128 channels
     (independent: four standard deviations of a uniform error) where codes are not used exactly.  A score that is off by d
-    changes a probability by d and the sum by as much.  fp32 sums and ex2.approx: 2e-5."""
+    changes a probability by d and the sum by as much.  fp32 sums and ex2.approx: 2e-5.  With exact_keys the scores (lse shows them) have no
+    term for the keys.  The output keeps it: where codes enter exactly, what is rounded is a probability times a scale, which is
+    off by half a step of |scale * code| <= |v| + |mid|, not of |v|."""
     out, lse, spread, noise = ref
-    score = 2e-5 + (0.0 if exact_keys else 4 / 3 ** 0.5 * HALF) * noise
-    tol = EPS2[dt] * out.abs() + spread * (2 * HALF + 2 * score[..., None]) + 1e-7
+    rounded = 4 / 3 ** 0.5 * HALF * noise
+    score = 2e-5 + (0.0 if exact_keys else 1.0) * rounded
+    tol = EPS2[dt] * out.abs() + spread * (2 * HALF + 2 * (2e-5 + rounded)[..., None]) + 1e-7
     err = (got.double().cpu() - out).abs()
     assert torch.isfinite(got.float()).all()
     worst = (err / tol).max().item()

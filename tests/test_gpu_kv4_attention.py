@@ -94,7 +94,7 @@ def test_one_token_of_grouped_heads(L, page, dt):
 @pytest.mark.parametrize("n,Hq,Hkv", [(1, 4, 4), (2, 8, 2), (8, 2, 2), (16, 1, 1), (5, 6, 2), (7, 10, 2), (3, 40, 8), (33, 2, 1), (64, 4, 4), (100, 10, 2),
                                       (200, 8, 1), (65, 16, 2)])
 def test_trees_and_groups(n, Hq, Hkv, dt):
-    Case([77, 200], n, Hq, Hkv, 32, dt, seed=n, mask="each").check()
+    Case([77, 200], n, Hq, Hkv, 32, dt, seed=n, mask="each").check(exact_keys=dt == torch.float16)
 
 
 @pytest.mark.parametrize("n,Hq", [(1, 2), (1, 130), (40, 3), (130, 1), (129, 4)])
@@ -106,7 +106,7 @@ def test_chain_without_a_mask(n, Hq):
 @pytest.mark.parametrize("window,sinks", [(1, 0), (1, 3), (16, 0), (40, 4), (100, 33), (127, 1), (128, 0), (129, 300), (5000, 2), (1 << 30, 1 << 30)])
 @pytest.mark.parametrize("n,Hq", [(1, 8), (12, 1), (40, 4)])
 def test_window_and_sinks(window, sinks, n, Hq, dt):
-    Case([0, 5, 300, 431], n, Hq, 1, 16, dt, seed=window, mask="each").check(window=window, sinks=sinks)
+    Case([0, 5, 300, 431], n, Hq, 1, 16, dt, seed=window, mask="each").check(exact_keys=dt == torch.float16, window=window, sinks=sinks)
 
 
 def test_window_inside_a_deep_tree():
@@ -141,7 +141,25 @@ def test_many_ragged_requests(n, Hq):
 
 @pytest.mark.parametrize("n,Hq", [(1, 4), (50, 4)])
 def test_a_long_prefix_of_one_request(n, Hq):
-    Case([6001], n, Hq, 1, 64, torch.float16, seed=5).check()
+    Case([6001], n, Hq, 1, 64, torch.float16, seed=5).check(exact_keys=True)
+
+
+@BOTH
+@pytest.mark.parametrize("n,Hq", [(1, 8), (40, 4)])
+def test_scales_of_many_magnitudes(n, Hq, dt):
+    """Values from 1e-3 to 1e4 among the keys and values, large ones where a window hides them, rows of one number (scale 0)."""
+    c = Case([300, 200], n, Hq, 1, 16, dt, seed=12, mask="each")
+    rng = np.random.default_rng(5)
+    for r, L in enumerate(c.lengths):
+        for t in range(L):
+            for kv in range(2):
+                size = 10.0 ** rng.uniform(-3, -1) if t < L // 2 else 10.0 ** rng.uniform(-1, 1 if kv == 0 else 4)
+                x = rng.standard_normal(128) * size + size if t % 7 else np.full(128, size)
+                U.store(c.pool, c.table[r, t // 16], 0, 0, 16, t, kv, *U.quantise(x))
+    c.pool_dev = torch.from_numpy(c.pool).reshape(c.pool.shape[0], 1, 1, -1).cuda()
+    c.q = c.q * 0.1
+    c.check()
+    c.check(window=64, sinks=30)
 
 
 def test_same_call_same_bits_and_any_workspace_contents():
