@@ -18,10 +18,11 @@ struct Kv4Args {
   int32_t window, sinks;
   int32_t num_pages, page_size, page_shift;
   int32_t row_tile, tiles, ctas, min_steps, cluster;
-  int32_t unit_cost;   // positions at a unit's start that stand for what a unit costs
+  int32_t unit_cost;   // positions at a unit's start that stand for what a unit costs,
+  int32_t tree_cost;   // ... and as many for each of its steps of the tree, for what these take longer
   int32_t tree_steps;  // of the last tile of rows; a tile has those up to its last node
   int32_t tree_from[kKv4TreeSteps];  // the first tile with more than k steps of the tree
-  int32_t tree_total;  // the tree's steps of all tiles
+  int32_t tree_total;  // positions of all tiles' steps of the tree, with what they take longer
   const uint8_t* q; int64_t q_req, q_tok, q_head;  // all strides in bytes
   const uint8_t* kt; const uint8_t* vt; int64_t t_req, t_tok, t_head;
   const uint8_t* pages; int64_t page_stride;
@@ -59,6 +60,8 @@ __device__ __forceinline__ Kv4Prefix kv4_prefix(const Kv4Args& a, int L) {
 
 // Request r's prefix; -1: idle
 __device__ __forceinline__ int kv4_len(const Kv4Args& a, int r) { return min(max(a.lengths[r], -1), a.max_len); }
+
+__host__ __device__ __forceinline__ int kv4_tree_positions(const Kv4Args& a, int steps) { return steps * (1 + a.tree_cost); }
 
 // Positions of a request
 template <int kStep>
@@ -110,7 +113,7 @@ __device__ __forceinline__ Kv4Ranges kv4_ranges(const Kv4Plan* plan, const Kv4Ar
 
 struct Kv4Unit {
   int32_t r, g, m, L;
-  int32_t begin, end;  // positions
+  int32_t begin, work, end;  // positions: what stands for costs, the steps
   Kv4Prefix prefix;
 };
 template <int kStep>
@@ -132,14 +135,15 @@ __device__ __forceinline__ Kv4Unit kv4_unit(const Kv4Plan* plan, const Kv4Args& 
   int k = 0, at = 0;
 #pragma unroll 1
   for (; k + 1 < a.tree_steps; ++k) {
-    const int next = at + (a.tree_from[k + 1] - a.tree_from[k]) * (fixed + k + 1);
+    const int next = at + (a.tree_from[k + 1] - a.tree_from[k]) * (fixed + kv4_tree_positions(a, k + 1));
     if (rem < next) break;
     at = next;
   }
-  const int steps = fixed + k + 1, x = (rem - at) / steps;
+  const int steps = fixed + kv4_tree_positions(a, k + 1), x = (rem - at) / steps;
   u.m = a.tree_from[k] + x;
   u.begin = pos - (rem - at - x * steps);
   u.end = u.begin + steps;
+  u.work = u.end - (k + 1) - u.prefix.steps;
   return u;
 }
 // Where CTA c leaves its piece of a unit that begins at `begin`: the piece that opens its range, or the one that closes it.
@@ -188,7 +192,7 @@ int launch_kv4_rows(const seq_tree_kv4_attention_params& p, cudaStream_t stream)
 size_t kv4_tiles_workspace_bytes();
 int launch_kv4_tiles(const seq_tree_kv4_attention_params& p, cudaStream_t stream);
 // Arguments, for tiles of so many query rows and steps of so many keys of the tree
-Kv4Args kv4_args(const seq_tree_kv4_attention_params& p, int row_tile, int step);
+Kv4Args kv4_args(const seq_tree_kv4_attention_params& p, int row_tile, int step, int unit_cost, int tree_cost);
 // Adds the pieces of the units that are cut.  tiles: which kernel left them.
 int launch_kv4_merge(const Kv4Args& a, bool bf16, bool tiles, cudaStream_t stream);
 // The workspace's parts: ws_o, ws_ml, ws_cut

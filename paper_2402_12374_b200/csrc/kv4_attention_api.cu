@@ -77,7 +77,7 @@ int launch_kv4_merge(const Kv4Args& a, bool bf16, bool tiles, cudaStream_t strea
   return SEQ_OK;
 }
 
-Kv4Args kv4_args(const seq_tree_kv4_attention_params& p, int row_tile, int step) {
+Kv4Args kv4_args(const seq_tree_kv4_attention_params& p, int row_tile, int step, int unit_cost, int tree_cost) {
   Kv4Args a = {};
   a.batch = p.batch; a.n = p.n_tree; a.max_len = p.max_len; a.Hq = p.num_q_heads; a.Hkv = p.num_kv_heads;
   a.group = p.num_q_heads / p.num_kv_heads;
@@ -96,11 +96,13 @@ Kv4Args kv4_args(const seq_tree_kv4_attention_params& p, int row_tile, int step)
   a.scale_log2 = (p.softmax_scale > 0.f ? p.softmax_scale : 0.08838834764831845f) * kLog2e;
   a.status = p.dev_status;
   a.row_tile = row_tile;
+  a.unit_cost = unit_cost;
+  a.tree_cost = tree_cost;
   a.tiles = (a.rows + row_tile - 1) / row_tile;
   for (int m = 0; m < a.tiles; ++m) {
     const int nodes = std::min(a.n, ((m + 1) * row_tile + a.group - 1) / a.group), steps = (nodes + step - 1) / step;
     while (a.tree_steps < steps) a.tree_from[a.tree_steps++] = m;
-    a.tree_total += steps;
+    a.tree_total += kv4_tree_positions(a, steps);
   }
   return a;
 }

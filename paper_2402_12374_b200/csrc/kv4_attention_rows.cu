@@ -729,7 +729,7 @@ size_t kv4_rows_workspace_bytes(const seq_tree_kv4_attention_params& p) {
 
 int launch_kv4_rows(const seq_tree_kv4_attention_params& p, cudaStream_t stream) {
   const int nt = rows_nt(p);
-  Kv4Args a = kv4_args(p, 8 * nt, kTreeStep);
+  Kv4Args a = kv4_args(p, 8 * nt, kTreeStep, 0, 0);
   a.min_steps = kRowsWarps;
   a.cluster = kv4_rows_cluster(p);
   const bool bf16 = p.dtype == SEQ_BF16;

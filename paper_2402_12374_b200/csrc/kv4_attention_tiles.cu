@@ -43,7 +43,8 @@ constexpr int kStageBytes = kHalfKeys / kGranule * kGranuleBytes;
 constexpr int kTreeTiles = SEQ_MAX_TREE / kTilesStep;
 
 constexpr int kParamTiles = 5;  // tiles of scales and mids: one is written again behind the scores that follow its own three tiles later
-constexpr int kUnitCost = 2;  // steps that a unit's start and end take (0, 1, 2, 3: 172.7, 172.4, 171.5, 171.7 us)
+constexpr int kUnitCost = 2;  // steps that a unit's start and end take (768 nodes on 4096 tokens, 0, 1, 2, 3: 172.7, 172.4, 171.5, 171.7 us)
+constexpr int kTreeCost = 1;  // steps that one of the tree takes longer (0, 1/2, 1, 3/2: 165.1, 161.4, 160.4, 164.0 us)
 constexpr uint32_t kTmemS = 128;  // tensor memory: O in columns 0..127, then the S/P buffers
 
 template <bool kExact>
@@ -132,8 +133,8 @@ __device__ __forceinline__ TilesSeg tiles_seg(const Kv4Plan* plan, const Kv4Args
   s.u = kv4_unit<kTilesStep>(plan, a, pos);
   s.next = min(s.u.end, range_hi);
   s.whole = pos == s.u.begin && s.next == s.u.end;
-  s.t0 = max(pos - s.u.begin - a.unit_cost, 0);
-  s.steps = max(s.next - s.u.begin - a.unit_cost, 0) - s.t0;
+  s.t0 = max(pos - s.u.work, 0);
+  s.steps = max(s.next - s.u.work, 0) - s.t0;
   return s;
 }
 
@@ -740,10 +741,9 @@ size_t kv4_tiles_workspace_bytes() {
 
 int launch_kv4_tiles(const seq_tree_kv4_attention_params& p, cudaStream_t stream) {
   const int sms = device_sm_count();
-  Kv4Args a = kv4_args(p, kTileM, kTilesStep);
-  a.unit_cost = kUnitCost;
+  Kv4Args a = kv4_args(p, kTileM, kTilesStep, kUnitCost, kTreeCost);
   a.min_steps = 2 + kUnitCost;
-  const int64_t most = (int64_t)a.batch * a.Hkv * a.tiles * ((p.max_len + kTilesStep - 1) / kTilesStep + 1 + a.unit_cost + a.tree_steps);
+  const int64_t most = (int64_t)a.batch * a.Hkv * a.tiles * ((p.max_len + kTilesStep - 1) / kTilesStep + 1 + a.unit_cost + kv4_tree_positions(a, a.tree_steps));
   if (most > 0x7fffffff) return SEQ_ERR_UNSUPPORTED;
   const int64_t want = (most + a.min_steps - 1) / a.min_steps;
   a.ctas = want < sms ? (int)want : sms;
