@@ -472,7 +472,8 @@ int seq_tree_kv_commit(const seq_tree_kv_commit_params* p, void* stream);
  *                    CTAs share.  Two calls that can run at the same time need one each.
  * All rows 16-byte aligned, head_dim 128, SEQ_F16 or SEQ_BF16.  Products run in half precision with fp32 sums.  q enters
  * exactly (a bf16 row scaled by a power of two); tree rows of bf16 are rounded to half.  The pages' codes enter exactly, scales and mids
- * are applied in fp32, and a value's scale times its probability is rounded to half (2^-11 of it).  Only where the rows are bf16 and
+ * are applied in fp32, and a value's scale times its probability is rounded to half (2^-11 of it, but no finer than 2^-24 of the
+ * largest scale among the keys that are read).  Only where the rows are bf16 and
  * a kv head has many of them, a key's and a value's number, scale * (code - 8) + mid, and its probability are each rounded to
  * half, out's own rounding being eight times as coarse.  Softmax and sums are fp32.  The same call on the same inputs returns the same bits.  Returns SEQ_OK,
  * SEQ_ERR_INVALID_ARG, SEQ_ERR_UNSUPPORTED (head_dim, dtype, page size, 2^31 tiles of work), SEQ_ERR_WORKSPACE or SEQ_ERR_CUDA.

@@ -39,6 +39,7 @@ constexpr int kUnpackWarp = 4, kGroupWarp = 12, kGroups = 2, kSBufs = 3;
 constexpr int kTilesStep = 128;     // keys
 constexpr int kRegsIssue = 40, kRegsUnpack = 56, kRegsGroup = 160;  // 128 * 40 + 256 * 56 + 256 * 160 <= 640 * 96
 constexpr int kHalfKeys = 64;       // keys of a ring stage
+constexpr float kLargestHalf = 65504.f;
 constexpr int kStageBytes = kHalfKeys / kGranule * kGranuleBytes;
 constexpr int kTreeTiles = SEQ_MAX_TREE / kTilesStep;
 
@@ -326,6 +327,21 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
                 asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(cd[y].x), "=r"(cd[y].y), "=r"(cd[y].z), "=r"(cd[y].w)
                              : "r"(granule + which * kGranuleV + (8 * y + r8) * kCodeBytes + quad * 16));
                 asm volatile("ld.shared.u32 %0, [%1];" : "=r"(params[y]) : "r"(granule + kGranuleParams + which * (kGranule * 4) + (8 * y + r8) * 4));
+              }
+            }
+            if (!kExact) {
+              // A row's largest value can be past the largest half (65504 comes back as 65536), and an infinity in a tile of V gets
+              // into rows that do not see it: where 8 scale + |mid| is, the scale is cut to what fits, by a step of half's at most.
+              const uint32_t most = hfma2_bits(__byte_perm(params[0], params[1], 0x5410) & 0x7fff7fffu, 0x48004800u, __byte_perm(params[0], params[1], 0x7632) & 0x7fff7fffu);
+              if (__any_sync(0xffffffffu, (((most & 0x7fff7fffu) + 0x04000400u) & 0x80008000u) != 0)) {
+#pragma unroll 1
+                for (int y = 0; y < 2; ++y) {
+                  const uint32_t one = y == 0 ? params[0] : params[1];
+                  const float2 v = __half22float2(*reinterpret_cast<const __half2*>(&one));
+                  const __half fits = __float2half_rz(fminf(v.x, fminf((kLargestHalf - v.y) * (1.f / 7.f), (kLargestHalf + v.y) * 0.125f)));
+                  const uint32_t now = (one & 0xffff0000u) | __half_as_ushort(fits);
+                  if (y == 0) params[0] = now; else params[1] = now;
+                }
               }
             }
 #pragma unroll

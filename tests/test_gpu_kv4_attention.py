@@ -92,7 +92,7 @@ def test_one_token_of_grouped_heads(L, page, dt):
 
 @BOTH
 @pytest.mark.parametrize("n,Hq,Hkv", [(1, 4, 4), (2, 8, 2), (8, 2, 2), (16, 1, 1), (5, 6, 2), (7, 10, 2), (3, 40, 8), (33, 2, 1), (64, 4, 4), (100, 10, 2),
-                                      (200, 8, 1), (65, 16, 2)])
+                                      (200, 8, 1), (65, 16, 2), (1024, 1, 1), (700, 2, 1)])
 def test_trees_and_groups(n, Hq, Hkv, dt):
     Case([77, 200], n, Hq, Hkv, 32, dt, seed=n, mask="each").check(exact_keys=dt == torch.float16)
 
@@ -142,6 +142,23 @@ def test_many_ragged_requests(n, Hq):
 @pytest.mark.parametrize("n,Hq", [(1, 4), (50, 4)])
 def test_a_long_prefix_of_one_request(n, Hq):
     Case([6001], n, Hq, 1, 64, torch.float16, seed=5).check(exact_keys=True)
+
+
+@BOTH
+@pytest.mark.parametrize("n,Hq", [(1, 8), (40, 4)])
+def test_the_largest_magnitudes_stay_finite(n, Hq, dt):
+    """Rows up to +-65504, whose 4-bit forms reach past the largest half, before the window; rows below 6e4 inside."""
+    c = Case([300], n, Hq, 1, 16, dt, seed=12, mask="each")
+    rng = np.random.default_rng(5)
+    for t in range(300):
+        for kv in range(2):
+            x = rng.uniform(-1, 1, 128) * (65504 if t < 150 else 1.0 if kv == 0 else 6e4)
+            if t < 150:
+                x[:2] = (65504, -65504) if t % 2 else (65504, 65000)
+                x = np.clip(x, 65000, 65504) if t % 4 == 0 else x
+            U.store(c.pool, c.table[0, t // 16], 0, 0, 16, t, kv, *U.quantise(x))
+    c.pool_dev = torch.from_numpy(c.pool).reshape(c.pool.shape[0], 1, 1, -1).cuda()
+    c.check(window=100)
 
 
 @BOTH
@@ -221,9 +238,10 @@ def test_rows_that_a_node_does_not_see_may_hold_anything(n, Hq, dt):
             assert torch.equal(out[0, i], clean[0, i]), i
 
 
+@BOTH
 @pytest.mark.parametrize("n,Hq", [(1, 8), (20, 4)])
-def test_a_row_of_q_that_is_not_finite_stays_alone(n, Hq):
-    c = Case([45], n, Hq, 1, 16, torch.bfloat16, seed=8)
+def test_a_row_of_q_that_is_not_finite_stays_alone(n, Hq, dt):
+    c = Case([45], n, Hq, 1, 16, dt, seed=8)
     clean = c.call().run().clone()
     c.q[0, n - 1, 1, 3] = float("nan")
     out = c.call().run()
@@ -276,6 +294,12 @@ def test_bad_pages_and_lengths_are_reported():
         got = call.run().clone()
         assert int(c.status) == B.SEQ_DEV_BAD_LENGTH
         c.lengths = [60]
+        assert torch.equal(got, c.call(max_len=60).run())
+        c = Case([100] + [45] * 299, n, 8, 2, 16, torch.float16, seed=4)
+        call = c.call(max_len=60)
+        got = call.run().clone()
+        assert call.workspace_bytes_needed > 0 and int(c.status) == B.SEQ_DEV_BAD_LENGTH
+        c.lengths[0] = 60
         assert torch.equal(got, c.call(max_len=60).run())
 
 
