@@ -571,7 +571,7 @@ int seq_tree_kv4_read(const seq_tree_kv4_append_params* p, void* stream);
  * Every call reads them and writes the state after it to table_out (rows table_out_stride apart), count_out, refs_out and
  * lengths_out: either all of them the arrays they came from (then only what changes is written) or none, and nothing overlaps
  * (then they are written whole).  Free pages are always taken lowest number first, slots are served in order, so the
- * result is the same whatever runs first.  slots <= SEQ_MAX_SLOTS, num_pages below 2^30.
+ * result is the same whatever runs first.  slots <= SEQ_MAX_SLOTS, num_pages below 2^30, slots * max_pages below 2^31.
  *
  * _resize   tokens[slots]: slot r holds ceil(tokens[r] / page_size) pages afterwards (0 frees it; negative: left alone).
  *           Pages given up lose a reference; pages that are needed are free ones, after all that this call gives up.

@@ -587,6 +587,7 @@ static int check_pages(const seq_tree_pages_params* p) {
   if (p->slots < 1 || p->slots > SEQ_MAX_SLOTS || p->max_pages < 1 || p->max_pages >= (1 << 30) || p->num_pages < 1 || p->num_pages >= (1 << 30) ||
       p->table_stride < p->max_pages || p->table_out_stride < p->max_pages)
     return SEQ_ERR_INVALID_ARG;
+  if ((int64_t)p->slots * p->max_pages > 0x7fffffff) return SEQ_ERR_INVALID_ARG;  // what slots need is summed in 32 bits
   // all arrays in place, or none: what copies rows of the one reads the others while the plan writes them
   const bool in_place = p->table_out == p->page_table;
   if (in_place != (p->refs_out == p->ref_count) || (in_place && p->table_out_stride != p->table_stride)) return SEQ_ERR_INVALID_ARG;
@@ -596,7 +597,7 @@ static int check_pool(const seq_tree_pages_params* p) {
   if (p->pages == nullptr || reinterpret_cast<uintptr_t>(p->pages) % 16 != 0 || p->num_planes < 1) return SEQ_ERR_INVALID_ARG;
   if (p->page_bytes < 16 || p->page_bytes % 16 != 0 || p->page_stride_bytes < p->page_bytes || p->page_stride_bytes % 16 != 0) return SEQ_ERR_INVALID_ARG;
   if (p->num_planes > 1 && (p->plane_stride_bytes < p->page_bytes || p->plane_stride_bytes % 16 != 0)) return SEQ_ERR_INVALID_ARG;
-  if (p->page_bytes / kMoveChunk > (1 << 24)) return SEQ_ERR_INVALID_ARG;
+  if (p->page_bytes / kMoveChunk > (1 << 24) || p->num_planes * (p->page_bytes / kMoveChunk + 1) > 0x7fffffff) return SEQ_ERR_INVALID_ARG;
   return SEQ_OK;
 }
 static int check_workspace(const seq_tree_pages_params* p) {

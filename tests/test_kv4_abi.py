@@ -138,7 +138,8 @@ def pages(**kw):
 
 @pytest.mark.parametrize("bad", [dict(page_table=None), dict(page_count=None), dict(ref_count=None), dict(table_out=None), dict(refs_out=None), dict(slots=0),
                                  dict(slots=2049), dict(max_pages=0), dict(num_pages=0), dict(num_pages=1 << 30), dict(table_stride=9),
-                                 dict(table_out_stride=9), dict(table_out_stride=11), dict(table_out=FAKE + 8192), dict(refs_out=FAKE + 8192)])
+                                 dict(table_out_stride=9), dict(table_out_stride=11), dict(table_out=FAKE + 8192), dict(refs_out=FAKE + 8192),
+                                 dict(max_pages=1 << 29, table_stride=1 << 29, table_out_stride=1 << 29)])
 def test_pages_calls_refuse(lib, bad):
     for fn in (lib.seq_tree_pages_resize, lib.seq_tree_pages_fork, lib.seq_tree_pages_compact):
         assert fn(C.byref(pages(**bad)), None) == B.SEQ_ERR_INVALID_ARG
@@ -154,7 +155,8 @@ def test_pages_calls_refuse_what_each_needs(lib):
         assert lib.seq_tree_pages_resize(C.byref(pages(**bad)), None) == B.SEQ_ERR_WORKSPACE
     for fn in (lib.seq_tree_pages_fork, lib.seq_tree_pages_compact):
         for bad in (dict(pages=None), dict(pages=FAKE + 8), dict(num_planes=0), dict(page_bytes=0), dict(page_bytes=24), dict(page_stride_bytes=4080),
-                    dict(page_stride_bytes=4104), dict(num_planes=2, plane_stride_bytes=16), dict(workspace=FAKE + 4)):
+                    dict(page_stride_bytes=4104), dict(num_planes=2, plane_stride_bytes=16), dict(workspace=FAKE + 4),
+                    dict(num_planes=1 << 30, plane_stride_bytes=1 << 20, page_stride_bytes=1 << 20, page_bytes=1 << 20)):
             assert fn(C.byref(pages(**bad)), None) == B.SEQ_ERR_INVALID_ARG, bad
         for bad in (dict(workspace=None), dict(workspace_bytes=need - 1)):
             assert fn(C.byref(pages(**bad)), None) == B.SEQ_ERR_WORKSPACE
