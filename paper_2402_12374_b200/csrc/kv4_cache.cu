@@ -62,15 +62,19 @@ __device__ __forceinline__ uint32_t extremes(uint4 x) {
 }
 
 // The eight codes of a lane's channels.  Quotients are taken as products with the reciprocal (off by less than 3e-6 at +-8); `near`: one
-// lies so near the middle between two codes that this could decide.
+// lies so near the middle between two codes that this could decide, or outside the codes (where a row's mid is large against its
+// scale, so that mid's rounding counts): such lanes divide and clamp.
 constexpr float kMagic = 12582920.f;  // 1.5 * 2^23 + 8: adding it rounds to a whole number, even in the middle, 8 more in the last bits
-__device__ __forceinline__ uint32_t join8(const float* c) {
+__device__ __forceinline__ uint32_t join8(const float* c, uint32_t& outside) {
   // the last bits of each, four apart; what else the numbers hold is the same and taken off
   uint32_t word = 0, rest = 0;
+  outside = 0;
 #pragma unroll
   for (int i = 7; i >= 0; --i) {
-    word = word * 16u + __float_as_uint(fminf(fmaxf(c[i], kMagic - 8.f), kMagic + 7.f));
+    const uint32_t bits = __float_as_uint(c[i]);
+    word = word * 16u + bits;
     rest = rest * 16u + 0x4b400000u;
+    outside |= bits ^ 0x4b400000u;  // (above 15: not a code)
   }
   return word - rest;
 }
@@ -85,14 +89,17 @@ __device__ __forceinline__ uint32_t quantise8(const float* v, float inv, float m
     off = max3(off, fabsf(a), fabsf(b));
     unpair(y, c[i], c[i + 1]);
   }
-  near = off > 0.499995f;
-  return join8(c);
+  uint32_t outside;
+  const uint32_t word = join8(c, outside);
+  near = off > 0.499995f || outside > 15u;
+  return word;
 }
 __device__ __forceinline__ uint32_t divide8(const float* v, float scale, float mid) {
   float c[8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) c[i] = (scale > 0.f ? __fdiv_rn(v[i] - mid, scale) : 0.f) + kMagic;
-  return join8(c);
+  for (int i = 0; i < 8; ++i) c[i] = fminf(fmaxf((scale > 0.f ? __fdiv_rn(v[i] - mid, scale) : 0.f) + kMagic, kMagic - 8.f), kMagic + 7.f);
+  uint32_t outside;
+  return join8(c, outside);
 }
 __device__ __forceinline__ uint64_t shfl64(uint64_t x, int from) {
   const uint32_t lo = __shfl_sync(0xffffffffu, (uint32_t)x, from, 16), hi = __shfl_sync(0xffffffffu, (uint32_t)(x >> 32), from, 16);

@@ -90,6 +90,8 @@ def test_rows_that_are_hard_to_round(dt):
     rows.append(rng.standard_normal(128) * 1e-7)
     rows.append(rng.standard_normal(128) * 1e-4)
     rows.append(1000 + rng.standard_normal(128))
+    rows.append(2000.0 + np.arange(128) % 4)              # the mid's rounding is several codes
+    rows.append(-30000.0 - 16 * (np.arange(128) % 3))
     rows.append(rng.standard_normal(128) * 2e4 if dt == torch.float16 else rng.standard_normal(128) * 1e4)
     rows += [np.round(rng.standard_normal(128) * 4) / 8 for _ in range(40)]
     x = torch.tensor(np.stack(rows)).to(dt).reshape(1, 1, len(rows), 1, 128)
