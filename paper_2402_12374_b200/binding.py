@@ -186,8 +186,22 @@ def _stream(stream) -> int:
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
+def _ptr(t, name: str, dtype, device: int):
+    """The address of a tensor of the device that the call's other tensors are on (which ``_here`` looks at), in one step each."""
+    if t is None:
+        return None
+    if t.get_device() != device:
+        raise ValueError(f"{name} must be on the CUDA device that the other tensors are on")
+    if t.dtype is not dtype:
+        raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
+    return t.data_ptr()
+
+
 def _here(*tensors) -> int:
     """The current device, where the launch goes: the tensors have to be there."""
+    for t in tensors:
+        if t is not None and not t.is_cuda:
+            raise ValueError("tensors must live on a CUDA device (there is no CPU path)")
     device = _raw_device()
     for t in tensors:
         if t is not None and t.get_device() != device:
@@ -542,21 +556,21 @@ def _kv4_pool(pool):
     return layers, heads, part // 136, strides[0] if pages > 1 else layers * heads * part, strides[1] if layers > 1 else heads * part, pages
 
 
-def _table(page_table):
+def _table(page_table, device: int):
     """(address, entries between rows, rows, entries of a row)"""
     slots, most = page_table.shape
     row, one = page_table.stride()
     if one != 1:
         raise ValueError("page_table must be [slots, max_pages] with contiguous rows")
-    return _dev(page_table, "page_table", torch.int32), row if slots > 1 else most, slots, most
+    return _ptr(page_table, "page_table", torch.int32, device), row if slots > 1 else most, slots, most
 
 
-def _per_slot(t, slots: int, name: str):
+def _per_slot(t, slots: int, name: str, device: int):
     if t is None:
         return None
-    if t.dim() != 1 or t.shape[0] != slots or (t.stride(0) != 1 and slots > 1):
+    if t.shape != (slots,) or not t.is_contiguous():
         raise ValueError(f"{name} must be [{slots}], contiguous")
-    return _dev(t, name, torch.int32)
+    return _ptr(t, name, torch.int32, device)
 
 
 class KV4AttentionCall:
@@ -599,8 +613,8 @@ class KV4AttentionCall:
         p.k_tree, p.v_tree = _dev(k_tree, "k_tree"), _dev(v_tree, "v_tree")
         p.t_stride_req, p.t_stride_tok, p.t_stride_head = k_tree.stride()[:3]
         p.pages, p.page_stride_bytes, p.num_pages, p.page_size = _dev(pool, "pool"), page_stride, pages, page_size
-        p.page_table, p.table_stride, _, p.max_pages = _table(page_table)
-        p.lengths = _per_slot(lengths, R, "lengths")
+        p.page_table, p.table_stride, _, p.max_pages = _table(page_table, q.get_device())
+        p.lengths = _per_slot(lengths, R, "lengths", q.get_device())
         if mask_bits is not None:
             if mask_bits.stride(-1) != 1 or mask_bits.shape[-2] != n or (mask_bits.dim() == 3 and mask_bits.shape[0] != R) or mask_bits.dim() not in (2, 3):
                 raise ValueError("mask_bits must be [nodes, words] or [requests, nodes, words] with contiguous words")
@@ -645,21 +659,21 @@ def seq_tree_kv4_attention(q, k_tree, v_tree, pool, page_table, lengths, **kw):
 
 def _kv4_rows(k, v, pool, page_table, lengths, count, dev_status, what):
     layers, heads, page_size, page_stride, layer_stride, pages = _kv4_pool(pool)
-    shape, strides, dtype = k.shape, k.stride(), k.dtype
+    shape, strides, dtype, device = k.shape, k.stride(), k.dtype, pool.get_device()
     if len(shape) == 4:
         shape, strides = (1, *shape), (0, *strides)
     if len(shape) != 5 or v.shape != k.shape or v.stride() != k.stride() or strides[4] != 1:
         raise ValueError(f"{what} must be [layers, requests, rows, kv heads, head_dim] (layers optional) with the same strides, rows contiguous")
     if (dtype is not torch.float16 and dtype is not torch.bfloat16) or v.dtype is not dtype:
         raise ValueError(f"{what} must be float16 or bfloat16")
-    table, table_stride, slots, max_pages = _table(page_table)
+    table, table_stride, slots, max_pages = _table(page_table, device)
     R = shape[1]
     if shape[0] != layers or shape[3] != heads or slots != R:
         raise ValueError(f"{what}: layers and kv heads as in the pool, one row of page_table per request")
-    return Kv4AppendParams(layers, R, shape[2], heads, shape[4], SEQ_F16 if dtype is torch.float16 else SEQ_BF16, _dev(k, "k"), _dev(v, "v"),
-                           strides[0], strides[1], strides[2], strides[3], _dev(pool, "pool"), page_stride, layer_stride, pages, page_size,
-                           table, table_stride, max_pages, _per_slot(lengths, R, "lengths"), _per_slot(count, R, "count"), None, 0, None,
-                           _dev(dev_status, "dev_status", torch.int32))
+    return Kv4AppendParams(layers, R, shape[2], heads, shape[4], SEQ_F16 if dtype is torch.float16 else SEQ_BF16, _ptr(k, "k", dtype, device), _ptr(v, "v", dtype, device),
+                           strides[0], strides[1], strides[2], strides[3], pool.data_ptr(), page_stride, layer_stride, pages, page_size,
+                           table, table_stride, max_pages, _per_slot(lengths, R, "lengths", device), _per_slot(count, R, "count", device), None,
+                           0, None, _ptr(dev_status, "dev_status", torch.int32, device))
 
 
 def seq_tree_kv4_append(k, v, pool, page_table, lengths, *, count=None, path=None, new_lengths=None, dev_status=None, stream=None):
@@ -670,9 +684,9 @@ def seq_tree_kv4_append(k, v, pool, page_table, lengths, *, count=None, path=Non
     if path is not None:
         if path.dim() != 2 or path.shape[0] != p.batch or path.shape[1] < p.n_rows or path.stride(1) != 1:
             raise ValueError("path must be [requests, rows] with contiguous rows")
-        p.path, p.path_stride = _dev(path, "path", torch.int32), path.stride(0) if p.batch > 1 else path.shape[1]
-    p.new_lengths = _per_slot(new_lengths, p.batch, "new_lengths")
-    _here(k, v, pool, page_table, lengths, count, path, new_lengths, dev_status)
+        p.path, p.path_stride = _ptr(path, "path", torch.int32, pool.get_device()), path.stride(0) if p.batch > 1 else path.shape[1]
+    p.new_lengths = _per_slot(new_lengths, p.batch, "new_lengths", pool.get_device())
+    _here(pool)
     _check("seq_tree_kv4_append", load().seq_tree_kv4_append(C.byref(p), _stream(stream)))
 
 
@@ -680,34 +694,35 @@ def seq_tree_kv4_read(pool, page_table, k_out, v_out, *, start=None, count=None,
     """Tokens start[r] (0 without it) .. start[r] + count[r] - 1 of each request as 16-bit rows into k_out, v_out [layers, R, rows,
     Hkv, 128] (layers optional); rows from count[r] on are left as they are."""
     p = _kv4_rows(k_out, v_out, pool, page_table, start, count, dev_status, "k_out and v_out")
-    _here(k_out, v_out, pool, page_table, start, count, dev_status)
+    _here(pool)
     _check("seq_tree_kv4_read", load().seq_tree_kv4_read(C.byref(p), _stream(stream)))
     return k_out, v_out
 
 
 def _pages_params(page_table, page_count, ref_count, page_size, table_out, count_out, refs_out, dev_status):
-    table, table_stride, slots, max_pages = _table(page_table)
+    device = page_table.get_device()
+    table, table_stride, slots, max_pages = _table(page_table, device)
     out, out_stride = table, table_stride
     if table_out is not None:
-        out, out_stride, s, m = _table(table_out)
+        out, out_stride, s, m = _table(table_out, device)
         if s != slots or m != max_pages:
             raise ValueError("table_out must be like page_table")
     pages = ref_count.shape[0]
-    count, refs = _per_slot(page_count, slots, "page_count"), _per_slot(ref_count, pages, "ref_count")
+    count, refs = _per_slot(page_count, slots, "page_count", device), _per_slot(ref_count, pages, "ref_count", device)
     return PagesParams(slots, max_pages, pages, page_size, table, table_stride, count, refs, None, out, out_stride,
-                       count if count_out is None else _per_slot(count_out, slots, "count_out"),
-                       refs if refs_out is None else _per_slot(refs_out, pages, "refs_out"), None, None, None, None, 0, 0, 0, 0, None, None, 0,
-                       _dev(dev_status, "dev_status", torch.int32))
+                       count if count_out is None else _per_slot(count_out, slots, "count_out", device),
+                       refs if refs_out is None else _per_slot(refs_out, pages, "refs_out", device), None, None, None, None, 0, 0, 0, 0, None,
+                       None, 0, _ptr(dev_status, "dev_status", torch.int32, device))
 
 
 def _pages_workspace(p, workspace, like):
     if workspace is None:
         workspace = like.new_empty(load().seq_tree_pages_workspace_bytes(C.byref(p)) // 4)
-    p.workspace, p.workspace_bytes = _dev(workspace, "workspace"), workspace.numel() * workspace.element_size()
+    p.workspace, p.workspace_bytes = _ptr(workspace, "workspace", workspace.dtype, like.get_device()), workspace.numel() * workspace.element_size()
     return workspace  # (until the call is enqueued)
 
 
-def _pages_pool(p, pool, planes: bool):
+def _pages_pool(p, pool, planes: bool, device: int):
     """pool [pages, ...] (planes: [planes, pages, ...]) of any type, a page contiguous."""
     shape, strides, e = pool.shape, pool.stride(), pool.element_size()
     at = 1 if planes else 0  # the dimension of the pages
@@ -718,7 +733,7 @@ def _pages_pool(p, pool, planes: bool):
         size *= n
     if len(shape) < at + 2 or shape[at] != p.num_pages:
         raise ValueError("pool must be [pages, ...] ([planes, pages, ...] with planes=True), as many pages as ref_count")
-    p.pages, p.page_bytes = _dev(pool, "pool"), size * e
+    p.pages, p.page_bytes = _ptr(pool, "pool", pool.dtype, device), size * e
     p.page_stride_bytes = strides[at] * e if shape[at] > 1 else size * e
     p.num_planes = shape[0] if planes else 1
     p.plane_stride_bytes = strides[0] * e if planes and shape[0] > 1 else p.page_stride_bytes * p.num_pages
@@ -729,9 +744,9 @@ def seq_tree_pages_resize(page_table, page_count, ref_count, tokens, page_size: 
     """Slot r holds ceil(tokens[r] / page_size) pages afterwards (0: freed, negative: left alone).  In place, or into
     table_out, count_out, refs_out (all of them)."""
     p = _pages_params(page_table, page_count, ref_count, page_size, table_out, count_out, refs_out, dev_status)
-    p.tokens = _per_slot(tokens, p.slots, "tokens")
+    _here(page_table)
+    p.tokens = _per_slot(tokens, p.slots, "tokens", page_table.get_device())
     workspace = _pages_workspace(p, workspace, page_count)
-    _here(page_table, page_count, ref_count, tokens, table_out, count_out, refs_out, workspace, dev_status)
     _check("seq_tree_pages_resize", load().seq_tree_pages_resize(C.byref(p), _stream(stream)))
     _hold(workspace, stream)
 
@@ -741,11 +756,11 @@ def seq_tree_pages_fork(pool, page_table, page_count, ref_count, lengths, source
     """Empty slot r with source[r] = s >= 0 becomes a fork of slot s: full pages are shared, the open one is copied.  pool [pages,
     ...] of any type (planes=True: [planes, pages, ...]).  In place, or into the four outputs (all of them)."""
     p = _pages_params(page_table, page_count, ref_count, page_size, table_out, count_out, refs_out, dev_status)
-    p.lengths, p.source = _per_slot(lengths, p.slots, "lengths"), _per_slot(source, p.slots, "source")
-    p.lengths_out = p.lengths if lengths_out is None else _per_slot(lengths_out, p.slots, "lengths_out")
-    _pages_pool(p, pool, planes)
+    device = _here(page_table)
+    p.lengths, p.source = _per_slot(lengths, p.slots, "lengths", device), _per_slot(source, p.slots, "source", device)
+    p.lengths_out = p.lengths if lengths_out is None else _per_slot(lengths_out, p.slots, "lengths_out", device)
+    _pages_pool(p, pool, planes, device)
     workspace = _pages_workspace(p, workspace, page_count)
-    _here(pool, page_table, page_count, ref_count, lengths, source, table_out, count_out, refs_out, lengths_out, workspace, dev_status)
     _check("seq_tree_pages_fork", load().seq_tree_pages_fork(C.byref(p), _stream(stream)))
     _hold(workspace, stream)
 
@@ -755,10 +770,10 @@ def seq_tree_pages_compact(pool, page_table, page_count, ref_count, *, table_out
     """Moves the pages that are held to the front of the pool, contents, tables and reference counts; ``live`` int32 [1] receives how
     many they are.  In place, or (tables and counts) into table_out, refs_out."""
     p = _pages_params(page_table, page_count, ref_count, 1, table_out, None, refs_out, dev_status)
-    p.live = _dev(live, "live", torch.int32)
-    _pages_pool(p, pool, planes)
+    device = _here(page_table)
+    p.live = _ptr(live, "live", torch.int32, device)
+    _pages_pool(p, pool, planes, device)
     workspace = _pages_workspace(p, workspace, page_count)
-    _here(pool, page_table, page_count, ref_count, table_out, refs_out, live, workspace, dev_status)
     _check("seq_tree_pages_compact", load().seq_tree_pages_compact(C.byref(p), _stream(stream)))
     _hold(workspace, stream)
 
