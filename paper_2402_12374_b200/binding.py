@@ -579,7 +579,9 @@ class KV4AttentionCall:
     q [R, n, Hq, 128]; k_tree, v_tree [R, n, Hkv, 128] (the tree's own rows, 16-bit); pool uint8 [pages, Hkv, page_size *
     136]; page_table int32 [R, max_pages]; lengths int32 [R], negative for an idle slot.  mask_bits: int32 words [n, w] of
     ``seq_tree_mask_from_parents`` for all requests, or [R, n, w]; None: a chain.  max_len bounds the lengths (default: what
-    the page table reaches).  window > 0: only keys less than ``window`` positions back are seen, and the first ``sinks``."""
+    the page table reaches; it also chooses the kernel, so a bound far above the lengths costs time).  window > 0: only keys less
+    than ``window`` positions back are seen, and the first ``sinks``.  A call owns out and a workspace: runs of it, and graphs that
+    hold it, must not overlap."""
 
     def __init__(self, q, k_tree, v_tree, pool, page_table, lengths, *, mask_bits=None, max_len: int | None = None, window: int = 0,
                  sinks: int = 0, out=None, lse=None, softmax_scale: float = 0.0, workspace=None, dev_status=None):

@@ -23,7 +23,7 @@
 // What bounds it: instructions, 1650 a scheduler and key tile (600 to unpack K and V, 500 for the 128 x 128 scores, the rest
 // waits, hand-overs, the tree's tiles and the segments' ends), of which 0.61 are issued a cycle; and that they have to be in the
 // instruction caches: five warps of a scheduler run four different loops.  So loops are rolled and there is one copy of each: a
-// third of the code less gave 203 -> 188 us (768 nodes on 4096 tokens of 64/8 heads, 64 us at the tensor cores' rate; 175 now).
+// third of the code less gave 203 -> 188 us (768 nodes on 4096 tokens of 64/8 heads, 64 us at the tensor cores' rate; 172 now).
 // Without effect or slower, for that reason or another: three groups (182 us against 180), sixteen unpacking warps (185), 16 scores
 // at a time (186 against 181), the ancestor words fetched ahead (181 against 171), 16 rows of the tree in flight (70b 168 against
 // 171, 64 nodes of 32/32 heads 63 against 59), and two tiles of 128 rows that shared the unpacked keys.
