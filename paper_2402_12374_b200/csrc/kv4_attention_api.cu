@@ -7,12 +7,12 @@
 namespace seqtree {
 
 // The pieces of the units that are cut.  A CTA has some rows of one unit (16 of the tiles kernel's, whose pieces are [channel / 4][row], 8 of the
-// other's, [row][channel]), a thread eight channels of a row, or twice eight; four pieces are on their way at once.
+// other's, [row][channel]), a thread eight channels of a row, or twice eight; four pieces, (m, l) and rows, are on their way at once (32 requests 54 -> 52 us against (m, l) first).
 // The launch behind it is not let in early: its CTAs took the places that these leave first and were spread unevenly (32 requests of 8192
 // tokens, launch after launch: 54 us, 74 with it).
 template <bool kBf16, bool kTiles>
 __global__ void __launch_bounds__(128) kv4_merge_kernel(const Kv4Args a) {
-  constexpr int kRows = kTiles ? 16 : 8, kSets = kTiles ? 2 : 1;
+  constexpr int kRows = kTiles ? 16 : 8, kSets = kTiles ? 2 : 1, kFlight = 4;
   const int slices = a.row_tile / kRows, c = blockIdx.x / slices;
   const int x = threadIdx.x & 15, y = threadIdx.x >> 4;
   const int row = (blockIdx.x - c * slices) * kRows + (kTiles ? x : y), set = kTiles ? y : x;
@@ -23,30 +23,55 @@ __global__ void __launch_bounds__(128) kv4_merge_kernel(const Kv4Args a) {
   const int pieces = cut.z - c + 1;
   auto piece = [&](int p) -> int64_t { return (int64_t)(p == 0 ? cut.y : 2 * (c + p)) * a.row_tile; };
   float M = -INFINITY, sum = 0.f;
-#pragma unroll 4
-  for (int p = 0; p < pieces; ++p) M = fmaxf(M, a.ws_ml[piece(p) + row].x);
   float o[kSets][8];
 #pragma unroll
   for (int s = 0; s < kSets; ++s)
 #pragma unroll
     for (int e = 0; e < 8; ++e) o[s][e] = 0.f;
-#pragma unroll 4
-  for (int p = 0; p < pieces; ++p) {
-    const float2 ml = a.ws_ml[piece(p) + row];
-    const float4* from = reinterpret_cast<const float4*>(a.ws_o + piece(p) * kHeadDim);
-    const float f = ml.x == -INFINITY ? 0.f : ex2(ml.x - M);
-    sum = fmaf(ml.y, f, sum);
+  for (int p0 = 0; p0 < pieces; p0 += kFlight) {
+    float2 ml[kFlight];
+    float4 v[kFlight][kSets][2];
+#pragma unroll
+    for (int p = 0; p < kFlight; ++p) {
+      ml[p] = make_float2(-INFINITY, 0.f);
+#pragma unroll
+      for (int s = 0; s < kSets; ++s) v[p][s][0] = v[p][s][1] = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (p0 + p < pieces) {
+        ml[p] = a.ws_ml[piece(p0 + p) + row];
+        const float4* from = reinterpret_cast<const float4*>(a.ws_o + piece(p0 + p) * kHeadDim);
+#pragma unroll
+        for (int s = 0; s < kSets; ++s)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const int quad = 2 * (set + 8 * s) + e;
+            v[p][s][e] = from[kTiles ? quad * a.row_tile + row : row * (kHeadDim / 4) + quad];
+          }
+      }
+    }
+    float now = M;
+#pragma unroll
+    for (int p = 0; p < kFlight; ++p) now = fmaxf(now, ml[p].x);
+    const float old = M == -INFINITY ? 0.f : ex2(M - now);
+    M = now;
+    sum *= old;
 #pragma unroll
     for (int s = 0; s < kSets; ++s)
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const int quad = 2 * (set + 8 * s) + e;
-        const float4 v = from[kTiles ? quad * a.row_tile + row : row * (kHeadDim / 4) + quad];
-        o[s][4 * e] = fmaf(v.x, f, o[s][4 * e]);
-        o[s][4 * e + 1] = fmaf(v.y, f, o[s][4 * e + 1]);
-        o[s][4 * e + 2] = fmaf(v.z, f, o[s][4 * e + 2]);
-        o[s][4 * e + 3] = fmaf(v.w, f, o[s][4 * e + 3]);
-      }
+      for (int e = 0; e < 8; ++e) o[s][e] *= old;
+#pragma unroll
+    for (int p = 0; p < kFlight; ++p) {
+      const float f = ml[p].x == -INFINITY ? 0.f : ex2(ml[p].x - M);
+      sum = fmaf(ml[p].y, f, sum);
+#pragma unroll
+      for (int s = 0; s < kSets; ++s)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          o[s][4 * e] = fmaf(v[p][s][e].x, f, o[s][4 * e]);
+          o[s][4 * e + 1] = fmaf(v[p][s][e].y, f, o[s][4 * e + 1]);
+          o[s][4 * e + 2] = fmaf(v[p][s][e].z, f, o[s][4 * e + 2]);
+          o[s][4 * e + 3] = fmaf(v[p][s][e].w, f, o[s][4 * e + 3]);
+        }
+    }
   }
   const float inv = 1.f / sum;
   const int r = rg / a.Hkv, nd = rw / a.group, h = (rg - r * a.Hkv) * a.group + rw - nd * a.group;

@@ -15,9 +15,9 @@
 // Two ways to cut the work.  Few units: a cluster of CTAs each, which meet in shared memory, one launch without a workspace.  Many:
 // the ranges of kv4_attention.cuh, equal whatever the requests' lengths are.
 //
-// What bounds it: HBM while it streams (6.0 of 6.5 TB/s: 17.8 us for each 107 MB), and 17 us of a call with ranges that are the start (lengths, plan,
+// What bounds it: HBM while it streams (6.0 of 6.5 TB/s: 17.8 us for each 107 MB), and 15 us of a call with ranges that are the start (lengths, plan,
 // page numbers and the first codes are loads that wait for one another), the pieces and the kernel that adds them: 32 requests of 4096 to
-// 8192 tokens, 32/8 heads, in 54 us.  A single token on 500 of one request takes 5.9 us, a launch's latency and one meeting of a cluster.
+// 8192 tokens, 32/8 heads, in 52 us.  A single token on 500 of one request takes 5.9 us, a launch's latency and one meeting of a cluster.
 // Three stages of 32 keys a warp: more of them, or 64 keys, cost the registers or the shared memory of a third CTA on an SM (89 us then).
 #include "kv4_attention.cuh"
 #include "umma.cuh"
