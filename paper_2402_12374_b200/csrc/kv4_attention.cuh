@@ -185,8 +185,8 @@ __device__ __forceinline__ uint32_t kv4_window_word(const Kv4Args& a, int r, int
   return bits;
 }
 
-// CTAs of a unit's cluster in the kernel for few rows, 0: ranges
-int kv4_rows_cluster(const seq_tree_kv4_attention_params& p);
+// Whether the kernel for few rows takes it
+bool kv4_few_rows(const seq_tree_kv4_attention_params& p);
 size_t kv4_rows_workspace_bytes(const seq_tree_kv4_attention_params& p);
 int launch_kv4_rows(const seq_tree_kv4_attention_params& p, cudaStream_t stream);
 size_t kv4_tiles_workspace_bytes();

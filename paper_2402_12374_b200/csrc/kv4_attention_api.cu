@@ -132,14 +132,6 @@ Kv4Args kv4_args(const seq_tree_kv4_attention_params& p, int row_tile, int step,
   return a;
 }
 
-// The kernel in registers takes 16 query rows of a kv head at a time, the tensor-core one 128 and some 20 us for its start and its last
-// pieces.  So few rows are the former's, and whatever its clusters cut to a few dozen steps (bf16, 64/8 heads, 6 nodes on 4096 tokens:
-// 14 us against 28; 64 nodes of 32/32 heads on 1024: 17 against 24).  With ranges it is ahead to two tiles of rows (32 rows of 32 heads, four
-// requests of 2048: 32 us against 38; 48 rows: 65 against 39).
-static bool few_rows(const seq_tree_kv4_attention_params& p) {
-  return p.n_tree * (p.num_q_heads / p.num_kv_heads) <= 32 || kv4_rows_cluster(p) != 0;
-}
-
 static int check_kv4_attention(const seq_tree_kv4_attention_params* p) {
   if (p == nullptr || p->q == nullptr || p->k_tree == nullptr || p->v_tree == nullptr || p->pages == nullptr || p->page_table == nullptr ||
       p->lengths == nullptr || p->out == nullptr)
@@ -169,7 +161,7 @@ using namespace seqtree;
 
 extern "C" size_t seq_tree_kv4_attention_workspace_bytes(const seq_tree_kv4_attention_params* p) {
   if (p == nullptr || p->num_kv_heads < 1 || p->num_q_heads < 1 || p->n_tree < 1) return 0;
-  return few_rows(*p) ? kv4_rows_workspace_bytes(*p) : kv4_tiles_workspace_bytes();
+  return kv4_few_rows(*p) ? kv4_rows_workspace_bytes(*p) : kv4_tiles_workspace_bytes();
 }
 
 extern "C" int seq_tree_kv4_attention(const seq_tree_kv4_attention_params* p, void* stream) {
@@ -178,5 +170,5 @@ extern "C" int seq_tree_kv4_attention(const seq_tree_kv4_attention_params* p, vo
   const size_t need = seq_tree_kv4_attention_workspace_bytes(p);
   if (need > 0 && (p->workspace == nullptr || p->workspace_bytes < need)) return SEQ_ERR_WORKSPACE;
   if (need > 0 && reinterpret_cast<uintptr_t>(p->workspace) % 256 != 0) return SEQ_ERR_INVALID_ARG;
-  return few_rows(*p) ? launch_kv4_rows(*p, static_cast<cudaStream_t>(stream)) : launch_kv4_tiles(*p, static_cast<cudaStream_t>(stream));
+  return kv4_few_rows(*p) ? launch_kv4_rows(*p, static_cast<cudaStream_t>(stream)) : launch_kv4_tiles(*p, static_cast<cudaStream_t>(stream));
 }

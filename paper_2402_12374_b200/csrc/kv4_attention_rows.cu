@@ -716,7 +716,7 @@ static int rows_steps(const seq_tree_kv4_attention_params& p) {
   return (L + 31) / 32 + (p.n_tree + kTreeStep - 1) / kTreeStep;
 }
 // CTAs of a unit's cluster, 0 for ranges.
-int kv4_rows_cluster(const seq_tree_kv4_attention_params& p) {
+static int rows_cluster(const seq_tree_kv4_attention_params& p) {
   const int64_t units = rows_units(p);
   const int steps = rows_steps(p);
   int c = 1;
@@ -726,8 +726,21 @@ int kv4_rows_cluster(const seq_tree_kv4_attention_params& p) {
   return c;
 }
 
+// This kernel takes 16 query rows of a kv head at a time, the one of tiles 128 and 15 us for its start and its last pieces.  So up to 16 rows are
+// this one's.  More: where clusters cut a unit to few steps a warp (64/8 heads, 12 nodes on 4096 tokens, 8 steps: 19 us against 19; on 8192, 16 steps: 29
+// against 22; 64 nodes of 32/32 heads on 1024: 17 against 19, on 4096 32 against 26), but for two tiles of rows always (16 steps: 18 to 31 us
+// against 21 to 34); with ranges two tiles up to 20 steps a warp, or any number for half-precision rows, whose tiles take longer (32 nodes of
+// 32/32 heads, 4 requests of 2048: 32 us against 36; 16 requests: 131 against 98, half precision 122 against 112; 24 nodes, 16 of 4096: 167
+// against 147, half precision 161 against 177).
+bool kv4_few_rows(const seq_tree_kv4_attention_params& p) {
+  const int rows = p.n_tree * (p.num_q_heads / p.num_kv_heads), c = rows_cluster(p);
+  if (rows <= 16) return true;
+  if (c != 0) return rows <= 32 || rows_steps(p) <= 9 * c * kRowsWarps;
+  return rows <= 32 && (p.dtype == SEQ_F16 || rows_units(p) * rows_steps(p) <= (int64_t)20 * kRowsWarps * rows_ctas(rows_nt(p)));
+}
+
 size_t kv4_rows_workspace_bytes(const seq_tree_kv4_attention_params& p) {
-  if (kv4_rows_cluster(p) != 0) return 0;
+  if (rows_cluster(p) != 0) return 0;
   const int nt = rows_nt(p);
   return kv4_ranges_bytes(rows_ctas(nt), 8 * nt);
 }
@@ -736,7 +749,7 @@ int launch_kv4_rows(const seq_tree_kv4_attention_params& p, cudaStream_t stream)
   const int nt = rows_nt(p);
   Kv4Args a = kv4_args(p, 8 * nt, kTreeStep, 0, 0);
   a.min_steps = kRowsWarps;
-  a.cluster = kv4_rows_cluster(p);
+  a.cluster = rows_cluster(p);
   const bool bf16 = p.dtype == SEQ_BF16;
   cudaLaunchConfig_t cfg = {};
   cfg.blockDim = dim3(32 * kRowsWarps);
