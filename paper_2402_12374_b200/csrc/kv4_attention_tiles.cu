@@ -479,6 +479,13 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
           uint4 x[8];
 #pragma unroll
           for (int p = 0; p < 8; ++p) x[p] = valid ? src[p * kGroups] : make_uint4(0u, 0u, 0u, 0u);
+          // The scores of the segment before are complete: its q is read, and, as they took all warps' q, every row is through with what
+          // the groups exchanged for it (behind the CTA's first segment no barrier says so, and a group without a tile in it would be ahead).
+          if (have && cur.sg.steps > 0) {
+            const int x = step - 1, u = x / kSBufs;
+            ok = kv4_wait(sm, &sm->s_full[x - u * kSBufs], u & 1, a.status);
+            __syncwarp();
+          }
           float f = 1.f;
           if (kBf16) {
             uint32_t top = 0;
@@ -507,11 +514,6 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
             sm->q_sum[grp][row] = sum;
             rows_sync();
             next.q_sum = sm->q_sum[0][row] + sm->q_sum[1][row];
-          }
-          if (have && cur.sg.steps > 0) {  // the scores of the segment before are complete
-            const int x = step - 1, u = x / kSBufs;
-            ok = kv4_wait(sm, &sm->s_full[x - u * kSBufs], u & 1, a.status);
-            __syncwarp();
           }
           const uint32_t line = smem_u32(sm->q) + row * 128;
 #pragma unroll
