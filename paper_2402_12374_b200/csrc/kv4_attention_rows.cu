@@ -572,11 +572,16 @@ __global__ void __launch_bounds__(32 * kRowsWarps, NT == 1 ? 3 : 2) kv4_rows_ker
             for (int i = 0; i < 16; ++i) v[z][i] &= keep;
           }
         }
+        // A key that is not finite in half precision has no finite score (q is finite, or its row NaN anyway), and could have that of a hidden
+        // one, -inf: rows that see it become NaN.
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (!((seen[nt][e & 1] >> (16 * gr + g8 + 8 * (e >> 1))) & 1u)) s[0][nt][e] = -INFINITY;
+          for (int e = 0; e < 4; ++e) {
+            const bool hidden = !((seen[nt][e & 1] >> (16 * gr + g8 + 8 * (e >> 1))) & 1u), finite = fabsf(s[0][nt][e]) < INFINITY;
+            if (!hidden && !finite) st.l[nt][e & 1] = NAN;
+            if (hidden || !finite) s[0][nt][e] = -INFINITY;
+          }
         follow<1, NT>(s, y, st.e, st);
         uint32_t pf[NT][2];
 #pragma unroll

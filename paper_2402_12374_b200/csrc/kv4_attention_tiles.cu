@@ -64,7 +64,7 @@ struct TilesSmem {
   float ref[kTileM];             // the rows' reference maximum, handed on in the keys' order
   float sum[kGroups][kTileM];
   uint32_t top[kGroups][kTileM]; // q's largest magnitudes
-  uint32_t bad[4][kTreeTiles][4];  // [segment mod 4]: tree rows whose V is not finite in half precision
+  uint32_t bad[2][4][kTreeTiles][4];  // [K, V][segment mod 4]: tree rows that are not finite in half precision
   uint32_t tmem_base;
   volatile int abort_flag;
   Kv4Plan plan;
@@ -408,24 +408,23 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
               }
               big = __vmaxu2(__vmaxu2(big, in[p].x & 0x7c007c00u), __vmaxu2(in[p].y & 0x7c007c00u, __vmaxu2(in[p].z & 0x7c007c00u, in[p].w & 0x7c007c00u)));
             }
+            // a row that is not finite counts as zeros, so that it stays out of the rows that do not see it; those that do become
+            // NaN when they are written.  (A key's infinity could make its score -inf, which is what a hidden key has.)
             uint32_t keep = 0xffffffffu;
-            if (which == 1) {
-              // a row of V that is not finite counts as zeros, so that it stays out of the rows that do not see it; those
-              // that do become NaN when they are written
-              const uint32_t b4 = __ballot_sync(0xffffffffu, (big & 0xffffu) == 0x7c00u || (big >> 16) == 0x7c00u);
-              if ((b4 >> (lane & 28)) & 15u) keep = 0u;
-              if (b4 != 0)
+            const uint32_t b4 = __ballot_sync(0xffffffffu, (big & 0xffffu) == 0x7c00u || (big >> 16) == 0x7c00u);
+            if ((b4 >> (lane & 28)) & 15u) keep = 0u;
+            if (b4 != 0)
 #pragma unroll 1
-                for (int z = 0; z < 8; ++z) bad |= (b4 >> (4 * z)) & 15u ? 1u << (8 * y + z) : 0u;
-            }
+              for (int z = 0; z < 8; ++z) bad |= (b4 >> (4 * z)) & 15u ? 1u << (8 * y + z) : 0u;
             const uint32_t line = tile + (w4 * 32 + 8 * y) * 128;
 #pragma unroll
             for (int p = 0; p < 4; ++p)
               sts128(line + place[p], __byte_perm(in[p].x, in[p].z, 0x5410) & keep, __byte_perm(in[p].x, in[p].z, 0x7632) & keep,
                      __byte_perm(in[p].y, in[p].w, 0x5410) & keep, __byte_perm(in[p].y, in[p].w, 0x7632) & keep);
           }
-          // (four segments' words: this warp is two tiles ahead of the rows that look at them, at most)
-          if (which == 1 && lane == 0) sm->bad[seg & 3][key0 / kTilesStep][w4] = bad;
+          // Four segments' words: the rows look at a segment's when it is through.  The warps of V are two tiles ahead of that at most;
+          // those of K two ahead of the scores, which do not go beyond the segment whose q the rows have brought: the next one.
+          if (lane == 0) sm->bad[which][seg & 3][key0 / kTilesStep][w4] = bad;
         }
         if (!ok) break;
         if (kExact && which == 0) {
@@ -557,7 +556,7 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
           const int tt = sg.t0 + i - sg.u.prefix.steps;
 #pragma unroll 1
           for (int w = 0; w < 4; ++w) {
-            const uint32_t bad = sm->bad[(seg - 1) & 3][tt][w];
+            const uint32_t bad = sm->bad[0][(seg - 1) & 3][tt][w] | sm->bad[1][(seg - 1) & 3][tt][w];
             if (bad != 0) poison |= bad & kv4_window_word(a, r, L, depth, 4 * tt + w, kv4_mask_word(a, mask_row, node, 4 * tt + w));
           }
         }

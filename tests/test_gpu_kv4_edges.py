@@ -3,6 +3,8 @@ import numpy as np
 import pytest
 import torch
 
+from tests import kv4_util as U
+from tests import test_gpu_kv4_attention as T
 from tests.test_gpu_kv4_attention import Case
 
 pytestmark = pytest.mark.gpu
@@ -24,3 +26,37 @@ def test_ranges_that_open_with_the_last_step_of_a_unit(R, seed, dt):
     out, lse = out.clone(), call.lse.clone()
     for _ in range(20):
         assert torch.equal(call.run(), out) and torch.equal(call.lse, lse)
+
+
+@pytest.fixture(params=["tight", "roomy"])
+def room(request, monkeypatch):
+    """With room for 40000 tokens no cluster takes the few rows, nor small trees."""
+    monkeypatch.setattr(T, "ROOM", 40000 if request.param == "roomy" else 0)
+
+
+@pytest.mark.parametrize("which", ["k", "v"])
+@pytest.mark.parametrize("sign", [1.0, -1.0, 0.0])
+@pytest.mark.parametrize("n,Hq,dt", [(6, 2, torch.float16), (6, 2, torch.bfloat16), (14, 1, torch.bfloat16), (40, 4, torch.float16), (40, 4, torch.bfloat16),
+                                     (150, 2, torch.float16), (150, 2, torch.bfloat16)])
+def test_a_row_of_the_tree_beyond_half_precision(n, Hq, dt, sign, which, room):
+    """Keys alone and values alone: whoever sees such a row becomes NaN, whatever the sign of the score it would have; nobody else changes."""
+    c = Case([45], n, Hq, 1, 16, dt, seed=8)
+    star = np.eye(n, dtype=bool)
+    star[:, 0] = True
+    star[n - 1, 1] = True  # (a node that sees a bad row of another one)
+    c.seen, c.mask = [star], torch.from_numpy(U.mask_words(star)).cuda()
+    c.q[..., 5] = sign
+    clean = c.call().run().clone()
+    assert torch.isfinite(clean).all()
+    rows = c.kt if which == "k" else c.vt
+    bad = {1: 1e5, 2: float("nan"), 3: float("inf"), n - 2: -float("inf")}  # (1e5: an infinity in half precision)
+    for j, x in bad.items():
+        rows[0, j, 0, 5] = x
+    call = c.call()
+    out = call.run()
+    assert int(c.status) == 0
+    for i in range(n):
+        if i in bad or i == n - 1:
+            assert torch.isnan(out[0, i]).all() and torch.isnan(call.lse[0, :, i]).all(), i
+        else:
+            assert torch.equal(out[0, i], clean[0, i]) and torch.isfinite(call.lse[0, :, i]).all(), i
