@@ -639,17 +639,20 @@ class KV4AttentionCall:
         self._ref, self._fn = C.byref(p), load().seq_tree_kv4_attention
         self._keep = (q, k_tree, v_tree, pool, page_table, lengths, mask_bits, out, lse, workspace, dev_status)
         self._device = _here(*self._keep)
+        self._streams = {_raw_stream(self._device)}  # that out and the workspace are held for
 
     def run(self, stream=None):
         device = _raw_device()
         if device != self._device:
             raise ValueError(f"the call's tensors live on cuda:{self._device}, the current device is cuda:{device}")
-        rc = self._fn(self._ref, _raw_stream(device) if stream is None else _stream(stream))
+        handle = _raw_stream(device) if stream is None else _stream(stream)
+        if handle not in self._streams:  # (the current stream, too, can be another one than the call was made on)
+            for t in self._own:
+                _hold(t, handle)
+            self._streams.add(handle)
+        rc = self._fn(self._ref, handle)
         if rc:
             _check("seq_tree_kv4_attention", rc)
-        if stream is not None:
-            for t in self._own:
-                _hold(t, stream)
         return self.out
 
 

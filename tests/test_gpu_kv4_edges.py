@@ -60,3 +60,26 @@ def test_a_row_of_the_tree_beyond_half_precision(n, Hq, dt, sign, which, room):
             assert torch.isnan(out[0, i]).all() and torch.isnan(call.lse[0, :, i]).all(), i
         else:
             assert torch.equal(out[0, i], clean[0, i]) and torch.isfinite(call.lse[0, :, i]).all(), i
+
+
+@pytest.mark.parametrize("given", [True, False])
+@pytest.mark.parametrize("n,times", [(1, 30), (1, 110), (20, 30)])  # clusters (no workspace), ranges, tiles
+def test_memory_of_a_call_on_another_current_stream_is_not_handed_out(n, times, given):
+    """What a call owns outlives the call object until the stream of its runs is through, however that stream was chosen."""
+    c = Case([300, 20, 411] * times, n, 8, 2, 16, torch.float16, seed=3)
+    want = c.call().run().clone()
+    call = c.call()
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    need, held = call.workspace_bytes_needed, {t.data_ptr() for t in (call.out, call.workspace) if t is not None}
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(50_000_000)
+        out = call.run() if not given else None
+    if given:
+        out = call.run(stream=side.cuda_stream)
+    del call
+    others = [torch.empty(max(need, 1), dtype=torch.uint8, device="cuda") for _ in range(4)]
+    others += [torch.empty_like(out) for _ in range(4)]
+    assert (need > 0) == (len(held) == 2) and not held & {t.data_ptr() for t in others}
+    side.synchronize()
+    assert torch.equal(out, want)
