@@ -209,10 +209,14 @@ def _here(*tensors) -> int:
     return device
 
 
+def _stream_object(stream, device):
+    return stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(_stream(stream), device=device)
+
+
 def _hold(tensor, stream) -> None:
     """A tensor of the binding's own that a call on ``stream`` uses: its memory is not given to another stream before that."""
     if stream is not None:
-        tensor.record_stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(_stream(stream), device=tensor.device))
+        tensor.record_stream(_stream_object(stream, tensor.device))
 
 
 def _check(fn: str, code: int) -> None:
@@ -581,7 +585,8 @@ class KV4AttentionCall:
     ``seq_tree_mask_from_parents`` for all requests, or [R, n, w]; None: a chain.  max_len bounds the lengths (default: what
     the page table reaches; it also chooses the kernel, so a bound far above the lengths costs time).  window > 0: only keys less
     than ``window`` positions back are seen, and the first ``sinks``.  A call owns out and a workspace: runs of it, and graphs that
-    hold it, must not overlap."""
+    hold it, must not overlap, and it is kept as long as such a graph is.  Its runs may be on any stream; the first one on another than it was
+    made on waits for what was on that one when the call was made."""
 
     def __init__(self, q, k_tree, v_tree, pool, page_table, lengths, *, mask_bits=None, max_len: int | None = None, window: int = 0,
                  sinks: int = 0, out=None, lse=None, softmax_scale: float = 0.0, workspace=None, dev_status=None):
@@ -640,6 +645,11 @@ class KV4AttentionCall:
         self._keep = (q, k_tree, v_tree, pool, page_table, lengths, mask_bits, out, lse, workspace, dev_status)
         self._device = _here(*self._keep)
         self._streams = {_raw_stream(self._device)}  # that out and the workspace are held for
+        # That memory may have been another tensor's, with work on this stream that still uses it: other streams wait for it.
+        self._made = None
+        if self._own and not torch.cuda.is_current_stream_capturing():
+            self._made = torch.cuda.Event()
+            self._made.record()
 
     def run(self, stream=None):
         device = _raw_device()
@@ -647,18 +657,31 @@ class KV4AttentionCall:
             raise ValueError(f"the call's tensors live on cuda:{self._device}, the current device is cuda:{device}")
         handle = _raw_stream(device) if stream is None else _stream(stream)
         if handle not in self._streams:  # (the current stream, too, can be another one than the call was made on)
-            for t in self._own:
-                _hold(t, handle)
-            self._streams.add(handle)
+            self._first_run_on(handle)
         rc = self._fn(self._ref, handle)
         if rc:
             _check("seq_tree_kv4_attention", rc)
         return self.out
 
+    def _first_run_on(self, handle: int) -> None:
+        stream = _stream_object(handle, self.out.device)
+        for t in self._own:
+            t.record_stream(stream)
+        with torch.cuda.stream(stream):
+            if torch.cuda.is_current_stream_capturing():
+                return  # (a capture takes no event from outside; torch.cuda.graph waits for the device before it begins one)
+        if self._made is not None:
+            stream.wait_event(self._made)
+        self._streams.add(handle)
+
 
 def seq_tree_kv4_attention(q, k_tree, v_tree, pool, page_table, lengths, **kw):
-    """Attention of tree tokens over prefixes in 4-bit pages (see ``KV4AttentionCall``); returns out [R, n, Hq, 128]."""
+    """Attention of tree tokens over prefixes in 4-bit pages (see ``KV4AttentionCall``); returns out [R, n, Hq, 128].  On a ``stream``
+    other than the current one, and without ``out``, it waits for what is on the current one: out's memory comes from there."""
     stream = kw.pop("stream", None)
+    if stream is not None and kw.get("out") is not None:  # the workspace is that stream's
+        with torch.cuda.stream(_stream_object(stream, q.device)):
+            return KV4AttentionCall(q, k_tree, v_tree, pool, page_table, lengths, **kw).run()
     return KV4AttentionCall(q, k_tree, v_tree, pool, page_table, lengths, **kw).run(stream)
 
 

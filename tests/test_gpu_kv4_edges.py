@@ -3,6 +3,7 @@ import numpy as np
 import pytest
 import torch
 
+from paper_2402_12374_b200 import binding as B
 from tests import kv4_util as U
 from tests import test_gpu_kv4_attention as T
 from tests.test_gpu_kv4_attention import Case
@@ -82,4 +83,44 @@ def test_memory_of_a_call_on_another_current_stream_is_not_handed_out(n, times, 
     others += [torch.empty_like(out) for _ in range(4)]
     assert (need > 0) == (len(held) == 2) and not held & {t.data_ptr() for t in others}
     side.synchronize()
+    assert torch.equal(out, want)
+
+
+@pytest.mark.parametrize("how", ["current", "given", "function", "out given"])
+@pytest.mark.parametrize("n,times", [(1, 110), (20, 30)])
+def test_memory_that_a_call_takes_over_is_not_used_before_its_last_user_is_through(n, times, how):
+    """out (and the workspace) lie where another tensor was that the stream of the call's making still writes to; the run is elsewhere."""
+    c = Case([300, 20, 411] * times, n, 8, 2, 16, torch.float16, seed=3)
+    call = c.call()
+    want, need = call.run().clone(), call.workspace_bytes_needed
+    del call
+    q, kt, vt, pool, table = c.q.cuda(), c.kt.cuda(), c.vt.cuda(), c.pool_dev[:, 0], torch.from_numpy(c.table).cuda()
+    lengths = torch.tensor(c.lengths, dtype=torch.int32, device="cuda")
+    mine = torch.full_like(q, 5.0) if how == "out given" else None
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()
+    before = [torch.empty_like(q), torch.empty(need, dtype=torch.uint8, device="cuda")]
+    places = {t.data_ptr() for t in before}
+    torch.cuda._sleep(50_000_000)
+    for t in before:
+        t.fill_(77)
+    through = torch.cuda.Event()
+    through.record()
+    del t, before
+    kw = dict(mask_bits=c.mask)
+    if how in ("current", "given"):
+        call = B.KV4AttentionCall(q, kt, vt, pool, table, lengths, **kw)
+        assert {call.out.data_ptr(), call.workspace.data_ptr()} & places
+        if how == "current":
+            with torch.cuda.stream(side):
+                out = call.run()
+        else:
+            out = call.run(stream=side)
+    else:
+        out = B.seq_tree_kv4_attention(q, kt, vt, pool, table, lengths, out=mine, stream=side, **kw)
+        assert mine is not None or out.data_ptr() in places
+    side.synchronize()
+    assert how != "out given" or not through.query()  # nothing of the call's is that stream's: it did not wait
+    torch.cuda.synchronize()
     assert torch.equal(out, want)
