@@ -743,9 +743,14 @@ def _pages_params(page_table, page_count, ref_count, page_size, table_out, count
                        None, 0, _ptr(dev_status, "dev_status", torch.int32, device))
 
 
-def _pages_workspace(p, workspace, like):
+def _pages_workspace(p, workspace, like, stream):
     if workspace is None:
-        workspace = like.new_empty(load().seq_tree_pages_workspace_bytes(C.byref(p)) // 4)
+        words = load().seq_tree_pages_workspace_bytes(C.byref(p)) // 4
+        if stream is None:
+            workspace = like.new_empty(words)
+        else:  # memory of the stream that uses it: another one's may still have work on it
+            with torch.cuda.stream(_stream_object(stream, like.device)):
+                workspace = like.new_empty(words)
     p.workspace, p.workspace_bytes = _ptr(workspace, "workspace", workspace.dtype, like.get_device()), workspace.numel() * workspace.element_size()
     return workspace  # (until the call is enqueued)
 
@@ -774,7 +779,7 @@ def seq_tree_pages_resize(page_table, page_count, ref_count, tokens, page_size: 
     p = _pages_params(page_table, page_count, ref_count, page_size, table_out, count_out, refs_out, dev_status)
     _here(page_table)
     p.tokens = _per_slot(tokens, p.slots, "tokens", page_table.get_device())
-    workspace = _pages_workspace(p, workspace, page_count)
+    workspace = _pages_workspace(p, workspace, page_count, stream)
     _check("seq_tree_pages_resize", load().seq_tree_pages_resize(C.byref(p), _stream(stream)))
     _hold(workspace, stream)
 
@@ -788,7 +793,7 @@ def seq_tree_pages_fork(pool, page_table, page_count, ref_count, lengths, source
     p.lengths, p.source = _per_slot(lengths, p.slots, "lengths", device), _per_slot(source, p.slots, "source", device)
     p.lengths_out = p.lengths if lengths_out is None else _per_slot(lengths_out, p.slots, "lengths_out", device)
     _pages_pool(p, pool, planes, device)
-    workspace = _pages_workspace(p, workspace, page_count)
+    workspace = _pages_workspace(p, workspace, page_count, stream)
     _check("seq_tree_pages_fork", load().seq_tree_pages_fork(C.byref(p), _stream(stream)))
     _hold(workspace, stream)
 
@@ -801,7 +806,7 @@ def seq_tree_pages_compact(pool, page_table, page_count, ref_count, *, table_out
     device = _here(page_table)
     p.live = _ptr(live, "live", torch.int32, device)
     _pages_pool(p, pool, planes, device)
-    workspace = _pages_workspace(p, workspace, page_count)
+    workspace = _pages_workspace(p, workspace, page_count, stream)
     _check("seq_tree_pages_compact", load().seq_tree_pages_compact(C.byref(p), _stream(stream)))
     _hold(workspace, stream)
 

@@ -265,3 +265,37 @@ def test_a_serving_loop_in_one_graph():
         assert lengths.tolist() == [len(x[0]) for x in rows]
     held = table[table >= 0]
     assert torch.equal(torch.bincount(held.long(), minlength=pages).int(), refs)
+
+
+@pytest.mark.parametrize("handle", [False, True])
+def test_a_workspace_on_another_stream_is_that_streams_own(handle):
+    """The current stream still writes to memory of the workspace's size that it has given back: a call on another stream does not get it."""
+    table, count, refs, lengths, rng = state(33, 40, 30000, 16, 3)
+    tokens = rng.integers(-1, 40 * 16 + 1, 33).astype(np.int32)
+    source = np.where(count == 0, int(np.argmax(lengths)), -1).astype(np.int32)
+    pool = rng.integers(0, 256, (30000, 16), dtype=np.uint8)
+    want_resize, want_fork, want_compact = (U.resize(table, count, refs, tokens, 16), U.fork(pool, table, count, refs, lengths, source, 16),
+                                            U.compact(pool, table, count, refs))
+    side = torch.cuda.Stream()
+    on = side.cuda_stream if handle else side
+    for call in ("resize", "fork", "compact"):
+        p, t, c, f, n, tok, src = dev(pool, table, count, refs, lengths, tokens, source)
+        torch.cuda.synchronize()
+        torch.cuda.empty_cache()
+        before = torch.empty(1 + 3 * 30000, dtype=torch.int32, device="cuda")
+        torch.cuda._sleep(20_000_000)
+        before.fill_(7)
+        through = torch.cuda.Event()
+        through.record()
+        del before
+        if call == "resize":
+            B.seq_tree_pages_resize(t, c, f, tok, 16, stream=on)
+        elif call == "fork":
+            B.seq_tree_pages_fork(p, t, c, f, n, src, 16, stream=on)
+        else:
+            B.seq_tree_pages_compact(p, t, c, f, stream=on)
+        side.synchronize()
+        assert not through.query()  # (it did not wait for the current stream either)
+        torch.cuda.synchronize()
+        want = {"resize": (t, want_resize[0], f, want_resize[2]), "fork": (t, want_fork[1], f, want_fork[3]), "compact": (t, want_compact[1], f, want_compact[2])}[call]
+        assert np.array_equal(want[0].cpu().numpy(), want[1]) and np.array_equal(want[2].cpu().numpy(), want[3])
