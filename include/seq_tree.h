@@ -592,10 +592,12 @@ int seq_tree_kv4_read(const seq_tree_kv4_append_params* p, void* stream);
  *                layer: a plane each)
  *   workspace    seq_tree_pages_workspace_bytes(p) bytes, 16-byte aligned, device; contents undefined; two calls that can run
  *                at the same time need one each.
- * Table entries outside [0, num_pages) that a call meets raise SEQ_DEV_BAD_PAGE and count as no page (compact leaves -1); a
- * page_count outside [0, max_pages] raises SEQ_DEV_BAD_SLOT and the slot is left alone; a ref_count below what is
- * given up, or negative, raises SEQ_DEV_BAD_SLOT and counts as 0.  Returns SEQ_OK, SEQ_ERR_INVALID_ARG, SEQ_ERR_WORKSPACE or
- * SEQ_ERR_CUDA.
+ * Table entries outside [0, num_pages) that a call meets raise SEQ_DEV_BAD_PAGE and count as no page (fork and compact leave -1; a fork
+ * whose open page is none gets a page of its own with nothing copied); a page_count outside [0, max_pages] raises
+ * SEQ_DEV_BAD_SLOT and the slot is left alone: its count and all of its row are the same afterwards, also where they are written to other
+ * arrays; a ref_count below what is given up, or negative, raises SEQ_DEV_BAD_SLOT and counts as 0; a page that a fork's source holds
+ * and that counts as free raises SEQ_DEV_BAD_SLOT, as a call may hand it out: shared, it is counted from 0, open, it is not copied.
+ * Returns SEQ_OK, SEQ_ERR_INVALID_ARG, SEQ_ERR_WORKSPACE or SEQ_ERR_CUDA.
  */
 #define SEQ_MAX_SLOTS 2048
 typedef struct {

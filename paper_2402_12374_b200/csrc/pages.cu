@@ -121,15 +121,18 @@ __device__ __forceinline__ Share share_of(int num_pages, uint32_t rank) {
   return {(int)min(lo, (int64_t)num_pages), (int)min(lo + per, (int64_t)num_pages)};
 }
 
+// Entries of slot r's row that are its own; all of them where its count cannot be: such a row stays as it is.
+__device__ __forceinline__ int held_of(const PagesArgs& a, int r, bool tell) {
+  const int have = a.count[r];
+  if (have >= 0 && have <= a.max_pages) return have;
+  if (tell) dev_flag(a.status, SEQ_DEV_BAD_SLOT);
+  return a.max_pages;
+}
+
 // How slot r is resized: pages before and after
 __device__ __forceinline__ bool wanted_of(const PagesArgs& a, int r, int& have, int& want, bool tell) {
-  have = a.count[r];
-  want = have;
-  if (have < 0 || have > a.max_pages) {
-    if (tell) dev_flag(a.status, SEQ_DEV_BAD_SLOT);
-    have = want = min(max(have, 0), a.max_pages);
-    return false;
-  }
+  have = want = held_of(a, r, tell);
+  if (have != a.count[r]) return false;
   const int t = a.tokens[r];
   if (t < 0) return false;
   const int w = ceil_pages(t, a.page_size);
@@ -166,7 +169,7 @@ __device__ void copy_rows(const PagesArgs& a) {
       wanted_of(a, r, have, want, false);
     } else {
       if (fork_source(a, r, false) >= 0) continue;
-      have = want = min(max(a.count[r], 0), a.max_pages);
+      have = want = held_of(a, r, false);
     }
     const int keep = min(have, want), end = max(have, want);
     const int32_t* from = a.table + r * a.table_stride;
@@ -363,15 +366,15 @@ __global__ void __launch_bounds__(kPlanThreads, 1) pages_resize_kernel(const Pag
   // the slots' counts, and what is not there for those that do not grow
   for (int r = rank * kPlanThreads + threadIdx.x; r < a.slots; r += ctas * kPlanThreads) {
     int have, want;
-    const bool sound = wanted_of(a, r, have, want, false);
+    wanted_of(a, r, have, want, false);
     const bool grows = want > have;
     const bool fits = !grows || sm->before[r + 1] <= free_pages;
     if (!fits) {
       dev_flag(a.status, SEQ_DEV_NO_PAGES);
       for (int i = have; i < want; ++i) a.table_out[r * a.table_out_stride + i] = -1;
     }
-    const int c = fits ? want : have;
-    if (a.count_out != a.count || (sound && c != have)) a.count_out[r] = c;
+    const int was = a.count[r], c = have != was ? was : fits ? want : have;
+    if (a.count_out != a.count || c != was) a.count_out[r] = c;
   }
 }
 
@@ -393,6 +396,7 @@ __global__ void __launch_bounds__(kPlanThreads, 1) pages_fork_kernel(const Pages
   for (int j = 0; j < kSlotsPerThread; ++j) {
     need[j] = 0;
     if (first + j < a.slots) {
+      held_of(a, first + j, rank == 0);
       const int s = fork_source(a, first + j, rank == 0);
       const int n = s >= 0 ? a.lengths[s] : 0;
       sm->source[first + j] = s;  // (kept: in place, counts and lengths change below)
@@ -413,24 +417,51 @@ __global__ void __launch_bounds__(kPlanThreads, 1) pages_fork_kernel(const Pages
   const int needed = sm->before[a.slots];
   int32_t* from = a.ws + 1;
   int32_t* to = from + a.slots;
+  const uint32_t ctas = cluster_size();
   int free_pages = 0;
+  // The open pages that are copied: asked for here, looked at below
+  int open[kSlotsPerThread];
+#pragma unroll
+  for (int j = 0; j < kSlotsPerThread; ++j) {
+    const int k = (j * ctas + rank) * kPlanThreads + threadIdx.x;
+    open[j] = -1;
+    if (k < needed) {
+      const int r = slot_of(sm, a.slots, k);
+      open[j] = a.table[sm->source[r] * a.table_stride + sm->length[r] / a.page_size];
+    }
+  }
   const auto give = [&](int k, int page) {
     const int r = slot_of(sm, a.slots, k);
-    const int s = sm->source[r], full = sm->length[r] / a.page_size;
-    const int old = a.table[s * a.table_stride + full];
-    const bool good = old >= 0 && old < a.num_pages;
-    if (!good) dev_flag(a.status, SEQ_DEV_BAD_PAGE);
-    from[k] = good ? old : page;
     to[k] = page;
-    a.table_out[r * a.table_out_stride + full] = page;
+    a.table_out[r * a.table_out_stride + sm->length[r] / a.page_size] = page;
   };
-  number_pages(sm, rank, share, a.refs_out, needed, [](int, int v) { return v <= 0; }, give, free_pages);
+  const auto is_free = [&](int page, int v) -> bool {
+    if (v < 0) {
+      dev_flag(a.status, SEQ_DEV_BAD_SLOT);
+      a.refs_out[page] = 0;
+    }
+    return v <= 0;
+  };
+  number_pages(sm, rank, share, a.refs_out, needed, is_free, give, free_pages);
   const int given = min(needed, free_pages);
   if (rank == 0 && threadIdx.x == 0) a.ws[0] = given;
+#pragma unroll
+  for (int j = 0; j < kSlotsPerThread; ++j) {
+    const int k = (j * ctas + rank) * kPlanThreads + threadIdx.x;
+    if (k >= given) continue;
+    int page = open[j];
+    if (page < 0 || page >= a.num_pages) {
+      dev_flag(a.status, SEQ_DEV_BAD_PAGE);
+      page = -1;
+    } else if (__ldcg(a.refs_out + page) <= 0) {  // held, but counted as free: it may be written in this call
+      dev_flag(a.status, SEQ_DEV_BAD_SLOT);
+      page = -1;
+    }
+    from[k] = page;  // (-1: nothing is copied)
+  }
   cluster_sync();  // every free page is numbered: from here on counts change
-  const uint32_t ctas = cluster_size();
-  for (int k = rank * kPlanThreads + threadIdx.x; k < given; k += ctas * kPlanThreads) a.refs_out[__ldcg(to + k)] = 1;
-  // The forks' rows, a warp each
+  // The forks' rows, a warp each.  (The pages of their own are counted by the launch that fills them: what is counted here, references to
+  // pages that are shared, finds 0 where a page is held but counted as free, whatever runs first.)
   const int lane = threadIdx.x & 31;
   for (int r = (threadIdx.x >> 5) * ctas + rank; r < a.slots; r += ctas * (kPlanThreads / 32)) {
     const int s = sm->source[r], n = sm->length[r];
@@ -447,9 +478,10 @@ __global__ void __launch_bounds__(kPlanThreads, 1) pages_fork_kernel(const Pages
 #pragma unroll
         for (int y = 0; y < kInFlight; ++y) {
           if (i0 + 32 * y >= full) break;
-          row[i0 + 32 * y] = page[y];
-          if (page[y] < 0 || page[y] >= a.num_pages) dev_flag(a.status, SEQ_DEV_BAD_PAGE);
-          else atomicAdd(a.refs_out + page[y], 1);
+          const bool good = page[y] >= 0 && page[y] < a.num_pages;
+          row[i0 + 32 * y] = good ? page[y] : -1;
+          if (!good) dev_flag(a.status, SEQ_DEV_BAD_PAGE);
+          else if (atomicAdd(a.refs_out + page[y], 1) <= 0) dev_flag(a.status, SEQ_DEV_BAD_SLOT);
         }
       }
       for (int i = held + lane; i < a.max_pages; i += 32) row[i] = -1;
@@ -460,7 +492,7 @@ __global__ void __launch_bounds__(kPlanThreads, 1) pages_fork_kernel(const Pages
         else if (a.lengths_out != a.lengths) a.lengths_out[r] = a.lengths[r];
       }
     } else if (lane == 0) {
-      if (a.count_out != a.count) a.count_out[r] = min(max(a.count[r], 0), a.max_pages);
+      if (a.count_out != a.count) a.count_out[r] = a.count[r];
       if (a.lengths_out != a.lengths) a.lengths_out[r] = a.lengths[r];
     }
   }
@@ -522,6 +554,7 @@ struct MoveArgs {
   int32_t list_stride, num_pages;
   uint8_t* pages; int32_t planes; int64_t plane_stride, page_stride; int32_t chunks;  // pieces of a plane's page
   int64_t page_bytes;
+  int32_t* refs;  // where the pages that are filled get a reference (fork)
   // the table, rewritten by `map` where there is one
   const int32_t* map; int32_t slots, max_pages;
   const int32_t* table; int64_t table_stride; const int32_t* count;
@@ -544,7 +577,9 @@ __global__ void __launch_bounds__(kMoveThreads) pages_move_kernel(const MoveArgs
       for (int i = threadIdx.x; i < a.max_pages; i += kMoveThreads) {
         if (i >= have && a.table == a.table_out) break;
         int page = -1;
-        if (i < have && !bad) {
+        if (bad) {  // such a row stays as it is
+          page = a.table[r * a.table_stride + i];
+        } else if (i < have) {
           page = a.table[r * a.table_stride + i];
           if (page < 0 || page >= a.num_pages) {
             dev_flag(a.status, SEQ_DEV_BAD_PAGE);
@@ -564,7 +599,8 @@ __global__ void __launch_bounds__(kMoveThreads) pages_move_kernel(const MoveArgs
     const int k = (int)(w / per_page);
     const int rest = (int)(w - k * per_page), x = rest / a.chunks, c = rest - x * a.chunks;
     const int src = a.list[1 + k], dst = a.list[1 + a.list_stride + k];
-    if (src == dst) continue;
+    if (a.refs != nullptr && rest == 0 && threadIdx.x == 0) atomicAdd(a.refs + dst, 1);
+    if (src < 0) continue;
     const int64_t at = (int64_t)c * kMoveChunk + threadIdx.x * 16;
     const uint8_t* from = a.pages + src * a.page_stride + x * a.plane_stride + at;
     uint8_t* to = a.pages + dst * a.page_stride + x * a.plane_stride + at;
@@ -648,12 +684,13 @@ static int launch_plan(Kernel kernel, int* done, const seq_tree_pages_params* p,
   return SEQ_OK;
 }
 
-static int launch_move(const seq_tree_pages_params* p, int list_stride, const int32_t* map, int64_t most_pages, void* stream) {
+static int launch_move(const seq_tree_pages_params* p, int list_stride, int32_t* refs, const int32_t* map, int64_t most_pages, void* stream) {
   MoveArgs a;
   a.list = static_cast<const int32_t*>(p->workspace); a.list_stride = list_stride; a.num_pages = p->num_pages;
   a.pages = static_cast<uint8_t*>(p->pages); a.planes = p->num_planes; a.plane_stride = p->plane_stride_bytes; a.page_stride = p->page_stride_bytes;
   a.chunks = (int)((p->page_bytes + kMoveChunk - 1) / kMoveChunk);
   a.page_bytes = p->page_bytes;
+  a.refs = refs;
   a.map = map; a.slots = p->slots; a.max_pages = p->max_pages;
   a.table = p->page_table; a.table_stride = p->table_stride; a.count = p->page_count;
   a.table_out = p->table_out; a.table_out_stride = p->table_out_stride;
@@ -707,7 +744,7 @@ extern "C" int seq_tree_pages_fork(const seq_tree_pages_params* p, void* stream)
   static int done[64];
   rc = launch_plan(pages_fork_kernel, done, p, p->table_out != p->page_table, stream);
   if (rc != SEQ_OK) return rc;
-  return launch_move(p, p->slots, nullptr, p->slots, stream);
+  return launch_move(p, p->slots, p->refs_out, nullptr, p->slots, stream);
 }
 
 extern "C" int seq_tree_pages_compact(const seq_tree_pages_params* p, void* stream) {
@@ -720,5 +757,5 @@ extern "C" int seq_tree_pages_compact(const seq_tree_pages_params* p, void* stre
   rc = launch_plan(pages_compact_kernel, done, p, false, stream);
   if (rc != SEQ_OK) return rc;
   const int32_t* map = static_cast<const int32_t*>(p->workspace) + 1 + 2 * (size_t)p->num_pages;
-  return launch_move(p, p->num_pages, map, p->num_pages, stream);
+  return launch_move(p, p->num_pages, nullptr, map, p->num_pages, stream);
 }

@@ -299,3 +299,92 @@ def test_a_workspace_on_another_stream_is_that_streams_own(handle):
         torch.cuda.synchronize()
         want = {"resize": (t, want_resize[0], f, want_resize[2]), "fork": (t, want_fork[1], f, want_fork[3]), "compact": (t, want_compact[1], f, want_compact[2])}[call]
         assert np.array_equal(want[0].cpu().numpy(), want[1]) and np.array_equal(want[2].cpu().numpy(), want[3])
+
+
+def both_ways(call, arrays, outs):
+    """``call(arrays, outputs)`` in place and into other arrays: the same status and the same results, which are returned."""
+    results = []
+    for in_place in (True, False):
+        on = dict(zip(arrays, dev(*arrays.values())))
+        to = {x: on[x] if in_place else torch.full_like(on[x], 77) for x in outs}
+        st = status()
+        call(on, to if not in_place else {}, st)
+        results.append([int(st)] + [to[x].cpu().numpy() for x in outs] + ([on["pool"].cpu().numpy()] if "pool" in on else []))
+    for a, b in zip(*results):
+        assert np.array_equal(a, b), (a, b)
+    return results[0]
+
+
+def resize_call(on, to, st):
+    kw = {x + "_out": y for x, y in to.items()}
+    B.seq_tree_pages_resize(on["table"], on["count"], on["refs"], on["tokens"], 16, dev_status=st, **kw)
+
+
+def fork_call(on, to, st):
+    kw = {x + "_out": y for x, y in to.items()}
+    B.seq_tree_pages_fork(on["pool"], on["table"], on["count"], on["refs"], on["lengths"], on["source"], 16, dev_status=st, **kw)
+
+
+def compact_call(on, to, st):
+    kw = {x + "_out": y for x, y in to.items()}
+    B.seq_tree_pages_compact(on["pool"], on["table"], on["count"], on["refs"], dev_status=st, **kw)
+
+
+def i32(x):
+    return np.array(x, dtype=np.int32)
+
+
+@pytest.mark.parametrize("wrong", [-1, -(1 << 31), 4, 1 << 30])
+def test_a_slot_whose_count_cannot_be_is_left_alone(wrong):
+    """Slot 1 takes no part in the calls; its row has something behind what a sound slot would have."""
+    table, refs = i32([[5, -1, -1], [2, 9, 8], [-1, -1, -1]]), i32([0, 0, 1, 0, 0, 1, 0])
+    count, pool = i32([1, wrong, 0]), np.arange(7 * 16, dtype=np.uint8).reshape(7, 16)
+    got = both_ways(resize_call, dict(table=table, count=count, refs=refs, tokens=i32([17, 0, 1])), ("table", "count", "refs"))
+    assert got[0] == B.SEQ_DEV_BAD_SLOT and got[1].tolist() == [[5, 0, -1], [2, 9, 8], [1, -1, -1]] and got[2].tolist() == [2, wrong, 1]
+    assert got[3].tolist() == [1, 1, 1, 0, 0, 1, 0]
+    got = both_ways(fork_call, dict(pool=pool, table=table, count=count, refs=refs, lengths=i32([16, 40, 0]), source=i32([-1, -1, 0])),
+                    ("table", "count", "refs", "lengths"))
+    assert got[0] == B.SEQ_DEV_BAD_SLOT and got[1].tolist() == [[5, -1, -1], [2, 9, 8], [5, -1, -1]] and got[2].tolist() == [1, wrong, 1]
+    assert got[3].tolist() == [0, 0, 1, 0, 0, 2, 0] and got[4].tolist() == [16, 40, 16]
+    got = both_ways(compact_call, dict(pool=pool, table=table, count=count, refs=refs), ("table", "refs"))
+    assert got[0] == B.SEQ_DEV_BAD_SLOT and got[1].tolist() == [[1, -1, -1], [2, 9, 8], [-1, -1, -1]] and got[2].tolist() == [1, 1, 0, 0, 0, 0, 0]
+
+
+def test_fork_counts_a_negative_reference_as_none():
+    table, count, lengths = i32([[3, 4], [-1, -1], [-1, -1]]), i32([2, 0, 0]), i32([20, 0, 0])
+    pool = np.arange(6 * 16, dtype=np.uint8).reshape(6, 16)
+    # page 0: free but for its count; page 5 as well, and nobody gets it
+    got = both_ways(fork_call, dict(pool=pool, table=table, count=count, refs=i32([-3, 1, 1, 1, 1, -1]), lengths=lengths, source=i32([-1, 0, -1])),
+                    ("table", "count", "refs", "lengths"))
+    assert got[0] == B.SEQ_DEV_BAD_SLOT and got[1].tolist() == [[3, 4], [3, 0], [-1, -1]] and got[3].tolist() == [1, 1, 1, 2, 1, 0]
+    assert np.array_equal(got[5][0], pool[4])
+    got = both_ways(fork_call, dict(pool=pool, table=table, count=count, refs=i32([0, 1, 1, 1, 1, -1]), lengths=lengths, source=i32([-1, -1, -1])),
+                    ("table", "count", "refs", "lengths"))
+    assert got[0] == B.SEQ_DEV_BAD_SLOT and got[3].tolist() == [0, 1, 1, 1, 1, 0] and got[1].tolist() == table.tolist()
+
+
+@pytest.mark.parametrize("held", [0, -1])
+def test_fork_of_pages_that_count_as_free(held):
+    table, count, lengths, source = i32([[3, 4], [-1, -1], [-1, -1]]), i32([2, 0, 0]), i32([20, 0, 0]), i32([-1, 0, 0])
+    pool = np.arange(6 * 16, dtype=np.uint8).reshape(6, 16)
+    # the full page: shared by two from 0 on, and by what it is handed out to
+    for refs, own in (([1, 0, 1, held, 1, 1], [1, 3]), ([1, 1, 1, held, 1, 1], [3, None])):
+        got = both_ways(fork_call, dict(pool=pool, table=table, count=count, refs=i32(refs), lengths=lengths, source=source), ("table", "count", "refs", "lengths"))
+        short = own[1] is None
+        assert got[0] == B.SEQ_DEV_BAD_SLOT | (B.SEQ_DEV_NO_PAGES if short else 0)
+        assert got[1].tolist() == [[3, 4], [3, own[0]], [-1, -1] if short else [3, own[1]]]
+        assert got[3][3] == (2 if short else 3) and np.array_equal(got[5][own[0]], pool[4])
+    # the open page: its contents may be another's, so they are not copied
+    got = both_ways(fork_call, dict(pool=pool, table=table, count=count, refs=i32([0, 0, 1, 1, held, 1]), lengths=lengths, source=source),
+                    ("table", "count", "refs", "lengths"))
+    assert got[0] == B.SEQ_DEV_BAD_SLOT and got[1].tolist() == [[3, 4], [3, 0], [3, 1]] and got[3].tolist() == [1, 1, 1, 3, 0, 1]
+    assert np.array_equal(got[5], pool)
+
+
+def test_fork_of_a_row_that_names_no_page():
+    table, count, lengths, source = i32([[6, 2, -7], [-1, -1, -1]]), i32([3, 0]), i32([40, 0]), i32([-1, 0])
+    pool = np.arange(6 * 16, dtype=np.uint8).reshape(6, 16)
+    got = both_ways(fork_call, dict(pool=pool, table=table, count=count, refs=i32([0, 0, 1, 0, 0, 0]), lengths=lengths, source=source),
+                    ("table", "count", "refs", "lengths"))
+    assert got[0] == B.SEQ_DEV_BAD_PAGE and got[1].tolist() == [[6, 2, -7], [-1, 2, 0]] and got[2].tolist() == [3, 3]
+    assert got[3].tolist() == [1, 0, 2, 0, 0, 0] and got[4].tolist() == [40, 40] and np.array_equal(got[5], pool)
