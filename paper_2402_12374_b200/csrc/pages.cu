@@ -652,17 +652,38 @@ static PagesArgs pages_args(const seq_tree_pages_params* p) {
   return a;
 }
 
+// CTAs of a planning cluster at most: kPlanCtas where the device can place such a cluster (a partition may not have as many SMs side by side), the
+// portable 8 otherwise.  `known` keeps the answer per device.
 template <typename Kernel>
-static int launch_plan(Kernel kernel, int* done, const seq_tree_pages_params* p, bool rows_are_copied, void* stream) {
-  const int rc = once_per_device(done, [&]() -> int {
-    SEQ_CUDA_OK(cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
-    return SEQ_OK;
-  });
-  if (rc != SEQ_OK) return rc;
+static int most_plan_ctas(Kernel kernel, int* known) {
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 8;
+  int most = __atomic_load_n(&known[dev], __ATOMIC_ACQUIRE);
+  if (most == 0) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(kPlanCtas);
+    cfg.blockDim = dim3(kPlanThreads);
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = kPlanCtas; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    int clusters = 0;
+    most = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) == cudaSuccess &&
+           cudaOccupancyMaxActiveClusters(&clusters, kernel, &cfg) == cudaSuccess && clusters > 0 ? kPlanCtas : 8;
+    if (most != kPlanCtas) cudaGetLastError();
+    __atomic_store_n(&known[dev], most, __ATOMIC_RELEASE);
+  }
+  return most;
+}
+
+template <typename Kernel>
+static int launch_plan(Kernel kernel, int* known, const seq_tree_pages_params* p, bool rows_are_copied, void* stream) {
+  const int most = most_plan_ctas(kernel, known);
   // A cluster plans: a CTA for every kPagesPerCta pages or table entries (exchanges between CTAs cost more than a few loads), a power of two.
   int ctas = 1;
   const int64_t entries = (int64_t)p->slots * p->max_pages;
-  while (ctas < kPlanCtas && (int64_t)ctas * kPagesPerCta < (p->num_pages > entries ? p->num_pages : entries)) ctas *= 2;
+  while (ctas < most && (int64_t)ctas * kPagesPerCta < (p->num_pages > entries ? p->num_pages : entries)) ctas *= 2;
   // CTAs that copy the table, in clusters of the same size: one for every 8 Ki entries, up to 96
   int copiers = 0;
   if (rows_are_copied) {
@@ -728,8 +749,8 @@ extern "C" int seq_tree_pages_resize(const seq_tree_pages_params* p, void* strea
   if ((p->count_out == p->page_count) != (p->table_out == p->page_table)) return SEQ_ERR_INVALID_ARG;
   rc = check_workspace(p);
   if (rc != SEQ_OK) return rc;
-  static int done[64];
-  return launch_plan(pages_resize_kernel, done, p, p->table_out != p->page_table, stream);
+  static int known[64];
+  return launch_plan(pages_resize_kernel, known, p, p->table_out != p->page_table, stream);
 }
 
 extern "C" int seq_tree_pages_fork(const seq_tree_pages_params* p, void* stream) {
@@ -741,8 +762,8 @@ extern "C" int seq_tree_pages_fork(const seq_tree_pages_params* p, void* stream)
   rc = check_pool(p);
   if (rc == SEQ_OK) rc = check_workspace(p);
   if (rc != SEQ_OK) return rc;
-  static int done[64];
-  rc = launch_plan(pages_fork_kernel, done, p, p->table_out != p->page_table, stream);
+  static int known[64];
+  rc = launch_plan(pages_fork_kernel, known, p, p->table_out != p->page_table, stream);
   if (rc != SEQ_OK) return rc;
   return launch_move(p, p->slots, p->refs_out, nullptr, p->slots, stream);
 }
@@ -753,8 +774,8 @@ extern "C" int seq_tree_pages_compact(const seq_tree_pages_params* p, void* stre
   rc = check_pool(p);
   if (rc == SEQ_OK) rc = check_workspace(p);
   if (rc != SEQ_OK) return rc;
-  static int done[64];
-  rc = launch_plan(pages_compact_kernel, done, p, false, stream);
+  static int known[64];
+  rc = launch_plan(pages_compact_kernel, known, p, false, stream);
   if (rc != SEQ_OK) return rc;
   const int32_t* map = static_cast<const int32_t*>(p->workspace) + 1 + 2 * (size_t)p->num_pages;
   return launch_move(p, p->num_pages, nullptr, map, p->num_pages, stream);
