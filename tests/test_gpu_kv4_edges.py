@@ -74,7 +74,7 @@ def test_memory_of_a_call_on_another_current_stream_is_not_handed_out(n, times, 
     torch.cuda.synchronize()
     need, held = call.workspace_bytes_needed, {t.data_ptr() for t in (call.out, call.workspace) if t is not None}
     with torch.cuda.stream(side):
-        torch.cuda._sleep(50_000_000)
+        torch.cuda._sleep(1_000_000_000)
         out = call.run() if not given else None
     if given:
         out = call.run(stream=side.cuda_stream)
@@ -102,7 +102,9 @@ def test_memory_that_a_call_takes_over_is_not_used_before_its_last_user_is_throu
     torch.cuda.empty_cache()
     before = [torch.empty_like(q), torch.empty(need, dtype=torch.uint8, device="cuda")]
     places = {t.data_ptr() for t in before}
-    torch.cuda._sleep(50_000_000)
+    for t in before:
+        t.fill_(0)  # (what is asked for behind the wait has been loaded)
+    torch.cuda._sleep(1_000_000_000)
     for t in before:
         t.fill_(77)
     through = torch.cuda.Event()

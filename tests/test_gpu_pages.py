@@ -283,7 +283,8 @@ def test_a_workspace_on_another_stream_is_that_streams_own(handle):
         torch.cuda.synchronize()
         torch.cuda.empty_cache()
         before = torch.empty(1 + 3 * 30000, dtype=torch.int32, device="cuda")
-        torch.cuda._sleep(20_000_000)
+        before.fill_(0)  # (what is asked for behind the wait has been loaded)
+        torch.cuda._sleep(1_000_000_000)
         before.fill_(7)
         through = torch.cuda.Event()
         through.record()
