@@ -11,6 +11,9 @@
 
 namespace seqtree {
 
+// A score's unit at the least, the smallest normal number: hidden scores, -inf, times zero would be NaN.  (Sums of products are below
+// 2^9 * 65504 * 128: what units below it stand for rounds to zero.)
+constexpr float kLeastUnit = 1.17549435e-38f;
 constexpr int kKv4TreeSteps = SEQ_MAX_TREE / 32;  // steps of the tree, at most
 
 struct Kv4Args {

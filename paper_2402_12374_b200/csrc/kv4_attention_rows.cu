@@ -361,7 +361,7 @@ __global__ void __launch_bounds__(32 * kRowsWarps, NT == 1 ? 3 : 2) kv4_rows_ker
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         sq[nt][i] = __shfl_sync(0xffffffffu, sum, (2 * t4 + i) * 4);
-        st.rs[nt][i] = a.scale_log2 * __shfl_sync(0xffffffffu, inv_f, (2 * t4 + i) * 4);
+        st.rs[nt][i] = fmaxf(a.scale_log2 * __shfl_sync(0xffffffffu, inv_f, (2 * t4 + i) * 4), kLeastUnit);
         if (a.window > 0) {  // (every warp finds the same)
           const int begin = u.L + 1 - a.window + kv4_depth(a, u.r, min(row0 + nt * 8 + 2 * t4 + i, a.rows - 1) / a.group);
           sm->begin[nt * 8 + 2 * t4 + i] = begin;

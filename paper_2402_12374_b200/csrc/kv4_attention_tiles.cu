@@ -530,7 +530,7 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
           __syncwarp();
           if (lane == 0) mbar_arrive(&sm->q_full);
         }
-        next.rs = rs;
+        next.rs = fmaxf(rs, kLeastUnit);
         next.mask = kv4_mask_row(a, r, node);
         next.depth = a.window > 0 ? kv4_depth(a, r, node) : 0;
         next.begin = a.window > 0 ? next.sg.u.L + next.depth + 1 - a.window : 0;

@@ -126,3 +126,13 @@ def test_memory_that_a_call_takes_over_is_not_used_before_its_last_user_is_throu
     assert how != "out given" or not through.query()  # nothing of the call's is that stream's: it did not wait
     torch.cuda.synchronize()
     assert torch.equal(out, want)
+
+
+@BOTH
+@pytest.mark.parametrize("n,Hq", [(1, 8), (14, 1), (40, 4)])
+@pytest.mark.parametrize("scale", [1e-45, 1e-38, 1e-30])
+def test_a_scale_that_makes_all_scores_alike(scale, n, Hq, dt, room):
+    """Hidden keys stay hidden: their -inf is not multiplied by a scale of zero."""
+    c = Case([45, 0, 300], n, Hq, 1, 16, dt, seed=3, mask="each")
+    c.check(softmax_scale=scale)
+    c.check(softmax_scale=scale, window=20, sinks=3)
