@@ -337,7 +337,7 @@ __global__ void __launch_bounds__(32 * kRowsWarps, NT == 1 ? 3 : 2) kv4_rows_ker
       const int e = (int)(__float_as_uint(top) >> 23);
       float f = 1.f, inv_f = 1.f;
       if (e > 8 && e < 255) {
-        const int up = min(max(8 + 127 - e, -100), 100);
+        const int up = 8 + 127 - e;  // -119..126
         f = __uint_as_float((uint32_t)(127 + up) << 23);
         inv_f = __uint_as_float((uint32_t)(127 - up) << 23);
       }

@@ -494,7 +494,7 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
             rows_sync();
             const int e = (int)(max(top, sm->top[grp ^ 1][row]) >> 7);
             if (e > 8 && e < 255) {  // the largest magnitude into [2^8, 2^9)
-              const int up = min(max(8 + 127 - e, -100), 100);
+              const int up = 8 + 127 - e;  // -119..126
               f = __uint_as_float((uint32_t)(127 + up) << 23);
               rs *= __uint_as_float((uint32_t)(127 - up) << 23);
             }

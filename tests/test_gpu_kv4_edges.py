@@ -136,3 +136,11 @@ def test_a_scale_that_makes_all_scores_alike(scale, n, Hq, dt, room):
     c = Case([45, 0, 300], n, Hq, 1, 16, dt, seed=3, mask="each")
     c.check(softmax_scale=scale)
     c.check(softmax_scale=scale, window=20, sinks=3)
+
+
+@pytest.mark.parametrize("n,Hq", [(1, 8), (14, 1), (40, 4)])
+@pytest.mark.parametrize("size,scale", [(1e36, 1e-37), (1e30, 1e-31), (1e-28, 1e27)])
+def test_rows_of_q_at_the_ends_of_bfloat16s_range(size, scale, n, Hq, room):
+    c = Case([45, 300], n, Hq, 1, 16, torch.bfloat16, seed=8, mask="each")
+    c.q = (c.q.double() * size).to(torch.bfloat16)
+    c.check(softmax_scale=scale)
