@@ -14,6 +14,10 @@ namespace seqtree {
 // A score's unit at the least, the smallest normal number: hidden scores, -inf, times zero would be NaN.  (Sums of products are below
 // 2^9 * 65504 * 128: what units below it stand for rounds to zero.)
 constexpr float kLeastUnit = 1.17549435e-38f;
+// A score less the reference is one fused operation, whose product is not rounded, while the reference is a rounded one: the largest
+// exponent is off by up to 2^-24 of its score, and beyond 2^31 no probability would be left, or all be infinite.  Scores beyond this are
+// rounded first.
+constexpr float kWideScore = 4194304.f;
 constexpr int kKv4TreeSteps = SEQ_MAX_TREE / 32;  // steps of the tree, at most
 
 struct Kv4Args {

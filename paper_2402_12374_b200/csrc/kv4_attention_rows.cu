@@ -27,7 +27,7 @@ namespace seqtree {
 constexpr int kRowsWarps = 4;
 constexpr int kTreeStep = 32;  // rows of the tree in a step
 constexpr int kRowsCluster = 8;  // CTAs of a cluster, at most
-constexpr float kNoRef = -1e30f;  // a row that has seen no key yet
+constexpr float kNoRef = -3e38f;  // a row that has seen no key yet
 
 constexpr int kKeys = 32;    // of a step
 constexpr int kStages = 3;
@@ -110,6 +110,7 @@ struct RowsState {
   float pm[NT][2], pr[NT][2];  // sums of mid * probability and of P as rounded, over the thread's keys
   float o[NT][8][4];           // codes x P; or, once finished, values x probabilities
   int e;                       // P holds scale * probability / 2^e
+  bool wide;                   // scores of the warp's rows may be beyond kWideScore
 };
 
 // Scores a (-inf where masked) become exponents y against the reference, which follows scores that exceed it by more than the
@@ -123,6 +124,13 @@ __device__ __forceinline__ void follow(const float (&a)[NG][NT][4], float (&y)[N
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
         for (int v = 0; v < 4; ++v) y[gr][nt][v] = fmaf(a[gr][nt][v], st.rs[nt][v & 1], -st.m[nt][v & 1]);
+    if (!st.wide) return;
+#pragma unroll
+    for (int gr = 0; gr < NG; ++gr)
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) y[gr][nt][v] = __fadd_rn(__fmul_rn(a[gr][nt][v], st.rs[nt][v & 1]), -st.m[nt][v & 1]);
   };
   exponents();
   bool move = e > st.e;
@@ -135,6 +143,7 @@ __device__ __forceinline__ void follow(const float (&a)[NG][NT][4], float (&y)[N
   if (!__any_sync(0xffffffffu, move)) return;
   const float shrink = e > st.e ? (st.e - e < -126 ? 0.f : __uint_as_float((uint32_t)(127 + st.e - e) << 23)) : 1.f;
   st.e = max(st.e, e);
+  bool wide = false;
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -148,6 +157,7 @@ __device__ __forceinline__ void follow(const float (&a)[NG][NT][4], float (&y)[N
       top = fmaxf(top, st.m[nt][i]);
       const float alpha = ex2(st.m[nt][i] - top);
       st.m[nt][i] = top;
+      wide |= fabsf(top) > kWideScore && top != kNoRef;
       st.l[nt][i] *= alpha;
       st.pm[nt][i] *= alpha;
       st.pr[nt][i] *= alpha * shrink;
@@ -157,6 +167,7 @@ __device__ __forceinline__ void follow(const float (&a)[NG][NT][4], float (&y)[N
         st.o[nt][mt][i + 2] *= alpha * shrink;
       }
     }
+  st.wide = __any_sync(0xffffffffu, wide);
   exponents();
 }
 
@@ -305,6 +316,7 @@ __global__ void __launch_bounds__(32 * kRowsWarps, NT == 1 ? 3 : 2) kv4_rows_ker
     float sq[NT][2];
     RowsState<NT> st;
     st.e = -1000;
+    st.wide = false;
     int latest = 0;  // the last begin of a row's window
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {

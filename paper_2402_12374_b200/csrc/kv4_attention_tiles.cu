@@ -70,6 +70,7 @@ struct TilesSmem {
   Kv4Plan plan;
   // exact codes: scales and mids of the tiles' keys and values (two keys' scales, their mids), the largest scale's bits of 32 values, the
   // rows' sums of q, and of mid * probability
+  float ref_scale[kExact ? kTileM : 1];  // exact codes: ref is for ref + ref_scale
   float4 key_params[kExact ? kParamTiles : 1][kTilesStep / 2], value_params[kExact ? kParamTiles : 1][kTilesStep / 2];
   int4 largest[kExact ? kParamTiles : 1];
   float q_sum[kExact ? kGroups : 1][kTileM], mids[kExact ? kGroups : 1][kTileM];
@@ -459,7 +460,7 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
     };
     Row cur;
     bool have = false;
-    float m_used = -INFINITY, l = 0.f, mids = 0.f;
+    float m_used = -INFINITY, m_scale = 0.f, l = 0.f, mids = 0.f;
     for (int pos = range_lo;;) {
       // ---- the next segment's rows; its first scores are computed while the last segment's results are written
       Row next;
@@ -561,12 +562,14 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
           }
         }
         // ---- the groups' sums, against the reference that O ended in: the last one settled
-        const float M = any ? sm->ref[row] : -INFINITY;
-        sm->sum[grp][row] = poison != 0 ? NAN : m_used == -INFINITY ? l : l * ex2(m_used - M);
-        if (kExact) sm->mids[grp][row] = m_used == -INFINITY ? 0.f : mids * ex2(m_used - M);
+        const float M = any ? sm->ref[row] : -INFINITY, M_scale = kExact && any ? sm->ref_scale[row] : 0.f;
+        const float behind = m_used == -INFINITY ? 0.f : ex2((m_used - M) + (kExact ? m_scale - M_scale : 0.f));
+        sm->sum[grp][row] = poison != 0 ? NAN : m_used == -INFINITY ? l : l * behind;
+        if (kExact) sm->mids[grp][row] = mids * behind;
         rows_sync();
-        const float sum = sm->sum[0][row] + sm->sum[1][row];
-        const float all_mids = kExact ? sm->mids[0][row] + sm->mids[1][row] : 0.f;
+        const float unit = kExact ? __uint_as_float((uint32_t)(127 + (int)M_scale) << 23) : 1.f;  // (-15..16: what a piece leaves is for M)
+        const float own_sum = sm->sum[0][row] + sm->sum[1][row], sum = own_sum * unit;
+        const float all_mids = kExact ? (sm->mids[0][row] + sm->mids[1][row]) * unit : 0.f;
         const float inv = 1.f / sum;
         const int64_t mine = (int64_t)kv4_slot(ranges, blockIdx.x, sg.u.begin) * kTileM;
 #pragma unroll 1
@@ -575,7 +578,7 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
           tmem_get32(tmem_o + 32u * c, o);
           if (kExact) {
 #pragma unroll
-            for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) + all_mids);
+            for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(fmaf(__uint_as_float(o[e]), unit, all_mids));
           }
           if (!sg.whole) {  // a piece, unnormalised
             uint4* to = reinterpret_cast<uint4*>(a.ws_o + mine * kHeadDim) + 8 * c * kTileM + row;  // [channel / 4][row]
@@ -610,7 +613,7 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
       const float rs = cur.rs;
       const bool warp_live = cur.warp_live;
       m_used = -INFINITY;
-      l = mids = 0.f;
+      m_scale = l = mids = 0.f;
       for (int i = (grp ^ step) & 1; i < sg.steps; i += kGroups, ++own) {
         const int t = sg.t0 + i, x = step + i, u = x / kSBufs, sb = x - u * kSBufs;
         const uint32_t tmem_s = tmem + kTmemS + 128u * sb + lane_sel;
@@ -655,23 +658,32 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
           }
           if (masked || kExact) tc_wait_st();
           float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * rs;  // rs > 0
-          if (kExact) {  // scale * probability is what is rounded: the reference counts the tile's largest scale
+          // Scale * probability is what is rounded: the reference counts the tile's largest scale, apart from the scores where their last bits
+          // are too coarse for it.
+          float top_scale = 0.f;
+          if (kExact) {
             const int4 big = sm->largest[slot];
-            top += (float)((max(max(big.x, big.y), max(big.z, big.w)) >> 10) - 15);
+            top_scale = (float)((max(max(big.x, big.y), max(big.z, big.w)) >> 10) - 15);
+            if (!(fabsf(top) > kWideScore)) {
+              top += top_scale;
+              top_scale = 0.f;
+            }
           }
           // All groups add to one accumulator, so they share the rows' reference: it is settled tile by tile, in order, before the
           // exponentials.  It moves only when a score exceeds it by more than the threshold, or with the first score.
-          float ref = -INFINITY;
+          float ref = -INFINITY, ref_scale = 0.f;
           if (i > 0) {
             ok = kv4_wait(sm, &sm->settled[grp ^ 1][quarter], (own - (grp == 0)) & 1, a.status);
             __syncwarp();
             if (!ok) break;
             ref = sm->ref[row];
+            if (kExact) ref_scale = sm->ref_scale[row];
           }
-          const bool move = top > ref + kRescaleThreshold || (ref == -INFINITY && top != -INFINITY);
-          const float now = move ? top : ref;
+          const float above = (top - ref) + (kExact ? top_scale - ref_scale : 0.f);
+          const bool move = above > kRescaleThreshold;  // (of two that are -inf: NaN)
+          const float now = move ? top : ref, now_scale = move ? top_scale : ref_scale;
           if (__any_sync(0xffffffffu, move) || i == 0) {
-            const float alpha = move && ref != -INFINITY ? ex2(ref - top) : 1.f;
+            const float alpha = move && ref != -INFINITY ? ex2(-above) : 1.f;
             if (i > 0) {
               // O may still be taking the tile before
               ok = kv4_wait(sm, &sm->pv_done[sb == 0 ? kSBufs - 1 : sb - 1], (u - (sb == 0)) & 1, a.status);
@@ -690,17 +702,31 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
               tc_fence_before();
             }
             sm->ref[row] = now;
+            if (kExact) sm->ref_scale[row] = now_scale;
             __syncwarp();
           }
           if (lane == 0) mbar_arrive(&sm->settled[grp][quarter]);
-          if (now != m_used) {
-            const float f = m_used == -INFINITY ? 0.f : ex2(m_used - now);
+          if (now != m_used || (kExact && now_scale != m_scale)) {
+            const float f = m_used == -INFINITY ? 0.f : ex2((m_used - now) + (kExact ? m_scale - now_scale : 0.f));
             l *= f;
             mids *= f;
             m_used = now;
+            m_scale = now_scale;
           }
           const float neg_m = now == -INFINITY ? 0.f : -now;
-          const uint64_t rs2 = pair_of(rs, rs), neg_m2 = pair_of(neg_m, neg_m);
+          const bool wide = __any_sync(0xffffffffu, fabsf(neg_m) > kWideScore);
+          const float less = wide ? -now_scale : neg_m;  // (not wide: no scale apart)
+          const uint64_t rs2 = pair_of(rs, rs), unit2 = wide ? pair_of(1.f, 1.f) : rs2, less2 = pair_of(less, less);
+          if (wide) {  // scores in units of 1, less the reference.  (A packed product and sum would be made one operation by the assembler.)
+#pragma unroll 1
+            for (int c = 0; c < 4; ++c) {
+              tmem_get32(tmem_s + 32u * c, s);
+#pragma unroll
+              for (int e = 0; e < 32; ++e) s[e] = __float_as_uint(__fadd_rn(__fmul_rn(__uint_as_float(s[e]), rs), neg_m));
+              tmem_st32(tmem_s + 32u * c, s, 0);
+            }
+            tc_wait_st();
+          }
           uint64_t sums[2] = {pair_of(0.f, 0.f), pair_of(0.f, 0.f)}, mids2 = pair_of(0.f, 0.f);
 #pragma unroll 1
           for (int c = 0; c < 4; ++c) {
@@ -709,7 +735,7 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
               float y0, y1;
-              unpair(fma2(pair_of(__uint_as_float(s[2 * e]), __uint_as_float(s[2 * e + 1])), rs2, neg_m2), y0, y1);
+              unpair(fma2(pair_of(__uint_as_float(s[2 * e]), __uint_as_float(s[2 * e + 1])), unit2, less2), y0, y1);
               float p0 = ex2(y0), p1 = ex2(y1);
               sums[e & 1] = add2(sums[e & 1], pair_of(p0, p1));
               if (kExact) {

@@ -144,3 +144,52 @@ def test_rows_of_q_at_the_ends_of_bfloat16s_range(size, scale, n, Hq, room):
     c = Case([45, 300], n, Hq, 1, 16, torch.bfloat16, seed=8, mask="each")
     c.q = (c.q.double() * size).to(torch.bfloat16)
     c.check(softmax_scale=scale)
+
+
+@BOTH
+@pytest.mark.parametrize("n,Hq", [(1, 8), (14, 1), (40, 4), (100, 2)])
+@pytest.mark.parametrize("scale", [1e3, 1e7, 1e15, 1e30])
+@pytest.mark.parametrize("sign", [1, -1])
+def test_scores_far_from_zero(sign, scale, n, Hq, dt, room):
+    """One key is so far above the others that it alone counts, and its score is up to 1e33 from zero: a row's own node, whose key is
+    larger than all others, or smaller where q is negative."""
+    c = Case([0, 33, 700], n, Hq, 1, 16, dt, seed=8, mask="chain")
+    for r, L in enumerate(c.lengths):
+        for t in range(L):
+            U.store(c.pool, c.table[r, t // 16], 0, 0, 16, t, 0, *U.quantise(np.full(128, 8.0)))
+    c.pool_dev = torch.from_numpy(c.pool).reshape(c.pool.shape[0], 1, 1, -1).cuda()
+    c.q[:] = sign
+    i = torch.arange(n).reshape(1, n, 1, 1)
+    c.kt[:] = 8.5 + i / 16 if sign > 0 else 7.5 - i / 32  # (exact in both types; steps of 1/32: scores are 4 * scale apart)
+    call = c.call(softmax_scale=scale)
+    out = call.run()
+    torch.cuda.synchronize()
+    assert int(c.status) == 0
+    # its probability over the sum of itself: P's rounding to half precision and the output's
+    v = c.vt.double()
+    assert ((out.double().cpu() - v).abs() <= (U.EPS2[dt] + 1.01 * U.HALF) * v.abs() + 2.0 ** -24).all()
+    # half a step each: the scale as fp32, log2(e), their product, the score, the logarithm of the sum added, ln(2), the result
+    want = 128 * scale * sign * c.kt[:, :, 0, 0].double()[:, None]
+    assert ((call.lse.double().cpu() - want).abs() <= 7.01 * 2.0 ** -24 * want.abs()).all()
+
+
+@pytest.mark.parametrize("n,Hq", [(1, 8), (14, 1), (40, 4)])
+def test_the_largest_rows_of_half_precision(n, Hq, room):
+    """q, keys and values near the largest half: scores beyond 1e8."""
+    c = Case([45, 300], n, Hq, 1, 16, torch.float16, seed=8, mask="each")
+    rng = np.random.default_rng(5)
+    for r, L in enumerate(c.lengths):
+        for t in range(L):
+            U.store(c.pool, c.table[r, t // 16], 0, 0, 16, t, 0, *U.quantise(rng.uniform(-6e4, 6e4, 128)))
+    c.pool_dev = torch.from_numpy(c.pool).reshape(c.pool.shape[0], 1, 1, -1).cuda()
+    c.q, c.kt = (c.q * 1e4).clamp(-6e4, 6e4), (c.kt * 1e4).clamp(-6e4, 6e4)
+    out, _ = c.check()
+    for r, L in enumerate(c.lengths):  # the key with the largest score, where that is no matter of rounding
+        k, v = U.prefix_rows(c.pool, 0, c.table[r], L, 1, 16)
+        k, v = torch.cat([torch.as_tensor(k[0]), c.kt[r, :, 0].double()]), torch.cat([torch.as_tensor(v[0]), c.vt[r, :, 0].double()])
+        s = torch.einsum("nhc,jc->nhj", c.q[r].double(), k).masked_fill(~torch.cat([torch.ones(n, L, dtype=torch.bool), torch.as_tensor(c.seen[r])], 1)[:, None], -torch.inf)
+        top = s.topk(2, -1)
+        sure = top.values[..., 0] - top.values[..., 1] > 1e-4 * s.abs().nan_to_num(posinf=0).amax(-1)
+        assert sure.double().mean() > 0.9
+        got, want = out[r].double().cpu()[sure], v[top.indices[..., 0]][sure]
+        assert ((got - want).abs() <= 3 * U.HALF * (want.abs() + 8)).all()  # (out's rounding, and scale * 1's: codes up to 8 scales, |value| + |mid| <= 8)
