@@ -543,10 +543,11 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
         const int L = sg.u.L, r = sg.u.r, node = cur.node, h = cur.h, depth = cur.depth;
         const uint32_t* mask_row = cur.mask;
         const bool valid = cur.valid;
-        // ---- the last product
+        // ---- the last product.  Its tile may be the other group's, and this one be there before the scores are: the barrier would then still
+        // wait for the product of three tiles ago, and its parity look like that of the one after.  The scores come behind that product.
         if (sg.steps > 0 && ok) {
           const int x = step - 1, u = x / kSBufs;
-          ok = kv4_wait(sm, &sm->pv_done[x - u * kSBufs], u & 1, a.status);
+          ok = kv4_wait(sm, &sm->s_full[x - u * kSBufs], u & 1, a.status) && kv4_wait(sm, &sm->pv_done[x - u * kSBufs], u & 1, a.status);
         }
         __syncwarp();
         tc_fence_after();

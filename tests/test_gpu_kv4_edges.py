@@ -193,3 +193,17 @@ def test_the_largest_rows_of_half_precision(n, Hq, room):
         assert sure.double().mean() > 0.9
         got, want = out[r].double().cpu()[sure], v[top.indices[..., 0]][sure]
         assert ((got - want).abs() <= 3 * U.HALF * (want.abs() + 8)).all()  # (out's rounding, and scale * 1's: codes up to 8 scales, |value| + |mid| <= 8)
+
+
+@BOTH
+@pytest.mark.parametrize("L", [200, 300, 420, 560, 700])
+def test_last_segments_that_end_with_either_groups_tile(L, dt):
+    """A unit a range or nearly so: the group of threads that does not have the last key tile is through before that tile's product, and
+    takes the rows' sums and reference as the other one leaves them."""
+    c = Case([L] * 30, 40, 8, 2, 16, dt, seed=L)
+    c.kt *= 3  # (the tree's tile, the last one, has the largest scores)
+    out, call = c.check()
+    assert call.workspace is not None
+    out, lse = out.clone(), call.lse.clone()
+    for _ in range(20):
+        assert torch.equal(call.run(), out) and torch.equal(call.lse, lse)
