@@ -115,13 +115,6 @@ __device__ __forceinline__ void tmem_get32(uint32_t taddr, uint32_t (&r)[32]) {
 #pragma unroll
   for (int e = 0; e < 32; ++e) asm volatile("" : "+r"(r[e]));  // (nothing of it moves ahead of the wait)
 }
-__device__ __forceinline__ void tmem_get64(uint32_t taddr, uint32_t (&r)[64]) {
-  tmem_ld32(taddr, r, 0);
-  tmem_ld32(taddr + 32u, r, 32);
-  tc_wait_ld();
-#pragma unroll
-  for (int e = 0; e < 64; ++e) asm volatile("" : "+r"(r[e]));  // (nothing of it moves ahead of the wait)
-}
 __device__ __forceinline__ uint32_t bits_below(int x) { return x <= 0 ? 0u : (x >= 32 ? 0xffffffffu : (1u << x) - 1u); }
 
 // The steps of a unit that fall into a CTA's range: none, if that is only what stands for its cost
