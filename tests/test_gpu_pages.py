@@ -278,6 +278,11 @@ def test_a_workspace_on_another_stream_is_that_streams_own(handle):
                                             U.compact(pool, table, count, refs))
     side = torch.cuda.Stream()
     on = side.cuda_stream if handle else side
+    # (kernels are loaded at their first launch, which waits for the device)
+    p, t, c, f, n, tok, src = dev(pool, table, count, refs, lengths, tokens, source)
+    B.seq_tree_pages_fork(p, t, c, f, n, src, 16)
+    B.seq_tree_pages_compact(p, t, c, f)
+    B.seq_tree_pages_resize(t, c, f, tok, 16)
     for call in ("resize", "fork", "compact"):
         p, t, c, f, n, tok, src = dev(pool, table, count, refs, lengths, tokens, source)
         torch.cuda.synchronize()
