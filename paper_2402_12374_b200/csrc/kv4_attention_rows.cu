@@ -642,7 +642,6 @@ __global__ void __launch_bounds__(32 * kRowsWarps, NT == 1 ? 3 : 2) kv4_rows_ker
     const bool whole = !kCluster && pos == u.begin && seg_end == u.end;
     const int64_t slot = kCluster ? 0 : (int64_t)kv4_slot(ranges, blockIdx.x, u.begin) * a.row_tile;
     // Warp w: rows w, w + 4, ...; a lane has four channels of a row.
-    using T = typename std::conditional<kBf16, __nv_bfloat16, __half>::type;
     auto write_row = [&](int row, float M, float sum, float4 acc) {
       const int rw = row0 + row, nd = rw / a.group, h = u.g * a.group + rw - nd * a.group;
       const float inv = 1.f / sum;
