@@ -536,11 +536,14 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv4_tiles_kernel(const Kv4Ar
         const int L = sg.u.L, r = sg.u.r, node = cur.node, h = cur.h, depth = cur.depth;
         const uint32_t* mask_row = cur.mask;
         const bool valid = cur.valid;
-        // ---- the last product.  Its tile may be the other group's, and this one be there before the scores are: the barrier would then still
-        // wait for the product of three tiles ago, and its parity look like that of the one after.  The scores come behind that product.
+        // ---- the last product.  Its tile may be the other group's, and this one be here before that tile's scores are: the barrier would then
+        // still wait for the product of three tiles ago, and its parity look like that of the one after.  The scores come behind that product, so
+        // they are waited for: above, where a next segment's q is brought, and here where none is.  (Behind the next q they could be two
+        // phases on.)
         if (sg.steps > 0 && ok) {
           const int x = step - 1, u = x / kSBufs;
-          ok = kv4_wait(sm, &sm->s_full[x - u * kSBufs], u & 1, a.status) && kv4_wait(sm, &sm->pv_done[x - u * kSBufs], u & 1, a.status);
+          if (!more || next.sg.steps == 0) ok = kv4_wait(sm, &sm->s_full[x - u * kSBufs], u & 1, a.status);
+          if (ok) ok = kv4_wait(sm, &sm->pv_done[x - u * kSBufs], u & 1, a.status);
         }
         __syncwarp();
         tc_fence_after();

@@ -207,3 +207,16 @@ def test_last_segments_that_end_with_either_groups_tile(L, dt):
     out, lse = out.clone(), call.lse.clone()
     for _ in range(20):
         assert torch.equal(call.run(), out) and torch.equal(call.lse, lse)
+
+
+@pytest.mark.parametrize("lengths,n,Hq,Hkv,window,dt,seed", [([-1, 1651], 620, 15, 3, 667, torch.bfloat16, 21), ([1200, 900], 500, 12, 3, 300, torch.float16, 2),
+                                                          ([3000], 768, 16, 2, 0, torch.bfloat16, 3), ([3000], 768, 16, 2, 0, torch.float16, 4)])
+def test_many_tiles_of_rows_a_range(lengths, n, Hq, Hkv, window, dt, seed):
+    """The scores of the next tile of rows are computed, and its buffers go round, while the last one's results are still being written."""
+    c = Case(lengths, n, Hq, Hkv, 128, dt, seed=seed, mask="each")
+    out, call = c.check(window=window, sinks=3 if window else 0)
+    out, lse = out.clone(), call.lse.clone()
+    live = [r for r, L in enumerate(lengths) if L >= 0]
+    for _ in range(10):
+        assert torch.equal(call.run()[live], out[live]) and torch.equal(call.lse[live], lse[live])
+    assert int(c.status) == 0
