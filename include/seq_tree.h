@@ -60,11 +60,12 @@ typedef enum { SEQ_F16 = 0, SEQ_BF16 = 1, SEQ_F32 = 2 } seq_dtype;
 enum {
   SEQ_DEV_BAD_PARENT = 1,  /* parent[i] not in {-1} u [0,i): read as -1 */
   SEQ_DEV_BAD_TOKEN = 2,   /* token id outside [0,vocab): the child is rejected, R and D untouched */
-  SEQ_DEV_NONFINITE = 4,   /* NaN or +inf logit on a visited row */
+  SEQ_DEV_NONFINITE = 4,   /* NaN or +inf logit on a visited row; a row beyond half precision (seq_tree_kv4_append) */
   SEQ_DEV_DEGENERATE = 8,  /* sum max(R-D,0) == 0 after a rejection (impossible in exact arithmetic): R kept */
   SEQ_DEV_TIMEOUT = 16,    /* a bounded on-chip wait ran out; outputs of that call are undefined, but for the verification's
                               path_len and bonus_token: 0 and -1, or what had been decided */
-  SEQ_DEV_BAD_PATH = 32,   /* seq_tree_kv_commit: path not a root-to-node path (see there); nothing was moved */
+  SEQ_DEV_BAD_PATH = 32,   /* seq_tree_kv_commit: path not a root-to-node path (see there); nothing was moved.  seq_tree_kv4_append,
+                              _read: a count or a path entry outside the rows; that request was left alone */
   SEQ_DEV_BAD_LENGTH = 64, /* *prefix_len_dev outside [0, prefix_len] (lengths[r] above max_len or the page table's reach):
                               clamped into that range */
   SEQ_DEV_BAD_PAGE = 128,  /* a page number outside [0, num_pages): read as page 0, never written */
@@ -470,12 +471,15 @@ int seq_tree_kv_commit(const seq_tree_kv_commit_params* p, void* stream);
  *   workspace        seq_tree_kv4_attention_workspace_bytes(p) bytes (0 where little work is cut within clusters; then it may be
  *                    NULL), 256-byte aligned, device, contents undefined before and after: the pieces of work that several
  *                    CTAs share.  Two calls that can run at the same time need one each.
+ * batch <= SEQ_MAX_BATCH, n_tree <= SEQ_MAX_TREE, num_q_heads <= 4096, max_len, window and sinks <= 2^30.
  * All rows 16-byte aligned, head_dim 128, SEQ_F16 or SEQ_BF16.  Products run in half precision with fp32 sums.  q enters
- * exactly (a bf16 row scaled by a power of two); tree rows of bf16 are rounded to half.  The pages' codes enter exactly, scales and mids
+ * exactly (scaled by a power of two; to a multiple of 2^-28 of the row's largest value); tree rows of bf16 are rounded
+ * to half, which is exact from 2^-17 to 65504 and to a multiple of 2^-24 below.  The pages' codes enter exactly, scales and mids
  * are applied in fp32, and a value's scale times its probability is rounded to half (2^-11 of it, but no finer than 2^-24 of the
  * largest scale among the keys that are read).  Only where the rows are bf16 and
  * a kv head has many of them, a key's and a value's number, scale * (code - 8) + mid, and its probability are each rounded to
- * half, out's own rounding being eight times as coarse.  Softmax and sums are fp32.  The same call on the same inputs returns the same bits.  Returns SEQ_OK,
+ * half, out's own rounding being eight times as coarse; lse then has the keys' rounding too, at most 2^-11
+ * of each product.  Softmax and sums are fp32.  The same call on the same inputs returns the same bits.  Returns SEQ_OK,
  * SEQ_ERR_INVALID_ARG, SEQ_ERR_UNSUPPORTED (head_dim, dtype, page size, 2^31 tiles of work), SEQ_ERR_WORKSPACE or SEQ_ERR_CUDA.
  */
 typedef struct {
@@ -518,7 +522,7 @@ int seq_tree_kv4_attention(const seq_tree_kv4_attention_params* p, void* stream)
  * each step in fp32, rint to even; scale 0 gives code 8.  A row with an inf, a NaN or a magnitude above 65504 raises
  * SEQ_DEV_NONFINITE and is stored as zeros.
  *   k, v          element (l,r,i,g,c) at l*stride_layer + r*stride_req + i*stride_tok + g*stride_head + c, f16 or bf16, rows
- *                 16-byte aligned, i < n_rows
+ *                 16-byte aligned, i < n_rows (1 to 2^20 - 16; at most 1024 layers and kv heads, a table's reach at most 2^30 tokens)
  *   pages         layer l, kv head g of page p at p*page_stride_bytes + l*layer_stride_bytes + g*page_size*136
  *   count         nullable [batch]; as path_len of seq_tree_verify_batch.  path nullable, request r's at r*path_stride.
  *                 A count outside [0, n_rows], or a path entry outside it, raises SEQ_DEV_BAD_PATH; tokens that would lie
@@ -554,7 +558,8 @@ int seq_tree_kv4_append(const seq_tree_kv4_append_params* p, void* stream);
  * seq_tree_kv4_read -- tokens of the pages as 16-bit rows (to look at them, to hand a prefix to a 16-bit cache, or to
  * attend over what later steps will see): row i < m = count[r] (all n_rows without count) of request r, layer l, head g is
  * token start[r] + i (i without start), scale * (code - 8) + mid in fp32, rounded once.  Rows i >= m are left as they are, as
- * are all rows of a request whose start is negative.  The struct is seq_tree_kv4_append_params with `lengths` as start
+ * are all rows of a request whose start is negative.  (In SEQ_F16 a value past the largest half is infinite: a row that reaches 65504 can
+ * have one, as its scale and mid are rounded.)  The struct is seq_tree_kv4_append_params with `lengths` as start
  * (nullable), k and v written; path, new_lengths must be NULL.  Bad counts, tokens behind the page table's reach and page
  * numbers outside the pool raise what they raise there, and the rows concerned are left as they are.
  */

@@ -15,9 +15,9 @@
 // Two ways to cut the work.  Few units: a cluster of CTAs each, which meet in shared memory, one launch without a workspace.  Many:
 // the ranges of kv4_attention.cuh, equal whatever the requests' lengths are.
 //
-// What bounds it: HBM while it streams (6.0 of 6.5 TB/s: 17.8 us for each 107 MB), and 15 us of a call with ranges that are the start (lengths, plan,
+// What bounds it: HBM while it streams (6.0 of 6.5 TB/s: 17.8 us for each 107 MB), and 17 us of a call with ranges that are the start (lengths, plan,
 // page numbers and the first codes are loads that wait for one another), the pieces and the kernel that adds them: 32 requests of 4096 to
-// 8192 tokens, 32/8 heads, in 52 us.  A single token on 500 of one request takes 5.9 us, a launch's latency and one meeting of a cluster.
+// 8192 tokens, 32/8 heads, in 53 us.  A single token on 500 of one request takes 6.0 us, a launch's latency and one meeting of a cluster.
 // Three stages of 32 keys a warp: more of them, or 64 keys, cost the registers or the shared memory of a third CTA on an SM (89 us then).
 #include "kv4_attention.cuh"
 #include "umma.cuh"
@@ -285,7 +285,7 @@ __global__ void __launch_bounds__(32 * kRowsWarps, NT == 1 ? 3 : 2) kv4_rows_ker
     if (lane == 0) {
       const int key = (lt < l_split ? lt : lt + l_gap) * kKeys;
       const uint32_t dst = ring + load_stage * kBytes, bar = bars + 8 * load_stage;
-      const uint8_t* head = a.pages + l_g * (a.page_size * 136);  // (1024 heads of 17408 bytes at most)
+      const uint8_t* head = a.pages + l_g * (a.page_size * 136);  // (4096 heads of 17408 bytes at most)
       const bool all = a.page_size > kGranule || key + kGranule < l_len;
       asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(all ? kBytes : kGranuleBytes) : "memory");
       if (a.page_size > kGranule) {
@@ -743,11 +743,14 @@ static int rows_cluster(const seq_tree_kv4_attention_params& p) {
 }
 
 // This kernel takes 16 query rows of a kv head at a time, the one of tiles 128 and 15 us for its start and its last pieces.  So up to 16 rows are
-// this one's.  More: where clusters cut a unit to few steps a warp (64/8 heads, 12 nodes on 4096 tokens, 8 steps: 19 us against 19; on 8192, 16 steps: 29
-// against 22; 64 nodes of 32/32 heads on 1024: 17 against 19, on 4096 32 against 26), but for two tiles of rows always (16 steps: 18 to 31 us
-// against 21 to 34); with ranges two tiles up to 20 steps a warp, or any number for half-precision rows, whose tiles take longer (32 nodes of
-// 32/32 heads, 4 requests of 2048: 32 us against 36; 16 requests: 131 against 98, half precision 122 against 112; 24 nodes, 16 of 4096: 167
-// against 147, half precision 161 against 177).
+// this one's.  More rows, each pair the time of this kernel and of the tiles' (us, bfloat16 where nothing is said):
+//   clusters, more than two tiles of rows: this one where a warp has at most 9 steps.
+//     8 steps   12 nodes of 64/8 heads on 4096 tokens   19, 19        64 nodes of 32/32 heads on 1024 tokens   17, 19
+//     16 steps  12 nodes of 64/8 heads on 8192 tokens   29, 22        more: 64 nodes of 32/32 heads on 4096    32, 26
+//   clusters, two tiles of rows: always this one (16 steps: 18 to 31 against 21 to 34).
+//   ranges, two tiles of rows: this one up to 20 steps a warp, and at any number for half-precision rows, whose tiles take longer.
+//     4 requests of 2048 tokens, 32 nodes of 32/32 heads   32, 36     16 of them                                131, 98; fp16 122, 112
+//     16 requests of 4096, 24 nodes of 32/32 heads         167, 147; fp16 161, 177
 bool kv4_few_rows(const seq_tree_kv4_attention_params& p) {
   const int rows = p.n_tree * (p.num_q_heads / p.num_kv_heads), c = rows_cluster(p);
   if (rows <= 16) return true;

@@ -10,7 +10,7 @@
 // scales and mids are applied in fp32: a score is s * (q . code) + m * sum(q), P is scale * probability (the rows' reference counts the
 // tile's largest scale, so that it fits), and the sum of m * probability is added to all channels of O.  One rounding instead of three,
 // 3.0e-4 instead of 4.6e-4 of the output (2.1e-4 are out's own), and scores as exact as fp32 is, for 20 % of the time (64 nodes of
-// 32/32 heads over a window of 4096: 59 -> 71 us).  Eight channels leave a code word in the order 0,4,1,5,2,6,3,7 (two nibbles of a 32-bit word per instruction);
+// 32/32 heads over a window of 4096: 59 -> 71 us; 72 now).  Eight channels leave a code word in the order 0,4,1,5,2,6,3,7 (two nibbles of a 32-bit word per instruction);
 // Q's channels are stored in that order too, and O's columns are put back when the rows are written.  The tree's 16-bit rows go
 // through the same warps.
 //
@@ -20,13 +20,14 @@
 // less than the registers and the code that keep them.  While a segment's results are written the next one's Q is in place already
 // and its first scores are computed.
 //
-// What bounds it: instructions, 1650 a scheduler and key tile (600 to unpack K and V, 500 for the 128 x 128 scores, the rest
+// What bounds it: instructions, 1700 a scheduler and key tile (600 to unpack K and V, 500 for the 128 x 128 scores, the rest
 // waits, hand-overs, the tree's tiles and the segments' ends), of which 0.61 are issued a cycle; and that they have to be in the
 // instruction caches: five warps of a scheduler run four different loops.  So loops are rolled and there is one copy of each: a
-// third of the code less gave 203 -> 188 us (768 nodes on 4096 tokens of 64/8 heads, 64 us at the tensor cores' rate; 172 now).
+// third of the code less gave 203 -> 188 us (768 nodes on 4096 tokens of 64/8 heads, 64 us at the tensor cores' rate; 172 now, 163 with the
+// same inputs in a graph).
 // Without effect or slower, for that reason or another: three groups (182 us against 180), sixteen unpacking warps (185), 16 scores
-// at a time (186 against 181), the ancestor words fetched ahead (181 against 171), 16 rows of the tree in flight (70b 168 against
-// 171, 64 nodes of 32/32 heads 63 against 59), and two tiles of 128 rows that shared the unpacked keys.
+// at a time (186 against 181), the ancestor words fetched ahead (181 against 171), and two tiles of 128 rows that shared the unpacked keys.
+// Faster here and slower there: 16 rows of the tree in flight (these 168 against 171, but 64 nodes of 32/32 heads 63 against 59).
 //
 // Every mbarrier wait is bounded; one that runs out raises SEQ_DEV_TIMEOUT and the CTA drains.
 #include "kv4_attention.cuh"
@@ -44,8 +45,16 @@ constexpr int kStageBytes = kHalfKeys / kGranule * kGranuleBytes;
 constexpr int kTreeTiles = SEQ_MAX_TREE / kTilesStep;
 
 constexpr int kParamTiles = 5;  // tiles of scales and mids: one is written again behind the scores that follow its own three tiles later
-constexpr int kUnitCost = 2;  // steps that a unit's start and end take (768 nodes on 4096 tokens, 0, 1, 2, 3: 172.7, 172.4, 171.5, 171.7 us)
-constexpr int kTreeCost = 1;  // steps that one of the tree takes longer (0, 1/2, 1, 3/2: 165.1, 161.4, 160.4, 164.0 us)
+// What a unit's start and end take, and what a step of the tree takes longer than one of the prefix, in steps.  Chosen on 768 nodes of 64/8 heads on
+// 4096 tokens; us in a graph there and on batches of trees with short prefixes, where the constants are near the best but not always it:
+//                                             2, 1 (these)   tree 0   tree 2   unit 0   unit 4
+//   768 nodes on 4096 tokens, 64/8 heads          162.8       168.8    170.6    164.3    162.9
+//   768 nodes on 300 tokens, 64/8 heads            67.7        63.0     76.7     74.1     66.1
+//   16 x 64 nodes on 300 tokens, 32/32 heads       49.9        51.3     51.6     52.9     52.5
+//   32 x 64 nodes on 100 tokens, 32/32 heads       67.2        65.5     65.2     67.0     66.6
+//   16 x 128 nodes on 200 tokens, 40/40 heads      73.5        67.8     74.5     69.8     76.8
+constexpr int kUnitCost = 2;
+constexpr int kTreeCost = 1;
 constexpr uint32_t kTmemS = 128;  // tensor memory: O in columns 0..127, then the S/P buffers
 
 template <bool kExact>
